@@ -314,6 +314,73 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
                             int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t n_ctx,
                             int32_t cap_ctx, void *hip_stream);
 
+/* ---- several sequences over one prompt: the step of k independent passes or of a beam search ----
+ * Section 4.3 holds Superposed Decoding against k independent passes and against beam search: n_seq sequences that
+ * agree in their first positions.  These operators take such a batch through a step on a PAGED cache, for programs
+ * that run those decoders' products themselves:
+ *   K, V   DEVICE [n_pages, n_kv_heads, page_size, d_head] in `dtype` (fp32, fp16 or bf16), 16-byte aligned; page_size a
+ *          power of two up to 1024, d_head a power of two from 8 to 256;
+ *   table  DEVICE int32 [n_seq, table_stride]: position p of sequence s is row p % page_size of page
+ *          table[s][p / page_size].  Entries no call needs may hold anything.
+ * Sequences come in groups of `width` consecutive ones (one prompt each).  Lengths and page numbers live on the device,
+ * so that a captured step can be replayed; what the host cannot check is bounded by the kernels: a page number outside
+ * [0, n_pages), a row of the table or a length out of range is never followed, and *err (DEVICE int32, may be NULL) is
+ * set to 1 (and never cleared).  Calls do not synchronise and allocate nothing; those that need scratch take it from the caller, 256-byte
+ * aligned and of the size the function beside them gives (SPD_EWORKSPACE if less), and leave nothing in it for a
+ * later call: calls that may overlap need scratch of their own. */
+
+/* New tokens' keys and values into the cache, rotated on the way: token i, at position pos[i] of sequence seq[i] (DEVICE int32
+ * [n_tokens]), has k and v rows DEVICE float [n_kv_heads, d_head] at k + i kv_stride, v + i kv_stride; k (and q) are rotated on adjacent
+ * pairs by pos * rope_theta^(-2i/d_head).  q (may be NULL, then n_heads is 0): rows [n_heads, d_head] at q + i q_stride; q_out
+ * [n_tokens, n_heads, d_head] gets them rotated, in fp32 (it may be q where q_stride is n_heads d_head).  Strides are in elements and
+ * multiples of 4, so that the parts of one product's rows can be passed as they lie; pointers 16-byte aligned.  seq[i] < 0:
+ * padding, nothing of that token is read or written.  A token whose position or page is out of range is left out whole, *err is set.  No two tokens of a
+ * call may name the same position of the same page. */
+int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                        int32_t d_head, int32_t n_seq, int32_t table_stride, const float *q, int64_t q_stride, const float *k, const float *v,
+                        int64_t kv_stride, const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t n_heads, float rope_theta,
+                        float *q_out, int32_t *err, void *hip_stream);
+
+/* One query per sequence and head: out[s][h] = softmax(q[s][h] . K / sqrt(d_head)) V over positions [0, len[s]) of
+ * sequence s.  Positions below shared[g] are the same in all sequences of group g: they are read once, through the table of
+ * the group's first sequence.  q, out DEVICE float [n_seq, n_heads, d_head]; shared DEVICE int32 [n_seq / width], len DEVICE int32 [n_seq].
+ * max_shared >= every shared[g] and max_own >= every len[s] - shared[g] size the launch (host values; neither more than a row of
+ * the table holds).  len[s] may be less than shared[g].  A sequence of length 0 gets zeros; so does one whose lengths are out of these bounds
+ * (*err is set).  A position on a page out of range does not count (*err is set).  Nothing behind a sequence's last position gets into its result,
+ * whatever it holds. */
+size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared,
+                                             int32_t max_own);
+int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
+                            int32_t page_size, int32_t d_head, int32_t n_seq, int32_t table_stride, const int32_t *shared, const int32_t *len,
+                            int32_t width, int32_t n_heads, int32_t max_shared, int32_t max_own, float *out, void *scratch, size_t scratch_bytes,
+                            int32_t *err, void *hip_stream);
+
+/* The n_out best continuations of each group's n_in beams (both 1..SPD_K_MAX; n_in 1 at a search's first step): continuation (b, v)
+ * scores scores[g][b] + log softmax(logits[g][b] / tau)[v], and the lower b, then the lower v goes first among equals.  logits
+ * DEVICE [n_groups n_in rows of row_stride elements] in `dtype` (a logit that is no number counts as -inf, +inf as the largest finite
+ * number; -inf is no continuation); scores DEVICE float [n_groups, n_in] (-inf or no number: no such beam).  ended (DEVICE int32
+ * [n_groups, n_in], may be NULL): a beam with a value other than 0 has one continuation, itself, with token end_token and its score
+ * unchanged; neither its logits nor those of an absent beam are read.  Outputs DEVICE [n_groups, n_out], best first: scores, tokens (in
+ * [0, vocab)), parents (in [0, n_in)) and, unless NULL, whether the beam has ended (its parent had, or the token is end_token).
+ * Where there are fewer continuations, the others have score -inf, token 0, not ended, and as parent their own place (0 where that is no beam).  With
+ * n_out = n_in the outputs may be the inputs' buffers. */
+size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab);
+int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row_stride, int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab,
+                       const float *scores, const int32_t *ended, int32_t end_token, float tau, float *out_scores, int32_t *out_tokens,
+                       int32_t *out_parents, int32_t *out_ended, void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* The cache follows a selection: beam j of group g goes on from beam parents[g][j] (DEVICE int32 [n_seq / width, width], width <=
+ * SPD_K_MAX).  len DEVICE int32 [n_seq]: positions cached so far, the same for all beams of a group; entry e = len / page_size of a
+ * row is the page being filled, which like those behind it must be the row's own.  A row's first child keeps the whole row; each
+ * further child, in order, takes its parent's entries before e and, from e on, those of a row without a child (in order), into
+ * whose page e the rows filled so far are copied in all n_layers (layer l's pools start l * layer_stride elements after K and V).  So
+ * every beam has pages of its own to write into and none has to be found.  table_out [n_seq, table_stride] must not overlap table.
+ * A group with a parent outside [0, width), unequal lengths, or a page to be copied that is out of range or not its row's own is
+ * left as it was (its table copied unchanged) and *err is set. */
+int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                        int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
+                        const int32_t *parents, const int32_t *len, int32_t *table_out, int32_t *err, void *hip_stream);
+
 /* ---- test hooks for the error path of the persistent kernel's bounded waits ----
  * A wait of the persistent forward kernel that gives up (its grid was not co-resident) sets an
  * error word in the device-side draft state; every entry point that copies that state back

@@ -64,7 +64,7 @@ def lib():
         if not os.path.exists(path):
             raise ImportError(f"{path} is missing: build it first (python -m paper_2405_18400_amd.build)")
         L = C.CDLL(path)
-        vp, i32, f32, sz = C.c_void_p, C.c_int32, C.c_float, C.c_size_t
+        vp, i32, i64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
         sig = {
             "spd_workspace_bytes": [C.POINTER(SpdModelCfg), C.POINTER(sz)],
             "spd_create": [C.POINTER(SpdModelCfg), C.POINTER(SpdWeightPtrs), vp, sz, vp, C.POINTER(vp)],
@@ -103,6 +103,10 @@ def lib():
             "spd_op_swiglu": [i32, vp, vp, vp, f32, vp, vp, i32, i32, vp],
             "spd_op_attention": [i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp],
             "spd_op_attention_static": [i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp],
+            "spd_op_append_paged": [i32, vp, vp, vp] + [i32] * 6 + [vp, i64, vp, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp],
+            "spd_op_attention_shared": [i32, vp, vp, vp, vp] + [i32] * 6 + [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp, vp],
+            "spd_op_beam_select": [i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
+            "spd_op_beam_reorder": [i32, vp, vp, vp] + [i32] * 7 + [i64, i32, vp, vp, vp, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -111,6 +115,8 @@ def lib():
         L.spd_last_error.argtypes, L.spd_last_error.restype = [vp], C.c_char_p
         L.spd_strerror.argtypes, L.spd_strerror.restype = [C.c_int], C.c_char_p
         L.spd_op_attention_scratch_bytes.argtypes, L.spd_op_attention_scratch_bytes.restype = [i32, i32, i32], sz
+        L.spd_op_attention_shared_scratch_bytes.argtypes, L.spd_op_attention_shared_scratch_bytes.restype = [i32] * 7, sz
+        L.spd_op_beam_select_scratch_bytes.argtypes, L.spd_op_beam_select_scratch_bytes.restype = [i32] * 4, sz
         L.hipStreamSynchronize.argtypes, L.hipStreamSynchronize.restype = [vp], C.c_int   # (the runtime that libspd is linked to)
         _lib = L
     return _lib
@@ -433,6 +439,144 @@ def spd_op_attention_static(dtype: str, q, K, V, out, n_ctx: int):
                                        n_heads, n_kv, d_head, n_ctx, cap_ctx, _stream_ptr())
     if rc:
         raise SpdError(rc, "spd_op_attention_static")
+
+
+# ---- several sequences over one prompt, on a paged cache: K, V [pages, n_kv_heads, page_size, d_head], table int32 [n_seq, entries].
+# Nothing here waits for the GPU; `err`, an int32 tensor of one element, is set to 1 by what only the kernels can see (spd.h).
+def _on_gpu(where, **tensors):
+    """Every tensor given: (tensor, torch type, shape or None), whole, on the current device; entries of a shape that are None are not checked."""
+    device = _torch().cuda.current_device()
+    for name, (t, dtype, shape) in tensors.items():
+        if t.get_device() != device:
+            raise ValueError(f"{where}: {name} is not on the current device")
+        if t.dtype != dtype:
+            raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{where}: {name} is not contiguous")
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+
+
+def _kv_type(where, dtype):
+    torch = _torch()
+    types = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+    if dtype not in types:
+        raise ValueError(f"{where}: no element type {dtype!r}")
+    return types[dtype]
+
+
+def _rows_of(where, device, **tensors):
+    """[tokens, heads, d_head] tensors whose tokens may lie apart (parts of one product's rows): the tokens' stride."""
+    strides = set()
+    for name, t in tensors.items():
+        if t.get_device() != device or t.dtype != _torch().float32:
+            raise ValueError(f"{where}: {name} has to be float32 on the current device")
+        n, heads, d = t.shape
+        if t.stride(2) != 1 and d > 1 or t.stride(1) != d and heads > 1:
+            raise ValueError(f"{where}: the heads of {name}'s tokens have to lie one behind the other")
+        strides.add(t.stride(0) if n > 1 else max(t.stride(0), heads * d))
+    if len(strides) != 1:
+        raise ValueError(f"{where}: {' and '.join(tensors)} differ in their tokens' stride")
+    return strides.pop()
+
+
+def _raise(rc, where):
+    if rc:
+        raise SpdError(rc, where)
+
+
+def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: float, q=None, q_out=None, err=None):
+    """k, v [tokens, n_kv_heads, d_head] (and q [tokens, n_heads, d_head] -> q_out), rotated by pos, to the rows of their sequences; seq < 0: padding."""
+    torch, where = _torch(), "spd_op_append_paged"
+    kv = _kv_type(where, dtype)
+    n_pages, n_kv, page_size, d = K.shape
+    n = k.shape[0]
+    i32 = torch.int32
+    _on_gpu(where, K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)))
+    if err is not None:
+        _on_gpu(where, err=(err, i32, (1,)))
+    if tuple(k.shape) != (n, n_kv, d) or k.shape != v.shape:
+        raise ValueError(f"{where}: k and v have to be [{n}, {n_kv}, {d}]")
+    kv_stride, q_stride, heads, device = _rows_of(where, K.get_device(), k=k, v=v), 0, 0, K.get_device()
+    if (q is None) != (q_out is None):
+        raise ValueError(f"{where}: q and q_out come together")
+    if q is not None:
+        heads = q.shape[1]
+        if tuple(q.shape) != (n, heads, d):
+            raise ValueError(f"{where}: q has to be [{n}, heads, {d}]")
+        q_stride = _rows_of(where, device, q=q)
+        _on_gpu(where, q_out=(q_out, torch.float32, (n, heads, d)))
+    n_seq, entries = table.shape
+    _raise(lib().spd_op_append_paged(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries,
+                                     None if q is None else q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), kv_stride, seq.data_ptr(), pos.data_ptr(),
+                                     n, heads, rope_theta, None if q is None else q_out.data_ptr(), None if err is None else err.data_ptr(), _stream_ptr()), where)
+
+
+def _scratch(n_bytes, device):
+    """-> (a tensor that keeps the memory, its first 256-byte aligned address, bytes from there).  It goes back to torch's pool when the call has
+    been enqueued: that pool hands it out again in the order of the stream the call runs on, the current one."""
+    buf = _torch().empty(n_bytes + 256, dtype=_torch().uint8, device=device)
+    return buf, (buf.data_ptr() + 255) // 256 * 256, n_bytes
+
+
+def spd_op_attention_shared(dtype: str, q, K, V, table, shared, length, out, width: int, max_shared: int, max_own: int, err=None):
+    """q, out [n_seq, n_heads, d_head]; shared int32 [n_seq / width], length int32 [n_seq]."""
+    torch, where = _torch(), "spd_op_attention_shared"
+    kv, i32 = _kv_type(where, dtype), torch.int32
+    n_pages, n_kv, page_size, d = K.shape
+    n_seq, heads, _ = q.shape
+    if width < 1 or n_seq % width:
+        raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
+    _on_gpu(where, q=(q, torch.float32, (n_seq, heads, d)), K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, (n_seq, table.shape[-1])),
+            shared=(shared, i32, (n_seq // width,)), length=(length, i32, (n_seq,)), out=(out, torch.float32, (n_seq, heads, d)))
+    if err is not None:
+        _on_gpu(where, err=(err, i32, (1,)))
+    L = lib()
+    _keep, scratch, n_bytes = _scratch(L.spd_op_attention_shared_scratch_bytes(n_seq, width, heads, n_kv, d, max_shared, max_own), q.device)
+    _raise(L.spd_op_attention_shared(SPD_DTYPE[dtype], q.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq,
+                                     table.shape[1], shared.data_ptr(), length.data_ptr(), width, heads, max_shared, max_own, out.data_ptr(), scratch, n_bytes,
+                                     None if err is None else err.data_ptr(), _stream_ptr()), where)
+
+
+def spd_op_beam_select(dtype: str, logits, scores, out_scores, out_tokens, out_parents, tau: float = 1.0, ended=None, end_token: int = -1, out_ended=None):
+    """logits [n_groups, n_in, vocab] (rows may lie apart), scores [n_groups, n_in] -> out_* [n_groups, n_out]."""
+    torch, where = _torch(), "spd_op_beam_select"
+    groups, n_in, vocab = logits.shape
+    n_out, i32 = out_scores.shape[-1], torch.int32
+    if logits.dtype != _kv_type(where, dtype):
+        raise ValueError(f"{where}: logits are {logits.dtype}, not {dtype}")
+    stride = logits.stride(1) if n_in > 1 else logits.stride(0) if groups > 1 else vocab
+    if (logits.stride(2) != 1 and vocab > 1) or (groups > 1 and logits.stride(0) != n_in * stride) or logits.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{where}: logits have to be rows of one stride on the current device")
+    outs = {"out_tokens": (out_tokens, i32, (groups, n_out)), "out_parents": (out_parents, i32, (groups, n_out))}
+    if ended is not None:
+        outs["ended"] = (ended, i32, (groups, n_in))
+    if out_ended is not None:
+        outs["out_ended"] = (out_ended, i32, (groups, n_out))
+    _on_gpu(where, scores=(scores, torch.float32, (groups, n_in)), out_scores=(out_scores, torch.float32, (groups, n_out)), **outs)
+    L = lib()
+    _keep, scratch, n_bytes = _scratch(L.spd_op_beam_select_scratch_bytes(groups, n_in, n_out, vocab), logits.device)
+    _raise(L.spd_op_beam_select(SPD_DTYPE[dtype], logits.data_ptr(), stride, groups, n_in, n_out, vocab, scores.data_ptr(),
+                                None if ended is None else ended.data_ptr(), end_token, tau, out_scores.data_ptr(), out_tokens.data_ptr(),
+                                out_parents.data_ptr(), None if out_ended is None else out_ended.data_ptr(), scratch, n_bytes, _stream_ptr()), where)
+
+
+def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, width: int, err=None):
+    """K, V [pages, ...] or [layers, pages, n_kv_heads, page_size, d_head]; parents int32 [n_seq / width, width], length int32 [n_seq]; table -> table_out."""
+    torch, where = _torch(), "spd_op_beam_reorder"
+    kv, i32 = _kv_type(where, dtype), torch.int32
+    layers = K.shape[0] if K.dim() == 5 else 1
+    n_pages, n_kv, page_size, d = K.shape[-4:]
+    n_seq, entries = table.shape
+    if width < 1 or n_seq % width:
+        raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
+    _on_gpu(where, K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, None), parents=(parents, i32, (n_seq // width, width)),
+            length=(length, i32, (n_seq,)), table_out=(table_out, i32, (n_seq, entries)))
+    if err is not None:
+        _on_gpu(where, err=(err, i32, (1,)))
+    _raise(lib().spd_op_beam_reorder(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
+                                     n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), table_out.data_ptr(),
+                                     None if err is None else err.data_ptr(), _stream_ptr()), where)
 
 
 def spd_test_state_layout():

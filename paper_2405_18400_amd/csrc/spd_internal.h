@@ -259,7 +259,57 @@ constexpr int ATTN_CHUNK_MAX = 512;
 struct FillRange { int32_t *p; int32_t v, n; };
 struct DraftArgs { int32_t k, tails[SPD_K_MAX][SPD_TAIL]; float logscore[SPD_K_MAX]; };
 
+// ---------------------------------------------------------------- several sequences over one paged cache
+// K, V [n_pages, n_kv_heads, page size, d_head]; position p of sequence s: page table[s * table_stride + (p >> page_shift)],
+// row p mod page size.
+struct PagedCache {
+    void *K, *V;
+    const int32_t *table;
+    int32_t n_pages, n_kv_heads, page_shift, d_head, n_seq, table_stride;
+};
+struct AppendArgs {
+    PagedCache c;
+    const float *q, *k, *v;      // [n_tokens] rows, strides in elements
+    int64_t q_stride, kv_stride;
+    const int32_t *seq, *pos;    // per token
+    int32_t n_tokens, n_heads, parts;
+    double log2_theta;
+    float *q_out;                // [n_tokens, n_heads, d_head]
+    int32_t *err;
+};
+struct ReorderArgs {
+    PagedCache c;                // layer 0's; layer l's pools start layer_bytes * l later
+    const int32_t *parents, *len;
+    int32_t *table_out, *err;
+    int32_t n_layers, width, n_groups, row_bytes, shares, heads_per_share;
+    size_t layer_bytes;
+};
+struct SharedAttnArgs {
+    PagedCache c;
+    const float *q;              // [n_seq, n_heads, d_head]
+    float *out;
+    const int32_t *shared, *len; // per group, per sequence
+    int32_t *err;
+    int32_t width, n_heads, max_shared, max_own;
+};
+struct SelectArgs {
+    const void *logits;
+    int64_t row_stride;          // elements
+    int32_t n_groups, n_in, n_out, vocab;
+    const float *scores;         // [n_groups, n_in]
+    const int32_t *ended;        // [n_groups, n_in], or null
+    int32_t end_token;
+    float tau;
+    float *out_scores;           // [n_groups, n_out], as the next three
+    int32_t *out_tokens, *out_parents, *out_ended;
+    int32_t slices;
+    unsigned long long *best;    // scratch, [rows, slices, n_out]: sort keys, best first
+    float *top, *sum;            // scratch, [rows, slices]: largest logit, sum of exp((logit - that) / tau)
+};
+
 namespace spdk {
+int paged_cache_status(int dtype, const PagedCache &c, int page_size);   // an spd_status
+PagedCache paged_cache(void *K, void *V, const int32_t *table, int n_pages, int n_kv_heads, int page_size, int d_head, int n_seq, int table_stride);
 hipError_t gemv(hipStream_t s, int dtype, int epi, const GemvArgs &a, int num_cu);
 size_t gemv_lds_bytes(int dtype, int cols);
 hipError_t attention(hipStream_t s, int dtype, const AttnArgs &a);
