@@ -319,7 +319,7 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
  * agree in their first positions.  These operators take such a batch through a step on a PAGED cache, for programs
  * that run those decoders' products themselves:
  *   K, V   DEVICE [n_pages, n_kv_heads, page_size, d_head] in `dtype` (fp32, fp16 or bf16), 16-byte aligned; page_size a
- *          power of two up to 1024, d_head a power of two from 8 to 256;
+ *          power of two from 4 to 1024, d_head a power of two from 8 to 256;
  *   table  DEVICE int32 [n_seq, table_stride]: position p of sequence s is row p % page_size of page
  *          table[s][p / page_size].  Entries no call needs may hold anything.
  * Sequences come in groups of `width` consecutive ones (one prompt each).  Lengths and page numbers live on the device,

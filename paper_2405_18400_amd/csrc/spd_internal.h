@@ -291,6 +291,9 @@ struct SharedAttnArgs {
     const int32_t *shared, *len; // per group, per sequence
     int32_t *err;
     int32_t width, n_heads, max_shared, max_own;
+    // how the positions are cut: blocks 0 .. shared_blocks - 1 take shared chunks, the others sequences' own ones
+    int32_t shared_chunks, shared_chunk, own_chunks, slots, row_tiles, own_tiles, shared_blocks, shared_blocks_per_tile;
+    float *part_ml, *part;       // scratch, [n_seq, n_heads, slots]: maximum and sum; O [.., d_head]
 };
 struct SelectArgs {
     const void *logits;

@@ -209,7 +209,7 @@ int paged_cache_status(int dtype, const PagedCache &c, int page_size) {
     if (dtype != SPD_DTYPE_FP32 && dtype != SPD_DTYPE_BF16 && dtype != SPD_DTYPE_FP16) return SPD_EINVAL;
     if (!c.K || !c.V || (!c.table && c.n_seq > 0) || ((uintptr_t)c.K | (uintptr_t)c.V) % 16 || (uintptr_t)c.table % 4) return SPD_EINVAL;
     if (c.n_pages <= 0 || c.n_kv_heads <= 0 || c.n_seq < 0 || c.table_stride <= 0) return SPD_EINVAL;
-    if (page_size <= 0 || page_size > 1024 || (page_size & (page_size - 1))) return SPD_EINVAL;
+    if (page_size < 4 || page_size > 1024 || (page_size & (page_size - 1))) return SPD_EINVAL;
     if (c.d_head < 8 || c.d_head > 256 || (c.d_head & (c.d_head - 1))) return SPD_EINVAL;
     return SPD_OK;
 }

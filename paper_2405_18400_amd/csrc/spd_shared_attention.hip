@@ -1,80 +1,604 @@
 // Attention of one query per sequence and head over a paged cache, for groups of sequences that
 // share their first positions.
 //
-// A block per (sequence, query head): groups of lanes that hold a position's row side by side walk
-// through the positions with a running maximum and sum of their own, and meet in LDS at the end.
+// Bound: the cached keys and values stream through once -- a group's shared ones once for all its
+// sequences, which is what the operator is for -- so the work is cut by KEYS, and all query rows
+// that need a key meet it in one place:
+//   * a "shared" block owns (group, key/value head, chunk of shared positions, tile of query rows); its rows are the
+//     query heads of that key/value head in all sequences of the group;
+//   * an "own" block owns (sequence, key/value head, chunk of its own positions); its rows are that sequence's query heads;
+//   * each leaves (maximum, sum, O) per row and a second kernel puts a row's chunks together in chunk order.
+// Both products run on the matrix cores, S^T [key, row] = K Q^T and O^T [feature, row] = V^T P^T, operands straight from
+// memory into registers:
+//   * 16 keys x 32 features of K are one operand as they lie (a lane holds eight features of one key);
+//   * S^T's accumulator holds keys 16 u + 4 kk + r (kk: the lane's group of 16) of one row, which is P^T's operand layout
+//     when the eight k indices of a lane stand for those keys, so probabilities never leave their registers;
+//   * a lane fetches DH / 16 features of each of those eight keys of V, 16 lanes a whole row, and turns them round in registers.
+// K and V of a 16-bit cache are exact in their type; queries and probabilities go in as two fp16 numbers (22 bits, scaled by
+// powers of two into fp16's range) or three bf16 numbers (24 bits): the error against 64 bits is that of fp32 arithmetic.
+// An fp32 cache takes the fp32 products.  Four waves share a block's keys, 32 each in turn, with a running maximum and sum of their own.
 #include "spd_device.h"
+
+#include <algorithm>
 
 using namespace spdd;
 
 namespace {
 
 constexpr int NTS = 256, NWS = NTS / WAVE;
+constexpr int KEYS = 32;                         // keys of a wave's turn
+constexpr int ROWS = 16;                         // query rows of a tile
+constexpr int CHUNK_MAX = 4096;                  // positions of a chunk at most (its page numbers lie in LDS)
+constexpr int PAGE_MIN = 4;                      // the smallest page: four keys of a lane lie on one
+constexpr int BLOCKS = 512;                      // blocks the positions are cut for: two to a compute unit
+constexpr float SLACK = 8.f;                     // a row's reference is raised when a score passes it by 2^8: seldom
+constexpr float P_BITS = 7.f;                    // probabilities are scaled by 2^7, at most 2^15 then: two fp16 numbers keep 22 bits down to 2^-19
 
-// exp(a - b) with exp(-inf - anything) = 0, also where b is -inf (nothing seen yet).
-__device__ __forceinline__ float exp_below(float a, float b) { return expf(a - (b == -INFINITY ? 0.f : b)); }
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-template <typename KT>
-__global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs a) {
-    constexpr int VEC = Store<KT>::VEC;
-    __shared__ float acc_s[NTS * VEC], m_s[NTS], l_s[NTS];
-    const int tid = threadIdx.x, d = a.c.d_head, lpp = d / VEC, groups = NTS / lpp, gi = tid / lpp, li = tid % lpp;
-    const int s = blockIdx.x / a.n_heads, hq = blockIdx.x % a.n_heads, lead = s - s % a.width, kvh = hq / (a.n_heads / a.c.n_kv_heads);
-    const int shift = a.c.page_shift, page_size = 1 << shift;
-    const int shared = as_global(a.shared)[s / a.width], len = as_global(a.len)[s];
-    const long long room = (long long)a.c.table_stride << shift;
-    const bool fits = shared >= 0 && len >= 0 && shared <= a.max_shared && (len <= shared || len - shared <= a.max_own) && len <= room;
-    if (!fits && a.err && tid == 0) *as_global(a.err) = 1;
-    const int n = fits ? len : 0;
-    const float scale = 1.0f / sqrtf((float)d);
-    float qv[VEC], acc[VEC], m = -INFINITY, l = 0.f;
+// exp2(a - b) with exp2(-inf - anything) = 0, also where b is -inf (nothing seen yet).
+__device__ __forceinline__ float exp2_below(float a, float b) { return __builtin_amdgcn_exp2f(a - (b == -INFINITY ? 0.f : b)); }
+
+template <typename KT> struct Type;              // PARTS: numbers of the cache's type that stand for one fp32 number
+template <> struct Type<half_t> { static constexpr int PARTS = 2; };
+template <> struct Type<bf16_t> { static constexpr int PARTS = 3; };
+template <> struct Type<float> { static constexpr int PARTS = 1; };
+
+// Two fp32 numbers as pairs of the cache's type, most significant part first.
+template <typename KT> __device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[Type<KT>::PARTS]);
+template <> __device__ __forceinline__ void parts_of<half_t>(float x, float y, uint32_t (&out)[2]) {
+    const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x, y));
+    out[0] = __builtin_bit_cast(uint32_t, hi);
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x - (float)hi.x, y - (float)hi.y));
+}
+template <> __device__ __forceinline__ void parts_of<bf16_t>(float x, float y, uint32_t (&out)[3]) {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) { qv[v] = as_global(a.q)[((size_t)s * a.n_heads + hq) * d + li * VEC + v]; acc[v] = 0.f; }
-    for (int p0 = 0; p0 < n; p0 += groups) {
-        const int p = p0 + gi;
-        const int page = p < n ? as_global(a.c.table)[(size_t)(p < shared ? lead : s) * a.c.table_stride + (p >> shift)] : 0;
-        const bool good = (unsigned)page < (unsigned)a.c.n_pages, there = p < n && good;
-        if (!good && a.err) *as_global(a.err) = 1;
-        float kf[VEC], vf[VEC], x = 0.f;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) kf[v] = vf[v] = 0.f;
-        if (there) {
-            const size_t at = (((size_t)page * a.c.n_kv_heads + kvh) * page_size + (p & (page_size - 1))) * d + li * VEC;
-            Store<KT>::unpack(global_load16((const char *)a.c.K + at * sizeof(KT)), kf);
-            Store<KT>::unpack(global_load16((const char *)a.c.V + at * sizeof(KT)), vf);
-        }
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) x = fmaf(kf[v], qv[v], x);
-        for (int o = 1; o < lpp; o <<= 1) x += __shfl_xor(x, o, WAVE);
-        x = there ? x * scale : -INFINITY;
-        const float mx = fmaxf(m, x), corr = exp_below(m, mx), w = there ? exp_below(x, mx) : 0.f;
-        m = mx;
-        l = l * corr + w;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) acc[v] = fmaf(w, vf[v], acc[v] * corr);
-    }
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) acc_s[gi * d + li * VEC + v] = acc[v];
-    if (li == 0) { m_s[gi] = m; l_s[gi] = l; }
-    __syncthreads();
-    for (int c = tid; c < d; c += NTS) {
-        float M = -INFINITY, L = 0.f, O = 0.f;
-        for (int g = 0; g < groups; ++g) M = fmaxf(M, m_s[g]);
-        for (int g = 0; g < groups; ++g) {
-            const float f = exp_below(m_s[g], M);
-            L += f * l_s[g];
-            O += f * acc_s[g * d + c];
-        }
-        as_global(a.out)[((size_t)s * a.n_heads + hq) * d + c] = L == 0.f ? 0.f : O / L;   // a row that sees nothing: zeros
+    for (int p = 0; p < 3; ++p) {                // eight bits each, cut off: the remainders are exact
+        const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+        out[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        x -= __uint_as_float(a & 0xFFFF0000u);
+        y -= __uint_as_float(b & 0xFFFF0000u);
     }
 }
+
+template <typename KT> __device__ __forceinline__ f32x4v mfma16(u32x4 a, u32x4 b, f32x4v c);
+template <> __device__ __forceinline__ f32x4v mfma16<half_t>(u32x4 a, u32x4 b, f32x4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4v mfma16<bf16_t>(u32x4 a, u32x4 b, f32x4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// B bytes of one lane, in words.
+template <int B> __device__ __forceinline__ void load_words(const char *p, uint32_t (&w)[B / 4]) {
+    if constexpr (B == 4) w[0] = *(const uint32_t __attribute__((address_space(1))) *)p;
+    else if constexpr (B == 8) { const u32x2 v = *(const u32x2 __attribute__((address_space(1))) *)p; w[0] = v.x; w[1] = v.y; }
+    else {
+#pragma unroll
+        for (int i = 0; i < B / 16; ++i) {
+            const u32x4 v = global_load16(p + 16 * i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+    }
+}
+
+// A stretch of positions read through one row of the table.
+struct Stretch { int row, lo, hi; };
+
+// What a block does: rows r0 .. r0 + n_rows - 1 of the sequences from `seq` on (row r: sequence seq + r / group, query head
+// kvh * group + r % group), over one or two stretches; its results go to `slot`, or to the output where there is one slot.
+// `shared`: positions that a row's sequence must have to take part (those that end before have a block of their own), or -1.
+struct Unit { int seq, kvh, r0, n_rows, slot, shared; Stretch a, b; };
+
+// Whether a sequence's lengths are in bounds.
+__device__ __forceinline__ bool seq_fits(const SharedAttnArgs &p, int shared, int len) {
+    return shared >= 0 && len >= 0 && shared <= p.max_shared && (len <= shared || len - shared <= p.max_own) && (long long)len <= (long long)p.c.table_stride << p.c.page_shift;
+}
+
+template <typename KT, int DH, int RT>
+struct Lds {
+    static constexpr int PARTS = Type<KT>::PARTS;
+    static constexpr int Q_WORDS = RT * ROWS * DH * (sizeof(KT) == 4 ? 1 : 0) + RT * ROWS * DH * PARTS / 2 * (sizeof(KT) == 2 ? 1 : 0);
+    static constexpr int HALF = DH > 128 ? 128 : DH, STRIDE = HALF + 4;      // the waves' results meet 128 features at a time
+    static constexpr int O_WORDS = NWS * ROWS * STRIDE;
+    static constexpr int WORDS = Q_WORDS > O_WORDS ? Q_WORDS : O_WORDS;
+};
+
+constexpr int PAGES = CHUNK_MAX / PAGE_MIN + 4;
+
+template <typename KT, int DH, int RT>
+__device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, uint32_t *lds, int *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
+    constexpr bool F32 = sizeof(KT) == 4;
+    constexpr int PARTS = Type<KT>::PARTS;
+    constexpr int NJ = F32 ? DH / 16 : DH / 32;                              // 16-byte pieces of a key per lane
+    constexpr int FV = DH / 16, VB = FV * (int)sizeof(KT), VW = VB / 4;      // features, bytes, words of a value row per lane
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
+    const int d = p.c.d_head, shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
+    const int tiles = (min(un.n_rows, RT * ROWS) + ROWS - 1) / ROWS;
+
+    // queries, as the products take them: piece (step j, part) of a tile holds a lane's eight (fp32: four) features
+    {
+        constexpr int TPR = NTS / (RT * ROWS), N8 = DH / 8, PP = (N8 + TPR - 1) / TPR;   // threads per row; pieces of eight features
+        const int row = tid / TPR, t = tid % TPR;
+        const int r = un.r0 + row, s = un.seq + r / group, hq = un.kvh * group + r % group;
+        float x[PP][8], top = 0.f;
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+            const int at = 8 * (t + i * TPR);
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (row < un.n_rows && at + e < d) v = global_load_float4(p.q + ((size_t)s * p.n_heads + hq) * d + at + e);
+                x[i][e] = v.x; x[i][e + 1] = v.y; x[i][e + 2] = v.z; x[i][e + 3] = v.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+        }
+        float up = 1.f, down = 1.f;
+        if constexpr (sizeof(KT) == 2 && PARTS == 2) {
+#pragma unroll
+            for (int o = 1; o < TPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
+            int ex = 15;
+            if (top > 0.f && top < INFINITY) (void)frexpf(top, &ex);
+            ex = max(ex, -100);
+            up = ldexpf(1.f, 15 - ex);
+            down = ldexpf(1.f, ex - 15);
+        }
+        if (t == 0) row_scale[row] = down * (1.4426950408889634f / sqrtf((float)d));     // to logarithms of base 2
+#pragma unroll
+        for (int i = 0; i < PP; ++i) {
+            const int piece = t + i * TPR;
+            if (piece >= N8) break;
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {    // feature 16 j + 4 kk + c of piece j: word c
+                    const int f = 8 * piece + e;
+                    lds[(((row / ROWS) * NJ + f / 16) * WAVE + ((f / 4) % 4) * ROWS + row % ROWS) * 4 + f % 4] = __float_as_uint(x[i][e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    uint32_t part[PARTS];
+                    parts_of<KT>(x[i][e] * up, x[i][e + 1] * up, part);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q)
+                        lds[((((row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + row % ROWS) * 4 + e / 2] = part[q];
+                }
+            }
+        }
+    }
+    __syncthreads();
+    const u32x4 *Q = (const u32x4 *)lds;
+    f32x4v o[RT][FV];
+    float m[RT], l[RT], scale[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int e = 0; e < FV; ++e) o[rt][e] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        m[rt] = -INFINITY; l[rt] = 0.f; scale[rt] = row_scale[rt * ROWS + col];
+    }
+
+    const size_t row_bytes = (size_t)d * sizeof(KT), head_bytes = row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
+    const char *Kh = (const char *)p.c.K + (size_t)un.kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)un.kvh * head_bytes;
+    u32x4 kf[2][NJ];
+    uint32_t vf[2][4][VW];
+    const int k_at = 16 * kk, v_at = col * VB;               // this lane's bytes of a row (a head narrower than DH: only those inside)
+    // A stretch longer than a chunk (a long sequence that ends inside the shared positions) goes panel by panel; one panel
+    // takes both stretches where there are two.
+    for (int panel = un.a.lo;;) {
+    const int lo_a = panel, hi_a = min(un.a.hi, (panel & ~3) + CHUNK_MAX);
+    // page numbers of both stretches; -1 where there is none
+    const int first_a = lo_a >> shift, n_a = hi_a > lo_a ? ((hi_a - 1) >> shift) - first_a + 1 : 0;
+    const int first_b = un.b.lo >> shift, n_b = un.b.hi > un.b.lo ? ((un.b.hi - 1) >> shift) - first_b + 1 : 0;
+    bool bad = false;
+    for (int i = tid; i < n_a + n_b; i += NTS) {
+        const int row = i < n_a ? un.a.row : un.b.row, entry = i < n_a ? first_a + i : first_b + i - n_a;
+        const int page = as_global(p.c.table)[(size_t)row * p.c.table_stride + entry];
+        const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
+        pages[i] = ok ? page : -1;
+        bad = bad || !ok;
+    }
+    const bool any_bad = __syncthreads_or(bad);
+    if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
+    // turns of 32 keys, from a multiple of four on
+    const int base_a = lo_a & ~3, base_b = un.b.lo & ~3;
+    const int turns_a = n_a ? (hi_a - base_a + KEYS - 1) / KEYS : 0, turns_b = n_b ? (un.b.hi - base_b + KEYS - 1) / KEYS : 0, turns = turns_a + turns_b;
+    auto stretch = [&](int t, int &tb, int &lo, int &hi, int &index0) {
+        const bool in_a = t < turns_a;
+        tb = in_a ? base_a + KEYS * t : base_b + KEYS * (t - turns_a);
+        lo = in_a ? lo_a : un.b.lo;
+        hi = in_a ? hi_a : un.b.hi;
+        index0 = in_a ? -first_a : n_a - first_b;
+    };
+    auto fetch_k = [&](int t) {
+        int tb, lo, hi, index0;
+        stretch(t, tb, lo, hi, index0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int pos = min(max(tb + 16 * u + col, lo), hi - 1), page = max(pages[(pos >> shift) + index0], 0);
+            const char *row = Kh + (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * row_bytes + k_at;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if (DH > 32 || 64 * j + k_at < (int)row_bytes) kf[u][j] = global_load16(row + 64 * j);
+                else kf[u][j] = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    auto fetch_v = [&](int t) {
+        int tb, lo, hi, index0;
+        stretch(t, tb, lo, hi, index0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3), page = max(pages[(pos >> shift) + index0], 0);
+            const char *row = Vh + (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * row_bytes + v_at;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (DH > 32 || v_at < (int)row_bytes) load_words<VB>(row + r * row_bytes, vf[u][r]);
+                else {
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) vf[u][r][i] = 0;
+                }
+            }
+        }
+    };
+    int t = w;
+    if (t < turns) { fetch_k(t); fetch_v(t); }
+    for (; t < turns; t += NWS) {
+        int tb, lo, hi, index0;
+        stretch(t, tb, lo, hi, index0);
+        f32x4v st[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (rt >= tiles) break;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) st[rt][u] = f32x4v{0.f, 0.f, 0.f, 0.f};
+            if constexpr (F32) {
+                f32x4v part[2][4];               // four sums per tile: one chain of d_head / 4 products would double the error
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) part[u][c] = f32x4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const u32x4 q = Q[(rt * NJ + j) * WAVE + lane];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) part[u][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[u][j][c]), __uint_as_float(q[c]), part[u][c], 0, 0, 0);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) st[rt][u] = (part[u][0] + part[u][1]) + (part[u][2] + part[u][3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q) {
+                        const u32x4 b = Q[((rt * NJ + j) * PARTS + q) * WAVE + lane];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) st[rt][u] = mfma16<KT>(kf[u][j], b, st[rt][u]);
+                    }
+            }
+        }
+        if (t + NWS < turns) fetch_k(t + NWS);
+        // keys outside the stretch, or on no page: no score, and no value that could be a NaN
+        if (tb < lo || tb + KEYS > hi || any_bad) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
+                const bool page_ok = pages[(pos >> shift) + index0] >= 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = tb + 16 * u + 4 * kk + r;
+                    const bool in = at >= lo && at < hi && page_ok;
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) st[rt][u][r] = in ? st[rt][u][r] : -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) vf[u][r][i] = in ? vf[u][r][i] : 0;
+                }
+            }
+        }
+        uint32_t pt[RT][PARTS][4];               // 16-bit caches: eight probabilities per lane and part
+        float pf[RT][8];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (rt >= tiles) break;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    st[rt][u][r] *= scale[rt];
+                    mx = fmaxf(mx, st[rt][u][r]);
+                }
+            if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
+                mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));    // the lane groups hold different keys of the same rows
+                mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+                mx = fmaxf(mx, m[rt]);
+                const float corr = exp2_below(m[rt], mx);
+                m[rt] = mx;
+                l[rt] *= corr;
+#pragma unroll
+                for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
+            }
+            const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                pf[rt][i] = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4] - ref);
+                l[rt] += pf[rt][i];
+            }
+            if constexpr (!F32) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    uint32_t part[PARTS];
+                    parts_of<KT>(pf[rt][i], pf[rt][i + 1], part);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) pt[rt][q][i / 2] = part[q];
+                }
+            }
+        }
+        if constexpr (F32) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                if (rt >= tiles) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < FV; ++e)
+                        o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i / 4][i % 4][e]), pf[rt][i], o[rt][e], 0, 0, 0);
+            }
+        } else {
+            // two features of eight keys at a time, turned round: eight keys of each
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                u32x4 even, odd;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t x = vf[k / 2][2 * (k % 2)][i], y = vf[k / 2][2 * (k % 2) + 1][i];
+                    even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                    odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    if (rt >= tiles) break;
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q) {
+                        const u32x4 b = u32x4{pt[rt][q][0], pt[rt][q][1], pt[rt][q][2], pt[rt][q][3]};
+                        o[rt][2 * i] = mfma16<KT>(even, b, o[rt][2 * i]);
+                        o[rt][2 * i + 1] = mfma16<KT>(odd, b, o[rt][2 * i + 1]);
+                    }
+                }
+            }
+        }
+        if (t + NWS < turns) fetch_v(t + NWS);
+    }
+    panel = hi_a;
+    if (panel >= un.a.hi) break;
+    __syncthreads();                             // the page numbers have been read
+    }
+
+    // the four waves' results, a tile of rows and 128 features at a time, in wave order
+    constexpr int HALF = Lds<KT, DH, RT>::HALF, STRIDE = Lds<KT, DH, RT>::STRIDE, NH = DH / HALF, FH = FV / NH;
+    float *O = (float *)lds;
+    for (int rt = 0; rt < tiles; ++rt) {
+        float mt = m[0], lt = l[0];
+#pragma unroll
+        for (int i = 1; i < RT; ++i) { mt = i == rt ? m[i] : mt; lt = i == rt ? l[i] : lt; }
+        lt += __shfl_xor(lt, 16, WAVE);
+        lt += __shfl_xor(lt, 32, WAVE);
+        for (int h = 0; h < NH; ++h) {
+            __syncthreads();                     // Q, or the tile before, has been read
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int hh = 0; hh < NH; ++hh)
+                    if (i == rt && hh == h) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int e = 0; e < FH; ++e) O[(w * ROWS + col) * STRIDE + FH * (4 * kk + r) + e] = o[i][hh * FH + e][r];
+                    }
+            if (kk == 0) { lds_m[w][col] = mt; lds_l[w][col] = lt; }
+            __syncthreads();
+            for (int i = tid; i < ROWS * HALF / 4; i += NTS) {
+                const int row = i / (HALF / 4), c = 4 * (i % (HALF / 4)), r = un.r0 + rt * ROWS + row;
+                if (rt * ROWS + row >= un.n_rows) continue;
+                float M = lds_m[0][row], L = 0.f;
+#pragma unroll
+                for (int v = 1; v < NWS; ++v) M = fmaxf(M, lds_m[v][row]);
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int v = 0; v < NWS; ++v) {
+                    const float f = exp2_below(lds_m[v][row], M);
+                    L += f * lds_l[v][row];
+                    const float4 z = *(const float4 *)&O[(v * ROWS + row) * STRIDE + c];
+                    y.x += f * z.x; y.y += f * z.y; y.z += f * z.z; y.w += f * z.w;
+                }
+                const int feature = NH * FH * (c / FH) + h * FH + c % FH, s = un.seq + r / group, hq = un.kvh * group + r % group;
+                if (feature >= d) continue;
+                const size_t at = (size_t)s * p.n_heads + hq;
+                float *to = p.out + at * d + feature;
+                if (p.slots > 1) {
+                    to = p.part + (at * p.slots + un.slot) * d + feature;
+                    if (feature == 0) {
+                        const int len = un.shared < 0 ? 0 : as_global(p.len)[s];
+                        const bool on = un.shared < 0 || (len >= un.shared && seq_fits(p, un.shared, len));
+                        as_global(p.part_ml)[2 * (at * p.slots + un.slot)] = on ? M : -INFINITY;
+                        as_global(p.part_ml)[2 * (at * p.slots + un.slot) + 1] = on ? L : 0.f;
+                    }
+                } else {
+                    const float inv = L == 0.f ? 0.f : 1.f / L;               // (nothing seen: zeros)
+                    y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
+                }
+                if constexpr (FH >= 4) *(f32x4 __attribute__((address_space(1))) *)to = f32x4{y.x, y.y, y.z, y.w};
+                else {                            // two features of a lane lie side by side
+                    as_global(to)[0] = y.x; as_global(to)[1] = y.y;
+                    as_global(to)[2] = y.z; as_global(to)[3] = y.w;
+                }
+            }
+        }
+    }
+}
+
+// A unit without positions, or rows that take no part in it: no sum.
+__device__ __forceinline__ void nothing(const SharedAttnArgs &p, const Unit &un, int row) {
+    const int group = p.n_heads / p.c.n_kv_heads, r = un.r0 + row, s = un.seq + r / group, hq = un.kvh * group + r % group;
+    const size_t at = (size_t)s * p.n_heads + hq;
+    if (p.slots > 1) {
+        as_global(p.part_ml)[2 * (at * p.slots + un.slot)] = -INFINITY;
+        as_global(p.part_ml)[2 * (at * p.slots + un.slot) + 1] = 0.f;
+    } else {
+        for (int c = 0; c < p.c.d_head; ++c) as_global(p.out)[at * p.c.d_head + c] = 0.f;
+    }
+}
+
+template <typename KT, int DH, int RT>
+__global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs p) {
+    __shared__ __align__(16) uint32_t lds[Lds<KT, DH, RT>::WORDS];
+    __shared__ int pages[PAGES];
+    __shared__ float lds_m[NWS][ROWS], lds_l[NWS][ROWS], row_scale[RT * ROWS];
+    const int group = p.n_heads / p.c.n_kv_heads;
+    int b = blockIdx.x;
+    Unit un;
+    un.b = Stretch{0, 0, 0};
+    un.shared = -1;
+    if (b < p.shared_blocks) {
+        // row tiles of a chunk on one XCD (blocks go to the eight in turn), so that its keys come through that L2
+        const int per = 8 * p.row_tiles, chunk8 = b / per * 8 + b % 8, tile = b % per / 8;
+        if (chunk8 >= p.shared_blocks_per_tile) return;
+        const int c = chunk8 % p.shared_chunks, gh = chunk8 / p.shared_chunks, g = gh / p.c.n_kv_heads;
+        un.kvh = gh % p.c.n_kv_heads;
+        un.seq = g * p.width;
+        un.r0 = tile * RT * ROWS;
+        un.n_rows = min(p.width * group - un.r0, RT * ROWS);
+        un.slot = c;
+        int to = as_global(p.shared)[g];
+        if (p.width == 1) {                      // nothing is shared: the whole sequence
+            const int len = as_global(p.len)[g];
+            to = seq_fits(p, to, len) ? len : -1;
+        } else if (to > p.max_shared) to = -1;
+        if (to < 0 && p.err && threadIdx.x == 0) *as_global(p.err) = 1;
+        un.a = Stretch{un.seq, c * p.shared_chunk, min((c + 1) * p.shared_chunk, to)};
+        if (un.a.hi <= un.a.lo) {
+            for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
+            return;
+        }
+        if (p.width > 1) un.shared = to;
+        attend<KT, DH, RT>(p, un, lds, pages, lds_m, lds_l, row_scale);
+        return;
+    }
+    b -= p.shared_blocks;
+    const int tile = b % p.own_tiles;
+    b /= p.own_tiles;
+    const int c = b % p.own_chunks, sh = b / p.own_chunks;
+    un.kvh = sh % p.c.n_kv_heads;
+    un.seq = sh / p.c.n_kv_heads;
+    un.r0 = tile * ROWS;
+    un.n_rows = min(group - un.r0, ROWS);
+    un.slot = p.shared_chunks + c;
+    const int lead = un.seq - un.seq % p.width;
+    int shared = as_global(p.shared)[un.seq / p.width], len = as_global(p.len)[un.seq];
+    if (!seq_fits(p, shared, len)) {
+        shared = len = 0;
+        if (p.err && threadIdx.x == 0) *as_global(p.err) = 1;
+    }
+    if (p.shared_chunks == 0) {                  // one block for all of it
+        un.a = Stretch{lead, 0, min(shared, len)};
+        un.b = Stretch{un.seq, shared, max(shared, len)};
+    } else {
+        const bool within = len < shared;
+        const int lo = within ? 0 : shared, each = ((within ? len : len - shared) + p.own_chunks - 1) / p.own_chunks;
+        un.a = Stretch{within ? lead : un.seq, min(lo + c * each, len), min(lo + (c + 1) * each, len)};
+    }
+    if (un.a.hi <= un.a.lo && un.b.hi <= un.b.lo) {
+        for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
+        return;
+    }
+    attend<KT, DH, 1>(p, un, lds, pages, lds_m, lds_l, row_scale);
+}
+
+// A wave per (sequence, query head): its chunks in order.
+__global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p, int rows) {
+    const int lane = threadIdx.x & (WAVE - 1), row = blockIdx.x * NWS + threadIdx.x / WAVE, d = p.c.d_head;
+    if (row >= rows) return;
+    const float *ml = p.part_ml + 2 * (size_t)row * p.slots, *part = p.part + (size_t)row * p.slots * d;
+    float M = -INFINITY;
+    for (int i = lane; i < p.slots; i += WAVE) M = fmaxf(M, as_global(ml)[2 * i]);
+    M = wave_max(M);
+    float L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < p.slots; ++i) {
+        const float l = as_global(ml)[2 * i + 1];
+        if (l == 0.f) continue;                  // nothing there: its O was not written
+        const float f = exp2_below(as_global(ml)[2 * i], M);
+        L += f * l;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (lane + v * WAVE < d) y[v] += f * as_global(part)[(size_t)i * d + lane + v * WAVE];
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (lane + v * WAVE < d) as_global(p.out)[(size_t)row * d + lane + v * WAVE] = y[v] * inv;
+}
+
+// How a call is cut: chunks of shared and of own positions per unit, and the positions of a shared chunk.
+struct Cut { int shared_chunks, shared_chunk, own_chunks; };
+constexpr int WHOLE = 512;                       // positions up to which a sequence's block takes shared and own ones in one go
+Cut cut_for(int n_seq, int width, int n_heads, int n_kv_heads, int max_shared, int max_own) {
+    const int groups = n_seq / width, group = n_heads / n_kv_heads;
+    if (width > 1 && (long long)max_shared + max_own <= WHOLE) return Cut{0, 0, 1};
+    const long long shared = width == 1 ? (long long)max_shared + max_own : max_shared, own = width == 1 ? 0 : max_own;
+    const long long tiles = (width * group + 4 * ROWS - 1) / (4 * ROWS);
+    const long long work = shared * groups * n_kv_heads * tiles + own * n_seq * n_kv_heads;
+    long long chunk = (work + BLOCKS - 1) / BLOCKS;
+    chunk = std::min<long long>(CHUNK_MAX, std::max<long long>(NWS * KEYS, (chunk + NWS * KEYS - 1) / (NWS * KEYS) * (NWS * KEYS)));
+    return Cut{(int)std::max<long long>(1, (shared + chunk - 1) / chunk), (int)chunk, width == 1 ? 0 : (int)std::max<long long>(1, (std::max<long long>(own, 1) + chunk - 1) / chunk)};
+}
+
+template <typename KT, int DH, int RT>
+hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
+    const int group = a.n_heads / a.c.n_kv_heads, groups = a.c.n_seq / a.width;
+    a.row_tiles = (a.width * group + RT * ROWS - 1) / (RT * ROWS);
+    a.own_tiles = (group + ROWS - 1) / ROWS;
+    a.shared_blocks_per_tile = groups * a.c.n_kv_heads * a.shared_chunks;
+    const long long shared_blocks = (long long)(a.shared_blocks_per_tile + 7) / 8 * 8 * a.row_tiles;
+    const long long blocks = shared_blocks + (long long)a.c.n_seq * a.c.n_kv_heads * a.own_chunks * a.own_tiles;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    a.shared_blocks = (int)shared_blocks;
+    hipLaunchKernelGGL((shared_attn_kernel<KT, DH, RT>), dim3((unsigned)blocks), dim3(NTS), 0, s, a);
+    if (a.slots > 1) hipLaunchKernelGGL(shared_merge_kernel, dim3((unsigned)((a.c.n_seq * a.n_heads + NWS - 1) / NWS)), dim3(NTS), 0, s, a, a.c.n_seq * a.n_heads);
+    return hipGetLastError();
+}
+
+template <typename KT, int DH>
+hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a) {
+    const int rows = a.shared_chunks ? a.width * (a.n_heads / a.c.n_kv_heads) : 1;
+    if (rows <= ROWS) return launch_tiles<KT, DH, 1>(s, a);
+    if constexpr (sizeof(KT) == 4 && DH > 128) return launch_tiles<KT, DH, 1>(s, a);
+    else if constexpr (sizeof(KT) == 4 || DH > 128) return launch_tiles<KT, DH, 2>(s, a);
+    else return rows <= 2 * ROWS ? launch_tiles<KT, DH, 2>(s, a) : launch_tiles<KT, DH, 4>(s, a);
+}
+
+template <typename KT>
+hipError_t launch_width(hipStream_t s, const SharedAttnArgs &a) {
+    if (a.c.d_head <= 32) return launch_rows<KT, 32>(s, a);
+    if (a.c.d_head == 64) return launch_rows<KT, 64>(s, a);
+    if (a.c.d_head == 128) return launch_rows<KT, 128>(s, a);
+    return launch_rows<KT, 256>(s, a);
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared,
                                                         int32_t max_own) {
-    if (n_seq <= 0 || width <= 0 || n_heads <= 0 || n_kv_heads <= 0 || d_head <= 0 || max_shared < 0 || max_own < 0) return 0;
-    return 256;
+    if (n_seq <= 0 || width <= 0 || n_seq % width || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || d_head <= 0 || max_shared < 0 || max_own < 0) return 0;
+    const Cut c = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
+    const size_t parts = (size_t)n_seq * n_heads * (c.shared_chunks + c.own_chunks);
+    return c.shared_chunks + c.own_chunks > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 256;
 }
 
 extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
@@ -88,15 +612,18 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     const long long room = (long long)table_stride * page_size;      // (the longest shared and the longest own part may be different sequences')
     if (max_shared > room || max_own > room || (long long)max_shared + max_own > INT32_MAX - 65536) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
+    if ((long long)n_seq * n_heads > (1 << 24)) return SPD_EINVAL;
     if (!q || !shared || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16) return SPD_EINVAL;
     if (!scratch || (uintptr_t)scratch % 256) return SPD_EINVAL;
     if (scratch_bytes < spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own)) return SPD_EWORKSPACE;
-    const long long blocks = (long long)n_seq * n_heads;
-    if (blocks > INT32_MAX) return SPD_EINVAL;
-    const SharedAttnArgs a{c, q, out, shared, len, err, width, n_heads, max_shared, max_own};
+    const Cut cut = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
+    SharedAttnArgs a{};
+    a.c = c; a.q = q; a.out = out; a.shared = shared; a.len = len; a.err = err;
+    a.width = width; a.n_heads = n_heads; a.max_shared = max_shared; a.max_own = max_own;
+    a.shared_chunks = cut.shared_chunks; a.shared_chunk = cut.shared_chunk; a.own_chunks = cut.own_chunks; a.slots = cut.shared_chunks + cut.own_chunks;
+    a.part_ml = (float *)scratch;
+    a.part = (float *)((char *)scratch + up256((size_t)n_seq * n_heads * a.slots * 8));
     hipStream_t s = (hipStream_t)hip_stream;
-    if (dtype == SPD_DTYPE_FP32) hipLaunchKernelGGL(shared_attn_kernel<float>, dim3((unsigned)blocks), dim3(NTS), 0, s, a);
-    else if (dtype == SPD_DTYPE_FP16) hipLaunchKernelGGL(shared_attn_kernel<half_t>, dim3((unsigned)blocks), dim3(NTS), 0, s, a);
-    else hipLaunchKernelGGL(shared_attn_kernel<bf16_t>, dim3((unsigned)blocks), dim3(NTS), 0, s, a);
-    return hipGetLastError() == hipSuccess ? SPD_OK : SPD_EHIP;
+    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_width<float>(s, a) : dtype == SPD_DTYPE_FP16 ? launch_width<half_t>(s, a) : launch_width<bf16_t>(s, a);
+    return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }

@@ -32,7 +32,7 @@ SELECT = dict(dtype=0, logits=A, row_stride=1000, n_groups=2, n_in=3, n_out=4, v
 REORDER = dict(CACHE, n_layers=2, layer_stride=40 * 2 * 16 * 64, width=3, parents=4 * A, len=5 * A, table_out=6 * A, err=None, stream=None)
 
 BAD_CACHE = [("dtype", 3), ("dtype", -1), ("K", None), ("V", None), ("table", None), ("K", A + 8), ("V", A + 4), ("table", A + 2), ("n_pages", 0), ("n_kv_heads", 0),
-             ("page_size", 0), ("page_size", 24), ("page_size", 2048), ("page_size", -16), ("d_head", 4), ("d_head", 96), ("d_head", 512), ("d_head", 0), ("n_seq", -1),
+             ("page_size", 0), ("page_size", 2), ("page_size", 24), ("page_size", 2048), ("page_size", -16), ("d_head", 4), ("d_head", 96), ("d_head", 512), ("d_head", 0), ("n_seq", -1),
              ("table_stride", 0)]
 
 

@@ -86,7 +86,7 @@ def check_append(dtype, heads, kv, d, K, V, table, rows, seq, pos, theta=THETA):
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("heads,kv,d,page,lengths,start", [
-    (4, 4, 128, 16, [1, 1, 1], 70), (8, 2, 64, 32, [5, 1, 40], 0), (3, 1, 256, 8, [17, 2], 30), (1, 1, 8, 1, [3], 2), (6, 3, 16, 1024, [9, 1], 1020), (40, 40, 128, 64, [3, 2], 63),
+    (4, 4, 128, 16, [1, 1, 1], 70), (8, 2, 64, 32, [5, 1, 40], 0), (3, 1, 256, 8, [17, 2], 30), (1, 1, 8, 4, [3], 2), (6, 3, 16, 1024, [9, 1], 1020), (40, 40, 128, 64, [3, 2], 63),
     (5, 5, 32, 4, [1], 0), (64, 8, 128, 16, [300], 1)])
 def test_append(dtype, heads, kv, d, page, lengths, start):
     say("append", dtype, heads, kv, d, page, lengths, start)
@@ -200,7 +200,7 @@ def close(got, want, bound=1e-5):
     (8, 1, 64, 8, [1], [1, 2], 2), (8, 2, 128, 32, [0, 40], [1, 0, 45, 40], 2),    # one position, none, none of its own
     (6, 2, 64, 16, [37, 16], [20, 37, 38, 0, 100, 17], 3),           # shorter than the shared part; ends inside pages
     (16, 1, 128, 64, [200], [231, 263], 2), (3, 3, 256, 16, [50], [51, 83, 90], 3),
-    (10, 2, 8, 4, [9], [12, 30], 2), (4, 2, 16, 1, [3], [4, 9], 2), (2, 1, 32, 1024, [700], [701, 1030], 2),
+    (10, 2, 8, 4, [9], [12, 30], 2), (4, 2, 16, 4, [3], [4, 9], 2), (2, 1, 32, 1024, [700], [701, 1030], 2),
     (1, 1, 128, 16, [], [], 1)])
 def test_attention(dtype, heads, kv, d, page, shared, lengths, width):
     if not lengths:
@@ -226,6 +226,15 @@ def test_attention_of_long_parts_and_many_rows(dtype, heads, kv, d, shared, own,
     got, err = attend(dtype, *case, width)
     assert err == 0
     close(got, R.attention(*case, width))
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+def test_attention_of_a_long_sequence_that_ends_inside_the_shared_positions(dtype):
+    """Its block takes more positions than a chunk has, on pages of four."""
+    case = attention_case(dtype, 2, 1, 32, 4, [9001], [9003, 8999, 4097, 9001], 4, seed=13)
+    got, err = attend(dtype, *case, 4)
+    assert err == 0
+    close(got, R.attention(*case, 4))
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
@@ -416,7 +425,7 @@ def check_reorder(dtype, K, V, table, length, parents, width, want=None, want_er
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "fp32"])
-@pytest.mark.parametrize("layers,kv,d,page,lengths,width", [(3, 2, 64, 16, [37, 10], 4), (1, 1, 8, 4, [7], 2), (2, 40, 128, 16, [31], 5), (2, 3, 16, 1, [5, 2], 3), (1, 2, 256, 64, [63, 65, 1], 16),
+@pytest.mark.parametrize("layers,kv,d,page,lengths,width", [(3, 2, 64, 16, [37, 10], 4), (1, 1, 8, 4, [7], 2), (2, 40, 128, 16, [31], 5), (2, 3, 16, 4, [5, 2], 3), (1, 2, 256, 64, [63, 65, 1], 16),
                                                             (2, 1, 32, 8, [16, 0, 8], 4), (1, 1, 16, 8, [20, 20], 1)])
 def test_reorder(dtype, layers, kv, d, page, lengths, width):
     K, V, table, length = reorder_case(dtype, layers, kv, d, page, lengths, width, seed=width)
