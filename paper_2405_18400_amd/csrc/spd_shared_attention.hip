@@ -519,28 +519,53 @@ __global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs p
     attend<KT, DH, 1>(p, un, lds, pages, lds_m, lds_l, row_scale);
 }
 
-// A wave per (sequence, query head): its chunks in order.
-__global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p, int rows) {
-    const int lane = threadIdx.x & (WAVE - 1), row = blockIdx.x * NWS + threadIdx.x / WAVE, d = p.c.d_head;
-    if (row >= rows) return;
-    const float *ml = p.part_ml + 2 * (size_t)row * p.slots, *part = p.part + (size_t)row * p.slots * d;
-    float M = -INFINITY;
-    for (int i = lane; i < p.slots; i += WAVE) M = fmaxf(M, as_global(ml)[2 * i]);
-    M = wave_max(M);
-    float L = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < p.slots; ++i) {
-        const float l = as_global(ml)[2 * i + 1];
-        if (l == 0.f) continue;                  // nothing there: its O was not written
-        const float f = exp2_below(as_global(ml)[2 * i], M);
-        L += f * l;
+// A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
+// memory for up to UM * groups chunks.  Sums in a fixed order.
+constexpr int UM = 4;
+__global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p) {
+    __shared__ float4 acc[NTS];
+    __shared__ float red[NWS];
+    const int tid = threadIdx.x, d = p.c.d_head, per = d / 4, groups = NTS / per, gi = tid / per, ci = tid % per;
+    const size_t row = blockIdx.x;
+    const float *ml = p.part_ml + 2 * row * p.slots, *part = p.part + row * p.slots * d + 4 * ci;
+    float4 x[UM];
+    float xm[UM], xl[UM];
+    auto fetch = [&](int i0) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (lane + v * WAVE < d) y[v] += f * as_global(part)[(size_t)i * d + lane + v * WAVE];
+        for (int u = 0; u < UM; ++u) {
+            const int i = min(i0 + u * groups, p.slots - 1);
+            xm[u] = as_global(ml)[2 * i];
+            xl[u] = i0 + u * groups < p.slots ? as_global(ml)[2 * i + 1] : 0.f;
+            x[u] = global_load_float4(part + (size_t)i * d);
+        }
+    };
+    fetch(gi);
+    float m = -INFINITY;
+    for (int i = tid; i < p.slots; i += NTS) m = fmaxf(m, as_global(ml)[2 * i]);
+    const float M = block_max<NTS>(m, red);
+    float L = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = gi; i0 < p.slots; i0 += UM * groups) {
+        if (i0 != gi) fetch(i0);
+#pragma unroll
+        for (int u = 0; u < UM; ++u) {
+            if (xl[u] == 0.f) continue;          // nothing there: its O was not written
+            const float f = exp2_below(xm[u], M);
+            if (ci == 0) L += f * xl[u];
+            y.x += f * x[u].x; y.y += f * x[u].y; y.z += f * x[u].z; y.w += f * x[u].w;
+        }
+    }
+    L = block_sum<NTS>(L, red);
+    acc[tid] = y;
+    __syncthreads();
+    if (tid >= per) return;
+    y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int g = 0; g < groups; ++g) {
+        const float4 z = acc[g * per + tid];
+        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (lane + v * WAVE < d) as_global(p.out)[(size_t)row * d + lane + v * WAVE] = y[v] * inv;
+    *(f32x4 __attribute__((address_space(1))) *)(p.out + row * d + 4 * tid) = f32x4{y.x * inv, y.y * inv, y.z * inv, y.w * inv};
 }
 
 // How a call is cut: chunks of shared and of own positions per unit, and the positions of a shared chunk.
@@ -568,7 +593,7 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     a.shared_blocks = (int)shared_blocks;
     hipLaunchKernelGGL((shared_attn_kernel<KT, DH, RT>), dim3((unsigned)blocks), dim3(NTS), 0, s, a);
-    if (a.slots > 1) hipLaunchKernelGGL(shared_merge_kernel, dim3((unsigned)((a.c.n_seq * a.n_heads + NWS - 1) / NWS)), dim3(NTS), 0, s, a, a.c.n_seq * a.n_heads);
+    if (a.slots > 1) hipLaunchKernelGGL(shared_merge_kernel, dim3((unsigned)(a.c.n_seq * a.n_heads)), dim3(NTS), 0, s, a);
     return hipGetLastError();
 }
 
