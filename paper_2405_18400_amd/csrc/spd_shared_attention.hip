@@ -64,6 +64,15 @@ template <> __device__ __forceinline__ void parts_of<bf16_t>(float x, float y, u
     }
 }
 
+// The power of two that takes a row whose largest value is `top` to the upper end of fp16's range, and its inverse.
+__device__ __forceinline__ void scaling(float top, float &up, float &down) {
+    int ex = 15;
+    if (top > 0.f && top < INFINITY) (void)frexpf(top, &ex);
+    ex = max(ex, -100);
+    up = ldexpf(1.f, 15 - ex);
+    down = ldexpf(1.f, ex - 15);
+}
+
 template <typename KT> __device__ __forceinline__ f32x4v mfma16(u32x4 a, u32x4 b, f32x4v c);
 template <> __device__ __forceinline__ f32x4v mfma16<half_t>(u32x4 a, u32x4 b, f32x4v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -141,11 +150,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
         if constexpr (sizeof(KT) == 2 && PARTS == 2) {
 #pragma unroll
             for (int o = 1; o < TPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
-            int ex = 15;
-            if (top > 0.f && top < INFINITY) (void)frexpf(top, &ex);
-            ex = max(ex, -100);
-            up = ldexpf(1.f, 15 - ex);
-            down = ldexpf(1.f, ex - 15);
+            scaling(top, up, down);
         }
         if (t == 0) row_scale[row] = down * (1.4426950408889634f / sqrtf((float)d));     // to logarithms of base 2
 #pragma unroll
@@ -442,6 +447,239 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
     }
 }
 
+// Many rows: the block's four waves share out ROWS instead of keys, so nothing has to be put together at the end.  Keys and values
+// come through LDS, 16 bytes per lane straight from memory, ST stages of SK keys deep; pieces of a row are permuted by the row number,
+// so that neither the operand reads (16 rows side by side) nor the row reads meet in a bank.  One barrier per stage says both "this
+// stage has arrived" and "the one before has been read".
+template <int DH> struct Stage {
+    static constexpr int SK = DH == 64 ? 64 : 32, ROWB = DH * 2, PIECES = ROWB / 16;   // keys; bytes and 16-byte pieces of a row
+    static constexpr int HALF = SK * ROWB, BYTES = 2 * HALF;                            // K, then V
+    static constexpr int LOADS = HALF / 16 / NTS;                                       // pieces per thread, of K as of V
+    static constexpr int ST = DH == 256 ? 3 : 4;
+};
+template <int DH> __device__ __forceinline__ int permuted(int row, int piece) {
+    return Stage<DH>::PIECES >= 16 ? piece ^ (row & 15) : piece ^ ((row & 7) ^ ((row >> 3) & 1));
+}
+__device__ __forceinline__ void to_lds16(const char *from, char *to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+#endif
+}
+
+template <typename KT, int DH, int RT>
+__device__ __forceinline__ void attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, int *pages) {
+    constexpr int PARTS = Type<KT>::PARTS, NJ = DH / 32, FV = DH / 16, VW = FV / 2;
+    constexpr int SK = Stage<DH>::SK, ROWB = Stage<DH>::ROWB, PIECES = Stage<DH>::PIECES, HALF = Stage<DH>::HALF, BYTES = Stage<DH>::BYTES, LOADS = Stage<DH>::LOADS, ST = Stage<DH>::ST;
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
+    const int shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
+    const int row0 = w * RT * ROWS;                          // this wave's rows of the unit
+    const int lo = un.a.lo, hi = un.a.hi, first = lo >> shift, n_pages = ((hi - 1) >> shift) - first + 1;
+    bool bad = false;
+    for (int i = tid; i < n_pages; i += NTS) {
+        const int page = as_global(p.c.table)[(size_t)un.a.row * p.c.table_stride + first + i];
+        const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
+        pages[i] = ok ? page : -1;
+        bad = bad || !ok;
+    }
+    const bool any_bad = __syncthreads_or(bad);
+    if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
+
+    const int base = lo & ~3, stages = (hi - base + SK - 1) / SK;
+    const size_t head_bytes = (size_t)ROWB << shift, page_bytes = head_bytes * p.c.n_kv_heads;
+    const char *Kh = (const char *)p.c.K + (size_t)un.kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)un.kvh * head_bytes;
+    auto fetch = [&](int t) {
+        char *to = lds + (t % ST) * BYTES + w * (WAVE * 16);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = tid + i * NTS, key = at / PIECES, pos = min(max(base + t * SK + key, lo), hi - 1), page = max(pages[(pos >> shift) - first], 0);
+            const size_t from = (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * ROWB + 16 * permuted<DH>(key, at % PIECES);
+            to_lds16(Kh + from, to + i * (NTS * 16));
+            to_lds16(Vh + from, to + HALF + i * (NTS * 16));
+        }
+    };
+#pragma unroll
+    for (int t = 0; t < ST - 1; ++t)
+        if (t < stages) fetch(t);
+
+    // this lane's queries: row col of each tile, features 32 j + 8 kk .. + 7
+    u32x4 Q[RT][NJ][PARTS];
+    float scale[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int rr = un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), s = un.seq + rr / group, hq = un.kvh * group + rr % group;   // (rows past the last repeat it)
+        const float *q = p.q + ((size_t)s * p.n_heads + hq) * DH + 8 * kk;
+        float x[NJ][8], top = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                const float4 v = global_load_float4(q + 32 * j + e);
+                x[j][e] = v.x; x[j][e + 1] = v.y; x[j][e + 2] = v.z; x[j][e + 3] = v.w;
+            }
+        float up = 1.f, down = 1.f;
+        if constexpr (PARTS == 2) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
+            top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+            top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+            scaling(top, up, down);
+        }
+        scale[rt] = down * (1.4426950408889634f / sqrtf((float)DH));
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                uint32_t part[PARTS];
+                parts_of<KT>(x[j][e] * up, x[j][e + 1] * up, part);
+#pragma unroll
+                for (int q2 = 0; q2 < PARTS; ++q2) Q[rt][j][q2][e / 2] = part[q2];
+            }
+    }
+    f32x4v o[RT][FV];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int e = 0; e < FV; ++e) o[rt][e] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        m[rt] = -INFINITY; l[rt] = 0.f;
+    }
+    for (int t = 0; t < stages; ++t) {
+        // the oldest stage under way has arrived (of this wave's loads: at most the ST - 2 younger ones are out)
+        const int younger = min(stages - 1 - t, ST - 2);
+        if (younger >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * 2 * LOADS) : "memory");
+        else if (younger == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + ST - 1 < stages) fetch(t + ST - 1);
+        const char *k_tile = lds + (t % ST) * BYTES, *v_tile = k_tile + HALF;
+#pragma unroll
+        for (int sub = 0; sub < SK / KEYS; ++sub) {
+            const int tb = base + t * SK + sub * KEYS;
+            f32x4v st[RT][2];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) st[rt][u] = f32x4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int key = sub * KEYS + 16 * u + col;
+                    const u32x4 k = *(const u32x4 *)(k_tile + key * ROWB + 16 * permuted<DH>(key, 4 * j + kk));
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) st[rt][u] = mfma16<KT>(k, Q[rt][j][q], st[rt][u]);
+                }
+            uint32_t vf[2][4][VW];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = sub * KEYS + 16 * u + 4 * kk + r;
+#pragma unroll
+                    for (int i = 0; i < VW; i += (VW < 4 ? VW : 4)) {
+                        const int byte = 2 * FV * col + 4 * i;
+                        const char *from = v_tile + key * ROWB + 16 * permuted<DH>(key, byte / 16) + byte % 16;
+                        if constexpr (VW == 2) {
+                            const u32x2 v = *(const u32x2 *)from;
+                            vf[u][r][0] = v.x; vf[u][r][1] = v.y;
+                        } else {
+                            const u32x4 v = *(const u32x4 *)from;
+                            vf[u][r][i] = v.x; vf[u][r][i + 1] = v.y; vf[u][r][i + 2] = v.z; vf[u][r][i + 3] = v.w;
+                        }
+                    }
+                }
+            if (tb < lo || tb + KEYS > hi || any_bad) {      // keys that do not count: no score, no value that could be a NaN
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
+                    const bool page_ok = pages[(pos >> shift) - first] >= 0;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int at = tb + 16 * u + 4 * kk + r;
+                        const bool in = at >= lo && at < hi && page_ok;
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) st[rt][u][r] = in ? st[rt][u][r] : -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < VW; ++i) vf[u][r][i] = in ? vf[u][r][i] : 0;
+                    }
+                }
+            }
+            u32x4 pt[RT][PARTS];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        st[rt][u][r] *= scale[rt];
+                        mx = fmaxf(mx, st[rt][u][r]);
+                    }
+                if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
+                    mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+                    mx = fmaxf(mx, m[rt]);
+                    const float corr = exp2_below(m[rt], mx);
+                    m[rt] = mx;
+                    l[rt] *= corr;
+#pragma unroll
+                    for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
+                }
+                const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4] - ref), p1 = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4 + 1] - ref);
+                    l[rt] += p0 + p1;
+                    uint32_t part[PARTS];
+                    parts_of<KT>(p0, p1, part);
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q) pt[rt][q][i / 2] = part[q];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                u32x4 even, odd;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t x = vf[k / 2][2 * (k % 2)][i], y = vf[k / 2][2 * (k % 2) + 1][i];
+                    even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                    odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                }
+#pragma unroll
+                for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        o[rt][2 * i] = mfma16<KT>(even, pt[rt][q], o[rt][2 * i]);
+                        o[rt][2 * i + 1] = mfma16<KT>(odd, pt[rt][q], o[rt][2 * i + 1]);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 16, WAVE);
+        l[rt] += __shfl_xor(l[rt], 32, WAVE);
+        const int r = row0 + rt * ROWS + col, rr = un.r0 + r, s = un.seq + rr / group, hq = un.kvh * group + rr % group;
+        if (r >= un.n_rows) continue;
+        const size_t at = ((size_t)s * p.n_heads + hq) * p.slots + un.slot;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < FV; e += 4)
+                *(f32x4 __attribute__((address_space(1))) *)(p.part + at * DH + FV * (4 * kk + i) + e) = f32x4{o[rt][e][i], o[rt][e + 1][i], o[rt][e + 2][i], o[rt][e + 3][i]};
+        if (kk == 0) {
+            const int len = as_global(p.len)[s];
+            const bool on = len >= un.shared && seq_fits(p, un.shared, len);
+            as_global(p.part_ml)[2 * at] = on ? m[rt] : -INFINITY;
+            as_global(p.part_ml)[2 * at + 1] = on ? l[rt] : 0.f;
+        }
+    }
+}
+
 // A unit without positions, or rows that take no part in it: no sum.
 __device__ __forceinline__ void nothing(const SharedAttnArgs &p, const Unit &un, int row) {
     const int group = p.n_heads / p.c.n_kv_heads, r = un.r0 + row, s = un.seq + r / group, hq = un.kvh * group + r % group;
@@ -454,9 +692,11 @@ __device__ __forceinline__ void nothing(const SharedAttnArgs &p, const Unit &un,
     }
 }
 
-template <typename KT, int DH, int RT>
-__global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs p) {
-    __shared__ __align__(16) uint32_t lds[Lds<KT, DH, RT>::WORDS];
+// TILE: query rows of a shared block; MANY: its waves share out rows, not keys.
+template <typename KT, int DH, int TILE, bool MANY>
+__global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 256 && TILE == ROWS) ? 2 : 1) void shared_attn_kernel(const SharedAttnArgs p) {
+    constexpr int RT = MANY ? 1 : TILE / ROWS;
+    extern __shared__ __align__(1024) uint32_t lds[];        // lds_bytes()
     __shared__ int pages[PAGES];
     __shared__ float lds_m[NWS][ROWS], lds_l[NWS][ROWS], row_scale[RT * ROWS];
     const int group = p.n_heads / p.c.n_kv_heads;
@@ -471,8 +711,8 @@ __global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs p
         const int c = chunk8 % p.shared_chunks, gh = chunk8 / p.shared_chunks, g = gh / p.c.n_kv_heads;
         un.kvh = gh % p.c.n_kv_heads;
         un.seq = g * p.width;
-        un.r0 = tile * RT * ROWS;
-        un.n_rows = min(p.width * group - un.r0, RT * ROWS);
+        un.r0 = tile * TILE;
+        un.n_rows = min(p.width * group - un.r0, TILE);
         un.slot = c;
         int to = as_global(p.shared)[g];
         if (p.width == 1) {                      // nothing is shared: the whole sequence
@@ -486,7 +726,8 @@ __global__ __launch_bounds__(NTS) void shared_attn_kernel(const SharedAttnArgs p
             return;
         }
         if (p.width > 1) un.shared = to;
-        attend<KT, DH, RT>(p, un, lds, pages, lds_m, lds_l, row_scale);
+        if constexpr (MANY) attend_many<KT, DH, TILE / (NWS * ROWS)>(p, un, (char *)lds, pages);
+        else attend<KT, DH, RT>(p, un, lds, pages, lds_m, lds_l, row_scale);
         return;
     }
     b -= p.shared_blocks;
@@ -582,17 +823,29 @@ Cut cut_for(int n_seq, int width, int n_heads, int n_kv_heads, int max_shared, i
     return Cut{(int)std::max<long long>(1, (shared + chunk - 1) / chunk), (int)chunk, width == 1 ? 0 : (int)std::max<long long>(1, (std::max<long long>(own, 1) + chunk - 1) / chunk)};
 }
 
-template <typename KT, int DH, int RT>
+template <typename KT, int DH, int TILE, bool MANY>
+constexpr int lds_bytes() {
+    int b = 4 * Lds<KT, DH, MANY ? 1 : TILE / ROWS>::WORDS;
+    if constexpr (MANY) b = std::max(b, Stage<DH>::ST * Stage<DH>::BYTES);
+    return b;
+}
+
+template <typename KT, int DH, int TILE, bool MANY>
 hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
     const int group = a.n_heads / a.c.n_kv_heads, groups = a.c.n_seq / a.width;
-    a.row_tiles = (a.width * group + RT * ROWS - 1) / (RT * ROWS);
+    a.row_tiles = (a.width * group + TILE - 1) / TILE;
     a.own_tiles = (group + ROWS - 1) / ROWS;
     a.shared_blocks_per_tile = groups * a.c.n_kv_heads * a.shared_chunks;
     const long long shared_blocks = (long long)(a.shared_blocks_per_tile + 7) / 8 * 8 * a.row_tiles;
     const long long blocks = shared_blocks + (long long)a.c.n_seq * a.c.n_kv_heads * a.own_chunks * a.own_tiles;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     a.shared_blocks = (int)shared_blocks;
-    hipLaunchKernelGGL((shared_attn_kernel<KT, DH, RT>), dim3((unsigned)blocks), dim3(NTS), 0, s, a);
+    constexpr int lds = lds_bytes<KT, DH, TILE, MANY>();
+    if (lds > 60 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)shared_attn_kernel<KT, DH, TILE, MANY>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((shared_attn_kernel<KT, DH, TILE, MANY>), dim3((unsigned)blocks), dim3(NTS), lds, s, a);
     if (a.slots > 1) hipLaunchKernelGGL(shared_merge_kernel, dim3((unsigned)(a.c.n_seq * a.n_heads)), dim3(NTS), 0, s, a);
     return hipGetLastError();
 }
@@ -600,10 +853,16 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
 template <typename KT, int DH>
 hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a) {
     const int rows = a.shared_chunks ? a.width * (a.n_heads / a.c.n_kv_heads) : 1;
-    if (rows <= ROWS) return launch_tiles<KT, DH, 1>(s, a);
-    if constexpr (sizeof(KT) == 4 && DH > 128) return launch_tiles<KT, DH, 1>(s, a);
-    else if constexpr (sizeof(KT) == 4 || DH > 128) return launch_tiles<KT, DH, 2>(s, a);
-    else return rows <= 2 * ROWS ? launch_tiles<KT, DH, 2>(s, a) : launch_tiles<KT, DH, 4>(s, a);
+    if constexpr (sizeof(KT) == 4 && DH > 128) return launch_tiles<KT, DH, ROWS, false>(s, a);
+    else {
+        if (rows <= ROWS) return launch_tiles<KT, DH, ROWS, false>(s, a);
+        if constexpr (sizeof(KT) == 2 && DH >= 64) {         // (sequences on their own may have one chunk, whose block writes the output: the other kernel)
+            if constexpr (DH <= 128 && Type<KT>::PARTS == 2)
+                if (rows > 4 * ROWS && a.width > 1) return launch_tiles<KT, DH, 8 * ROWS, true>(s, a);
+            if (rows > 2 * ROWS && a.width > 1) return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
+        }
+        return launch_tiles<KT, DH, 2 * ROWS, false>(s, a);
+    }
 }
 
 template <typename KT>
