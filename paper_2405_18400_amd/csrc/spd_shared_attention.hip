@@ -118,8 +118,10 @@ struct Lds {
 
 constexpr int PAGES = CHUNK_MAX / PAGE_MIN + 4;
 
-template <typename KT, int DH, int RT>
-__device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, uint32_t *lds, int *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
+// `resolve` reads the lengths and sets the stretches; false: there are none.  Queries are asked for before that, page numbers before
+// the queries are put in place: each of these is a trip to memory.
+template <typename KT, int DH, int RT, typename F>
+__device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&resolve, uint32_t *lds, int *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
     constexpr bool F32 = sizeof(KT) == 4;
     constexpr int PARTS = Type<KT>::PARTS;
     constexpr int NJ = F32 ? DH / 16 : DH / 32;                              // 16-byte pieces of a key per lane
@@ -128,40 +130,53 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
     const int d = p.c.d_head, shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
     const int tiles = (min(un.n_rows, RT * ROWS) + ROWS - 1) / ROWS;
 
-    // queries, as the products take them: piece (step j, part) of a tile holds a lane's eight (fp32: four) features
+    constexpr int TPR = NTS / (RT * ROWS), N8 = DH / 8, PP = (N8 + TPR - 1) / TPR;       // threads per row; pieces of eight features
+    const int q_row = tid / TPR, q_t = tid % TPR;
+    float x[PP][8];
     {
-        constexpr int TPR = NTS / (RT * ROWS), N8 = DH / 8, PP = (N8 + TPR - 1) / TPR;   // threads per row; pieces of eight features
-        const int row = tid / TPR, t = tid % TPR;
-        const int r = un.r0 + row, s = un.seq + r / group, hq = un.kvh * group + r % group;
-        float x[PP][8], top = 0.f;
+        const int r = un.r0 + min(q_row, un.n_rows - 1), s = un.seq + r / group, hq = un.kvh * group + r % group;   // (rows past the last repeat it)
+        const float *q = p.q + ((size_t)s * p.n_heads + hq) * d;
 #pragma unroll
-        for (int i = 0; i < PP; ++i) {
-            const int at = 8 * (t + i * TPR);
+        for (int i = 0; i < PP; ++i)
 #pragma unroll
             for (int e = 0; e < 8; e += 4) {
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (row < un.n_rows && at + e < d) v = global_load_float4(p.q + ((size_t)s * p.n_heads + hq) * d + at + e);
+                const int at = 8 * (q_t + i * TPR) + e;
+                const float4 v = at < d ? global_load_float4(q + at) : make_float4(0.f, 0.f, 0.f, 0.f);
                 x[i][e] = v.x; x[i][e + 1] = v.y; x[i][e + 2] = v.z; x[i][e + 3] = v.w;
             }
+    }
+    if (!resolve(un)) return false;
+    auto entry_page = [&](int lo_a, int n_a, int lo_b, int i) {
+        const int row = i < n_a ? un.a.row : un.b.row, entry = i < n_a ? (lo_a >> shift) + i : (lo_b >> shift) + i - n_a;
+        return as_global(p.c.table)[(size_t)row * p.c.table_stride + entry];
+    };
+    auto pages_of = [&](int lo, int hi) { return hi > lo ? ((hi - 1) >> shift) - (lo >> shift) + 1 : 0; };
+    const int first_n_a = pages_of(un.a.lo, min(un.a.hi, (un.a.lo & ~3) + CHUNK_MAX)), first_n = first_n_a + pages_of(un.b.lo, un.b.hi);
+    int early_page = 0;
+    if (tid < first_n) early_page = entry_page(un.a.lo, first_n_a, un.b.lo, tid);
+    // queries, as the products take them: piece (step j, part) of a tile holds a lane's eight (fp32: four) features
+    {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < PP; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
-        }
         float up = 1.f, down = 1.f;
         if constexpr (sizeof(KT) == 2 && PARTS == 2) {
 #pragma unroll
             for (int o = 1; o < TPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
             scaling(top, up, down);
         }
-        if (t == 0) row_scale[row] = down * (1.4426950408889634f / sqrtf((float)d));     // to logarithms of base 2
+        if (q_t == 0) row_scale[q_row] = down * (1.4426950408889634f / sqrtf((float)d));     // to logarithms of base 2
 #pragma unroll
         for (int i = 0; i < PP; ++i) {
-            const int piece = t + i * TPR;
+            const int piece = q_t + i * TPR;
             if (piece >= N8) break;
             if constexpr (F32) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {    // feature 16 j + 4 kk + c of piece j: word c
                     const int f = 8 * piece + e;
-                    lds[(((row / ROWS) * NJ + f / 16) * WAVE + ((f / 4) % 4) * ROWS + row % ROWS) * 4 + f % 4] = __float_as_uint(x[i][e]);
+                    lds[(((q_row / ROWS) * NJ + f / 16) * WAVE + ((f / 4) % 4) * ROWS + q_row % ROWS) * 4 + f % 4] = __float_as_uint(x[i][e]);
                 }
             } else {
 #pragma unroll
@@ -170,12 +185,11 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
                     parts_of<KT>(x[i][e] * up, x[i][e + 1] * up, part);
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q)
-                        lds[((((row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + row % ROWS) * 4 + e / 2] = part[q];
+                        lds[((((q_row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + q_row % ROWS) * 4 + e / 2] = part[q];
                 }
             }
         }
     }
-    __syncthreads();
     const u32x4 *Q = (const u32x4 *)lds;
     f32x4v o[RT][FV];
     float m[RT], l[RT], scale[RT];
@@ -183,7 +197,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
     for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
         for (int e = 0; e < FV; ++e) o[rt][e] = f32x4v{0.f, 0.f, 0.f, 0.f};
-        m[rt] = -INFINITY; l[rt] = 0.f; scale[rt] = row_scale[rt * ROWS + col];
+        m[rt] = -INFINITY; l[rt] = 0.f;
     }
 
     const size_t row_bytes = (size_t)d * sizeof(KT), head_bytes = row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
@@ -196,18 +210,18 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
     for (int panel = un.a.lo;;) {
     const int lo_a = panel, hi_a = min(un.a.hi, (panel & ~3) + CHUNK_MAX);
     // page numbers of both stretches; -1 where there is none
-    const int first_a = lo_a >> shift, n_a = hi_a > lo_a ? ((hi_a - 1) >> shift) - first_a + 1 : 0;
-    const int first_b = un.b.lo >> shift, n_b = un.b.hi > un.b.lo ? ((un.b.hi - 1) >> shift) - first_b + 1 : 0;
+    const int first_a = lo_a >> shift, n_a = pages_of(lo_a, hi_a), first_b = un.b.lo >> shift, n_b = pages_of(un.b.lo, un.b.hi);
     bool bad = false;
     for (int i = tid; i < n_a + n_b; i += NTS) {
-        const int row = i < n_a ? un.a.row : un.b.row, entry = i < n_a ? first_a + i : first_b + i - n_a;
-        const int page = as_global(p.c.table)[(size_t)row * p.c.table_stride + entry];
+        const int page = i == tid && panel == un.a.lo ? early_page : entry_page(lo_a, n_a, un.b.lo, i);
         const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
         pages[i] = ok ? page : -1;
         bad = bad || !ok;
     }
     const bool any_bad = __syncthreads_or(bad);
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) scale[rt] = row_scale[rt * ROWS + col];
     // turns of 32 keys, from a multiple of four on
     const int base_a = lo_a & ~3, base_b = un.b.lo & ~3;
     const int turns_a = n_a ? (hi_a - base_a + KEYS - 1) / KEYS : 0, turns_b = n_b ? (un.b.hi - base_b + KEYS - 1) / KEYS : 0, turns = turns_a + turns_b;
@@ -445,6 +459,7 @@ __device__ __forceinline__ void attend(const SharedAttnArgs &p, const Unit &un, 
             }
         }
     }
+    return true;
 }
 
 // Many rows: the block's four waves share out ROWS instead of keys, so nothing has to be put together at the end.  Keys and values
@@ -466,17 +481,40 @@ __device__ __forceinline__ void to_lds16(const char *from, char *to) {
 #endif
 }
 
+// False: none of the chunk's positions is there.
 template <typename KT, int DH, int RT>
-__device__ __forceinline__ void attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, int *pages) {
+__device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, int *pages) {
     constexpr int PARTS = Type<KT>::PARTS, NJ = DH / 32, FV = DH / 16, VW = FV / 2;
     constexpr int SK = Stage<DH>::SK, ROWB = Stage<DH>::ROWB, PIECES = Stage<DH>::PIECES, HALF = Stage<DH>::HALF, BYTES = Stage<DH>::BYTES, LOADS = Stage<DH>::LOADS, ST = Stage<DH>::ST;
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
     const int shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
     const int row0 = w * RT * ROWS;                          // this wave's rows of the unit
-    const int lo = un.a.lo, hi = un.a.hi, first = lo >> shift, n_pages = ((hi - 1) >> shift) - first + 1;
+    // asked for at once: the queries, the group's shared length and the page numbers of the whole chunk
+    float x[RT][NJ][8];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int rr = un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), s = un.seq + rr / group, hq = un.kvh * group + rr % group;   // (rows past the last repeat it)
+        const float *q = p.q + ((size_t)s * p.n_heads + hq) * DH + 8 * kk;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                const float4 v = global_load_float4(q + 32 * j + e);
+                x[rt][j][e] = v.x; x[rt][j][e + 1] = v.y; x[rt][j][e + 2] = v.z; x[rt][j][e + 3] = v.w;
+            }
+    }
+    const int lo = un.a.lo, first = lo >> shift;
+    const int last = min((un.a.hi - 1) >> shift, p.c.table_stride - 1);
+    int page = 0;
+    const int32_t *entries = p.c.table + (size_t)un.a.row * p.c.table_stride + first;
+    if (tid <= last - first) page = as_global(entries)[tid];
+    const int to = as_global(p.shared)[un.seq / p.width], hi = min(un.a.hi, to);
+    if ((to < 0 || to > p.max_shared) && p.err && tid == 0) *as_global(p.err) = 1;
+    if (hi <= lo || to > p.max_shared) return false;
+    const int n_pages = ((hi - 1) >> shift) - first + 1;     // (at most the row's entries: max_shared is)
     bool bad = false;
     for (int i = tid; i < n_pages; i += NTS) {
-        const int page = as_global(p.c.table)[(size_t)un.a.row * p.c.table_stride + first + i];
+        if (i != tid) page = as_global(entries)[i];
         const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
         pages[i] = ok ? page : -1;
         bad = bad || !ok;
@@ -506,22 +544,13 @@ __device__ __forceinline__ void attend_many(const SharedAttnArgs &p, const Unit 
     float scale[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int rr = un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), s = un.seq + rr / group, hq = un.kvh * group + rr % group;   // (rows past the last repeat it)
-        const float *q = p.q + ((size_t)s * p.n_heads + hq) * DH + 8 * kk;
-        float x[NJ][8], top = 0.f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const float4 v = global_load_float4(q + 32 * j + e);
-                x[j][e] = v.x; x[j][e + 1] = v.y; x[j][e + 2] = v.z; x[j][e + 3] = v.w;
-            }
+        float top = 0.f;
         float up = 1.f, down = 1.f;
         if constexpr (PARTS == 2) {
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[rt][j][e]));
             top = fmaxf(top, __shfl_xor(top, 16, WAVE));
             top = fmaxf(top, __shfl_xor(top, 32, WAVE));
             scaling(top, up, down);
@@ -532,7 +561,7 @@ __device__ __forceinline__ void attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
                 uint32_t part[PARTS];
-                parts_of<KT>(x[j][e] * up, x[j][e + 1] * up, part);
+                parts_of<KT>(x[rt][j][e] * up, x[rt][j][e + 1] * up, part);
 #pragma unroll
                 for (int q2 = 0; q2 < PARTS; ++q2) Q[rt][j][q2][e / 2] = part[q2];
             }
@@ -659,25 +688,37 @@ __device__ __forceinline__ void attend_many(const SharedAttnArgs &p, const Unit 
             }
         }
     }
+    // O by rows, through LDS (a lane's features of a row are FV here and FV there): whole lines
+    constexpr int STRIDE = DH + 4;
+    float *O = (float *)lds + w * ROWS * STRIDE;
+    __syncthreads();                                         // the stages have been read
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] += __shfl_xor(l[rt], 16, WAVE);
         l[rt] += __shfl_xor(l[rt], 32, WAVE);
-        const int r = row0 + rt * ROWS + col, rr = un.r0 + r, s = un.seq + rr / group, hq = un.kvh * group + rr % group;
-        if (r >= un.n_rows) continue;
-        const size_t at = ((size_t)s * p.n_heads + hq) * p.slots + un.slot;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < FV; e += 4)
-                *(f32x4 __attribute__((address_space(1))) *)(p.part + at * DH + FV * (4 * kk + i) + e) = f32x4{o[rt][e][i], o[rt][e + 1][i], o[rt][e + 2][i], o[rt][e + 3][i]};
-        if (kk == 0) {
-            const int len = as_global(p.len)[s];
-            const bool on = len >= un.shared && seq_fits(p, un.shared, len);
-            as_global(p.part_ml)[2 * at] = on ? m[rt] : -INFINITY;
-            as_global(p.part_ml)[2 * at + 1] = on ? l[rt] : 0.f;
+            for (int e = 0; e < FV; e += 4) *(f32x4v *)&O[col * STRIDE + FV * (4 * kk + i) + e] = f32x4v{o[rt][e][i], o[rt][e + 1][i], o[rt][e + 2][i], o[rt][e + 3][i]};
+        auto place = [&](int r) { return ((size_t)(un.seq + (un.r0 + r) / group) * p.n_heads + un.kvh * group + (un.r0 + r) % group) * p.slots + un.slot; };
+        const int r = row0 + rt * ROWS + col;
+        if (kk == 0 && r < un.n_rows) {
+            const int len = as_global(p.len)[un.seq + (un.r0 + r) / group];
+            const bool on = len >= to && seq_fits(p, to, len);
+            as_global(p.part_ml)[2 * place(r)] = on ? m[rt] : -INFINITY;
+            as_global(p.part_ml)[2 * place(r) + 1] = on ? l[rt] : 0.f;
         }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < ROWS * DH / 4 / WAVE; ++i) {
+            const int at = lane + i * WAVE, row = at / (DH / 4), c = 4 * (at % (DH / 4));
+            const f32x4v y = *(const f32x4v *)&O[row * STRIDE + c];
+            if (row0 + rt * ROWS + row < un.n_rows)
+                *(f32x4 __attribute__((address_space(1))) *)(p.part + place(row0 + rt * ROWS + row) * DH + c) = f32x4{y[0], y[1], y[2], y[3]};
+        }
+        __builtin_amdgcn_wave_barrier();
     }
+    return true;
 }
 
 // A unit without positions, or rows that take no part in it: no sum.
@@ -714,20 +755,27 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 256
         un.r0 = tile * TILE;
         un.n_rows = min(p.width * group - un.r0, TILE);
         un.slot = c;
-        int to = as_global(p.shared)[g];
-        if (p.width == 1) {                      // nothing is shared: the whole sequence
-            const int len = as_global(p.len)[g];
-            to = seq_fits(p, to, len) ? len : -1;
-        } else if (to > p.max_shared) to = -1;
-        if (to < 0 && p.err && threadIdx.x == 0) *as_global(p.err) = 1;
-        un.a = Stretch{un.seq, c * p.shared_chunk, min((c + 1) * p.shared_chunk, to)};
-        if (un.a.hi <= un.a.lo) {
-            for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
-            return;
+        if constexpr (MANY) {
+            un.a = Stretch{un.seq, c * p.shared_chunk, (c + 1) * p.shared_chunk};
+            if (!attend_many<KT, DH, TILE / (NWS * ROWS)>(p, un, (char *)lds, pages))
+                for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
+        } else {
+            const auto resolve = [&](Unit &u) {
+                int to = as_global(p.shared)[g];
+                if (p.width == 1) {              // nothing is shared: the whole sequence
+                    const int len = as_global(p.len)[g];
+                    to = seq_fits(p, to, len) ? len : -1;
+                } else {
+                    if (to > p.max_shared) to = -1;
+                    u.shared = to;
+                }
+                if (to < 0 && p.err && threadIdx.x == 0) *as_global(p.err) = 1;
+                u.a = Stretch{u.seq, c * p.shared_chunk, min((c + 1) * p.shared_chunk, to)};
+                return u.a.hi > u.a.lo;
+            };
+            if (!attend<KT, DH, RT>(p, un, resolve, lds, pages, lds_m, lds_l, row_scale))
+                for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
         }
-        if (p.width > 1) un.shared = to;
-        if constexpr (MANY) attend_many<KT, DH, TILE / (NWS * ROWS)>(p, un, (char *)lds, pages);
-        else attend<KT, DH, RT>(p, un, lds, pages, lds_m, lds_l, row_scale);
         return;
     }
     b -= p.shared_blocks;
@@ -739,25 +787,25 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 256
     un.r0 = tile * ROWS;
     un.n_rows = min(group - un.r0, ROWS);
     un.slot = p.shared_chunks + c;
-    const int lead = un.seq - un.seq % p.width;
-    int shared = as_global(p.shared)[un.seq / p.width], len = as_global(p.len)[un.seq];
-    if (!seq_fits(p, shared, len)) {
-        shared = len = 0;
-        if (p.err && threadIdx.x == 0) *as_global(p.err) = 1;
-    }
-    if (p.shared_chunks == 0) {                  // one block for all of it
-        un.a = Stretch{lead, 0, min(shared, len)};
-        un.b = Stretch{un.seq, shared, max(shared, len)};
-    } else {
-        const bool within = len < shared;
-        const int lo = within ? 0 : shared, each = ((within ? len : len - shared) + p.own_chunks - 1) / p.own_chunks;
-        un.a = Stretch{within ? lead : un.seq, min(lo + c * each, len), min(lo + (c + 1) * each, len)};
-    }
-    if (un.a.hi <= un.a.lo && un.b.hi <= un.b.lo) {
+    const auto resolve = [&](Unit &u) {
+        const int lead = u.seq - u.seq % p.width;
+        int shared = as_global(p.shared)[u.seq / p.width], len = as_global(p.len)[u.seq];
+        if (!seq_fits(p, shared, len)) {
+            shared = len = 0;
+            if (p.err && threadIdx.x == 0) *as_global(p.err) = 1;
+        }
+        if (p.shared_chunks == 0) {              // one block for all of it
+            u.a = Stretch{lead, 0, min(shared, len)};
+            u.b = Stretch{u.seq, shared, max(shared, len)};
+        } else {
+            const bool within = len < shared;
+            const int lo = within ? 0 : shared, each = ((within ? len : len - shared) + p.own_chunks - 1) / p.own_chunks;
+            u.a = Stretch{within ? lead : u.seq, min(lo + c * each, len), min(lo + (c + 1) * each, len)};
+        }
+        return u.a.hi > u.a.lo || u.b.hi > u.b.lo;
+    };
+    if (!attend<KT, DH, 1>(p, un, resolve, lds, pages, lds_m, lds_l, row_scale))
         for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
-        return;
-    }
-    attend<KT, DH, 1>(p, un, lds, pages, lds_m, lds_l, row_scale);
 }
 
 // A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
@@ -859,7 +907,7 @@ hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a) {
         if constexpr (sizeof(KT) == 2 && DH >= 64) {         // (sequences on their own may have one chunk, whose block writes the output: the other kernel)
             if constexpr (DH <= 128 && Type<KT>::PARTS == 2)
                 if (rows > 4 * ROWS && a.width > 1) return launch_tiles<KT, DH, 8 * ROWS, true>(s, a);
-            if (rows > 2 * ROWS && a.width > 1) return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
+            if (a.width > 1) return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
         }
         return launch_tiles<KT, DH, 2 * ROWS, false>(s, a);
     }
@@ -894,7 +942,7 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     if (rc != SPD_OK) return rc;
     if (width < 1 || n_seq % width || n_heads < 1 || n_heads % n_kv_heads || max_shared < 0 || max_own < 0) return SPD_EINVAL;
     const long long room = (long long)table_stride * page_size;      // (the longest shared and the longest own part may be different sequences')
-    if (max_shared > room || max_own > room || (long long)max_shared + max_own > INT32_MAX - 65536) return SPD_EINVAL;
+    if (max_shared > room || max_own > room || (long long)max_shared + max_own > INT32_MAX / 2) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
     if ((long long)n_seq * n_heads > (1 << 24)) return SPD_EINVAL;
     if (!q || !shared || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16) return SPD_EINVAL;
