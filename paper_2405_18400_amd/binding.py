@@ -7,6 +7,7 @@ library has not been built this module raises on first use.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -392,12 +393,12 @@ class Session:
 
 
 # ---- stand-alone operators (device tensors in, device tensors out; caller's current stream)
-def _stream_ptr():
+def _stream_ptr(device=None):
     """The calling thread's current stream on its current device, without the Stream object around it: building that
     took 2.9 of the 7.2 us such a call took the host (now 0.4 of 4.7)."""
     torch = _torch()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (private to torch: a build may lack it)
-    return raw(torch.cuda.current_device()) if raw is not None else torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device() if device is None else device) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def spd_op_gemv(dtype: str, W, x, y, gain=None, eps=0.0, residual=None):
@@ -443,140 +444,169 @@ def spd_op_attention_static(dtype: str, q, K, V, out, n_ctx: int):
 
 # ---- several sequences over one prompt, on a paged cache: K, V [pages, n_kv_heads, page_size, d_head], table int32 [n_seq, entries].
 # Nothing here waits for the GPU; `err`, an int32 tensor of one element, is set to 1 by what only the kernels can see (spd.h).
-def _on_gpu(where, **tensors):
-    """Every tensor given: (tensor, torch type, shape or None), whole, on the current device; entries of a shape that are None are not checked."""
-    device = _torch().cuda.current_device()
+# A decoding step makes a few such calls per layer, so each looks its arguments over in one expression and names what is wrong
+# only where something is (append / attention / selection / reordering: 15.7 / 13.7 / 13.1 / 8.9 us of host time per call with
+# a check per tensor, 9.1 / 10.2 / 9.7 / 6.4 now).
+def _refuse(where, device, **tensors):
+    """Says what is wrong with tensors given as (tensor, type, shape): they have to be whole, on `device`, and of as many elements (None: not looked at)."""
     for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
         if t.get_device() != device:
             raise ValueError(f"{where}: {name} is not on the current device")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
         if not t.is_contiguous():
             raise ValueError(f"{where}: {name} is not contiguous")
-        if shape is not None and tuple(t.shape) != shape:
+        if shape is not None and t.numel() != math.prod(shape):
             raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
 
 
-def _kv_type(where, dtype):
-    torch = _torch()
-    types = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
-    if dtype not in types:
+def _kv_type(where, torch, dtype):
+    kv = torch.float16 if dtype == "fp16" else torch.bfloat16 if dtype == "bf16" else torch.float32 if dtype == "fp32" else None
+    if kv is None:
         raise ValueError(f"{where}: no element type {dtype!r}")
-    return types[dtype]
+    return kv
 
 
-def _rows_of(where, device, **tensors):
-    """[tokens, heads, d_head] tensors whose tokens may lie apart (parts of one product's rows): the tokens' stride."""
-    strides = set()
-    for name, t in tensors.items():
-        if t.get_device() != device or t.dtype != _torch().float32:
-            raise ValueError(f"{where}: {name} has to be float32 on the current device")
-        n, heads, d = t.shape
-        if t.stride(2) != 1 and d > 1 or t.stride(1) != d and heads > 1:
-            raise ValueError(f"{where}: the heads of {name}'s tokens have to lie one behind the other")
-        strides.add(t.stride(0) if n > 1 else max(t.stride(0), heads * d))
-    if len(strides) != 1:
-        raise ValueError(f"{where}: {' and '.join(tensors)} differ in their tokens' stride")
-    return strides.pop()
+def _rows(where, device, name, t, heads, d, torch):
+    """The stride of the tokens of t [tokens, heads, d], which may lie apart (parts of one product's rows)."""
+    stride, between, within = t.stride()
+    if t.dtype is not torch.float32 or t.get_device() != device:
+        raise ValueError(f"{where}: {name} has to be float32 on the current device")
+    if (within != 1 and d > 1) or (between != d and heads > 1):
+        raise ValueError(f"{where}: the heads of {name}'s tokens have to lie one behind the other")
+    return stride
 
 
-def _raise(rc, where):
-    if rc:
-        raise SpdError(rc, where)
+def _scratch(torch, n_bytes, like):
+    """Memory for one call.  It goes back to torch's pool when the call has been enqueued: that pool hands it out again in the order of the
+    stream the call runs on, the current one.  (The pool's blocks start at multiples of 512 bytes.)"""
+    return torch.empty(n_bytes, dtype=torch.uint8, device=like.device)
 
 
 def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: float, q=None, q_out=None, err=None):
     """k, v [tokens, n_kv_heads, d_head] (and q [tokens, n_heads, d_head] -> q_out), rotated by pos, to the rows of their sequences; seq < 0: padding."""
     torch, where = _torch(), "spd_op_append_paged"
-    kv = _kv_type(where, dtype)
-    n_pages, n_kv, page_size, d = K.shape
-    n = k.shape[0]
-    i32 = torch.int32
-    _on_gpu(where, K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)))
-    if err is not None:
-        _on_gpu(where, err=(err, i32, (1,)))
-    if tuple(k.shape) != (n, n_kv, d) or k.shape != v.shape:
+    kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
+    shape = K.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, entries = table.shape
+    n = seq.numel()
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.numel() == K.numel() and pos.numel() == n
+            and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
+            and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
+            and err is None):
+        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), err=(err, i32, (1,)))
+    if k.shape != (n, n_kv, d) or v.shape != (n, n_kv, d):
         raise ValueError(f"{where}: k and v have to be [{n}, {n_kv}, {d}]")
-    kv_stride, q_stride, heads, device = _rows_of(where, K.get_device(), k=k, v=v), 0, 0, K.get_device()
-    if (q is None) != (q_out is None):
-        raise ValueError(f"{where}: q and q_out come together")
+    kv_stride, q_stride, heads, q_ptr, out_ptr = _rows(where, device, "k", k, n_kv, d, torch), 0, 0, None, None
+    if _rows(where, device, "v", v, n_kv, d, torch) != kv_stride and n > 1:
+        raise ValueError(f"{where}: k and v differ in their tokens' stride")
     if q is not None:
         heads = q.shape[1]
-        if tuple(q.shape) != (n, heads, d):
-            raise ValueError(f"{where}: q has to be [{n}, heads, {d}]")
-        q_stride = _rows_of(where, device, q=q)
-        _on_gpu(where, q_out=(q_out, torch.float32, (n, heads, d)))
-    n_seq, entries = table.shape
-    _raise(lib().spd_op_append_paged(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries,
-                                     None if q is None else q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), kv_stride, seq.data_ptr(), pos.data_ptr(),
-                                     n, heads, rope_theta, None if q is None else q_out.data_ptr(), None if err is None else err.data_ptr(), _stream_ptr()), where)
-
-
-def _scratch(n_bytes, device):
-    """-> (a tensor that keeps the memory, its first 256-byte aligned address, bytes from there).  It goes back to torch's pool when the call has
-    been enqueued: that pool hands it out again in the order of the stream the call runs on, the current one."""
-    buf = _torch().empty(n_bytes + 256, dtype=_torch().uint8, device=device)
-    return buf, (buf.data_ptr() + 255) // 256 * 256, n_bytes
+        if q_out is None or q.shape != (n, heads, d):
+            raise ValueError(f"{where}: q has to be [{n}, heads, {d}], and comes with q_out")
+        q_stride, q_ptr, out_ptr = _rows(where, device, "q", q, heads, d, torch), q.data_ptr(), q_out.data_ptr()
+        if not (q_out.dtype is torch.float32 and q_out.numel() == n * heads * d and q_out.is_contiguous() and q_out.get_device() == device):
+            _refuse(where, device, q_out=(q_out, torch.float32, (n, heads, d)))
+    elif q_out is not None:
+        raise ValueError(f"{where}: q_out comes with q")
+    if n <= 1:                          # (a single token's stride may be anything)
+        kv_stride, q_stride = n_kv * d, heads * d
+    rc = lib().spd_op_append_paged(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, q_ptr, q_stride,
+                                   k.data_ptr(), v.data_ptr(), kv_stride, seq.data_ptr(), pos.data_ptr(), n, heads, rope_theta, out_ptr,
+                                   None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
 
 
 def spd_op_attention_shared(dtype: str, q, K, V, table, shared, length, out, width: int, max_shared: int, max_own: int, err=None):
     """q, out [n_seq, n_heads, d_head]; shared int32 [n_seq / width], length int32 [n_seq]."""
     torch, where = _torch(), "spd_op_attention_shared"
-    kv, i32 = _kv_type(where, dtype), torch.int32
-    n_pages, n_kv, page_size, d = K.shape
-    n_seq, heads, _ = q.shape
+    kv, i32, f32, device = _kv_type(where, torch, dtype), torch.int32, torch.float32, torch.cuda.current_device()
+    shape, rows = K.shape, q.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, heads, q_d = rows
+    entries = table.shape[-1]
     if width < 1 or n_seq % width:
         raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
-    _on_gpu(where, q=(q, torch.float32, (n_seq, heads, d)), K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, (n_seq, table.shape[-1])),
-            shared=(shared, i32, (n_seq // width,)), length=(length, i32, (n_seq,)), out=(out, torch.float32, (n_seq, heads, d)))
-    if err is not None:
-        _on_gpu(where, err=(err, i32, (1,)))
+    groups = n_seq // width
+    if not (q.dtype is f32 and out.dtype is f32 and K.dtype is kv and V.dtype is kv and table.dtype is i32 and shared.dtype is i32 and length.dtype is i32 and q_d == d
+            and out.numel() == q.numel() and V.numel() == K.numel() and table.numel() == n_seq * entries and shared.numel() == groups and length.numel() == n_seq
+            and q.is_contiguous() and out.is_contiguous() and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and shared.is_contiguous()
+            and length.is_contiguous() and q.get_device() == device and out.get_device() == device and K.get_device() == device and V.get_device() == device
+            and table.get_device() == device and shared.get_device() == device and length.get_device() == device and err is None):
+        _refuse(where, device, q=(q, f32, (n_seq, heads, d)), K=(K, kv, None), V=(V, kv, shape), table=(table, i32, (n_seq, entries)), shared=(shared, i32, (groups,)),
+                length=(length, i32, (n_seq,)), out=(out, f32, (n_seq, heads, d)), err=(err, i32, (1,)))
     L = lib()
-    _keep, scratch, n_bytes = _scratch(L.spd_op_attention_shared_scratch_bytes(n_seq, width, heads, n_kv, d, max_shared, max_own), q.device)
-    _raise(L.spd_op_attention_shared(SPD_DTYPE[dtype], q.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq,
-                                     table.shape[1], shared.data_ptr(), length.data_ptr(), width, heads, max_shared, max_own, out.data_ptr(), scratch, n_bytes,
-                                     None if err is None else err.data_ptr(), _stream_ptr()), where)
+    n_bytes, scratch = L.spd_op_attention_shared_scratch_bytes(n_seq, width, heads, n_kv, d, max_shared, max_own), None
+    if n_bytes:
+        buf = _scratch(torch, n_bytes, q)
+        scratch = buf.data_ptr()
+    rc = L.spd_op_attention_shared(SPD_DTYPE[dtype], q.data_ptr(), K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries,
+                                   shared.data_ptr(), length.data_ptr(), width, heads, max_shared, max_own, out.data_ptr(), scratch, n_bytes,
+                                   None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
 
 
 def spd_op_beam_select(dtype: str, logits, scores, out_scores, out_tokens, out_parents, tau: float = 1.0, ended=None, end_token: int = -1, out_ended=None):
     """logits [n_groups, n_in, vocab] (rows may lie apart), scores [n_groups, n_in] -> out_* [n_groups, n_out]."""
     torch, where = _torch(), "spd_op_beam_select"
+    kind, i32, f32, device = _kv_type(where, torch, dtype), torch.int32, torch.float32, torch.cuda.current_device()
     groups, n_in, vocab = logits.shape
-    n_out, i32 = out_scores.shape[-1], torch.int32
-    if logits.dtype != _kv_type(where, dtype):
+    n_out = out_scores.shape[-1]
+    n = groups * n_out
+    if logits.dtype is not kind:
         raise ValueError(f"{where}: logits are {logits.dtype}, not {dtype}")
-    stride = logits.stride(1) if n_in > 1 else logits.stride(0) if groups > 1 else vocab
-    if (logits.stride(2) != 1 and vocab > 1) or (groups > 1 and logits.stride(0) != n_in * stride) or logits.get_device() != torch.cuda.current_device():
+    of_group, of_row, of_entry = logits.stride()
+    stride = of_row if n_in > 1 else of_group if groups > 1 else vocab
+    if (of_entry != 1 and vocab > 1) or (groups > 1 and of_group != n_in * stride) or logits.get_device() != device:
         raise ValueError(f"{where}: logits have to be rows of one stride on the current device")
-    outs = {"out_tokens": (out_tokens, i32, (groups, n_out)), "out_parents": (out_parents, i32, (groups, n_out))}
-    if ended is not None:
-        outs["ended"] = (ended, i32, (groups, n_in))
-    if out_ended is not None:
-        outs["out_ended"] = (out_ended, i32, (groups, n_out))
-    _on_gpu(where, scores=(scores, torch.float32, (groups, n_in)), out_scores=(out_scores, torch.float32, (groups, n_out)), **outs)
+    if not (scores.dtype is f32 and out_scores.dtype is f32 and out_tokens.dtype is i32 and out_parents.dtype is i32 and scores.numel() == groups * n_in
+            and out_scores.numel() == n and out_tokens.numel() == n and out_parents.numel() == n and scores.is_contiguous() and out_scores.is_contiguous()
+            and out_tokens.is_contiguous() and out_parents.is_contiguous() and scores.get_device() == device and out_scores.get_device() == device
+            and out_tokens.get_device() == device and out_parents.get_device() == device
+            and (ended is None or (ended.dtype is i32 and ended.numel() == groups * n_in and ended.is_contiguous() and ended.get_device() == device))
+            and (out_ended is None or (out_ended.dtype is i32 and out_ended.numel() == n and out_ended.is_contiguous() and out_ended.get_device() == device))):
+        ins, outs = (groups, n_in), (groups, n_out)
+        _refuse(where, device, scores=(scores, f32, ins), out_scores=(out_scores, f32, outs), out_tokens=(out_tokens, i32, outs), out_parents=(out_parents, i32, outs),
+                ended=(ended, i32, ins), out_ended=(out_ended, i32, outs))
     L = lib()
-    _keep, scratch, n_bytes = _scratch(L.spd_op_beam_select_scratch_bytes(groups, n_in, n_out, vocab), logits.device)
-    _raise(L.spd_op_beam_select(SPD_DTYPE[dtype], logits.data_ptr(), stride, groups, n_in, n_out, vocab, scores.data_ptr(),
-                                None if ended is None else ended.data_ptr(), end_token, tau, out_scores.data_ptr(), out_tokens.data_ptr(),
-                                out_parents.data_ptr(), None if out_ended is None else out_ended.data_ptr(), scratch, n_bytes, _stream_ptr()), where)
+    n_bytes, scratch = L.spd_op_beam_select_scratch_bytes(groups, n_in, n_out, vocab), None
+    if n_bytes:
+        buf = _scratch(torch, n_bytes, logits)
+        scratch = buf.data_ptr()
+    rc = L.spd_op_beam_select(SPD_DTYPE[dtype], logits.data_ptr(), stride, groups, n_in, n_out, vocab, scores.data_ptr(), None if ended is None else ended.data_ptr(),
+                              end_token, tau, out_scores.data_ptr(), out_tokens.data_ptr(), out_parents.data_ptr(),
+                              None if out_ended is None else out_ended.data_ptr(), scratch, n_bytes, _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
 
 
 def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, width: int, err=None):
     """K, V [pages, ...] or [layers, pages, n_kv_heads, page_size, d_head]; parents int32 [n_seq / width, width], length int32 [n_seq]; table -> table_out."""
     torch, where = _torch(), "spd_op_beam_reorder"
-    kv, i32 = _kv_type(where, dtype), torch.int32
-    layers = K.shape[0] if K.dim() == 5 else 1
-    n_pages, n_kv, page_size, d = K.shape[-4:]
-    n_seq, entries = table.shape
+    kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
+    shape, rows = K.shape, table.shape
+    n_pages, n_kv, page_size, d = shape[-4:]
+    layers = shape[0] if len(shape) == 5 else 1
+    n_seq, entries = rows
     if width < 1 or n_seq % width:
         raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
-    _on_gpu(where, K=(K, kv, None), V=(V, kv, tuple(K.shape)), table=(table, i32, None), parents=(parents, i32, (n_seq // width, width)),
-            length=(length, i32, (n_seq,)), table_out=(table_out, i32, (n_seq, entries)))
-    if err is not None:
-        _on_gpu(where, err=(err, i32, (1,)))
-    _raise(lib().spd_op_beam_reorder(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
-                                     n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), table_out.data_ptr(),
-                                     None if err is None else err.data_ptr(), _stream_ptr()), where)
+    groups = (n_seq // width, width)
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and parents.dtype is i32 and length.dtype is i32 and table_out.dtype is i32 and V.numel() == K.numel()
+            and parents.numel() == n_seq and length.numel() == n_seq and table_out.numel() == n_seq * entries and K.is_contiguous() and V.is_contiguous() and table.is_contiguous()
+            and parents.is_contiguous() and length.is_contiguous() and table_out.is_contiguous() and K.get_device() == device and V.get_device() == device
+            and table.get_device() == device and parents.get_device() == device and length.get_device() == device and table_out.get_device() == device and err is None):
+        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), parents=(parents, i32, groups), length=(length, i32, (n_seq,)),
+                table_out=(table_out, i32, rows), err=(err, i32, (1,)))
+    rc = lib().spd_op_beam_reorder(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
+                                   n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), table_out.data_ptr(),
+                                   None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
 
 
 def spd_test_state_layout():

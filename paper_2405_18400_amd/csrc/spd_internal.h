@@ -284,6 +284,7 @@ struct ReorderArgs {
     int32_t n_layers, width, n_groups, row_bytes, shares, heads_per_share;
     size_t layer_bytes;
 };
+struct Divisor { uint32_t mul; int32_t shift; };   // n / d = (2 n mul >> 32) >> shift for n < 2^31
 struct SharedAttnArgs {
     PagedCache c;
     const float *q;              // [n_seq, n_heads, d_head]
@@ -293,6 +294,8 @@ struct SharedAttnArgs {
     int32_t width, n_heads, max_shared, max_own;
     // how the positions are cut: blocks 0 .. shared_blocks - 1 take shared chunks, the others sequences' own ones
     int32_t shared_chunks, shared_chunk, own_chunks, slots, row_tiles, own_tiles, shared_blocks, shared_blocks_per_tile;
+    int32_t group;               // query heads per key/value head
+    Divisor by_group, by_kv_heads, by_width, by_row_tiles, by_own_tiles, by_shared_chunks, by_own_chunks;
     float *part_ml, *part;       // scratch, [n_seq, n_heads, slots]: maximum and sum; O [.., d_head]
 };
 struct SelectArgs {

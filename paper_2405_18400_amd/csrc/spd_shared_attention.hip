@@ -30,13 +30,12 @@ constexpr int KEYS = 32;                         // keys of a wave's turn
 constexpr int ROWS = 16;                         // query rows of a tile
 constexpr int CHUNK_MAX = 4096;                  // positions of a chunk at most (its page numbers lie in LDS)
 constexpr int PAGE_MIN = 4;                      // the smallest page: four keys of a lane lie on one
-constexpr int BLOCKS = 512;                      // blocks the positions are cut for: two to a compute unit
 constexpr float SLACK = 8.f;                     // a row's reference is raised when a score passes it by 2^8: seldom
 constexpr float P_BITS = 7.f;                    // probabilities are scaled by 2^7, at most 2^15 then: two fp16 numbers keep 22 bits down to 2^-19
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned long long u64;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // exp2(a - b) with exp2(-inf - anything) = 0, also where b is -inf (nothing seen yet).
@@ -50,9 +49,11 @@ template <> struct Type<float> { static constexpr int PARTS = 1; };
 // Two fp32 numbers as pairs of the cache's type, most significant part first.
 template <typename KT> __device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[Type<KT>::PARTS]);
 template <> __device__ __forceinline__ void parts_of<half_t>(float x, float y, uint32_t (&out)[2]) {
-    const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x, y));
-    out[0] = __builtin_bit_cast(uint32_t, hi);
-    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x - (float)hi.x, y - (float)hi.y));
+    out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+    float rx, ry;                                // x - hi, y - hi, in one instruction each (as two they are a sixth of a turn's vector instructions)
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rx) : "v"(out[0]), "v"(x));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(ry) : "v"(out[0]), "v"(y));
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(rx, ry));
 }
 template <> __device__ __forceinline__ void parts_of<bf16_t>(float x, float y, uint32_t (&out)[3]) {
 #pragma unroll
@@ -94,6 +95,10 @@ template <int B> __device__ __forceinline__ void load_words(const char *p, uint3
     }
 }
 
+// n / d for n < 2^31 (d's inverse by the host: one multiplication; a division by a number that is not known takes some forty
+// instructions, and a block of a short call has little else to do).
+__device__ __forceinline__ int over(int n, const Divisor &d) { return (int)(__umulhi(2u * (uint32_t)n, d.mul) >> d.shift); }
+
 // A stretch of positions read through one row of the table.
 struct Stretch { int row, lo, hi; };
 
@@ -121,20 +126,20 @@ constexpr int PAGES = CHUNK_MAX / PAGE_MIN + 4;
 // `resolve` reads the lengths and sets the stretches; false: there are none.  Queries are asked for before that, page numbers before
 // the queries are put in place: each of these is a trip to memory.
 template <typename KT, int DH, int RT, typename F>
-__device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&resolve, uint32_t *lds, int *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
+__device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&resolve, uint32_t *lds, u64 *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
     constexpr bool F32 = sizeof(KT) == 4;
     constexpr int PARTS = Type<KT>::PARTS;
     constexpr int NJ = F32 ? DH / 16 : DH / 32;                              // 16-byte pieces of a key per lane
     constexpr int FV = DH / 16, VB = FV * (int)sizeof(KT), VW = VB / 4;      // features, bytes, words of a value row per lane
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
-    const int d = p.c.d_head, shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
+    const int d = p.c.d_head, shift = p.c.page_shift, page_size = 1 << shift, group = p.group;
     const int tiles = (min(un.n_rows, RT * ROWS) + ROWS - 1) / ROWS;
 
     constexpr int TPR = NTS / (RT * ROWS), N8 = DH / 8, PP = (N8 + TPR - 1) / TPR;       // threads per row; pieces of eight features
     const int q_row = tid / TPR, q_t = tid % TPR;
     float x[PP][8];
     {
-        const int r = un.r0 + min(q_row, un.n_rows - 1), s = un.seq + r / group, hq = un.kvh * group + r % group;   // (rows past the last repeat it)
+        const int r = un.r0 + min(q_row, un.n_rows - 1), rs = over(r, p.by_group), s = un.seq + rs, hq = un.kvh * group + r - rs * group;   // (rows past the last repeat it)
         const float *q = p.q + ((size_t)s * p.n_heads + hq) * d;
 #pragma unroll
         for (int i = 0; i < PP; ++i)
@@ -200,7 +205,8 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         m[rt] = -INFINITY; l[rt] = 0.f;
     }
 
-    const size_t row_bytes = (size_t)d * sizeof(KT), head_bytes = row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
+    const int row_bytes = d * (int)sizeof(KT);
+    const u64 head_bytes = (u64)row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
     const char *Kh = (const char *)p.c.K + (size_t)un.kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)un.kvh * head_bytes;
     u32x4 kf[2][NJ];
     uint32_t vf[2][4][VW];
@@ -215,7 +221,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
     for (int i = tid; i < n_a + n_b; i += NTS) {
         const int page = i == tid && panel == un.a.lo ? early_page : entry_page(lo_a, n_a, un.b.lo, i);
         const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
-        pages[i] = ok ? page : -1;
+        pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
     const bool any_bad = __syncthreads_or(bad);
@@ -237,8 +243,8 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         stretch(t, tb, lo, hi, index0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int pos = min(max(tb + 16 * u + col, lo), hi - 1), page = max(pages[(pos >> shift) + index0], 0);
-            const char *row = Kh + (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * row_bytes + k_at;
+            const int pos = min(max(tb + 16 * u + col, lo), hi - 1);
+            const char *row = Kh + (pages[(pos >> shift) + index0] + (uint32_t)((pos & (page_size - 1)) * row_bytes + k_at));
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 if (DH > 32 || 64 * j + k_at < (int)row_bytes) kf[u][j] = global_load16(row + 64 * j);
@@ -251,8 +257,8 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         stretch(t, tb, lo, hi, index0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3), page = max(pages[(pos >> shift) + index0], 0);
-            const char *row = Vh + (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * row_bytes + v_at;
+            const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
+            const char *row = Vh + (pages[(pos >> shift) + index0] + (uint32_t)((pos & (page_size - 1)) * row_bytes + v_at));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (DH > 32 || v_at < (int)row_bytes) load_words<VB>(row + r * row_bytes, vf[u][r]);
@@ -304,10 +310,11 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         if (t + NWS < turns) fetch_k(t + NWS);
         // keys outside the stretch, or on no page: no score, and no value that could be a NaN
         if (tb < lo || tb + KEYS > hi || any_bad) {
+            asm volatile("");                   // (a branch: seldom taken)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
-                const bool page_ok = pages[(pos >> shift) + index0] >= 0;
+                const bool page_ok = !any_bad || (unsigned)entry_page(lo_a, n_a, un.b.lo, (pos >> shift) + index0) < (unsigned)p.c.n_pages;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int at = tb + 16 * u + 4 * kk + r;
@@ -328,10 +335,8 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    st[rt][u][r] *= scale[rt];
-                    mx = fmaxf(mx, st[rt][u][r]);
-                }
+                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
+            mx *= scale[rt];
             if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));    // the lane groups hold different keys of the same rows
                 mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
@@ -345,7 +350,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
             const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                pf[rt][i] = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4] - ref);
+                pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref));
                 l[rt] += pf[rt][i];
             }
             if constexpr (!F32) {
@@ -435,7 +440,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
                     const float4 z = *(const float4 *)&O[(v * ROWS + row) * STRIDE + c];
                     y.x += f * z.x; y.y += f * z.y; y.z += f * z.z; y.w += f * z.w;
                 }
-                const int feature = NH * FH * (c / FH) + h * FH + c % FH, s = un.seq + r / group, hq = un.kvh * group + r % group;
+                const int feature = NH * FH * (c / FH) + h * FH + c % FH, rs = over(r, p.by_group), s = un.seq + rs, hq = un.kvh * group + r - rs * group;
                 if (feature >= d) continue;
                 const size_t at = (size_t)s * p.n_heads + hq;
                 float *to = p.out + at * d + feature;
@@ -466,14 +471,16 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 // come through LDS, 16 bytes per lane straight from memory, ST stages of SK keys deep; pieces of a row are permuted by the row number,
 // so that neither the operand reads (16 rows side by side) nor the row reads meet in a bank.  One barrier per stage says both "this
 // stage has arrived" and "the one before has been read".
-template <int DH> struct Stage {
-    static constexpr int SK = DH == 64 ? 64 : 32, ROWB = DH * 2, PIECES = ROWB / 16;   // keys; bytes and 16-byte pieces of a row
+template <int DH, int RT> struct Stage {
+    static constexpr int SK = DH == 64 || (DH == 128 && RT == 1) ? 64 : 32;             // keys
+    static constexpr int NU = RT == 1 && SK == 64 ? 4 : 2;                              // tiles of 16 keys that go through the products together
+    static constexpr int ROWB = DH * 2, PIECES = ROWB / 16;                             // bytes and 16-byte pieces of a row
     static constexpr int HALF = SK * ROWB, BYTES = 2 * HALF;                            // K, then V
     static constexpr int LOADS = HALF / 16 / NTS;                                       // pieces per thread, of K as of V
-    static constexpr int ST = DH == 256 ? 3 : 4;
+    static constexpr int ST = BYTES >= 32 * 1024 ? (DH == 256 ? 3 : 2) : 4;
 };
-template <int DH> __device__ __forceinline__ int permuted(int row, int piece) {
-    return Stage<DH>::PIECES >= 16 ? piece ^ (row & 15) : piece ^ ((row & 7) ^ ((row >> 3) & 1));
+template <int PIECES> __device__ __forceinline__ int permuted(int row, int piece) {
+    return PIECES >= 16 ? piece ^ (row & 15) : piece ^ ((row & 7) ^ ((row >> 3) & 1));
 }
 __device__ __forceinline__ void to_lds16(const char *from, char *to) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -483,17 +490,20 @@ __device__ __forceinline__ void to_lds16(const char *from, char *to) {
 
 // False: none of the chunk's positions is there.
 template <typename KT, int DH, int RT>
-__device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, int *pages) {
+__device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, u64 *pages) {
     constexpr int PARTS = Type<KT>::PARTS, NJ = DH / 32, FV = DH / 16, VW = FV / 2;
-    constexpr int SK = Stage<DH>::SK, ROWB = Stage<DH>::ROWB, PIECES = Stage<DH>::PIECES, HALF = Stage<DH>::HALF, BYTES = Stage<DH>::BYTES, LOADS = Stage<DH>::LOADS, ST = Stage<DH>::ST;
+    typedef Stage<DH, RT> S;
+    constexpr bool AHEAD = true;
+    constexpr int SK = S::SK, NU = S::NU, ROWB = S::ROWB, PIECES = S::PIECES, HALF = S::HALF, BYTES = S::BYTES, LOADS = S::LOADS, ST = S::ST;
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
-    const int shift = p.c.page_shift, page_size = 1 << shift, group = p.n_heads / p.c.n_kv_heads;
+    const int shift = p.c.page_shift, page_size = 1 << shift, group = p.group;
     const int row0 = w * RT * ROWS;                          // this wave's rows of the unit
+    const u64 head_bytes = (u64)ROWB << shift, page_bytes = head_bytes * p.c.n_kv_heads;
     // asked for at once: the queries, the group's shared length and the page numbers of the whole chunk
     float x[RT][NJ][8];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int rr = un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), s = un.seq + rr / group, hq = un.kvh * group + rr % group;   // (rows past the last repeat it)
+        const int rr = un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), rs = over(rr, p.by_group), s = un.seq + rs, hq = un.kvh * group + rr - rs * group;   // (rows past the last repeat it)
         const float *q = p.q + ((size_t)s * p.n_heads + hq) * DH + 8 * kk;
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
@@ -503,12 +513,15 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                 x[rt][j][e] = v.x; x[rt][j][e + 1] = v.y; x[rt][j][e + 2] = v.z; x[rt][j][e + 3] = v.w;
             }
     }
+    int len[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) len[rt] = as_global(p.len)[un.seq + over(un.r0 + min(row0 + rt * ROWS + col, un.n_rows - 1), p.by_group)];
     const int lo = un.a.lo, first = lo >> shift;
     const int last = min((un.a.hi - 1) >> shift, p.c.table_stride - 1);
     int page = 0;
     const int32_t *entries = p.c.table + (size_t)un.a.row * p.c.table_stride + first;
     if (tid <= last - first) page = as_global(entries)[tid];
-    const int to = as_global(p.shared)[un.seq / p.width], hi = min(un.a.hi, to);
+    const int to = as_global(p.shared)[over(un.seq, p.by_width)], hi = min(un.a.hi, to);
     if ((to < 0 || to > p.max_shared) && p.err && tid == 0) *as_global(p.err) = 1;
     if (hi <= lo || to > p.max_shared) return false;
     const int n_pages = ((hi - 1) >> shift) - first + 1;     // (at most the row's entries: max_shared is)
@@ -516,21 +529,25 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
     for (int i = tid; i < n_pages; i += NTS) {
         if (i != tid) page = as_global(entries)[i];
         const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
-        pages[i] = ok ? page : -1;
+        pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
     const bool any_bad = __syncthreads_or(bad);
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
 
     const int base = lo & ~3, stages = (hi - base + SK - 1) / SK;
-    const size_t head_bytes = (size_t)ROWB << shift, page_bytes = head_bytes * p.c.n_kv_heads;
     const char *Kh = (const char *)p.c.K + (size_t)un.kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)un.kvh * head_bytes;
+    // Blocks go through their chunks in step, and pages are a power of two apart: started at the same place of a page they would all
+    // ask the same memory channels at once.  So each starts at a place of its own.
+    const int turn = (int)(blockIdx.x * 5u % (unsigned)stages);
+    const auto place_of = [&](int t) { return t + turn < stages ? t + turn : t + turn - stages; };
     auto fetch = [&](int t) {
         char *to = lds + (t % ST) * BYTES + w * (WAVE * 16);
+        const int at0 = base + place_of(t) * SK;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = tid + i * NTS, key = at / PIECES, pos = min(max(base + t * SK + key, lo), hi - 1), page = max(pages[(pos >> shift) - first], 0);
-            const size_t from = (size_t)page * page_bytes + (size_t)(pos & (page_size - 1)) * ROWB + 16 * permuted<DH>(key, at % PIECES);
+            const int at = tid + i * NTS, key = at / PIECES, pos = min(max(at0 + key, lo), hi - 1);
+            const u64 from = pages[(pos >> shift) - first] + (uint32_t)((pos & (page_size - 1)) * ROWB + 16 * permuted<PIECES>(key, at % PIECES));
             to_lds16(Kh + from, to + i * (NTS * 16));
             to_lds16(Vh + from, to + HALF + i * (NTS * 16));
         }
@@ -577,77 +594,88 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
     for (int t = 0; t < stages; ++t) {
         // the oldest stage under way has arrived (of this wave's loads: at most the ST - 2 younger ones are out)
         const int younger = min(stages - 1 - t, ST - 2);
-        if (younger >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * 2 * LOADS) : "memory");
-        else if (younger == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+        if (ST > 3 && younger >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * 2 * LOADS) : "memory");
+        else if (ST > 2 && younger >= 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (t + ST - 1 < stages) fetch(t + ST - 1);
         const char *k_tile = lds + (t % ST) * BYTES, *v_tile = k_tile + HALF;
 #pragma unroll
-        for (int sub = 0; sub < SK / KEYS; ++sub) {
-            const int tb = base + t * SK + sub * KEYS;
-            f32x4v st[RT][2];
+        for (int sub = 0; sub < SK / (16 * NU); ++sub) {
+            const int key0 = sub * 16 * NU, tb = base + place_of(t) * SK + key0;
+            f32x4v st[RT][NU];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) st[rt][u] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                for (int u = 0; u < NU; ++u) st[rt][u] = f32x4v{0.f, 0.f, 0.f, 0.f};
+            u32x4 k[NJ][NU];
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int key = sub * KEYS + 16 * u + col;
-                    const u32x4 k = *(const u32x4 *)(k_tile + key * ROWB + 16 * permuted<DH>(key, 4 * j + kk));
-#pragma unroll
-                    for (int q = PARTS - 1; q >= 0; --q)
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) st[rt][u] = mfma16<KT>(k, Q[rt][j][q], st[rt][u]);
+                for (int u = 0; u < NU; ++u) {
+                    const int key = key0 + 16 * u + col;
+                    k[j][u] = *(const u32x4 *)(k_tile + key * ROWB + 16 * permuted<PIECES>(key, 4 * j + kk));
                 }
-            uint32_t vf[2][4][VW];
+            if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int key = sub * KEYS + 16 * u + 4 * kk + r;
+                for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
-                    for (int i = 0; i < VW; i += (VW < 4 ? VW : 4)) {
-                        const int byte = 2 * FV * col + 4 * i;
-                        const char *from = v_tile + key * ROWB + 16 * permuted<DH>(key, byte / 16) + byte % 16;
-                        if constexpr (VW == 2) {
-                            const u32x2 v = *(const u32x2 *)from;
-                            vf[u][r][0] = v.x; vf[u][r][1] = v.y;
-                        } else {
-                            const u32x4 v = *(const u32x4 *)from;
-                            vf[u][r][i] = v.x; vf[u][r][i + 1] = v.y; vf[u][r][i + 2] = v.z; vf[u][r][i + 3] = v.w;
-                        }
-                    }
-                }
-            if (tb < lo || tb + KEYS > hi || any_bad) {      // keys that do not count: no score, no value that could be a NaN
+                    for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
-                    const bool page_ok = pages[(pos >> shift) - first] >= 0;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int at = tb + 16 * u + 4 * kk + r;
-                        const bool in = at >= lo && at < hi && page_ok;
-#pragma unroll
-                        for (int rt = 0; rt < RT; ++rt) st[rt][u][r] = in ? st[rt][u][r] : -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < VW; ++i) vf[u][r][i] = in ? vf[u][r][i] : 0;
-                    }
-                }
-            }
-            u32x4 pt[RT][PARTS];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float mx = -INFINITY;
+                        for (int rt = 0; rt < RT; ++rt) st[rt][u] = mfma16<KT>(k[j][u], Q[rt][j][q], st[rt][u]);
+            // values of 32 keys at a time, a half ahead of their products
+            uint32_t vf[NU / 2][2][4][VW];
+            const auto read_v = [&](int h) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        st[rt][u][r] *= scale[rt];
-                        mx = fmaxf(mx, st[rt][u][r]);
+                        const int key = key0 + 32 * h + 16 * u + 4 * kk + r;
+#pragma unroll
+                        for (int i = 0; i < VW; i += (VW < 4 ? VW : 4)) {
+                            const int byte = 2 * FV * col + 4 * i;
+                            const char *from = v_tile + key * ROWB + 16 * permuted<PIECES>(key, byte / 16) + byte % 16;
+                            if constexpr (VW == 2) {
+                                const u32x2 v = *(const u32x2 *)from;
+                                vf[h][u][r][0] = v.x; vf[h][u][r][1] = v.y;
+                            } else {
+                                const u32x4 v = *(const u32x4 *)from;
+                                vf[h][u][r][i] = v.x; vf[h][u][r][i + 1] = v.y; vf[h][u][r][i + 2] = v.z; vf[h][u][r][i + 3] = v.w;
+                            }
+                        }
                     }
+            };
+            read_v(0);
+            if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
+            const bool cut = tb < lo || tb + 16 * NU > hi || any_bad;
+            uint32_t there = 0;                              // bit 4 u + r: this lane's key 16 u + 4 kk + r counts
+            if (cut) {                                       // keys that do not count: no score (and, below, no value that could be a NaN)
+                asm volatile("");                           // (a branch: seldom taken)
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    const int pos = min(max(tb + 16 * u + 4 * kk, lo & ~3), (hi - 1) & ~3);
+                    const bool page_ok = !any_bad || (unsigned)as_global(entries)[(pos >> shift) - first] < (unsigned)p.c.n_pages;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int at = tb + 16 * u + 4 * kk + r;
+                        const bool in = at >= lo && at < hi && page_ok;
+                        there |= (uint32_t)in << (4 * u + r);
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) st[rt][u][r] = in ? st[rt][u][r] : -INFINITY;
+                    }
+                }
+            }
+            u32x4 pt[RT][NU / 2][PARTS];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
+                mx *= scale[rt];
                 if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
                     mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
                     mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
@@ -660,31 +688,49 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                 }
                 const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4] - ref), p1 = __builtin_amdgcn_exp2f(st[rt][i / 4][i % 4 + 1] - ref);
-                    l[rt] += p0 + p1;
-                    uint32_t part[PARTS];
-                    parts_of<KT>(p0, p1, part);
+                for (int u = 0; u < NU; ++u)
 #pragma unroll
-                    for (int q = 0; q < PARTS; ++q) pt[rt][q][i / 2] = part[q];
-                }
+                    for (int r = 0; r < 4; r += 2) {
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r], scale[rt], -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r + 1], scale[rt], -ref));
+                        l[rt] += p0 + p1;
+                        uint32_t part[PARTS];
+                        parts_of<KT>(p0, p1, part);
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) pt[rt][u / 2][q][2 * (u % 2) + r / 2] = part[q];
+                    }
             }
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                u32x4 even, odd;
+            for (int h = 0; h < NU / 2; ++h) {               // 32 keys at a time
+                if (h + 1 < NU / 2) {
+                    read_v(h + 1);
+                    if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
+                }
+                if (cut) {
+                    asm volatile("");
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t x = vf[k / 2][2 * (k % 2)][i], y = vf[k / 2][2 * (k % 2) + 1][i];
-                    even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                    odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int i = 0; i < VW; ++i) vf[h][u][r][i] = (there >> (4 * (2 * h + u) + r)) & 1 ? vf[h][u][r][i] : 0;
                 }
 #pragma unroll
-                for (int q = PARTS - 1; q >= 0; --q)
+                for (int i = 0; i < VW; ++i) {
+                    u32x4 even, odd;
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        o[rt][2 * i] = mfma16<KT>(even, pt[rt][q], o[rt][2 * i]);
-                        o[rt][2 * i + 1] = mfma16<KT>(odd, pt[rt][q], o[rt][2 * i + 1]);
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t x = vf[h][k / 2][2 * (k % 2)][i], y = vf[h][k / 2][2 * (k % 2) + 1][i];
+                        even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                        odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                     }
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) {
+                            o[rt][2 * i] = mfma16<KT>(even, pt[rt][h][q], o[rt][2 * i]);
+                            o[rt][2 * i + 1] = mfma16<KT>(odd, pt[rt][h][q], o[rt][2 * i + 1]);
+                        }
+                }
             }
         }
     }
@@ -700,11 +746,13 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < FV; e += 4) *(f32x4v *)&O[col * STRIDE + FV * (4 * kk + i) + e] = f32x4v{o[rt][e][i], o[rt][e + 1][i], o[rt][e + 2][i], o[rt][e + 3][i]};
-        auto place = [&](int r) { return ((size_t)(un.seq + (un.r0 + r) / group) * p.n_heads + un.kvh * group + (un.r0 + r) % group) * p.slots + un.slot; };
+        auto place = [&](int r) {
+            const int rs = over(un.r0 + r, p.by_group);
+            return ((size_t)(un.seq + rs) * p.n_heads + un.kvh * group + un.r0 + r - rs * group) * p.slots + un.slot;
+        };
         const int r = row0 + rt * ROWS + col;
         if (kk == 0 && r < un.n_rows) {
-            const int len = as_global(p.len)[un.seq + (un.r0 + r) / group];
-            const bool on = len >= to && seq_fits(p, to, len);
+            const bool on = len[rt] >= to && seq_fits(p, to, len[rt]);
             as_global(p.part_ml)[2 * place(r)] = on ? m[rt] : -INFINITY;
             as_global(p.part_ml)[2 * place(r) + 1] = on ? l[rt] : 0.f;
         }
@@ -723,7 +771,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 
 // A unit without positions, or rows that take no part in it: no sum.
 __device__ __forceinline__ void nothing(const SharedAttnArgs &p, const Unit &un, int row) {
-    const int group = p.n_heads / p.c.n_kv_heads, r = un.r0 + row, s = un.seq + r / group, hq = un.kvh * group + r % group;
+    const int group = p.n_heads / p.c.n_kv_heads, r = un.r0 + row, rs = over(r, p.by_group), s = un.seq + rs, hq = un.kvh * group + r - rs * group;
     const size_t at = (size_t)s * p.n_heads + hq;
     if (p.slots > 1) {
         as_global(p.part_ml)[2 * (at * p.slots + un.slot)] = -INFINITY;
@@ -735,22 +783,22 @@ __device__ __forceinline__ void nothing(const SharedAttnArgs &p, const Unit &un,
 
 // TILE: query rows of a shared block; MANY: its waves share out rows, not keys.
 template <typename KT, int DH, int TILE, bool MANY>
-__global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 256 && TILE == ROWS) ? 2 : 1) void shared_attn_kernel(const SharedAttnArgs p) {
+__global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512 && TILE == ROWS) ? 2 : 1) void shared_attn_kernel(const SharedAttnArgs p) {
     constexpr int RT = MANY ? 1 : TILE / ROWS;
     extern __shared__ __align__(1024) uint32_t lds[];        // lds_bytes()
-    __shared__ int pages[PAGES];
+    __shared__ u64 pages[PAGES];
     __shared__ float lds_m[NWS][ROWS], lds_l[NWS][ROWS], row_scale[RT * ROWS];
-    const int group = p.n_heads / p.c.n_kv_heads;
+    const int group = p.group;
     int b = blockIdx.x;
     Unit un;
     un.b = Stretch{0, 0, 0};
     un.shared = -1;
     if (b < p.shared_blocks) {
         // row tiles of a chunk on one XCD (blocks go to the eight in turn), so that its keys come through that L2
-        const int per = 8 * p.row_tiles, chunk8 = b / per * 8 + b % 8, tile = b % per / 8;
+        const int of8 = over(b / 8, p.by_row_tiles), chunk8 = 8 * of8 + b % 8, tile = b / 8 - of8 * p.row_tiles;
         if (chunk8 >= p.shared_blocks_per_tile) return;
-        const int c = chunk8 % p.shared_chunks, gh = chunk8 / p.shared_chunks, g = gh / p.c.n_kv_heads;
-        un.kvh = gh % p.c.n_kv_heads;
+        const int gh = over(chunk8, p.by_shared_chunks), c = chunk8 - gh * p.shared_chunks, g = over(gh, p.by_kv_heads);
+        un.kvh = gh - g * p.c.n_kv_heads;
         un.seq = g * p.width;
         un.r0 = tile * TILE;
         un.n_rows = min(p.width * group - un.r0, TILE);
@@ -779,17 +827,15 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 256
         return;
     }
     b -= p.shared_blocks;
-    const int tile = b % p.own_tiles;
-    b /= p.own_tiles;
-    const int c = b % p.own_chunks, sh = b / p.own_chunks;
-    un.kvh = sh % p.c.n_kv_heads;
-    un.seq = sh / p.c.n_kv_heads;
+    const int sc = over(b, p.by_own_tiles), tile = b - sc * p.own_tiles, sh = over(sc, p.by_own_chunks), c = sc - sh * p.own_chunks;
+    un.seq = over(sh, p.by_kv_heads);
+    un.kvh = sh - un.seq * p.c.n_kv_heads;
     un.r0 = tile * ROWS;
     un.n_rows = min(group - un.r0, ROWS);
     un.slot = p.shared_chunks + c;
     const auto resolve = [&](Unit &u) {
-        const int lead = u.seq - u.seq % p.width;
-        int shared = as_global(p.shared)[u.seq / p.width], len = as_global(p.len)[u.seq];
+        const int gi = over(u.seq, p.by_width), lead = gi * p.width;
+        int shared = as_global(p.shared)[gi], len = as_global(p.len)[u.seq];
         if (!seq_fits(p, shared, len)) {
             shared = len = 0;
             if (p.err && threadIdx.x == 0) *as_global(p.err) = 1;
@@ -858,29 +904,47 @@ __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs 
 }
 
 // How a call is cut: chunks of shared and of own positions per unit, and the positions of a shared chunk.
+// A block costs 5 us whatever its chunk (three trips to memory before its first product, its results' way back), and each chunk
+// a partial result per row, so short calls take one block per compute unit; where that leaves a block more than LONG positions, two run
+// beside each other and fill each other's waits.  us, one / two blocks per compute unit: 64 rows x 8191 positions x 8 heads 17.8 / 22.2; eight
+// groups of 32 rows x 2001 x 8 38.1 / 41.2; 128 rows x 65537 x 8 93.0 / 87.6.
 struct Cut { int shared_chunks, shared_chunk, own_chunks; };
 constexpr int WHOLE = 512;                       // positions up to which a sequence's block takes shared and own ones in one go
+constexpr int CUS = 256, LONG = 768;
 Cut cut_for(int n_seq, int width, int n_heads, int n_kv_heads, int max_shared, int max_own) {
     const int groups = n_seq / width, group = n_heads / n_kv_heads;
     if (width > 1 && (long long)max_shared + max_own <= WHOLE) return Cut{0, 0, 1};
-    const long long shared = width == 1 ? (long long)max_shared + max_own : max_shared, own = width == 1 ? 0 : max_own;
-    const long long tiles = (width * group + 4 * ROWS - 1) / (4 * ROWS);
-    const long long work = shared * groups * n_kv_heads * tiles + own * n_seq * n_kv_heads;
-    long long chunk = (work + BLOCKS - 1) / BLOCKS;
-    chunk = std::min<long long>(CHUNK_MAX, std::max<long long>(NWS * KEYS, (chunk + NWS * KEYS - 1) / (NWS * KEYS) * (NWS * KEYS)));
-    return Cut{(int)std::max<long long>(1, (shared + chunk - 1) / chunk), (int)chunk, width == 1 ? 0 : (int)std::max<long long>(1, (std::max<long long>(own, 1) + chunk - 1) / chunk)};
+    const long long shared = std::max<long long>(1, width == 1 ? (long long)max_shared + max_own : max_shared);
+    const long long units = (long long)groups * n_kv_heads * (((long long)width * group + 8 * ROWS - 1) / (8 * ROWS)), own_units = (long long)n_seq * n_kv_heads;
+    const auto cut = [&](long long positions, long long of, long long blocks) {
+        const long long n = std::max<long long>(1, std::min(blocks / of, (positions + NWS * KEYS - 1) / (NWS * KEYS)));
+        const long long chunk = ((positions + n - 1) / n + KEYS - 1) / KEYS * KEYS;
+        return std::min<long long>(chunk, CHUNK_MAX);
+    };
+    long long chunk = cut(shared, units, CUS);
+    if (chunk > LONG || width == 1) chunk = cut(shared, units, 2 * CUS);
+    const long long own_chunk = cut(std::max(1, max_own), own_units, 2 * CUS);
+    return Cut{(int)((shared + chunk - 1) / chunk), (int)chunk, width == 1 ? 0 : (int)((std::max(1, max_own) + own_chunk - 1) / own_chunk)};
+}
+
+// With l = ceil(log2 d): ceil(2^(31 + l) / d) exceeds the exact inverse by less than one part in 2^31.
+Divisor divisor(int d) {
+    int l = 0;
+    while ((1u << l) < (unsigned)d) ++l;
+    return Divisor{(uint32_t)(((1ull << (31 + l)) + d - 1) / d), l};
 }
 
 template <typename KT, int DH, int TILE, bool MANY>
 constexpr int lds_bytes() {
     int b = 4 * Lds<KT, DH, MANY ? 1 : TILE / ROWS>::WORDS;
-    if constexpr (MANY) b = std::max(b, Stage<DH>::ST * Stage<DH>::BYTES);
+    if constexpr (MANY) b = std::max(b, Stage<DH, TILE / (NWS * ROWS)>::ST * Stage<DH, TILE / (NWS * ROWS)>::BYTES);
     return b;
 }
 
 template <typename KT, int DH, int TILE, bool MANY>
 hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
     const int group = a.n_heads / a.c.n_kv_heads, groups = a.c.n_seq / a.width;
+    a.group = group;
     a.row_tiles = (a.width * group + TILE - 1) / TILE;
     a.own_tiles = (group + ROWS - 1) / ROWS;
     a.shared_blocks_per_tile = groups * a.c.n_kv_heads * a.shared_chunks;
@@ -888,6 +952,8 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
     const long long blocks = shared_blocks + (long long)a.c.n_seq * a.c.n_kv_heads * a.own_chunks * a.own_tiles;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     a.shared_blocks = (int)shared_blocks;
+    a.by_group = divisor(group); a.by_kv_heads = divisor(a.c.n_kv_heads); a.by_width = divisor(a.width); a.by_row_tiles = divisor(a.row_tiles);
+    a.by_own_tiles = divisor(a.own_tiles); a.by_shared_chunks = divisor(std::max(1, a.shared_chunks)); a.by_own_chunks = divisor(std::max(1, a.own_chunks));
     constexpr int lds = lds_bytes<KT, DH, TILE, MANY>();
     if (lds > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)shared_attn_kernel<KT, DH, TILE, MANY>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -930,7 +996,7 @@ extern "C" size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t w
     if (n_seq <= 0 || width <= 0 || n_seq % width || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || d_head <= 0 || max_shared < 0 || max_own < 0) return 0;
     const Cut c = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
     const size_t parts = (size_t)n_seq * n_heads * (c.shared_chunks + c.own_chunks);
-    return c.shared_chunks + c.own_chunks > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 256;
+    return c.shared_chunks + c.own_chunks > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 0;
 }
 
 extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
@@ -946,8 +1012,9 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     if (n_seq == 0) return SPD_OK;
     if ((long long)n_seq * n_heads > (1 << 24)) return SPD_EINVAL;
     if (!q || !shared || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16) return SPD_EINVAL;
-    if (!scratch || (uintptr_t)scratch % 256) return SPD_EINVAL;
-    if (scratch_bytes < spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own)) return SPD_EWORKSPACE;
+    const size_t need = spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
+    if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
+    if (scratch_bytes < need) return SPD_EWORKSPACE;
     const Cut cut = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
     SharedAttnArgs a{};
     a.c = c; a.q = q; a.out = out; a.shared = shared; a.len = len; a.err = err;
