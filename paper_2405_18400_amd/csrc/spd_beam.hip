@@ -3,11 +3,11 @@
 // Within a row the order of continuations is that of its logits; the log-sum-exp and the beam's
 // score move all of them alike.  So one pass over the logits leaves, per slice of a row, the
 // n_out best (sort keys, exact) with the slice's maximum and sum of exponentials, and a second,
-// small kernel puts a group's slices together and ranks what is left, at most n_in * n_out
+// small kernel puts a row's slices together and ranks what is left of a group, at most n_in * n_out
 // continuations, by score in 64 bits.
-// Selection within a wave: with E entries per lane the n_out-th largest of the 64 lanes' best
-// bounds the n_out-th largest entry from below, and is found in 32 ballots whatever n_out is;
-// about n_out entries lie above it.
+// A wave has a slice to itself, all of it in registers, NE entries per lane: no barrier anywhere, and the selection is paid once per
+// wave.  What bounds it are instructions, not the logits' bytes: 128 rows of 50258 took 18.7 us with 64-bit keys for every
+// entry, SLICE_US with keys for those alone that can be among the best.
 #include "spd_device.h"
 
 using namespace spdd;
@@ -17,188 +17,228 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int NTB = 256, NWB = NTB / WAVE;       // slices: threads and waves per block
-constexpr int E = 16;                            // entries per thread
-constexpr int SLICE = NTB * E;
 constexpr int NTM = 1024;                        // merge: a wave per row
-constexpr int EM = 4;                            // keys per lane and turn there
+constexpr int EM = 8;                            // keys per lane and turn there
+constexpr int WAVES = 3072;                      // three per SIMD: slices are made longer only where there would be more
 
-// Larger is better: higher logit, then lower id.  0: no entry (an excluded one, -inf, is none either).
-__device__ __forceinline__ u64 sort_key(float z, int id) {
+// Order of fp32 numbers as unsigned ones.
+__device__ __forceinline__ uint32_t ordered(float z) {
     const uint32_t u = __float_as_uint(z);
-    const uint32_t hi = (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return z == -INFINITY ? 0ull : ((u64)hi << 32) | (0xFFFFFFFFu - (uint32_t)id);
+    return (int32_t)u < 0 ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float key_logit(u64 k) {
-    const uint32_t hi = (uint32_t)(k >> 32);
-    return __uint_as_float((hi & 0x80000000u) ? hi & 0x7FFFFFFFu : ~hi);
-}
+__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float((int32_t)o < 0 ? o & 0x7FFFFFFFu : ~o); }
+
+// Larger is better: higher logit (-0 is 0), then lower id.  0: no entry.
+__device__ __forceinline__ u64 sort_key(float z, int id) { return ((u64)ordered(z + 0.f) << 32) | (0xFFFFFFFFu - (uint32_t)id); }
+__device__ __forceinline__ float key_logit(u64 k) { return from_ordered((uint32_t)(k >> 32)); }
 __device__ __forceinline__ int key_id(u64 k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
-// A logit as it counts: what is no number is excluded, +inf is the largest number, -0 is 0.
-__device__ __forceinline__ float clean(float z) {
-    if (z != z) return -INFINITY;
-    return fminf(z, 3.402823466e38f) + 0.f;
+// A logit as it counts: what is no number (a signalling NaN too, which a maximum or median would hand on) is excluded, +inf is the largest number.
+__device__ __forceinline__ float clean(float z) { return z >= -3.402823466e38f ? fminf(z, 3.402823466e38f) : -INFINITY; }
+
+__device__ __forceinline__ int lanes_below(u64 mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+__device__ __forceinline__ void lds_written() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
-// The n best of a wave's keys (N per lane), best first, into best[0 .. n) (LDS, this wave's); 0 where there are fewer.
-// `list`: LDS, WAVE keys of this wave's.
-template <int N>
-__device__ __forceinline__ void wave_best(const u64 (&key)[N], int n, u64 *list, u64 *best) {
-    const int lane = threadIdx.x & (WAVE - 1);
-    u64 top = 0;
+// Numbers of a wave's list that may be among its n largest values v (N per lane; -inf: none there), at most WAVE: put(place, e) stores what
+// stands for entry e.  Returns their number; more than WAVE: there are too many.  Of equal values those with the lower index (j, lane, x),
+// e = j * VEC + x, come first.
+//   * The n-th largest of the lanes' maxima, cut to its upper 16 bits, bounds the n-th largest value from below: 16 ballots.  About n
+//     entries are not below it.
+//   * Many equal values (masks of a finite number, ties): strictly above the bound there are few, and of the equal ones the first are taken.
+//   * Otherwise (few lanes hold all large values) the n-th largest value itself is found bit by bit.
+template <int N, int VEC, typename F>
+__device__ __forceinline__ int wave_candidates(const float (&v)[N], int n, F &&put) {
+    float top = v[0];
 #pragma unroll
-    for (int e = 0; e < N; ++e) top = key[e] > top ? key[e] : top;
-    const uint32_t top_hi = (uint32_t)(top >> 32);
-    uint32_t bound = 0;                          // the n-th largest of the lanes' best logits; 0 where fewer have one
+    for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
+    const uint32_t top_o = ordered(top) >> 16;
+    uint32_t bound = 0;
 #pragma unroll
-    for (int b = 31; b >= 0; --b) {
+    for (int b = 15; b >= 0; --b) {
         const uint32_t t = bound | (1u << b);
-        if (__popcll(__ballot(top_hi >= t)) >= n) bound = t;
+        if (__popcll(__ballot(top_o >= t)) >= n) bound = t;
     }
-    int count = 0;
+    const auto above = [&](float t) {            // (t is -inf at least: what is excluded is never above it)
+        int at = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) count += __popcll(__ballot(key[e] != 0 && (uint32_t)(key[e] >> 32) >= bound));
-    u64 least = (u64)bound << 32;
-    if (count > WAVE) {
-        // many equal logits: the n-th largest key itself (keys differ in their ids)
-        least = 0;
-        for (int b = 63; b >= 0; --b) {
-            const u64 t = least | (1ull << b);
-            int c = 0;
+        for (int e = 0; e < N; ++e) {
+            const u64 m = __ballot(v[e] > t);
+            if (m) {
+                const int place = at + lanes_below(m);
+                if (v[e] > t && place < WAVE) put(place, e);
+                at += __popcll(m);
+            }
+        }
+        return at;
+    };
+    constexpr uint32_t LEAST = 0x007Fu;          // the upper bits of -inf's order
+    // the number in front of the bound; in front of 0 that is not -0, which equals it
+    const float below = bound <= LEAST ? -INFINITY : from_ordered((bound << 16) - (bound == 0x8000u ? 2u : 1u));
+    int at = above(below);
+    if (at <= WAVE) return at;
+    float t = bound <= LEAST ? -INFINITY : from_ordered(bound << 16);
+    at = above(t);
+    if (at > WAVE) {
+        uint32_t o = 0;
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t c = o | (1u << b);
+            int count = 0;
 #pragma unroll
-            for (int e = 0; e < N; ++e) c += __popcll(__ballot(key[e] >= t));
-            if (c >= n) least = t;
+            for (int e = 0; e < N; ++e) count += __popcll(__ballot(ordered(v[e] + 0.f) >= c));
+            if (count >= n) o = c;
+        }
+        t = from_ordered(o);
+        at = above(t);
+    }
+    if (at >= n || t == -INFINITY) return at;
+#pragma unroll
+    for (int j = 0; j < N / VEC; ++j) {          // the first n - at of those equal to t
+        if (at < n) {
+            u64 m[VEC];
+            int place = at, all = 0;
+#pragma unroll
+            for (int x = 0; x < VEC; ++x) {
+                m[x] = __ballot(v[j * VEC + x] == t);
+                place += lanes_below(m[x]);
+                all += __popcll(m[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < VEC; ++x)
+                if (v[j * VEC + x] == t) {
+                    if (place < n) put(place, j * VEC + x);
+                    ++place;
+                }
+            at = min(at + all, n);
         }
     }
-    int at = 0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const bool in = key[e] != 0 && key[e] >= least;
-        const u64 m = __ballot(in);
-        if (in) list[at + __popcll(m & ((1ull << lane) - 1ull))] = key[e];
-        at += __popcll(m);
-    }
-    if (lane < n) best[lane] = 0;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const u64 mine = lane < at ? list[lane] : 0;
-    int rank = 0;
-    for (int i = 0; i < at; ++i) rank += list[i] > mine;
-    if (mine && rank < n) best[rank] = mine;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    return at;
 }
 
-template <typename LT> __device__ __forceinline__ float logit_at(const void *p, size_t i) { return Store<LT>::load1(p, i); }
+// The n best of the first `count` keys of a list (LDS, this wave's), best first; lane i returns the i-th, 0 past the last.  `best`: n keys of this wave's.
+__device__ __forceinline__ u64 ranked(const u64 *list, int count, int n, u64 *best) {
+    const int lane = threadIdx.x & (WAVE - 1);
+    if (lane < n) best[lane] = 0;
+    lds_written();
+    const u64 mine = lane < count ? list[lane] : 0;
+    int rank = 0;
+    for (int i = 0; i < count; ++i) rank += list[i] > mine;
+    if (lane < count && rank < n) best[rank] = mine;
+    lds_written();
+    const u64 k = lane < n ? best[lane] : 0;
+    lds_written();
+    return k;
+}
 
 __device__ __forceinline__ bool row_runs(const SelectArgs &a, int row) {
     const float score = as_global(a.scores)[row];
     return score > -INFINITY && !(a.ended && as_global(a.ended)[row] != 0);       // (a score that is no number: no beam)
 }
 
-// One block per (row, slice).
-template <typename LT, bool ALIGNED>
+// VEC logits of a lane, which lie side by side.
+template <typename LT, int VEC> __device__ __forceinline__ void load_logits(const char *p, float *f) {
+    if constexpr (VEC == Store<LT>::VEC) Store<LT>::unpack(global_load16(p), f);
+    else if constexpr (sizeof(LT) == 4) {
+        const u32x2 v = *(const u32x2 __attribute__((address_space(1))) *)p;
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y);
+    } else {
+        float g[8];
+        const uint32_t v = *(const uint32_t __attribute__((address_space(1))) *)p;
+        Store<LT>::unpack(u32x4{v, 0, 0, 0}, g);
+        f[0] = g[0]; f[1] = g[1];
+    }
+}
+
+// A wave per slice of 64 NE entries; lane l's vector j holds entries VEC (64 j + l) ...
+template <typename LT, int NE, int VEC>
 __global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
-    constexpr int VEC = Store<LT>::VEC;
     __shared__ u64 list[NWB][WAVE], best[NWB][SPD_K_MAX];
-    __shared__ float red[NWB];
-    const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = tid / WAVE;
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
-    if (!row_runs(a, row)) return;
+    const int lane = threadIdx.x & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int part = blockIdx.x * NWB + w, row = part / a.slices, slice = part - row * a.slices;
+    if (row >= a.n_groups * a.n_in || !row_runs(a, row)) return;
     const char *z_row = (const char *)a.logits + (size_t)row * a.row_stride * sizeof(LT);
-    const int lo = slice * SLICE;
-    float z[E];
+    const int lo = slice * WAVE * NE + lane * VEC;
+    const auto id = [&](int e) { return lo + (e / VEC) * WAVE * VEC + e % VEC; };
+    float z[NE];
+    if (slice * WAVE * NE + WAVE * NE <= a.vocab) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) z[i] = -INFINITY;
-    if (ALIGNED) {
-#pragma unroll
-        for (int j = 0; j < E / VEC; ++j) {
-            const int at = lo + (j * NTB + tid) * VEC;
-            if (at + VEC <= a.vocab) {
-                float f[VEC];
-                Store<LT>::unpack(global_load16(z_row + (size_t)at * sizeof(LT)), f);
-#pragma unroll
-                for (int v = 0; v < VEC; ++v) z[j * VEC + v] = f[v];
-            } else {
-#pragma unroll
-                for (int v = 0; v < VEC; ++v)
-                    if (at + v < a.vocab) z[j * VEC + v] = logit_at<LT>(z_row, at + v);
-            }
+        for (int j = 0; j < NE / VEC; ++j) {
+            if constexpr (VEC == 1) z[j] = Store<LT>::load1(z_row, id(j));
+            else load_logits<LT, VEC>(z_row + (size_t)id(j * VEC) * sizeof(LT), &z[j * VEC]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int at = lo + (i / VEC * NTB + tid) * VEC + i % VEC;
-            if (at < a.vocab) z[i] = logit_at<LT>(z_row, at);
-        }
+        for (int e = 0; e < NE; ++e) z[e] = id(e) < a.vocab ? Store<LT>::load1(z_row, id(e)) : -INFINITY;
     }
     float m = -INFINITY;
-    u64 key[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        z[i] = clean(z[i]);
-        m = fmaxf(m, z[i]);
-        key[i] = sort_key(z[i], lo + (i / VEC * NTB + tid) * VEC + i % VEC);
+    for (int e = 0; e < NE; ++e) {
+        z[e] = clean(z[e]);
+        m = fmaxf(m, z[e]);
     }
-    m = block_max<NTB>(m, red);
+    m = wave_max(m);
     const float c = 1.4426950408889634f / a.tau, ref = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum += exp2f((z[i] - ref) * c);
-    sum = block_sum<NTB>(sum, red);
-    wave_best<E>(key, a.n_out, list[w], best[w]);
-    __syncthreads();
-    const size_t part = (size_t)row * a.slices + slice;
-    if (w == 0) {
-        u64 k[1] = {lane < NWB * a.n_out ? best[lane / a.n_out][lane % a.n_out] : 0};
-        __builtin_amdgcn_wave_barrier();
-        int rank = 0;
-        for (int i = 0; i < NWB * a.n_out; ++i) {
-            const u64 other = best[i / a.n_out][i % a.n_out];
-            rank += other > k[0] || (other == k[0] && i < lane);
-        }
-        if (lane < NWB * a.n_out && rank < a.n_out) ((global_ptr<u64>)a.best)[part * a.n_out + rank] = k[0];
-    }
-    if (tid == NTB - 1) { as_global(a.top)[part] = m; as_global(a.sum)[part] = sum; }
+    for (int e = 0; e < NE; ++e) sum[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
+    const float s = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    const int count = wave_candidates<NE, VEC>(z, a.n_out, [&](int place, int e) { list[w][place] = sort_key(z[e], id(e)); });
+    const u64 k = ranked(list[w], min(count, WAVE), a.n_out, best[w]);
+    if (lane < a.n_out) ((global_ptr<u64>)a.best)[(size_t)part * a.n_out + lane] = k;
+    if (lane == 0) { as_global(a.top)[part] = m; as_global(a.sum)[part] = s; }
 }
 
 // One block per group, a wave per row; then the group's continuations are ranked.
 __global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
+    constexpr int MOST = SPD_K_MAX * SPD_K_MAX;
     __shared__ u64 list[SPD_K_MAX][WAVE], best[SPD_K_MAX][SPD_K_MAX];
-    __shared__ double score[SPD_K_MAX * SPD_K_MAX];
-    __shared__ int token[SPD_K_MAX * SPD_K_MAX];
-    __shared__ int s_ended[SPD_K_MAX];
-    __shared__ int present;
-    const int tid = threadIdx.x, lane = tid & (WAVE - 1), b = tid / WAVE, g = blockIdx.x, row = g * a.n_in + b;
-    if (tid == 0) present = 0;
+    __shared__ double score[MOST];
+    __shared__ int token[MOST], chosen[WAVE], s_ended[SPD_K_MAX], s_count;
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), b = __builtin_amdgcn_readfirstlane(tid / WAVE), g = blockIdx.x, row = g * a.n_in + b;
     if (b < a.n_in) {
         const float s = as_global(a.scores)[row];
         const bool ended = a.ended && as_global(a.ended)[row] != 0;
         if (row_runs(a, row)) {
             const size_t part = (size_t)row * a.slices;
-            float M = -INFINITY;
-            for (int i = lane; i < a.slices; i += WAVE) M = fmaxf(M, as_global(a.top)[part + i]);
-            M = wave_max(M);
-            const float c = 1.4426950408889634f / a.tau;
-            float sum = 0.f;
-            for (int i = lane; i < a.slices; i += WAVE) {
-                const float t = as_global(a.top)[part + i];
-                if (t > -INFINITY) sum += as_global(a.sum)[part + i] * exp2f((t - M) * c);
-            }
-            sum = wave_sum(sum);
             const u64 *keys = a.best + part * a.n_out;
             const int n = a.slices * a.n_out;
-            u64 kept = 0;                                         // lane i: the i-th best so far
-            for (int i0 = 0; i0 < n; i0 += EM * WAVE) {
-                u64 key[EM + 1];
+            u64 key[EM], kept = 0;                                // kept, lane i: the i-th best so far
+            const auto fetch = [&](int i0) {
 #pragma unroll
                 for (int e = 0; e < EM; ++e) {
                     const int i = i0 + e * WAVE + lane;
                     key[e] = i < n ? ((global_ptr<const u64>)keys)[i] : 0;
                 }
-                key[EM] = kept;
-                wave_best<EM + 1>(key, a.n_out, list[b], best[b]);
-                kept = lane < a.n_out ? best[b][lane] : 0;
+            };
+            fetch(0);
+            const float c = 1.4426950408889634f / a.tau;
+            float M = -INFINITY, sum = 0.f;
+            for (int i = lane; i < a.slices; i += WAVE) {
+                const float t = as_global(a.top)[part + i], x = as_global(a.sum)[part + i];
+                if (t == -INFINITY) continue;
+                const float up = fmaxf(M, t);
+                sum = sum * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - up) * c)) + x * __builtin_amdgcn_exp2f((t - up) * c);
+                M = up;
+            }
+            const float mine = M;
+            M = wave_max(M);
+            sum = wave_sum(mine == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((mine - M) * c));
+            for (int i0 = 0; i0 < n; i0 += EM * WAVE) {
+                if (i0) fetch(i0);
+                float v[EM + 1];
+                v[0] = kept ? key_logit(kept) : -INFINITY;
+#pragma unroll
+                for (int e = 0; e < EM; ++e) v[e + 1] = key[e] ? key_logit(key[e]) : -INFINITY;
+                // (keys with equal logits lie in the order of their ids: kept ones, then slice by slice)
+                const int count = wave_candidates<EM + 1, 1>(v, a.n_out, [&](int place, int e) {
+                    u64 k = kept;
+#pragma unroll
+                    for (int q = 0; q < EM; ++q) k = e == q + 1 ? key[q] : k;
+                    list[b][place] = k;
+                });
+                kept = ranked(list[b], min(count, WAVE), a.n_out, best[b]);
             }
             if (lane < a.n_out) {
                 const double lse = (double)M / a.tau + log((double)sum);
@@ -213,41 +253,80 @@ __global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
     }
     __syncthreads();
     const int n = a.n_in * a.n_out;
-    if (tid < n) {
-        const double mine = score[tid];
-        const int tok = token[tid], beam = tid / a.n_out;
-        const bool there = mine > -INFINITY;
-        int rank = 0;
-        for (int i = 0; i < n; ++i) {
-            const double other = score[i];
-            const int ob = i / a.n_out;
-            rank += other > mine || (other == mine && (ob < beam || (ob == beam && token[i] < tok)));
+    // those that can be among the best by their scores in fp32 (rounding keeps the order)
+    int present = 0;
+    if (b == 0) {
+        float v[MOST / WAVE];
+#pragma unroll
+        for (int e = 0; e < MOST / WAVE; ++e) {
+            const double x = e * WAVE + lane < n ? score[e * WAVE + lane] : -INFINITY;
+            present += __popcll(__ballot(x > -INFINITY));
+            v[e] = x > -INFINITY ? fmaxf((float)x, -3.402823466e38f) : -INFINITY;
         }
-        if (there) atomicAdd(&present, 1);
-        if (there && rank < a.n_out) {
-            const int at = g * a.n_out + rank;
-            as_global(a.out_scores)[at] = (float)mine;
-            as_global(a.out_tokens)[at] = tok;
-            as_global(a.out_parents)[at] = beam;
-            if (a.out_ended) as_global(a.out_ended)[at] = s_ended[beam] || tok == a.end_token;
-        }
+        const int count = wave_candidates<MOST / WAVE, 1>(v, a.n_out, [&](int place, int e) { chosen[place] = e * WAVE + lane; });
+        // equal ones in fp32 may differ in 64 bits: where some were left out for being equal, all are looked at
+        int reach = 0;
+        float least = INFINITY;
+        lds_written();
+        if (lane < min(count, WAVE)) least = fmaxf((float)score[chosen[lane]], -3.402823466e38f);
+        least = -wave_max(-least);
+#pragma unroll
+        for (int e = 0; e < MOST / WAVE; ++e) reach += __popcll(__ballot(v[e] >= least && v[e] > -INFINITY));
+        if (lane == 0) s_count = count <= WAVE && reach == count ? count : n;
     }
     __syncthreads();
-    if (tid < a.n_out && tid >= present) {                        // fewer continuations than asked for
-        const int at = g * a.n_out + tid;
-        as_global(a.out_scores)[at] = -INFINITY;
-        as_global(a.out_tokens)[at] = 0;
-        as_global(a.out_parents)[at] = tid < a.n_in ? tid : 0;
-        if (a.out_ended) as_global(a.out_ended)[at] = 0;
+    const bool all = s_count == n;
+    const int of = all ? n : s_count;
+    if (tid < of) {
+        const int at = all ? tid : chosen[tid];
+        const double mine = score[at];
+        const int tok = token[at], beam = at / a.n_out;
+        int rank = 0;
+        for (int i = 0; i < of; ++i) {
+            const int o = all ? i : chosen[i], ob = o / a.n_out;
+            const double other = score[o];
+            rank += other > mine || (other == mine && (ob < beam || (ob == beam && token[o] < tok)));
+        }
+        if (mine > -INFINITY && rank < a.n_out) {
+            const int to = g * a.n_out + rank;
+            as_global(a.out_scores)[to] = (float)mine;
+            as_global(a.out_tokens)[to] = tok;
+            as_global(a.out_parents)[to] = beam;
+            if (a.out_ended) as_global(a.out_ended)[to] = s_ended[beam] || tok == a.end_token;
+        }
+    }
+    if (b == 0 && lane < a.n_out && lane >= present) {            // fewer continuations than asked for
+        const int to = g * a.n_out + lane;
+        as_global(a.out_scores)[to] = -INFINITY;
+        as_global(a.out_tokens)[to] = 0;
+        as_global(a.out_parents)[to] = lane < a.n_in ? lane : 0;
+        if (a.out_ended) as_global(a.out_ended)[to] = 0;
     }
 }
 
+// Entries per lane of a slice: as few as WAVES waves allow (a wave's first word comes after one trip to memory whatever it holds).
+int entries_per_lane(long long rows, int vocab) {
+    for (int ne = 8; ne < 64; ne *= 2)
+        if (rows * ((vocab + WAVE * ne - 1) / (WAVE * ne)) <= WAVES) return ne;
+    return 64;
+}
+
+template <typename LT, int VEC>
+void launch_slices(hipStream_t s, const SelectArgs &a, int ne, unsigned blocks) {
+    if (ne == 8) hipLaunchKernelGGL((beam_slice_kernel<LT, 8, VEC>), dim3(blocks), dim3(NTB), 0, s, a);
+    else if (ne == 16) hipLaunchKernelGGL((beam_slice_kernel<LT, 16, VEC>), dim3(blocks), dim3(NTB), 0, s, a);
+    else if (ne == 32) hipLaunchKernelGGL((beam_slice_kernel<LT, 32, VEC>), dim3(blocks), dim3(NTB), 0, s, a);
+    else hipLaunchKernelGGL((beam_slice_kernel<LT, 64, VEC>), dim3(blocks), dim3(NTB), 0, s, a);
+}
+
 template <typename LT>
-hipError_t launch_select(hipStream_t s, const SelectArgs &a) {
-    const unsigned blocks = (unsigned)((long long)a.n_groups * a.n_in * a.slices);
-    const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.row_stride * (int64_t)sizeof(LT) % 16 == 0;
-    if (aligned) hipLaunchKernelGGL((beam_slice_kernel<LT, true>), dim3(blocks), dim3(NTB), 0, s, a);
-    else hipLaunchKernelGGL((beam_slice_kernel<LT, false>), dim3(blocks), dim3(NTB), 0, s, a);
+hipError_t launch_select(hipStream_t s, const SelectArgs &a, int ne) {
+    const unsigned blocks = (unsigned)(((long long)a.n_groups * a.n_in * a.slices + NWB - 1) / NWB);
+    // as many logits per load as the rows' addresses allow
+    const auto on = [&](int bytes) { return (uintptr_t)a.logits % bytes == 0 && (a.n_groups * a.n_in == 1 || a.row_stride * (int64_t)sizeof(LT) % bytes == 0); };
+    if (on(16)) launch_slices<LT, Store<LT>::VEC>(s, a, ne, blocks);
+    else if (on(2 * sizeof(LT))) launch_slices<LT, 2>(s, a, ne, blocks);
+    else launch_slices<LT, 1>(s, a, ne, blocks);
     hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_groups), dim3(NTM), 0, s, a);
     return hipGetLastError();
 }
@@ -258,7 +337,9 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 extern "C" size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab) {
     if (n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= 0) return 0;
-    const size_t parts = (size_t)n_groups * n_in * (((size_t)vocab + SLICE - 1) / SLICE);
+    const long long rows = (long long)n_groups * n_in;
+    const int slice = WAVE * entries_per_lane(rows, vocab);
+    const size_t parts = (size_t)rows * (((size_t)vocab + slice - 1) / slice);
     return up256(parts * n_out * 8) + 2 * up256(parts * 4);
 }
 
@@ -273,14 +354,15 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     if (!logits || !scores || !out_scores || !out_tokens || !out_parents || (uintptr_t)logits % (dtype == SPD_DTYPE_FP32 ? 4 : 2)) return SPD_EINVAL;
     if (!scratch || (uintptr_t)scratch % 256) return SPD_EINVAL;
     if (scratch_bytes < spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab)) return SPD_EWORKSPACE;
+    const int ne = entries_per_lane((long long)n_groups * n_in, vocab), slice = WAVE * ne;
     SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, tau, out_scores, out_tokens, out_parents, out_ended,
-                 (vocab + SLICE - 1) / SLICE, nullptr, nullptr, nullptr};
+                 (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};
     const long long parts = (long long)n_groups * n_in * a.slices;
-    if (parts > INT32_MAX) return SPD_EINVAL;
+    if (parts > INT32_MAX - NWB) return SPD_EINVAL;
     a.best = (u64 *)scratch;
     a.top = (float *)((char *)scratch + up256((size_t)parts * n_out * 8));
     a.sum = (float *)((char *)a.top + up256((size_t)parts * 4));
     hipStream_t s = (hipStream_t)hip_stream;
-    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_select<float>(s, a) : dtype == SPD_DTYPE_FP16 ? launch_select<half_t>(s, a) : launch_select<bf16_t>(s, a);
+    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_select<float>(s, a, ne) : dtype == SPD_DTYPE_FP16 ? launch_select<half_t>(s, a, ne) : launch_select<bf16_t>(s, a, ne);
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }
