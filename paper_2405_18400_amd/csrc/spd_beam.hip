@@ -6,8 +6,9 @@
 // small kernel puts a row's slices together and ranks what is left of a group, at most n_in * n_out
 // continuations, by score in 64 bits.
 // A wave has a slice to itself, all of it in registers, NE entries per lane: no barrier anywhere, and the selection is paid once per
-// wave.  What bounds it are instructions, not the logits' bytes: 128 rows of 50258 took 18.7 us with 64-bit keys for every
-// entry, SLICE_US with keys for those alone that can be among the best.
+// wave.  128 rows of 50258 (22.5 MB read of 112 of them, 4.7 us at a large copy's rate): 18.7 us with 64-bit keys for every
+// entry, 10.6 with keys for those alone that can be among the best; 64 rows of 131072 in bf16 22.8 -> 11.0.  The second kernel, a chain of
+// dependent steps in one block per group: 15.5 -> 6.0 and 34 -> 9.3 us.
 #include "spd_device.h"
 
 using namespace spdd;
@@ -19,7 +20,7 @@ typedef unsigned long long u64;
 constexpr int NTB = 256, NWB = NTB / WAVE;       // slices: threads and waves per block
 constexpr int NTM = 1024;                        // merge: a wave per row
 constexpr int EM = 8;                            // keys per lane and turn there
-constexpr int WAVES = 3072;                      // three per SIMD: slices are made longer only where there would be more
+constexpr int WAVES = 3300;                      // three per SIMD: slices are made longer only where there would be more
 
 // Order of fp32 numbers as unsigned ones.
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -37,9 +38,27 @@ __device__ __forceinline__ int key_id(u64 k) { return (int)(0xFFFFFFFFu - (uint3
 __device__ __forceinline__ float clean(float z) { return z >= -3.402823466e38f ? fminf(z, 3.402823466e38f) : -INFINITY; }
 
 __device__ __forceinline__ int lanes_below(u64 mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+// Over the wave, by the vector unit's own lane-crossing moves: a third of the time of six trips through the LDS crossbar.
+__device__ __forceinline__ float all_max(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(v)), WAVE - 1)); }
+__device__ __forceinline__ float all_sum(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_sum_last(v)), WAVE - 1)); }
+// log x for x > 0: of the mantissa, at most 1, in fp32 (2^-24 off), of the power of two in 64 bits.
+__device__ __forceinline__ double log_of(float x) {
+    return 0.69314718055994531 * ((double)__builtin_amdgcn_frexp_expf(x) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(x)));
+}
 __device__ __forceinline__ void lds_written() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+// The n-th largest of the lanes' 16-bit numbers.
+__device__ __forceinline__ uint32_t nth_upper(uint32_t x, int n) {
+    uint32_t bound = 0;
+#pragma unroll
+    for (int b = 15; b >= 0; --b) {
+        const uint32_t t = bound | (1u << b);
+        if (__popcll(__ballot(x >= t)) >= n) bound = t;
+    }
+    return bound;
 }
 
 // Numbers of a wave's list that may be among its n largest values v (N per lane; -inf: none there), at most WAVE: put(place, e) stores what
@@ -54,13 +73,7 @@ __device__ __forceinline__ int wave_candidates(const float (&v)[N], int n, F &&p
     float top = v[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
-    const uint32_t top_o = ordered(top) >> 16;
-    uint32_t bound = 0;
-#pragma unroll
-    for (int b = 15; b >= 0; --b) {
-        const uint32_t t = bound | (1u << b);
-        if (__popcll(__ballot(top_o >= t)) >= n) bound = t;
-    }
+    const uint32_t bound = nth_upper(ordered(top) >> 16, n);
     const auto above = [&](float t) {            // (t is -inf at least: what is excluded is never above it)
         int at = 0;
 #pragma unroll
@@ -118,13 +131,17 @@ __device__ __forceinline__ int wave_candidates(const float (&v)[N], int n, F &&p
 }
 
 // The n best of the first `count` keys of a list (LDS, this wave's), best first; lane i returns the i-th, 0 past the last.  `best`: n keys of this wave's.
-__device__ __forceinline__ u64 ranked(const u64 *list, int count, int n, u64 *best) {
+__device__ __forceinline__ u64 ranked(u64 *list, int count, int n, u64 *best) {
     const int lane = threadIdx.x & (WAVE - 1);
     if (lane < n) best[lane] = 0;
+    if (lane >= count && lane < ((count + 3) & ~3)) list[lane] = 0;
     lds_written();
     const u64 mine = lane < count ? list[lane] : 0;
     int rank = 0;
-    for (int i = 0; i < count; ++i) rank += list[i] > mine;
+    for (int i = 0; i < count; i += 4) {         // (four at a time: one wait for their way from LDS)
+        const u64 a = list[i], b = list[i + 1], c = list[i + 2], d = list[i + 3];
+        rank += (a > mine) + (b > mine) + (c > mine) + (d > mine);
+    }
     if (lane < count && rank < n) best[rank] = mine;
     lds_written();
     const u64 k = lane < n ? best[lane] : 0;
@@ -157,7 +174,7 @@ __global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
     __shared__ u64 list[NWB][WAVE], best[NWB][SPD_K_MAX];
     const int lane = threadIdx.x & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int part = blockIdx.x * NWB + w, row = part / a.slices, slice = part - row * a.slices;
-    if (row >= a.n_groups * a.n_in || !row_runs(a, row)) return;
+    if (row >= a.n_groups * a.n_in) return;
     const char *z_row = (const char *)a.logits + (size_t)row * a.row_stride * sizeof(LT);
     const int lo = slice * WAVE * NE + lane * VEC;
     const auto id = [&](int e) { return lo + (e / VEC) * WAVE * VEC + e % VEC; };
@@ -172,18 +189,19 @@ __global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
 #pragma unroll
         for (int e = 0; e < NE; ++e) z[e] = id(e) < a.vocab ? Store<LT>::load1(z_row, id(e)) : -INFINITY;
     }
+    if (!row_runs(a, row)) return;               // (looked at while the logits are under way: a trip to memory less)
     float m = -INFINITY;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
         z[e] = clean(z[e]);
         m = fmaxf(m, z[e]);
     }
-    m = wave_max(m);
-    const float c = 1.4426950408889634f / a.tau, ref = m == -INFINITY ? 0.f : m;
+    m = all_max(m);
+    const float c = a.log2_by_tau, ref = m == -INFINITY ? 0.f : m;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < NE; ++e) sum[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
-    const float s = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    const float s = all_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
     const int count = wave_candidates<NE, VEC>(z, a.n_out, [&](int place, int e) { list[w][place] = sort_key(z[e], id(e)); });
     const u64 k = ranked(list[w], min(count, WAVE), a.n_out, best[w]);
     if (lane < a.n_out) ((global_ptr<u64>)a.best)[(size_t)part * a.n_out + lane] = k;
@@ -195,54 +213,77 @@ __global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
     constexpr int MOST = SPD_K_MAX * SPD_K_MAX;
     __shared__ u64 list[SPD_K_MAX][WAVE], best[SPD_K_MAX][SPD_K_MAX];
     __shared__ double score[MOST];
-    __shared__ int token[MOST], chosen[WAVE], s_ended[SPD_K_MAX], s_count;
+    __shared__ int token[MOST], chosen[MOST], s_ended[SPD_K_MAX], s_count;
+    __shared__ double c_score[MOST];
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), b = __builtin_amdgcn_readfirstlane(tid / WAVE), g = blockIdx.x, row = g * a.n_in + b;
     if (b < a.n_in) {
+        // asked for at once (a row that does not run has nothing there: what comes is not looked at)
+        const size_t part = (size_t)row * a.slices;
+        const u64 *keys = a.best + part * a.n_out;
+        const int n = a.slices * a.n_out;
+        u64 key[EM], kept = 0;                                    // kept, lane i: the i-th best so far
+        const auto fetch = [&](int i0) {
+#pragma unroll
+            for (int e = 0; e < EM; ++e) {
+                const int i = i0 + EM * lane + e;                 // (a lane's keys are a stretch of a sorted list: its first is a good bound)
+                key[e] = i < n ? ((global_ptr<const u64>)keys)[i] : 0;
+            }
+        };
+        fetch(0);
+        const float first_top = lane < a.slices ? as_global(a.top)[part + lane] : -INFINITY, first_sum = lane < a.slices ? as_global(a.sum)[part + lane] : 0.f;
         const float s = as_global(a.scores)[row];
         const bool ended = a.ended && as_global(a.ended)[row] != 0;
-        if (row_runs(a, row)) {
-            const size_t part = (size_t)row * a.slices;
-            const u64 *keys = a.best + part * a.n_out;
-            const int n = a.slices * a.n_out;
-            u64 key[EM], kept = 0;                                // kept, lane i: the i-th best so far
-            const auto fetch = [&](int i0) {
-#pragma unroll
-                for (int e = 0; e < EM; ++e) {
-                    const int i = i0 + e * WAVE + lane;
-                    key[e] = i < n ? ((global_ptr<const u64>)keys)[i] : 0;
-                }
-            };
-            fetch(0);
-            const float c = 1.4426950408889634f / a.tau;
+        if (s > -INFINITY && !ended) {                            // (a score that is no number: no beam)
+            const float c = a.log2_by_tau;
             float M = -INFINITY, sum = 0.f;
             for (int i = lane; i < a.slices; i += WAVE) {
-                const float t = as_global(a.top)[part + i], x = as_global(a.sum)[part + i];
+                const float t = i < WAVE ? first_top : as_global(a.top)[part + i], x = i < WAVE ? first_sum : as_global(a.sum)[part + i];
                 if (t == -INFINITY) continue;
                 const float up = fmaxf(M, t);
                 sum = sum * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - up) * c)) + x * __builtin_amdgcn_exp2f((t - up) * c);
                 M = up;
             }
             const float mine = M;
-            M = wave_max(M);
-            sum = wave_sum(mine == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((mine - M) * c));
+            M = all_max(M);
+            sum = all_sum(mine == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((mine - M) * c));
             for (int i0 = 0; i0 < n; i0 += EM * WAVE) {
                 if (i0) fetch(i0);
-                float v[EM + 1];
-                v[0] = kept ? key_logit(kept) : -INFINITY;
+                u64 top = kept;
 #pragma unroll
-                for (int e = 0; e < EM; ++e) v[e + 1] = key[e] ? key_logit(key[e]) : -INFINITY;
-                // (keys with equal logits lie in the order of their ids: kept ones, then slice by slice)
-                const int count = wave_candidates<EM + 1, 1>(v, a.n_out, [&](int place, int e) {
-                    u64 k = kept;
+                for (int e = 0; e < EM; ++e) top = key[e] > top ? key[e] : top;
+                const uint32_t bound = nth_upper((uint32_t)(top >> 48), a.n_out);
+                const auto from = [&](u64 least) {                // the keys not below `least`
+                    int at = 0;
 #pragma unroll
-                    for (int q = 0; q < EM; ++q) k = e == q + 1 ? key[q] : k;
-                    list[b][place] = k;
-                });
-                kept = ranked(list[b], min(count, WAVE), a.n_out, best[b]);
+                    for (int e = 0; e <= EM; ++e) {
+                        const u64 k = e ? key[e - 1] : kept;
+                        const bool in = k >= least;
+                        const u64 m = __ballot(in);
+                        if (m) {
+                            const int place = at + lanes_below(m);
+                            if (in && place < WAVE) list[b][place] = k;
+                            at += __popcll(m);
+                        }
+                    }
+                    return at;
+                };
+                int count = from(bound ? (u64)bound << 48 : 1);
+                if (count > WAVE) {                               // many equal logits: the n-th largest key itself
+                    u64 least = 0;
+                    for (int q = 63; q >= 0; --q) {
+                        const u64 t = least | (1ull << q);
+                        int c = __popcll(__ballot(kept >= t));
+#pragma unroll
+                        for (int e = 0; e < EM; ++e) c += __popcll(__ballot(key[e] >= t));
+                        if (c >= a.n_out) least = t;
+                    }
+                    count = from(least);
+                }
+                kept = ranked(list[b], count, a.n_out, best[b]);
             }
             if (lane < a.n_out) {
-                const double lse = (double)M / a.tau + log((double)sum);
-                score[b * a.n_out + lane] = kept ? (double)s + ((double)key_logit(kept) / a.tau - lse) : -INFINITY;
+                const double lse = (double)M * a.by_tau + (sum > 0.f ? log_of(sum) : 0.0);
+                score[b * a.n_out + lane] = kept ? (double)s + ((double)key_logit(kept) * a.by_tau - lse) : -INFINITY;
                 token[b * a.n_out + lane] = key_id(kept);
             }
         } else if (lane < a.n_out) {                              // an ended beam goes on as it is; an absent one has no continuation
@@ -259,36 +300,47 @@ __global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
         float v[MOST / WAVE];
 #pragma unroll
         for (int e = 0; e < MOST / WAVE; ++e) {
-            const double x = e * WAVE + lane < n ? score[e * WAVE + lane] : -INFINITY;
+            const int at = lane * (MOST / WAVE) + e;
+            const double x = at < n ? score[at] : -INFINITY;
             present += __popcll(__ballot(x > -INFINITY));
             v[e] = x > -INFINITY ? fmaxf((float)x, -3.402823466e38f) : -INFINITY;
         }
-        const int count = wave_candidates<MOST / WAVE, 1>(v, a.n_out, [&](int place, int e) { chosen[place] = e * WAVE + lane; });
+        const int count = wave_candidates<MOST / WAVE, MOST / WAVE>(v, a.n_out, [&](int place, int e) { chosen[place] = lane * (MOST / WAVE) + e; });
         // equal ones in fp32 may differ in 64 bits: where some were left out for being equal, all are looked at
         int reach = 0;
         float least = INFINITY;
         lds_written();
         if (lane < min(count, WAVE)) least = fmaxf((float)score[chosen[lane]], -3.402823466e38f);
-        least = -wave_max(-least);
+        least = -all_max(-least);
 #pragma unroll
         for (int e = 0; e < MOST / WAVE; ++e) reach += __popcll(__ballot(v[e] >= least && v[e] > -INFINITY));
-        if (lane == 0) s_count = count <= WAVE && reach == count ? count : n;
+        const bool few = count <= WAVE && reach == count;
+        if (few && lane < count) c_score[lane] = score[chosen[lane]];
+        if (few && lane >= count && lane < ((count + 3) & ~3)) { c_score[lane] = -INFINITY; chosen[lane] = MOST; }
+        if (lane == 0) s_count = few ? count : -1;
     }
     __syncthreads();
-    const bool all = s_count == n;
-    const int of = all ? n : s_count;
+    if (s_count < 0) {
+        if (tid < MOST) {
+            chosen[tid] = tid;
+            c_score[tid] = tid < n ? score[tid] : -INFINITY;
+        }
+        __syncthreads();
+    }
+    const int of = s_count < 0 ? n : s_count;
     if (tid < of) {
-        const int at = all ? tid : chosen[tid];
-        const double mine = score[at];
-        const int tok = token[at], beam = at / a.n_out;
+        const int at = chosen[tid];
+        const double mine = c_score[tid];
         int rank = 0;
-        for (int i = 0; i < of; ++i) {
-            const int o = all ? i : chosen[i], ob = o / a.n_out;
-            const double other = score[o];
-            rank += other > mine || (other == mine && (ob < beam || (ob == beam && token[o] < tok)));
+        for (int i = 0; i < of; i += 4) {
+            const double o0 = c_score[i], o1 = c_score[i + 1], o2 = c_score[i + 2], o3 = c_score[i + 3];
+            // (continuations lie by beam, those of a beam by logit and id: among equals the lower place goes first)
+            const int p0 = chosen[i], p1 = chosen[i + 1], p2 = chosen[i + 2], p3 = chosen[i + 3];
+            rank += (o0 > mine || (o0 == mine && p0 < at)) + (o1 > mine || (o1 == mine && p1 < at));
+            rank += (o2 > mine || (o2 == mine && p2 < at)) + (o3 > mine || (o3 == mine && p3 < at));
         }
         if (mine > -INFINITY && rank < a.n_out) {
-            const int to = g * a.n_out + rank;
+            const int to = g * a.n_out + rank, tok = token[at], beam = at / a.n_out;
             as_global(a.out_scores)[to] = (float)mine;
             as_global(a.out_tokens)[to] = tok;
             as_global(a.out_parents)[to] = beam;
@@ -355,7 +407,7 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     if (!scratch || (uintptr_t)scratch % 256) return SPD_EINVAL;
     if (scratch_bytes < spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab)) return SPD_EWORKSPACE;
     const int ne = entries_per_lane((long long)n_groups * n_in, vocab), slice = WAVE * ne;
-    SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, tau, out_scores, out_tokens, out_parents, out_ended,
+    SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, 1.4426950408889634f / tau, 1.0 / (double)tau, out_scores, out_tokens, out_parents, out_ended,
                  (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};
     const long long parts = (long long)n_groups * n_in * a.slices;
     if (parts > INT32_MAX - NWB) return SPD_EINVAL;

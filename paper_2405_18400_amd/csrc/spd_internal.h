@@ -305,7 +305,8 @@ struct SelectArgs {
     const float *scores;         // [n_groups, n_in]
     const int32_t *ended;        // [n_groups, n_in], or null
     int32_t end_token;
-    float tau;
+    float log2_by_tau;           // log2(e) / tau
+    double by_tau;
     float *out_scores;           // [n_groups, n_out], as the next three
     int32_t *out_tokens, *out_parents, *out_ended;
     int32_t slices;
