@@ -326,7 +326,7 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
  * so that a captured step can be replayed; what the host cannot check is bounded by the kernels: a page number outside
  * [0, n_pages), a row of the table or a length out of range is never followed, and *err (DEVICE int32, may be NULL) is
  * set to 1 (and never cleared).  Calls do not synchronise and allocate nothing; those that need scratch take it from the caller, 256-byte
- * aligned and of the size the function beside them gives (SPD_EWORKSPACE if less), and leave nothing in it for a
+ * aligned and of the size the function beside them gives (0: none, NULL will do; SPD_EWORKSPACE if less), and leave nothing in it for a
  * later call: calls that may overlap need scratch of their own. */
 
 /* New tokens' keys and values into the cache, rotated on the way: token i, at position pos[i] of sequence seq[i] (DEVICE int32

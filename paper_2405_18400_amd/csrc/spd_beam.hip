@@ -142,7 +142,7 @@ __device__ __forceinline__ u64 ranked(u64 *list, int count, int n, u64 *best) {
         const u64 a = list[i], b = list[i + 1], c = list[i + 2], d = list[i + 3];
         rank += (a > mine) + (b > mine) + (c > mine) + (d > mine);
     }
-    if (lane < count && rank < n) best[rank] = mine;
+    if (mine && rank < n) best[rank] = mine;
     lds_written();
     const u64 k = lane < n ? best[lane] : 0;
     lds_written();
@@ -203,157 +203,230 @@ __global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
     for (int e = 0; e < NE; ++e) sum[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
     const float s = all_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
     const int count = wave_candidates<NE, VEC>(z, a.n_out, [&](int place, int e) { list[w][place] = sort_key(z[e], id(e)); });
-    const u64 k = ranked(list[w], min(count, WAVE), a.n_out, best[w]);
+    const u64 k = ranked(list[w], count, a.n_out, best[w]);
     if (lane < a.n_out) ((global_ptr<u64>)a.best)[(size_t)part * a.n_out + lane] = k;
     if (lane == 0) { as_global(a.top)[part] = m; as_global(a.sum)[part] = s; }
 }
 
-// One block per group, a wave per row; then the group's continuations are ranked.
-__global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
-    constexpr int MOST = SPD_K_MAX * SPD_K_MAX;
-    __shared__ u64 list[SPD_K_MAX][WAVE], best[SPD_K_MAX][SPD_K_MAX];
-    __shared__ double score[MOST];
-    __shared__ int token[MOST], chosen[MOST], s_ended[SPD_K_MAX], s_count;
-    __shared__ double c_score[MOST];
-    const int tid = threadIdx.x, lane = tid & (WAVE - 1), b = __builtin_amdgcn_readfirstlane(tid / WAVE), g = blockIdx.x, row = g * a.n_in + b;
-    if (b < a.n_in) {
-        // asked for at once (a row that does not run has nothing there: what comes is not looked at)
-        const size_t part = (size_t)row * a.slices;
-        const u64 *keys = a.best + part * a.n_out;
-        const int n = a.slices * a.n_out;
-        u64 key[EM], kept = 0;                                    // kept, lane i: the i-th best so far
-        const auto fetch = [&](int i0) {
-#pragma unroll
-            for (int e = 0; e < EM; ++e) {
-                const int i = i0 + EM * lane + e;                 // (a lane's keys are a stretch of a sorted list: its first is a good bound)
-                key[e] = i < n ? ((global_ptr<const u64>)keys)[i] : 0;
-            }
-        };
-        fetch(0);
-        const float first_top = lane < a.slices ? as_global(a.top)[part + lane] : -INFINITY, first_sum = lane < a.slices ? as_global(a.sum)[part + lane] : 0.f;
-        const float s = as_global(a.scores)[row];
-        const bool ended = a.ended && as_global(a.ended)[row] != 0;
-        if (s > -INFINITY && !ended) {                            // (a score that is no number: no beam)
-            const float c = a.log2_by_tau;
-            float M = -INFINITY, sum = 0.f;
-            for (int i = lane; i < a.slices; i += WAVE) {
-                const float t = i < WAVE ? first_top : as_global(a.top)[part + i], x = i < WAVE ? first_sum : as_global(a.sum)[part + i];
-                if (t == -INFINITY) continue;
-                const float up = fmaxf(M, t);
-                sum = sum * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - up) * c)) + x * __builtin_amdgcn_exp2f((t - up) * c);
-                M = up;
-            }
-            const float mine = M;
-            M = all_max(M);
-            sum = all_sum(mine == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((mine - M) * c));
-            for (int i0 = 0; i0 < n; i0 += EM * WAVE) {
-                if (i0) fetch(i0);
-                u64 top = kept;
-#pragma unroll
-                for (int e = 0; e < EM; ++e) top = key[e] > top ? key[e] : top;
-                const uint32_t bound = nth_upper((uint32_t)(top >> 48), a.n_out);
-                const auto from = [&](u64 least) {                // the keys not below `least`
-                    int at = 0;
-#pragma unroll
-                    for (int e = 0; e <= EM; ++e) {
-                        const u64 k = e ? key[e - 1] : kept;
-                        const bool in = k >= least;
-                        const u64 m = __ballot(in);
-                        if (m) {
-                            const int place = at + lanes_below(m);
-                            if (in && place < WAVE) list[b][place] = k;
-                            at += __popcll(m);
-                        }
-                    }
-                    return at;
-                };
-                int count = from(bound ? (u64)bound << 48 : 1);
-                if (count > WAVE) {                               // many equal logits: the n-th largest key itself
-                    u64 least = 0;
-                    for (int q = 63; q >= 0; --q) {
-                        const u64 t = least | (1ull << q);
-                        int c = __popcll(__ballot(kept >= t));
-#pragma unroll
-                        for (int e = 0; e < EM; ++e) c += __popcll(__ballot(key[e] >= t));
-                        if (c >= a.n_out) least = t;
-                    }
-                    count = from(least);
-                }
-                kept = ranked(list[b], count, a.n_out, best[b]);
-            }
-            if (lane < a.n_out) {
-                const double lse = (double)M * a.by_tau + (sum > 0.f ? log_of(sum) : 0.0);
-                score[b * a.n_out + lane] = kept ? (double)s + ((double)key_logit(kept) * a.by_tau - lse) : -INFINITY;
-                token[b * a.n_out + lane] = key_id(kept);
-            }
-        } else if (lane < a.n_out) {                              // an ended beam goes on as it is; an absent one has no continuation
-            score[b * a.n_out + lane] = ended && lane == 0 && s > -INFINITY ? (double)s : -INFINITY;
-            token[b * a.n_out + lane] = a.end_token;
-        }
-        if (lane == 0) s_ended[b] = ended;
-    }
+// What a group's block keeps of its rows: up to n_out continuations of each, best first, by place beam * n_out + rank.
+constexpr int MOST = SPD_K_MAX * SPD_K_MAX;
+struct Group {
+    u64 list[SPD_K_MAX][WAVE], best[SPD_K_MAX][SPD_K_MAX];
+    double score[MOST], c_score[MOST];
+    int token[MOST], chosen[MOST], ended[SPD_K_MAX], count;
+};
+
+// This wave's row: its best keys (lane i: the i-th, 0 where there is none), largest logit and sum of exponentials -> its continuations' scores.
+__device__ __forceinline__ void put_row(const SelectArgs &a, Group &s, int b, float row_score, u64 kept, float M, float sum) {
+    const int lane = threadIdx.x & (WAVE - 1);
+    if (lane >= a.n_out) return;
+    const double lse = (double)M * a.by_tau + (sum > 0.f ? log_of(sum) : 0.0);
+    s.score[b * a.n_out + lane] = kept ? (double)row_score + ((double)key_logit(kept) * a.by_tau - lse) : -INFINITY;
+    s.token[b * a.n_out + lane] = key_id(kept);
+}
+// An ended beam goes on as it is; an absent one has no continuation.
+__device__ __forceinline__ void put_no_row(const SelectArgs &a, Group &s, int b, float row_score, bool ended) {
+    const int lane = threadIdx.x & (WAVE - 1);
+    if (lane >= a.n_out) return;
+    s.score[b * a.n_out + lane] = ended && lane == 0 && row_score > -INFINITY ? (double)row_score : -INFINITY;
+    s.token[b * a.n_out + lane] = a.end_token;
+}
+
+// The group's continuations in order, by all threads of its block (any number of waves).
+__device__ __forceinline__ void rank_group(const SelectArgs &a, Group &s, int g) {
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), n = a.n_in * a.n_out;
     __syncthreads();
-    const int n = a.n_in * a.n_out;
     // those that can be among the best by their scores in fp32 (rounding keeps the order)
     int present = 0;
-    if (b == 0) {
+    if (tid < WAVE) {
         float v[MOST / WAVE];
 #pragma unroll
         for (int e = 0; e < MOST / WAVE; ++e) {
             const int at = lane * (MOST / WAVE) + e;
-            const double x = at < n ? score[at] : -INFINITY;
+            const double x = at < n ? s.score[at] : -INFINITY;
             present += __popcll(__ballot(x > -INFINITY));
             v[e] = x > -INFINITY ? fmaxf((float)x, -3.402823466e38f) : -INFINITY;
         }
-        const int count = wave_candidates<MOST / WAVE, MOST / WAVE>(v, a.n_out, [&](int place, int e) { chosen[place] = lane * (MOST / WAVE) + e; });
+        const int count = wave_candidates<MOST / WAVE, MOST / WAVE>(v, a.n_out, [&](int place, int e) { s.chosen[place] = lane * (MOST / WAVE) + e; });
         // equal ones in fp32 may differ in 64 bits: where some were left out for being equal, all are looked at
         int reach = 0;
         float least = INFINITY;
         lds_written();
-        if (lane < min(count, WAVE)) least = fmaxf((float)score[chosen[lane]], -3.402823466e38f);
+        if (lane < min(count, WAVE)) least = fmaxf((float)s.score[s.chosen[lane]], -3.402823466e38f);
         least = -all_max(-least);
 #pragma unroll
         for (int e = 0; e < MOST / WAVE; ++e) reach += __popcll(__ballot(v[e] >= least && v[e] > -INFINITY));
         const bool few = count <= WAVE && reach == count;
-        if (few && lane < count) c_score[lane] = score[chosen[lane]];
-        if (few && lane >= count && lane < ((count + 3) & ~3)) { c_score[lane] = -INFINITY; chosen[lane] = MOST; }
-        if (lane == 0) s_count = few ? count : -1;
+        if (few && lane < count) s.c_score[lane] = s.score[s.chosen[lane]];
+        if (few && lane >= count && lane < ((count + 3) & ~3)) { s.c_score[lane] = -INFINITY; s.chosen[lane] = MOST; }
+        if (lane == 0) s.count = few ? count : -1;
     }
     __syncthreads();
-    if (s_count < 0) {
-        if (tid < MOST) {
-            chosen[tid] = tid;
-            c_score[tid] = tid < n ? score[tid] : -INFINITY;
+    const int few = s.count;
+    if (few < 0) {
+        for (int i = tid; i < MOST; i += blockDim.x) {
+            s.chosen[i] = i;
+            s.c_score[i] = i < n ? s.score[i] : -INFINITY;
         }
         __syncthreads();
     }
-    const int of = s_count < 0 ? n : s_count;
-    if (tid < of) {
-        const int at = chosen[tid];
-        const double mine = c_score[tid];
+    const int of = few < 0 ? n : few;
+    for (int q = tid; q < of; q += blockDim.x) {
+        const int at = s.chosen[q];
+        const double mine = s.c_score[q];
         int rank = 0;
         for (int i = 0; i < of; i += 4) {
-            const double o0 = c_score[i], o1 = c_score[i + 1], o2 = c_score[i + 2], o3 = c_score[i + 3];
+            const double o0 = s.c_score[i], o1 = s.c_score[i + 1], o2 = s.c_score[i + 2], o3 = s.c_score[i + 3];
             // (continuations lie by beam, those of a beam by logit and id: among equals the lower place goes first)
-            const int p0 = chosen[i], p1 = chosen[i + 1], p2 = chosen[i + 2], p3 = chosen[i + 3];
+            const int p0 = s.chosen[i], p1 = s.chosen[i + 1], p2 = s.chosen[i + 2], p3 = s.chosen[i + 3];
             rank += (o0 > mine || (o0 == mine && p0 < at)) + (o1 > mine || (o1 == mine && p1 < at));
             rank += (o2 > mine || (o2 == mine && p2 < at)) + (o3 > mine || (o3 == mine && p3 < at));
         }
         if (mine > -INFINITY && rank < a.n_out) {
-            const int to = g * a.n_out + rank, tok = token[at], beam = at / a.n_out;
+            const int to = g * a.n_out + rank, tok = s.token[at], beam = at / a.n_out;
             as_global(a.out_scores)[to] = (float)mine;
             as_global(a.out_tokens)[to] = tok;
             as_global(a.out_parents)[to] = beam;
-            if (a.out_ended) as_global(a.out_ended)[to] = s_ended[beam] || tok == a.end_token;
+            if (a.out_ended) as_global(a.out_ended)[to] = s.ended[beam] || tok == a.end_token;
         }
     }
-    if (b == 0 && lane < a.n_out && lane >= present) {            // fewer continuations than asked for
-        const int to = g * a.n_out + lane;
+    if (tid < a.n_out && tid >= present) {                        // fewer continuations than asked for
+        const int to = g * a.n_out + tid;
         as_global(a.out_scores)[to] = -INFINITY;
         as_global(a.out_tokens)[to] = 0;
-        as_global(a.out_parents)[to] = lane < a.n_in ? lane : 0;
+        as_global(a.out_parents)[to] = tid < a.n_in ? tid : 0;
         if (a.out_ended) as_global(a.out_ended)[to] = 0;
     }
+}
+
+// One block per group, a wave per row, over the slices' results.
+__global__ __launch_bounds__(NTM) void beam_merge_kernel(const SelectArgs a) {
+    __shared__ Group s;
+    const int lane = threadIdx.x & (WAVE - 1), b = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), g = blockIdx.x, row = g * a.n_in + b;
+    // asked for at once (a row that does not run has nothing there: what comes is not looked at)
+    const size_t part = (size_t)row * a.slices;
+    const u64 *keys = a.best + part * a.n_out;
+    const int n = a.slices * a.n_out;
+    u64 key[EM], kept = 0;                                        // kept, lane i: the i-th best so far
+    const auto fetch = [&](int i0) {
+#pragma unroll
+        for (int e = 0; e < EM; ++e) {
+            const int i = i0 + EM * lane + e;                     // (a lane's keys are a stretch of a sorted list: its first is a good bound)
+            key[e] = i < n ? ((global_ptr<const u64>)keys)[i] : 0;
+        }
+    };
+    fetch(0);
+    const float first_top = lane < a.slices ? as_global(a.top)[part + lane] : -INFINITY, first_sum = lane < a.slices ? as_global(a.sum)[part + lane] : 0.f;
+    const float row_score = as_global(a.scores)[row];
+    const bool ended = a.ended && as_global(a.ended)[row] != 0;
+    if (lane == 0) s.ended[b] = ended;
+    if (row_score > -INFINITY && !ended) {                        // (a score that is no number: no beam)
+        const float c = a.log2_by_tau;
+        float M = -INFINITY, sum = 0.f;
+        for (int i = lane; i < a.slices; i += WAVE) {
+            const float t = i < WAVE ? first_top : as_global(a.top)[part + i], x = i < WAVE ? first_sum : as_global(a.sum)[part + i];
+            if (t == -INFINITY) continue;
+            const float up = fmaxf(M, t);
+            sum = sum * (M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - up) * c)) + x * __builtin_amdgcn_exp2f((t - up) * c);
+            M = up;
+        }
+        const float mine = M;
+        M = all_max(M);
+        sum = all_sum(mine == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f((mine - M) * c));
+        for (int i0 = 0; i0 < n; i0 += EM * WAVE) {
+            if (i0) fetch(i0);
+            u64 top = kept;
+#pragma unroll
+            for (int e = 0; e < EM; ++e) top = key[e] > top ? key[e] : top;
+            const uint32_t bound = nth_upper((uint32_t)(top >> 48), a.n_out);
+            const auto from = [&](u64 least) {                    // the keys not below `least`
+                int at = 0;
+#pragma unroll
+                for (int e = 0; e <= EM; ++e) {
+                    const u64 k = e ? key[e - 1] : kept;
+                    const bool in = k >= least;
+                    const u64 m = __ballot(in);
+                    if (m) {
+                        const int place = at + lanes_below(m);
+                        if (in && place < WAVE) s.list[b][place] = k;
+                        at += __popcll(m);
+                    }
+                }
+                return at;
+            };
+            int count = from(bound ? (u64)bound << 48 : 1);
+            if (count > WAVE) {                                   // many equal logits: the n-th largest key itself
+                u64 least = 0;
+                for (int q = 63; q >= 0; --q) {
+                    const u64 t = least | (1ull << q);
+                    int c = __popcll(__ballot(kept >= t));
+#pragma unroll
+                    for (int e = 0; e < EM; ++e) c += __popcll(__ballot(key[e] >= t));
+                    if (c >= a.n_out) least = t;
+                }
+                count = from(least);
+            }
+            kept = ranked(s.list[b], count, a.n_out, s.best[b]);
+        }
+        put_row(a, s, b, row_score, kept, M, sum);
+    } else {
+        put_no_row(a, s, b, row_score, ended);
+    }
+    rank_group(a, s, g);
+}
+
+// Small vocabularies, all in one launch: a block per group, a wave per row, 64 * 32 entries at a time in registers.
+constexpr int SMALL_NE = 32, SMALL = 4096;
+template <typename LT>
+__global__ __launch_bounds__(NTM) void beam_small_kernel(const SelectArgs a) {
+    __shared__ Group s;
+    const int lane = threadIdx.x & (WAVE - 1), b = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), g = blockIdx.x, row = g * a.n_in + b;
+    const char *z_row = (const char *)a.logits + (size_t)row * a.row_stride * sizeof(LT);
+    float z[SMALL_NE];
+    const auto fetch = [&](int lo) {
+#pragma unroll
+        for (int e = 0; e < SMALL_NE; ++e) {
+            const int i = lo + e * WAVE + lane;
+            z[e] = i < a.vocab ? Store<LT>::load1(z_row, i) : -INFINITY;
+        }
+    };
+    fetch(0);
+    const float row_score = as_global(a.scores)[row];
+    const bool ended = a.ended && as_global(a.ended)[row] != 0;
+    if (lane == 0) s.ended[b] = ended;
+    if (row_score > -INFINITY && !ended) {
+        const float c = a.log2_by_tau;
+        float M = -INFINITY, sum = 0.f;
+        u64 kept = 0;
+        for (int lo = 0; lo < a.vocab; lo += SMALL_NE * WAVE) {
+            if (lo) fetch(lo);
+            float m = M;
+#pragma unroll
+            for (int e = 0; e < SMALL_NE; ++e) {
+                z[e] = clean(z[e]);
+                m = fmaxf(m, z[e]);
+            }
+            m = all_max(m);
+            const float ref = m == -INFINITY ? 0.f : m;
+            sum *= M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - ref) * c);
+            M = m;
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < SMALL_NE; ++e) part[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            int count = wave_candidates<SMALL_NE, 1>(z, a.n_out, [&](int place, int e) { s.list[b][place] = sort_key(z[e], lo + e * WAVE + lane); });
+            const u64 before = kept;
+            kept = ranked(s.list[b], count, a.n_out, s.best[b]);
+            if (lo) {                                             // with those of the entries before
+                if (lane < a.n_out) { s.list[b][lane] = before; s.list[b][a.n_out + lane] = kept; }
+                kept = ranked(s.list[b], 2 * a.n_out, a.n_out, s.best[b]);
+            }
+        }
+        put_row(a, s, b, row_score, kept, M, all_sum(sum));
+    } else {
+        put_no_row(a, s, b, row_score, ended);
+    }
+    rank_group(a, s, g);
 }
 
 // Entries per lane of a slice: as few as WAVES waves allow (a wave's first word comes after one trip to memory whatever it holds).
@@ -373,13 +446,17 @@ void launch_slices(hipStream_t s, const SelectArgs &a, int ne, unsigned blocks) 
 
 template <typename LT>
 hipError_t launch_select(hipStream_t s, const SelectArgs &a, int ne) {
+    if (a.vocab <= SMALL) {
+        hipLaunchKernelGGL(beam_small_kernel<LT>, dim3(a.n_groups), dim3(a.n_in * WAVE), 0, s, a);
+        return hipGetLastError();
+    }
     const unsigned blocks = (unsigned)(((long long)a.n_groups * a.n_in * a.slices + NWB - 1) / NWB);
     // as many logits per load as the rows' addresses allow
     const auto on = [&](int bytes) { return (uintptr_t)a.logits % bytes == 0 && (a.n_groups * a.n_in == 1 || a.row_stride * (int64_t)sizeof(LT) % bytes == 0); };
     if (on(16)) launch_slices<LT, Store<LT>::VEC>(s, a, ne, blocks);
     else if (on(2 * sizeof(LT))) launch_slices<LT, 2>(s, a, ne, blocks);
     else launch_slices<LT, 1>(s, a, ne, blocks);
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_groups), dim3(NTM), 0, s, a);
+    hipLaunchKernelGGL(beam_merge_kernel, dim3(a.n_groups), dim3(a.n_in * WAVE), 0, s, a);
     return hipGetLastError();
 }
 
@@ -388,7 +465,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
 extern "C" size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab) {
-    if (n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= 0) return 0;
+    if (n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= SMALL) return 0;
     const long long rows = (long long)n_groups * n_in;
     const int slice = WAVE * entries_per_lane(rows, vocab);
     const size_t parts = (size_t)rows * (((size_t)vocab + slice - 1) / slice);
@@ -404,8 +481,9 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     if (ended && (end_token < 0 || end_token >= vocab)) return SPD_EINVAL;
     if (n_groups == 0) return SPD_OK;
     if (!logits || !scores || !out_scores || !out_tokens || !out_parents || (uintptr_t)logits % (dtype == SPD_DTYPE_FP32 ? 4 : 2)) return SPD_EINVAL;
-    if (!scratch || (uintptr_t)scratch % 256) return SPD_EINVAL;
-    if (scratch_bytes < spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab)) return SPD_EWORKSPACE;
+    const size_t need = spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab);
+    if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
+    if (scratch_bytes < need) return SPD_EWORKSPACE;
     const int ne = entries_per_lane((long long)n_groups * n_in, vocab), slice = WAVE * ne;
     SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, 1.4426950408889634f / tau, 1.0 / (double)tau, out_scores, out_tokens, out_parents, out_ended,
                  (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};

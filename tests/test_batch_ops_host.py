@@ -25,9 +25,9 @@ def pkg():
 
 CACHE = dict(dtype=2, K=A, V=2 * A, table=3 * A, n_pages=40, n_kv_heads=2, page_size=16, d_head=64, n_seq=6, table_stride=9)
 APPEND = dict(CACHE, q=4 * A, q_stride=256, k=5 * A, v=6 * A, kv_stride=128, seq=7 * A, pos=8 * A, n_tokens=6, n_heads=4, rope_theta=1e4, q_out=9 * A, err=None, stream=None)
-ATTEND = dict(dtype=2, q=4 * A, K=A, V=2 * A, table=3 * A, n_pages=40, n_kv_heads=2, page_size=16, d_head=64, n_seq=6, table_stride=9, shared=5 * A, len=6 * A, width=3, n_heads=4,
-              max_shared=100, max_own=20, out=7 * A, scratch=8 * A, scratch_bytes=1 << 30, err=None, stream=None)
-SELECT = dict(dtype=0, logits=A, row_stride=1000, n_groups=2, n_in=3, n_out=4, vocab=1000, scores=2 * A, ended=3 * A, end_token=2, tau=1.0, out_scores=4 * A, out_tokens=5 * A,
+ATTEND = dict(dtype=2, q=4 * A, K=A, V=2 * A, table=3 * A, n_pages=40, n_kv_heads=2, page_size=16, d_head=64, n_seq=6, table_stride=60, shared=5 * A, len=6 * A, width=3, n_heads=4,
+              max_shared=700, max_own=20, out=7 * A, scratch=8 * A, scratch_bytes=1 << 30, err=None, stream=None)
+SELECT = dict(dtype=0, logits=A, row_stride=5000, n_groups=2, n_in=3, n_out=4, vocab=5000, scores=2 * A, ended=3 * A, end_token=2, tau=1.0, out_scores=4 * A, out_tokens=5 * A,
               out_parents=6 * A, out_ended=7 * A, scratch=8 * A, scratch_bytes=1 << 30, stream=None)
 REORDER = dict(CACHE, n_layers=2, layer_stride=40 * 2 * 16 * 64, width=3, parents=4 * A, len=5 * A, table_out=6 * A, err=None, stream=None)
 
@@ -55,7 +55,7 @@ def test_append_in_place_wants_whole_rows(pkg):
     assert call(pkg, "spd_op_append_paged", APPEND, n_tokens=0, k=None, v=None, q=None, q_out=None, n_heads=0) == 0
 
 
-@pytest.mark.parametrize("what,value", BAD_CACHE + [("width", 0), ("width", 4), ("n_heads", 0), ("n_heads", 3), ("max_shared", -1), ("max_own", -1), ("max_shared", 145), ("max_own", 145),
+@pytest.mark.parametrize("what,value", BAD_CACHE + [("width", 0), ("width", 4), ("n_heads", 0), ("n_heads", 3), ("max_shared", -1), ("max_own", -1), ("max_shared", 961), ("max_own", 961),
                                                     ("max_own", (1 << 31) - 1), ("q", None), ("q", A + 4), ("out", None), ("out", A + 8), ("shared", None), ("len", None),
                                                     ("scratch", None), ("scratch", A + 64)])
 def test_attention_refuses(pkg, what, value):
@@ -64,29 +64,31 @@ def test_attention_refuses(pkg, what, value):
 
 def test_attention_scratch(pkg):
     f = pkg.lib().spd_op_attention_shared_scratch_bytes
-    need = f(6, 3, 4, 2, 64, 100, 20)
+    need = f(6, 3, 4, 2, 64, 700, 20)
     assert need > 0 and need % 256 == 0
     assert call(pkg, "spd_op_attention_shared", ATTEND, scratch_bytes=need - 1) == EWORKSPACE
     assert f(6, 3, 4, 2, 64, 4000, 20) >= need
+    assert f(6, 3, 4, 2, 64, 100, 20) == 0                    # one block per sequence and head: nothing to join
     for i, bad in enumerate([0, 0, 0, 0, 0, -1, -1]):
-        args = [6, 3, 4, 2, 64, 100, 20]
+        args = [6, 3, 4, 2, 64, 700, 20]
         args[i] = bad
         assert f(*args) == 0
     assert call(pkg, "spd_op_attention_shared", ATTEND, n_seq=0) == 0
 
 
-@pytest.mark.parametrize("what,value", [("dtype", 3), ("logits", None), ("logits", A + 2), ("row_stride", 999), ("n_groups", -1), ("n_in", 0), ("n_in", 17), ("n_out", 0), ("n_out", 17),
-                                        ("vocab", 0), ("vocab", -5), ("scores", None), ("end_token", -1), ("end_token", 1000), ("tau", 0.0), ("tau", -1.0), ("tau", math.nan),
+@pytest.mark.parametrize("what,value", [("dtype", 3), ("logits", None), ("logits", A + 2), ("row_stride", 4999), ("n_groups", -1), ("n_in", 0), ("n_in", 17), ("n_out", 0), ("n_out", 17),
+                                        ("vocab", 0), ("vocab", -5), ("scores", None), ("end_token", -1), ("end_token", 5000), ("tau", 0.0), ("tau", -1.0), ("tau", math.nan),
                                         ("tau", math.inf), ("tau", 1e-40), ("out_scores", None), ("out_tokens", None), ("out_parents", None), ("scratch", None), ("scratch", A + 8)])
 def test_select_refuses(pkg, what, value):
     assert call(pkg, "spd_op_beam_select", SELECT, **{what: value}) == EINVAL
 
 
 def test_select_scratch(pkg):
-    need = pkg.lib().spd_op_beam_select_scratch_bytes(2, 3, 4, 1000)
+    need = pkg.lib().spd_op_beam_select_scratch_bytes(2, 3, 4, 5000)
     assert need > 0 and need % 256 == 0
     assert call(pkg, "spd_op_beam_select", SELECT, scratch_bytes=need - 1) == EWORKSPACE
     assert pkg.lib().spd_op_beam_select_scratch_bytes(2, 3, 4, 0) == 0
+    assert pkg.lib().spd_op_beam_select_scratch_bytes(2, 3, 4, 4096) == 0    # one launch
     assert call(pkg, "spd_op_beam_select", SELECT, n_groups=0) == 0
 
 

@@ -330,7 +330,7 @@ def check_select(dtype, logits, scores, n_out, tau=1.0, ended=None, end_token=-1
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("groups,n_in,n_out,vocab,tau", [
     (1, 4, 4, 32000, 1.0), (3, 1, 5, 1000, 0.7), (2, 16, 16, 4097, 1.3), (1, 2, 16, 9, 1.0), (2, 8, 3, 4096, 0.4), (1, 16, 16, 1, 1.0), (1, 3, 1, 131074, 1.0), (5, 5, 10, 257, 2.0),
-    (1, 2, 2, 300_001, 1.0)])
+    (1, 2, 2, 300_001, 1.0), (2, 3, 16, 2049, 1.0), (1, 16, 16, 2048, 0.9), (30, 16, 16, 20_000, 1.0), (70, 16, 2, 9000, 1.0), (16, 16, 16, 33_000, 1.0)])
 def test_select(dtype, groups, n_in, n_out, vocab, tau):
     say("select", dtype, groups, n_in, n_out, vocab)
     g = gen(vocab)
@@ -350,9 +350,19 @@ def test_select_ties_go_to_the_lower_beam_and_token(dtype):
     z[0, 0, 3000:15_000] = 9.0
     z[0, 0, [100, 16_000]] = 10.0
     check_select(dtype, z, torch.zeros(1, 1), 16)
-    z = torch.zeros(1, 1, 5000, dtype=t)
-    z[0, 0, 1::2] = -0.0
-    check_select(dtype, z, torch.zeros(1, 1), 5)
+    for vocab in (5000, 3000):
+        z = torch.zeros(1, 1, vocab, dtype=t)
+        z[0, 0, 1::2] = -0.0
+        check_select(dtype, z, torch.zeros(1, 1), 5)
+        check_select(dtype, z - 1.0, torch.zeros(1, 1), 16)
+        z = torch.full((1, 2, vocab), -1e4, dtype=t)         # a few live among masked ones, fewer than asked for; one lane's entries hold all large values
+        z[0, 0, [7, vocab - 1, 1200]] = torch.tensor([1.0, 2.0, 1.0], dtype=t)
+        z[0, 1, 5:vocab:64] = torch.randn(len(range(5, vocab, 64)), generator=gen(2)).to(t)
+        check_select(dtype, z, torch.tensor([[-1.0, -1.0]]), 9)
+        z = torch.randn(1, 3, vocab, generator=gen(3)).to(t)
+        z[0, 1] = z[0, 0]
+        z[0, 2] = z[0, 0]
+        check_select(dtype, z, torch.tensor([[-1.0, -1.0, -1.0]]), 16)
 
 
 def test_select_values_that_are_excluded_or_no_numbers():
@@ -365,8 +375,10 @@ def test_select_values_that_are_excluded_or_no_numbers():
     z[4, 0] = -big                                   # masked with the lowest value, all of it and all but one
     z[4, 1], z[4, 1, 17] = -big, 1.0
     z[5] = -inf
+    z[0, 1, 100:200] = torch.tensor([0x7F800001, 0x7FBFFFFF, -4194305, 0x7FC00000], dtype=torch.int32).view(torch.float32).repeat(25)   # signalling NaN too
     s = -torch.rand(6, 2, generator=gen(3))
     check_select("fp32", z, s, 8)
+    check_select("fp32", z[..., :2500].contiguous(), s, 8)
     # the lowest values of fp16 and bf16 as masks
     for dtype in ("fp16", "bf16"):
         h = torch.randn(1, 2, 700, generator=gen(4)).to(R.TORCH[dtype])
