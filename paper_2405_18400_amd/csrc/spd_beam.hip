@@ -7,8 +7,8 @@
 // continuations, by score in 64 bits.
 // A wave has a slice to itself, all of it in registers, NE entries per lane: no barrier anywhere, and the selection is paid once per
 // wave.  128 rows of 50258 (22.5 MB read of 112 of them, 4.7 us at a large copy's rate): 18.7 us with 64-bit keys for every
-// entry, 10.6 with keys for those alone that can be among the best; 64 rows of 131072 in bf16 22.8 -> 11.0.  The second kernel, a chain of
-// dependent steps in one block per group: 15.5 -> 6.0 and 34 -> 9.3 us.
+// entry, 8.9 with keys for those alone that can be among the best; 64 rows of 131072 in bf16 22.8 -> 9.7.  The second kernel, a chain of
+// dependent steps in one block per group: 15.5 -> 6.3 and 34 -> 9.6 us.
 #include "spd_device.h"
 
 using namespace spdd;
@@ -20,7 +20,9 @@ typedef unsigned long long u64;
 constexpr int NTB = 256, NWB = NTB / WAVE;       // slices: threads and waves per block
 constexpr int NTM = 1024;                        // merge: a wave per row
 constexpr int EM = 8;                            // keys per lane and turn there
-constexpr int WAVES = 3300;                      // three per SIMD: slices are made longer only where there would be more
+// Waves that slices are made longer for: six per SIMD in fp32, three in 16 bits, whose loads bring twice the entries (us, three / six: 128 rows
+// of 50258 in fp32 11.7 / 8.9, 64 of 131072 in bf16 9.7 / 11.0).
+constexpr int WAVES_FP32 = 6600, WAVES_16 = 3300;
 
 // Order of fp32 numbers as unsigned ones.
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -69,10 +71,7 @@ __device__ __forceinline__ uint32_t nth_upper(uint32_t x, int n) {
 //   * Many equal values (masks of a finite number, ties): strictly above the bound there are few, and of the equal ones the first are taken.
 //   * Otherwise (few lanes hold all large values) the n-th largest value itself is found bit by bit.
 template <int N, int VEC, typename F>
-__device__ __forceinline__ int wave_candidates(const float (&v)[N], int n, F &&put) {
-    float top = v[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
+__device__ __forceinline__ int wave_candidates(const float (&v)[N], float top, int n, F &&put) {   // top: this lane's largest
     const uint32_t bound = nth_upper(ordered(top) >> 16, n);
     const auto above = [&](float t) {            // (t is -inf at least: what is excluded is never above it)
         int at = 0;
@@ -149,6 +148,29 @@ __device__ __forceinline__ u64 ranked(u64 *list, int count, int n, u64 *best) {
     return k;
 }
 
+// A wave's entries: their largest, that of this lane, and this lane's sum of exp2((z - largest) c).  A NaN or +inf among them leaves no number in
+// the sum; only then are they looked at one by one and replaced (clean(): three of the twelve instructions an entry would cost).
+template <int N>
+__device__ __forceinline__ void statistics(float (&z)[N], float c, float &top, float &largest, float &sum) {
+    const auto all = [&]() {
+        top = z[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
+        largest = all_max(top);
+        const float ref = largest == -INFINITY ? 0.f : largest;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < N; ++e) part[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
+        sum = (part[0] + part[1]) + (part[2] + part[3]);
+    };
+    all();
+    if (__any(sum != sum)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = clean(z[e]);
+        all();
+    }
+}
+
 __device__ __forceinline__ bool row_runs(const SelectArgs &a, int row) {
     const float score = as_global(a.scores)[row];
     return score > -INFINITY && !(a.ended && as_global(a.ended)[row] != 0);       // (a score that is no number: no beam)
@@ -190,22 +212,13 @@ __global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
         for (int e = 0; e < NE; ++e) z[e] = id(e) < a.vocab ? Store<LT>::load1(z_row, id(e)) : -INFINITY;
     }
     if (!row_runs(a, row)) return;               // (looked at while the logits are under way: a trip to memory less)
-    float m = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) {
-        z[e] = clean(z[e]);
-        m = fmaxf(m, z[e]);
-    }
-    m = all_max(m);
-    const float c = a.log2_by_tau, ref = m == -INFINITY ? 0.f : m;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < NE; ++e) sum[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
-    const float s = all_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
-    const int count = wave_candidates<NE, VEC>(z, a.n_out, [&](int place, int e) { list[w][place] = sort_key(z[e], id(e)); });
+    float top, m, sum;
+    statistics(z, a.log2_by_tau, top, m, sum);
+    sum = all_sum(sum);
+    const int count = wave_candidates<NE, VEC>(z, top, a.n_out, [&](int place, int e) { list[w][place] = sort_key(z[e], id(e)); });
     const u64 k = ranked(list[w], count, a.n_out, best[w]);
     if (lane < a.n_out) ((global_ptr<u64>)a.best)[(size_t)part * a.n_out + lane] = k;
-    if (lane == 0) { as_global(a.top)[part] = m; as_global(a.sum)[part] = s; }
+    if (lane == 0) { as_global(a.top)[part] = m; as_global(a.sum)[part] = sum; }
 }
 
 // What a group's block keeps of its rows: up to n_out continuations of each, best first, by place beam * n_out + rank.
@@ -239,15 +252,16 @@ __device__ __forceinline__ void rank_group(const SelectArgs &a, Group &s, int g)
     // those that can be among the best by their scores in fp32 (rounding keeps the order)
     int present = 0;
     if (tid < WAVE) {
-        float v[MOST / WAVE];
+        float v[MOST / WAVE], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < MOST / WAVE; ++e) {
             const int at = lane * (MOST / WAVE) + e;
             const double x = at < n ? s.score[at] : -INFINITY;
             present += __popcll(__ballot(x > -INFINITY));
             v[e] = x > -INFINITY ? fmaxf((float)x, -3.402823466e38f) : -INFINITY;
+            top = fmaxf(top, v[e]);
         }
-        const int count = wave_candidates<MOST / WAVE, MOST / WAVE>(v, a.n_out, [&](int place, int e) { s.chosen[place] = lane * (MOST / WAVE) + e; });
+        const int count = wave_candidates<MOST / WAVE, MOST / WAVE>(v, top, a.n_out, [&](int place, int e) { s.chosen[place] = lane * (MOST / WAVE) + e; });
         // equal ones in fp32 may differ in 64 bits: where some were left out for being equal, all are looked at
         int reach = 0;
         float least = INFINITY;
@@ -400,21 +414,12 @@ __global__ __launch_bounds__(NTM) void beam_small_kernel(const SelectArgs a) {
         u64 kept = 0;
         for (int lo = 0; lo < a.vocab; lo += SMALL_NE * WAVE) {
             if (lo) fetch(lo);
-            float m = M;
-#pragma unroll
-            for (int e = 0; e < SMALL_NE; ++e) {
-                z[e] = clean(z[e]);
-                m = fmaxf(m, z[e]);
-            }
-            m = all_max(m);
-            const float ref = m == -INFINITY ? 0.f : m;
-            sum *= M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - ref) * c);
-            M = m;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < SMALL_NE; ++e) part[e % 4] += __builtin_amdgcn_exp2f((z[e] - ref) * c);
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
-            int count = wave_candidates<SMALL_NE, 1>(z, a.n_out, [&](int place, int e) { s.list[b][place] = sort_key(z[e], lo + e * WAVE + lane); });
+            float top, m, more;
+            statistics(z, c, top, m, more);
+            const float up = fmaxf(M, m), ref = up == -INFINITY ? 0.f : up;
+            sum = sum * __builtin_amdgcn_exp2f((M - ref) * c) + more * __builtin_amdgcn_exp2f((m - ref) * c);    // (of nothing: 0 times 0)
+            M = up;
+            const int count = wave_candidates<SMALL_NE, 1>(z, top, a.n_out, [&](int place, int e) { s.list[b][place] = sort_key(z[e], lo + e * WAVE + lane); });
             const u64 before = kept;
             kept = ranked(s.list[b], count, a.n_out, s.best[b]);
             if (lo) {                                             // with those of the entries before
@@ -429,10 +434,10 @@ __global__ __launch_bounds__(NTM) void beam_small_kernel(const SelectArgs a) {
     rank_group(a, s, g);
 }
 
-// Entries per lane of a slice: as few as WAVES waves allow (a wave's first word comes after one trip to memory whatever it holds).
-int entries_per_lane(long long rows, int vocab) {
+// Entries per lane of a slice: as few as that many waves allow (a wave's first word comes after one trip to memory whatever it holds).
+int entries_per_lane(long long rows, int vocab, int waves) {
     for (int ne = 8; ne < 64; ne *= 2)
-        if (rows * ((vocab + WAVE * ne - 1) / (WAVE * ne)) <= WAVES) return ne;
+        if (rows * ((vocab + WAVE * ne - 1) / (WAVE * ne)) <= waves) return ne;
     return 64;
 }
 
@@ -467,7 +472,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 extern "C" size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab) {
     if (n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= SMALL) return 0;
     const long long rows = (long long)n_groups * n_in;
-    const int slice = WAVE * entries_per_lane(rows, vocab);
+    const int slice = WAVE * entries_per_lane(rows, vocab, WAVES_FP32);       // (the shorter slices, whatever the type)
     const size_t parts = (size_t)rows * (((size_t)vocab + slice - 1) / slice);
     return up256(parts * n_out * 8) + 2 * up256(parts * 4);
 }
@@ -484,7 +489,7 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     const size_t need = spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;
-    const int ne = entries_per_lane((long long)n_groups * n_in, vocab), slice = WAVE * ne;
+    const int ne = entries_per_lane((long long)n_groups * n_in, vocab, dtype == SPD_DTYPE_FP32 ? WAVES_FP32 : WAVES_16), slice = WAVE * ne;
     SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, 1.4426950408889634f / tau, 1.0 / (double)tau, out_scores, out_tokens, out_parents, out_ended,
                  (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};
     const long long parts = (long long)n_groups * n_in * a.slices;
