@@ -346,7 +346,7 @@ int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_t *table, i
  * the group's first sequence.  q, out DEVICE float [n_seq, n_heads, d_head]; shared DEVICE int32 [n_seq / width], len DEVICE int32 [n_seq].
  * max_shared >= every shared[g] and max_own >= every len[s] - shared[g] size the launch (host values; neither more than a row of
  * the table holds).  len[s] may be less than shared[g].  A sequence of length 0 gets zeros; so does one whose lengths are out of these bounds
- * (*err is set).  A position on a page out of range does not count (*err is set).  Nothing behind a sequence's last position gets into its result,
+ * (*err is set).  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result.  Nothing behind a sequence's last position gets into its result,
  * whatever it holds. */
 size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared,
                                              int32_t max_own);
@@ -360,7 +360,7 @@ int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const 
  * DEVICE [n_groups n_in rows of row_stride elements] in `dtype` (a logit that is no number counts as -inf, +inf as the largest finite
  * number; -inf is no continuation); scores DEVICE float [n_groups, n_in] (-inf or no number: no such beam).  ended (DEVICE int32
  * [n_groups, n_in], may be NULL): a beam with a value other than 0 has one continuation, itself, with token end_token and its score
- * unchanged; neither its logits nor those of an absent beam are read.  Outputs DEVICE [n_groups, n_out], best first: scores, tokens (in
+ * unchanged; neither its logits nor those of an absent beam count.  Outputs DEVICE [n_groups, n_out], best first: scores, tokens (in
  * [0, vocab)), parents (in [0, n_in)) and, unless NULL, whether the beam has ended (its parent had, or the token is end_token).
  * Where there are fewer continuations, the others have score -inf, token 0, not ended, and as parent their own place (0 where that is no beam).  With
  * n_out = n_in the outputs may be the inputs' buffers. */

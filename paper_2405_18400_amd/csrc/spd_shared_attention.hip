@@ -856,7 +856,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
 
 // A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
 // memory for up to UM * groups chunks.  Sums in a fixed order.
-constexpr int UM = 4;
+constexpr int UM = 8;
 __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p) {
     __shared__ float4 acc[NTS];
     __shared__ float red[NWS];
@@ -868,10 +868,13 @@ __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs 
     auto fetch = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < UM; ++u) {
-            const int i = min(i0 + u * groups, p.slots - 1);
-            xm[u] = as_global(ml)[2 * i];
-            xl[u] = i0 + u * groups < p.slots ? as_global(ml)[2 * i + 1] : 0.f;
-            x[u] = global_load_float4(part + (size_t)i * d);
+            const int i = i0 + u * groups;
+            xl[u] = 0.f;
+            if (i < p.slots) {
+                xm[u] = as_global(ml)[2 * i];
+                xl[u] = as_global(ml)[2 * i + 1];
+                x[u] = global_load_float4(part + (size_t)i * d);
+            }
         }
     };
     fetch(gi);
@@ -911,11 +914,17 @@ __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs 
 struct Cut { int shared_chunks, shared_chunk, own_chunks; };
 constexpr int WHOLE = 512;                       // positions up to which a sequence's block takes shared and own ones in one go
 constexpr int CUS = 256, LONG = 768;
-Cut cut_for(int n_seq, int width, int n_heads, int n_kv_heads, int max_shared, int max_own) {
+// Rows of a shared block.
+int tile_rows(int dtype, int d_head, int rows) {
+    if (rows <= ROWS || (dtype == SPD_DTYPE_FP32 && d_head > 128)) return ROWS;
+    if (dtype == SPD_DTYPE_FP32 || d_head < 64) return 2 * ROWS;
+    return rows > 4 * ROWS && d_head <= 128 && dtype == SPD_DTYPE_FP16 ? 8 * ROWS : 4 * ROWS;
+}
+Cut cut_for(int dtype, int n_seq, int width, int n_heads, int n_kv_heads, int d_head, int max_shared, int max_own) {
     const int groups = n_seq / width, group = n_heads / n_kv_heads;
     if (width > 1 && (long long)max_shared + max_own <= WHOLE) return Cut{0, 0, 1};
     const long long shared = std::max<long long>(1, width == 1 ? (long long)max_shared + max_own : max_shared);
-    const long long units = (long long)groups * n_kv_heads * (((long long)width * group + 8 * ROWS - 1) / (8 * ROWS)), own_units = (long long)n_seq * n_kv_heads;
+    const long long units = (long long)groups * n_kv_heads * ((width * group - 1) / tile_rows(dtype, d_head, width * group) + 1), own_units = (long long)n_seq * n_kv_heads;
     const auto cut = [&](long long positions, long long of, long long blocks) {
         const long long n = std::max<long long>(1, std::min(blocks / of, (positions + NWS * KEYS - 1) / (NWS * KEYS)));
         const long long chunk = ((positions + n - 1) / n + KEYS - 1) / KEYS * KEYS;
@@ -947,11 +956,11 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
     a.group = group;
     a.row_tiles = (a.width * group + TILE - 1) / TILE;
     a.own_tiles = (group + ROWS - 1) / ROWS;
-    a.shared_blocks_per_tile = groups * a.c.n_kv_heads * a.shared_chunks;
-    const long long shared_blocks = (long long)(a.shared_blocks_per_tile + 7) / 8 * 8 * a.row_tiles;
+    const long long per_tile = (long long)groups * a.c.n_kv_heads * a.shared_chunks, shared_blocks = (per_tile + 7) / 8 * 8 * a.row_tiles;
     const long long blocks = shared_blocks + (long long)a.c.n_seq * a.c.n_kv_heads * a.own_chunks * a.own_tiles;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     a.shared_blocks = (int)shared_blocks;
+    a.shared_blocks_per_tile = (int)per_tile;
     a.by_group = divisor(group); a.by_kv_heads = divisor(a.c.n_kv_heads); a.by_width = divisor(a.width); a.by_row_tiles = divisor(a.row_tiles);
     a.by_own_tiles = divisor(a.own_tiles); a.by_shared_chunks = divisor(std::max(1, a.shared_chunks)); a.by_own_chunks = divisor(std::max(1, a.own_chunks));
     constexpr int lds = lds_bytes<KT, DH, TILE, MANY>();
@@ -965,26 +974,28 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
 }
 
 template <typename KT, int DH>
-hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a) {
-    const int rows = a.shared_chunks ? a.width * (a.n_heads / a.c.n_kv_heads) : 1;
-    if constexpr (sizeof(KT) == 4 && DH > 128) return launch_tiles<KT, DH, ROWS, false>(s, a);
-    else {
-        if (rows <= ROWS) return launch_tiles<KT, DH, ROWS, false>(s, a);
-        if constexpr (sizeof(KT) == 2 && DH >= 64) {         // (sequences on their own may have one chunk, whose block writes the output: the other kernel)
-            if constexpr (DH <= 128 && Type<KT>::PARTS == 2)
-                if (rows > 4 * ROWS && a.width > 1) return launch_tiles<KT, DH, 8 * ROWS, true>(s, a);
-            if (a.width > 1) return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
-        }
+hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a, int dtype) {
+    const int tile = tile_rows(dtype, a.c.d_head, a.shared_chunks ? a.width * (a.n_heads / a.c.n_kv_heads) : 1);
+    if (tile == ROWS) return launch_tiles<KT, DH, ROWS, false>(s, a);
+    if constexpr (sizeof(KT) == 2 && DH >= 64) {
+        // (a sequence on its own may have a single chunk, whose block writes the output: the kernel whose waves share out keys)
+        if (a.width == 1) return launch_tiles<KT, DH, ROWS, false>(s, a);
+        if constexpr (DH <= 128 && Type<KT>::PARTS == 2)
+            if (tile == 8 * ROWS) return launch_tiles<KT, DH, 8 * ROWS, true>(s, a);
+        return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
+    } else if constexpr (sizeof(KT) == 4 && DH > 128) {
+        return hipErrorInvalidValue;             // (tiles of 16 rows alone)
+    } else {
         return launch_tiles<KT, DH, 2 * ROWS, false>(s, a);
     }
 }
 
 template <typename KT>
-hipError_t launch_width(hipStream_t s, const SharedAttnArgs &a) {
-    if (a.c.d_head <= 32) return launch_rows<KT, 32>(s, a);
-    if (a.c.d_head == 64) return launch_rows<KT, 64>(s, a);
-    if (a.c.d_head == 128) return launch_rows<KT, 128>(s, a);
-    return launch_rows<KT, 256>(s, a);
+hipError_t launch_width(hipStream_t s, const SharedAttnArgs &a, int dtype) {
+    if (a.c.d_head <= 32) return launch_rows<KT, 32>(s, a, dtype);
+    if (a.c.d_head == 64) return launch_rows<KT, 64>(s, a, dtype);
+    if (a.c.d_head == 128) return launch_rows<KT, 128>(s, a, dtype);
+    return launch_rows<KT, 256>(s, a, dtype);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -994,9 +1005,13 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 extern "C" size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared,
                                                         int32_t max_own) {
     if (n_seq <= 0 || width <= 0 || n_seq % width || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || d_head <= 0 || max_shared < 0 || max_own < 0) return 0;
-    const Cut c = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
-    const size_t parts = (size_t)n_seq * n_heads * (c.shared_chunks + c.own_chunks);
-    return c.shared_chunks + c.own_chunks > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 0;
+    int slots = 0;                               // (the most of the three types)
+    for (int dtype : {SPD_DTYPE_FP32, SPD_DTYPE_BF16, SPD_DTYPE_FP16}) {
+        const Cut c = cut_for(dtype, n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
+        slots = std::max(slots, c.shared_chunks + c.own_chunks);
+    }
+    const size_t parts = (size_t)n_seq * n_heads * slots;
+    return slots > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 0;
 }
 
 extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
@@ -1015,7 +1030,7 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     const size_t need = spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;
-    const Cut cut = cut_for(n_seq, width, n_heads, n_kv_heads, max_shared, max_own);
+    const Cut cut = cut_for(dtype, n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
     SharedAttnArgs a{};
     a.c = c; a.q = q; a.out = out; a.shared = shared; a.len = len; a.err = err;
     a.width = width; a.n_heads = n_heads; a.max_shared = max_shared; a.max_own = max_own;
@@ -1023,6 +1038,6 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     a.part_ml = (float *)scratch;
     a.part = (float *)((char *)scratch + up256((size_t)n_seq * n_heads * a.slots * 8));
     hipStream_t s = (hipStream_t)hip_stream;
-    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_width<float>(s, a) : dtype == SPD_DTYPE_FP16 ? launch_width<half_t>(s, a) : launch_width<bf16_t>(s, a);
+    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_width<float>(s, a, dtype) : dtype == SPD_DTYPE_FP16 ? launch_width<half_t>(s, a, dtype) : launch_width<bf16_t>(s, a, dtype);
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }

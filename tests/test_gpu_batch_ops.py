@@ -573,14 +573,16 @@ def test_a_beam_search(dtype, bound):
 
 
 # ------------------------------------------------------------------ streams and graphs
-def test_operators_in_a_graph_and_on_another_stream():
+@pytest.mark.parametrize("heads,max_own,vocab", [(8, 250, 5000), (16, 700, 3000), (8, 700, 5000)])
+def test_operators_in_a_graph_and_on_another_stream(heads, max_own, vocab):
     """A step of all four captured once and replayed with other lengths, positions and scores (they are on the device), between eager work; a second graph of the same
-    operators has scratch of its own.  Every replay equals the eager calls."""
+    operators has scratch of its own.  Every replay equals the eager calls.  One block per sequence and head, and shared positions cut into chunks, a tile of 32 rows
+    through LDS and one of 16; the selection in one launch and in two."""
     g = gen(12)
-    W, heads, kv, d, page, n_pages, vocab = 4, 8, 2, 128, 16, 200, 5000
+    W, kv, d, page, n_pages = 4, 2, 128, 16, 420
     n = 2 * W
     K0, V0 = (torch.randn(1, n_pages, kv, page, d, generator=g).half().cuda() for _ in range(2))
-    table = torch.randperm(n_pages, generator=g).int()[:n * 20].view(n, 20).cuda()
+    table = torch.randperm(n_pages, generator=g).int()[:n * 50].view(n, 50).cuda()
     qkv, logits = torch.randn(n, (heads + 2 * kv) * d, generator=g).cuda(), torch.randn(2, W, vocab, generator=g).cuda()
     seq = ints(range(n)).cuda()
 
@@ -603,7 +605,7 @@ def test_operators_in_a_graph_and_on_another_stream():
             q, k, v = split(qkv, heads, kv, d)
             pkg = P()
             pkg.spd_op_append_paged("fp16", self.K[0], self.V[0], table, k, v, seq, self.pos, THETA, q=q, q_out=self.q)
-            pkg.spd_op_attention_shared("fp16", self.q, self.K[0], self.V[0], table, self.shared, self.length, self.out, W, 100, 250)
+            pkg.spd_op_attention_shared("fp16", self.q, self.K[0], self.V[0], table, self.shared, self.length, self.out, W, 100, max_own)
             pkg.spd_op_beam_select("fp32", logits, self.scores, self.s, self.t, self.p)
             pkg.spd_op_beam_reorder("fp16", self.K, self.V, table, self.p, self.length, self.table, W)
 
