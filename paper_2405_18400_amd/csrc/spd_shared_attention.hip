@@ -30,8 +30,9 @@ constexpr int KEYS = 32;                         // keys of a wave's turn
 constexpr int ROWS = 16;                         // query rows of a tile
 constexpr int CHUNK_MAX = 4096;                  // positions of a chunk at most (its page numbers lie in LDS)
 constexpr int PAGE_MIN = 4;                      // the smallest page: four keys of a lane lie on one
-constexpr float SLACK = 8.f;                     // a row's reference is raised when a score passes it by 2^8: seldom
-constexpr float P_BITS = 7.f;                    // probabilities are scaled by 2^7, at most 2^15 then: two fp16 numbers keep 22 bits down to 2^-19
+constexpr float SLACK = 3.f;                     // a row's reference is raised when a probability would pass 2^3: seldom after the first turns
+constexpr float P_BITS = 12.f;                   // probabilities are scaled by 2^12, at most 2^15 then: two fp16 numbers hold them to 2^-36 of the reference
+                                                 // (cut off: sixty thousand keys may lose 2^-21 of the sum together)
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));

@@ -228,6 +228,23 @@ def test_attention_of_long_parts_and_many_rows(dtype, heads, kv, d, shared, own,
     close(got, R.attention(*case, width))
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("width", [1, 8])
+def test_attention_weights_add_up_to_one(dtype, width):
+    """One key far above twenty thousand others, at weights near 2^-20: values of one come out as one.  A weight is cut to 2^-36 of the largest (2^-24 in bf16 and fp32
+    of itself), so the many lose at most 20000 x 2^-36 = 3e-7; fp32 sums of 20000 terms in the waves' and chunks' order some 2^-22."""
+    n, d = 20_000, 64
+    q = torch.zeros(width, 4, d)
+    q[..., 0] = 8.0
+    K = torch.zeros(n // 16, 1, 16, d)
+    K[..., 0] = 0.25 * torch.rand(n // 16, 1, 16, generator=gen(14))
+    K[700, 0, 3, 0] = 14.0                                   # 8 x 14 / 8 = 14 = 20.2 log 2
+    V = torch.ones(n // 16, 1, 16, d)
+    table = torch.arange(n // 16, dtype=torch.int32).expand(width, -1).contiguous()
+    got, err = attend(dtype, q, K.to(R.TORCH[dtype]), V.to(R.TORCH[dtype]), table, ints([n]), ints([n] * width), width)
+    assert err == 0 and (got - 1.0).abs().max() < 1e-6, (got - 1.0).abs().max()
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "fp32"])
 def test_attention_of_a_long_sequence_that_ends_inside_the_shared_positions(dtype):
     """Its block takes more positions than a chunk has, on pages of four."""
