@@ -100,6 +100,17 @@ template <int B> __device__ __forceinline__ void load_words(const char *p, uint3
 // instructions, and a block of a short call has little else to do).
 __device__ __forceinline__ int over(int n, const Divisor &d) { return (int)(__umulhi(2u * (uint32_t)n, d.mul) >> d.shift); }
 
+// Whether any thread of the block found something bad, by one barrier, which also says that the pages' places have been written.
+__device__ __forceinline__ bool block_any(bool bad, int *flags) {
+    const bool mine = __any(bad);
+    if ((threadIdx.x & (WAVE - 1)) == 0) flags[threadIdx.x / WAVE] = mine;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int v = 0; v < NWS; ++v) all |= flags[v];
+    return all != 0;
+}
+
 // A stretch of positions read through one row of the table.
 struct Stretch { int row, lo, hi; };
 
@@ -127,7 +138,7 @@ constexpr int PAGES = CHUNK_MAX / PAGE_MIN + 4;
 // `resolve` reads the lengths and sets the stretches; false: there are none.  Queries are asked for before that, page numbers before
 // the queries are put in place: each of these is a trip to memory.
 template <typename KT, int DH, int RT, typename F>
-__device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&resolve, uint32_t *lds, u64 *pages, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
+__device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&resolve, uint32_t *lds, u64 *pages, int *flags, float (*lds_m)[ROWS], float (*lds_l)[ROWS], float *row_scale) {
     constexpr bool F32 = sizeof(KT) == 4;
     constexpr int PARTS = Type<KT>::PARTS;
     constexpr int NJ = F32 ? DH / 16 : DH / 32;                              // 16-byte pieces of a key per lane
@@ -178,21 +189,21 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         for (int i = 0; i < PP; ++i) {
             const int piece = q_t + i * TPR;
             if (piece >= N8) break;
+            u32x4 *to = (u32x4 *)lds;
             if constexpr (F32) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {    // feature 16 j + 4 kk + c of piece j: word c
+                for (int e = 0; e < 8; e += 4) { // feature 16 j + 4 kk + c of piece j: word c
                     const int f = 8 * piece + e;
-                    lds[(((q_row / ROWS) * NJ + f / 16) * WAVE + ((f / 4) % 4) * ROWS + q_row % ROWS) * 4 + f % 4] = __float_as_uint(x[i][e]);
+                    to[((q_row / ROWS) * NJ + f / 16) * WAVE + ((f / 4) % 4) * ROWS + q_row % ROWS] =
+                        u32x4{__float_as_uint(x[i][e]), __float_as_uint(x[i][e + 1]), __float_as_uint(x[i][e + 2]), __float_as_uint(x[i][e + 3])};
                 }
             } else {
+                uint32_t part[4][PARTS];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    uint32_t part[PARTS];
-                    parts_of<KT>(x[i][e] * up, x[i][e + 1] * up, part);
+                for (int e = 0; e < 8; e += 2) parts_of<KT>(x[i][e] * up, x[i][e + 1] * up, part[e / 2]);
 #pragma unroll
-                    for (int q = 0; q < PARTS; ++q)
-                        lds[((((q_row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + q_row % ROWS) * 4 + e / 2] = part[q];
-                }
+                for (int q = 0; q < PARTS; ++q)
+                    to[(((q_row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + q_row % ROWS] = u32x4{part[0][q], part[1][q], part[2][q], part[3][q]};
             }
         }
     }
@@ -216,7 +227,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
     // takes both stretches where there are two.
     for (int panel = un.a.lo;;) {
     const int lo_a = panel, hi_a = min(un.a.hi, (panel & ~3) + CHUNK_MAX);
-    // page numbers of both stretches; -1 where there is none
+    // where the pages of both stretches begin
     const int first_a = lo_a >> shift, n_a = pages_of(lo_a, hi_a), first_b = un.b.lo >> shift, n_b = pages_of(un.b.lo, un.b.hi);
     bool bad = false;
     for (int i = tid; i < n_a + n_b; i += NTS) {
@@ -225,7 +236,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
-    const bool any_bad = __syncthreads_or(bad);
+    const bool any_bad = block_any(bad, flags);
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) scale[rt] = row_scale[rt * ROWS + col];
@@ -491,10 +502,9 @@ __device__ __forceinline__ void to_lds16(const char *from, char *to) {
 
 // False: none of the chunk's positions is there.
 template <typename KT, int DH, int RT>
-__device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, u64 *pages) {
+__device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, u64 *pages, int *flags) {
     constexpr int PARTS = Type<KT>::PARTS, NJ = DH / 32, FV = DH / 16, VW = FV / 2;
     typedef Stage<DH, RT> S;
-    constexpr bool AHEAD = true;
     constexpr int SK = S::SK, NU = S::NU, ROWB = S::ROWB, PIECES = S::PIECES, HALF = S::HALF, BYTES = S::BYTES, LOADS = S::LOADS, ST = S::ST;
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane % ROWS, kk = lane / ROWS;
     const int shift = p.c.page_shift, page_size = 1 << shift, group = p.group;
@@ -533,7 +543,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
         pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
-    const bool any_bad = __syncthreads_or(bad);
+    const bool any_bad = block_any(bad, flags);
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
 
     const int base = lo & ~3, stages = (hi - base + SK - 1) / SK;
@@ -617,7 +627,6 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                     const int key = key0 + 16 * u + col;
                     k[j][u] = *(const u32x4 *)(k_tile + key * ROWB + 16 * permuted<PIECES>(key, 4 * j + kk));
                 }
-            if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -649,7 +658,6 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                     }
             };
             read_v(0);
-            if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
             const bool cut = tb < lo || tb + 16 * NU > hi || any_bad;
             uint32_t there = 0;                              // bit 4 u + r: this lane's key 16 u + 4 kk + r counts
             if (cut) {                                       // keys that do not count: no score (and, below, no value that could be a NaN)
@@ -702,10 +710,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
             }
 #pragma unroll
             for (int h = 0; h < NU / 2; ++h) {               // 32 keys at a time
-                if (h + 1 < NU / 2) {
-                    read_v(h + 1);
-                    if constexpr (AHEAD) __builtin_amdgcn_sched_barrier(0);
-                }
+                if (h + 1 < NU / 2) read_v(h + 1);
                 if (cut) {
                     asm volatile("");
 #pragma unroll
@@ -788,6 +793,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
     constexpr int RT = MANY ? 1 : TILE / ROWS;
     extern __shared__ __align__(1024) uint32_t lds[];        // lds_bytes()
     __shared__ u64 pages[PAGES];
+    __shared__ int flags[NWS];
     __shared__ float lds_m[NWS][ROWS], lds_l[NWS][ROWS], row_scale[RT * ROWS];
     const int group = p.group;
     int b = blockIdx.x;
@@ -806,7 +812,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
         un.slot = c;
         if constexpr (MANY) {
             un.a = Stretch{un.seq, c * p.shared_chunk, (c + 1) * p.shared_chunk};
-            if (!attend_many<KT, DH, TILE / (NWS * ROWS)>(p, un, (char *)lds, pages))
+            if (!attend_many<KT, DH, TILE / (NWS * ROWS)>(p, un, (char *)lds, pages, flags))
                 for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
         } else {
             const auto resolve = [&](Unit &u) {
@@ -822,7 +828,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
                 u.a = Stretch{u.seq, c * p.shared_chunk, min((c + 1) * p.shared_chunk, to)};
                 return u.a.hi > u.a.lo;
             };
-            if (!attend<KT, DH, RT>(p, un, resolve, lds, pages, lds_m, lds_l, row_scale))
+            if (!attend<KT, DH, RT>(p, un, resolve, lds, pages, flags, lds_m, lds_l, row_scale))
                 for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
         }
         return;
@@ -851,7 +857,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
         }
         return u.a.hi > u.a.lo || u.b.hi > u.b.lo;
     };
-    if (!attend<KT, DH, 1>(p, un, resolve, lds, pages, lds_m, lds_l, row_scale))
+    if (!attend<KT, DH, 1>(p, un, resolve, lds, pages, flags, lds_m, lds_l, row_scale))
         for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);
 }
 
