@@ -14,6 +14,7 @@ using namespace spdd;
 namespace {
 
 constexpr int NTP = 256;             // threads per block
+constexpr int COPIES = 8;            // 16-byte pieces under way per thread when pages are copied
 
 __device__ __forceinline__ bool page_ok(const PagedCache &c, int page) { return (unsigned)page < (unsigned)c.n_pages; }
 __device__ __forceinline__ void flag(int32_t *err) { if (err) *as_global(err) = 1; }
@@ -193,11 +194,23 @@ __global__ __launch_bounds__(NTP) void beam_reorder_kernel(const ReorderArgs a) 
     const size_t head_bytes = (size_t)page_size * a.row_bytes, page_bytes = head_bytes * a.c.n_kv_heads;
     const int per_head = filled * (a.row_bytes / 16), h0 = share * a.heads_per_share, h1 = min(a.c.n_kv_heads, h0 + a.heads_per_share);
     const int pieces = (h1 - h0) * per_head;
-    for (int i = threadIdx.x; i < 2 * pieces; i += NTP) {
-        const int p = i < pieces ? i : i - pieces;
-        char *pool = (char *)(i < pieces ? a.c.K : a.c.V) + (size_t)layer * a.layer_bytes;
-        const size_t at = (size_t)(h0 + p / per_head) * head_bytes + 16 * (size_t)(p % per_head);
-        *(u32x4 __attribute__((address_space(1))) *)(pool + to * page_bytes + at) = global_load16(pool + from * page_bytes + at);
+    const float by_head = 1.0f / (float)per_head;            // (at most 2^16 pieces: (p + 1/2) / per_head is never near a whole number)
+    for (int i0 = threadIdx.x; i0 < 2 * pieces; i0 += COPIES * NTP) {
+        u32x4 v[COPIES];
+        char *to_at[COPIES];
+#pragma unroll
+        for (int u = 0; u < COPIES; ++u) {                   // asked for together: one trip to memory
+            const int i = i0 + u * NTP;
+            if (i >= 2 * pieces) break;
+            const int p = i < pieces ? i : i - pieces, head = (int)(((float)p + 0.5f) * by_head);
+            char *pool = (char *)(i < pieces ? a.c.K : a.c.V) + (size_t)layer * a.layer_bytes;
+            const size_t at = (size_t)(h0 + head) * head_bytes + 16 * (size_t)(p - head * per_head);
+            v[u] = global_load16(pool + from * page_bytes + at);
+            to_at[u] = pool + to * page_bytes + at;
+        }
+#pragma unroll
+        for (int u = 0; u < COPIES; ++u)
+            if (i0 + u * NTP < 2 * pieces) *(u32x4 __attribute__((address_space(1))) *)to_at[u] = v[u];
     }
 }
 

@@ -862,45 +862,49 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
 }
 
 // A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
-// memory for up to UM * groups chunks.  Sums in a fixed order.
+// memory for up to UM * groups chunks.  Every wave forms the row's maximum and sum for itself, so the block meets once.  Sums in a fixed order.
 constexpr int UM = 8;
 __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p) {
     __shared__ float4 acc[NTS];
-    __shared__ float red[NWS];
-    const int tid = threadIdx.x, d = p.c.d_head, per = d / 4, groups = NTS / per, gi = tid / per, ci = tid % per;
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), d = p.c.d_head, per = d / 4, groups = NTS / per, gi = tid / per, ci = tid % per;
     const size_t row = blockIdx.x;
     const float *ml = p.part_ml + 2 * row * p.slots, *part = p.part + row * p.slots * d + 4 * ci;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const auto pair = [&](int i) { return ((global_ptr<const f32x2>)ml)[i]; };       // a chunk's maximum and sum
     float4 x[UM];
-    float xm[UM], xl[UM];
+    f32x2 xml[UM];
     auto fetch = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < UM; ++u) {
             const int i = i0 + u * groups;
-            xl[u] = 0.f;
+            xml[u] = f32x2{-INFINITY, 0.f};
             if (i < p.slots) {
-                xm[u] = as_global(ml)[2 * i];
-                xl[u] = as_global(ml)[2 * i + 1];
+                xml[u] = pair(i);
                 x[u] = global_load_float4(part + (size_t)i * d);
             }
         }
     };
     fetch(gi);
-    float m = -INFINITY;
-    for (int i = tid; i < p.slots; i += NTS) m = fmaxf(m, as_global(ml)[2 * i]);
-    const float M = block_max<NTS>(m, red);
-    float L = 0.f;
+    const f32x2 first = lane < p.slots ? pair(lane) : f32x2{-INFINITY, 0.f};
+    float M = first[0];
+    for (int i = lane + WAVE; i < p.slots; i += WAVE) M = fmaxf(M, pair(i)[0]);
+    M = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(M)), WAVE - 1));
+    float L = first[1] == 0.f ? 0.f : first[1] * exp2_below(first[0], M);
+    for (int i = lane + WAVE; i < p.slots; i += WAVE) {
+        const f32x2 v = pair(i);
+        if (v[1] != 0.f) L += v[1] * exp2_below(v[0], M);
+    }
+    L = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_sum_last(L)), WAVE - 1));
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i0 = gi; i0 < p.slots; i0 += UM * groups) {
         if (i0 != gi) fetch(i0);
 #pragma unroll
         for (int u = 0; u < UM; ++u) {
-            if (xl[u] == 0.f) continue;          // nothing there: its O was not written
-            const float f = exp2_below(xm[u], M);
-            if (ci == 0) L += f * xl[u];
+            if (xml[u][1] == 0.f) continue;      // nothing there: its O was not written
+            const float f = exp2_below(xml[u][0], M);
             y.x += f * x[u].x; y.y += f * x[u].y; y.z += f * x[u].z; y.w += f * x[u].w;
         }
     }
-    L = block_sum<NTS>(L, red);
     acc[tid] = y;
     __syncthreads();
     if (tid >= per) return;
