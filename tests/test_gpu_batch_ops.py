@@ -216,13 +216,16 @@ def test_attention(dtype, heads, kv, d, page, shared, lengths, width):
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
-@pytest.mark.parametrize("heads,kv,d,shared,own,width", [
-    (8, 1, 128, 1500, 7, 3), (32, 2, 64, 700, 300, 5), (2, 2, 128, 2100, 0, 1), (16, 2, 128, 400, 33, 17), (4, 1, 256, 900, 90, 6), (5, 5, 128, 1024, 512, 2), (24, 3, 128, 513, 1, 9)])
-def test_attention_of_long_parts_and_many_rows(dtype, heads, kv, d, shared, own, width):
+@pytest.mark.parametrize("heads,kv,d,shared,own,width,page", [
+    (8, 1, 128, 1500, 7, 3, 16), (32, 2, 64, 700, 300, 5, 16), (2, 2, 128, 2100, 0, 1, 16), (16, 2, 128, 400, 33, 17, 16), (4, 1, 256, 900, 90, 6, 16), (5, 5, 128, 1024, 512, 2, 16),
+    (24, 3, 128, 513, 1, 9, 16),
+    # more query heads per key/value head than a tile has rows, alone and in groups; several tiles of d_head 256; small and large pages on the LDS path
+    (34, 1, 128, 700, 60, 1, 16), (40, 2, 64, 600, 100, 3, 8), (16, 1, 256, 600, 10, 6, 16), (16, 2, 128, 1301, 40, 4, 4), (8, 1, 64, 1100, 40, 8, 1024)])
+def test_attention_of_long_parts_and_many_rows(dtype, heads, kv, d, shared, own, width, page):
     """Parts cut into several chunks, rows of queries past one tile, groups of heads that do not divide a tile."""
-    say("attention", dtype, heads, kv, d, shared, own, width)
+    say("attention", dtype, heads, kv, d, shared, own, width, page)
     lengths = [shared + max(0, own - 3 * w) for w in range(width)] + [shared + own // 2] * width
-    case = attention_case(dtype, heads, kv, d, 16, [shared, shared - 1], lengths, width, seed=own)
+    case = attention_case(dtype, heads, kv, d, page, [shared, shared - 1], lengths, width, seed=own)
     got, err = attend(dtype, *case, width)
     assert err == 0
     close(got, R.attention(*case, width))
@@ -301,6 +304,27 @@ def test_attention_with_lengths_and_pages_out_of_range(d):
         close(got, R.attention(q, K, V, bad, shared, length, 2))
     got, err = attend("fp16", q, K, V, torch.full_like(table, -1), shared, length, 2)
     assert err == 1 and (got == 0).all()
+
+
+@pytest.mark.parametrize("dtype,heads", [("fp16", 4), ("fp16", 16), ("bf16", 16), ("fp32", 16)])
+def test_attention_cut_into_chunks_with_lengths_and_pages_out_of_range(dtype, heads):
+    """The same where shared positions have blocks of their own, a tile of 8 rows and one of 32; a sequence that ends inside them beside one that is empty."""
+    q, K, V, table, shared, length = attention_case(dtype, heads, 2, 64, 16, [700, 650], [705, 690, 0, 720, 651, 700, 650, 1], 4, seed=15)
+    got, err = attend(dtype, q, K, V, table, shared, length, 4, max_shared=704, max_own=60)
+    assert err == 0
+    close(got, R.attention(q, K, V, table, shared, length, 4))
+    for bad_shared, bad_length, gone in (([700, 650], [705, -1, 0, 720, 651, 700, 650, 1], [1, 2]), ([700, 650], [705, 690, 0, 761, 651, 700, 650, 1], [2, 3]),
+                                         ([705, 650], [705, 690, 0, 720, 651, 700, 650, 1], [0, 1, 2, 3]), ([700, -1], [705, 690, 0, 720, 651, 700, 650, 1], [2, 4, 5, 6, 7])):
+        got, err = attend(dtype, q, K, V, table, ints(bad_shared), ints(bad_length), 4, max_shared=704, max_own=60)
+        here = [s for s in range(8) if s not in gone]
+        assert err == 1 and (got[gone] == 0).all()
+        close(got[here], R.attention(q, K, V, table, shared, length, 4)[here])
+    for s, e, page in ((0, 3, -1), (4, 40, len(K)), (3, 44, -2_000_000_000)):
+        bad = table.clone()
+        bad[s, e] = page
+        got, err = attend(dtype, q, K, V, bad, shared, length, 4)
+        assert err == 1
+        close(got, R.attention(q, K, V, bad, shared, length, 4))
 
 
 def test_attention_offsets_past_32_bits():
