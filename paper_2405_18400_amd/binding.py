@@ -458,7 +458,7 @@ def _refuse(where, device, **tensors):
             raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
         if not t.is_contiguous():
             raise ValueError(f"{where}: {name} is not contiguous")
-        if shape is not None and t.numel() != math.prod(shape):
+        if shape is not None and (t.numel() != math.prod(shape) or (name == "V" and t.shape != shape)):
             raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
 
 
@@ -493,7 +493,7 @@ def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: flo
     n_pages, n_kv, page_size, d = shape
     n_seq, entries = table.shape
     n = seq.numel()
-    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.numel() == K.numel() and pos.numel() == n
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n
             and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
             and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
             and err is None):
@@ -533,7 +533,7 @@ def spd_op_attention_shared(dtype: str, q, K, V, table, shared, length, out, wid
         raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
     groups = n_seq // width
     if not (q.dtype is f32 and out.dtype is f32 and K.dtype is kv and V.dtype is kv and table.dtype is i32 and shared.dtype is i32 and length.dtype is i32 and q_d == d
-            and out.numel() == q.numel() and V.numel() == K.numel() and table.numel() == n_seq * entries and shared.numel() == groups and length.numel() == n_seq
+            and out.numel() == q.numel() and V.shape == shape and table.numel() == n_seq * entries and shared.numel() == groups and length.numel() == n_seq
             and q.is_contiguous() and out.is_contiguous() and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and shared.is_contiguous()
             and length.is_contiguous() and q.get_device() == device and out.get_device() == device and K.get_device() == device and V.get_device() == device
             and table.get_device() == device and shared.get_device() == device and length.get_device() == device and err is None):
@@ -596,7 +596,7 @@ def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, wid
     if width < 1 or n_seq % width:
         raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
     groups = (n_seq // width, width)
-    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and parents.dtype is i32 and length.dtype is i32 and table_out.dtype is i32 and V.numel() == K.numel()
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and parents.dtype is i32 and length.dtype is i32 and table_out.dtype is i32 and V.shape == shape
             and parents.numel() == n_seq and length.numel() == n_seq and table_out.numel() == n_seq * entries and K.is_contiguous() and V.is_contiguous() and table.is_contiguous()
             and parents.is_contiguous() and length.is_contiguous() and table_out.is_contiguous() and K.get_device() == device and V.get_device() == device
             and table.get_device() == device and parents.get_device() == device and length.get_device() == device and table_out.get_device() == device and err is None):

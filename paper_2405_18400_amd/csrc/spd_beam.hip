@@ -486,6 +486,11 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     if (ended && (end_token < 0 || end_token >= vocab)) return SPD_EINVAL;
     if (n_groups == 0) return SPD_OK;
     if (!logits || !scores || !out_scores || !out_tokens || !out_parents || (uintptr_t)logits % (dtype == SPD_DTYPE_FP32 ? 4 : 2)) return SPD_EINVAL;
+    // a group's outputs may take the place of its own inputs, not of another's
+    const size_t in_bytes = (size_t)n_groups * n_in * 4, out_bytes = (size_t)n_groups * n_out * 4;
+    for (const void *in : {(const void *)scores, (const void *)ended})
+        for (const void *out : {(const void *)out_scores, (const void *)out_tokens, (const void *)out_parents, (const void *)out_ended})
+            if (in && out && !(in == out && n_in == n_out) && spdk::overlap(in, in_bytes, out, out_bytes)) return SPD_EINVAL;
     const size_t need = spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;

@@ -1038,6 +1038,7 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     if (n_seq == 0) return SPD_OK;
     if ((long long)n_seq * n_heads > (1 << 24)) return SPD_EINVAL;
     if (!q || !shared || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16) return SPD_EINVAL;
+    if (spdk::overlap(q, (size_t)n_seq * n_heads * d_head * 4, out, (size_t)n_seq * n_heads * d_head * 4)) return SPD_EINVAL;      // (blocks that share a head's queries)
     const size_t need = spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;

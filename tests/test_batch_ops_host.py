@@ -49,6 +49,22 @@ def test_append_refuses(pkg, what, value):
     assert call(pkg, "spd_op_append_paged", APPEND, **{what: value}) == EINVAL
 
 
+@pytest.mark.parametrize("out", [4 * A + 16, 4 * A - 16, 4 * A + 5 * 256 * 4, 5 * A, 5 * A + 5 * 128 * 4, 5 * A - 16, 6 * A - 6 * 256 * 4 + 16, 6 * A + 128 * 4])
+def test_append_refuses_results_over_what_other_blocks_read(pkg, out):
+    assert call(pkg, "spd_op_append_paged", APPEND, q_out=out) == EINVAL
+
+
+@pytest.mark.parametrize("out", [4 * A, 4 * A + 16, 4 * A - 16, 4 * A + 6 * 4 * 64 * 4 - 16, 4 * A - 6 * 4 * 64 * 4 + 16])
+def test_attention_refuses_results_over_its_queries(pkg, out):
+    assert call(pkg, "spd_op_attention_shared", ATTEND, out=out) == EINVAL
+
+
+@pytest.mark.parametrize("n_in,n_out,name,at", [(3, 4, "out_scores", 2 * A), (3, 4, "out_ended", 3 * A), (3, 3, "out_scores", 2 * A + 4), (3, 3, "out_ended", 3 * A - 4),
+                                                (4, 3, "out_tokens", 2 * A + 2 * 4 * 4 - 4), (4, 3, "out_parents", 3 * A - 2 * 3 * 4 + 4)])
+def test_select_refuses_results_over_another_groups_inputs(pkg, n_in, n_out, name, at):
+    assert call(pkg, "spd_op_beam_select", SELECT, n_in=n_in, n_out=n_out, **{name: at}) == EINVAL
+
+
 def test_append_in_place_wants_whole_rows(pkg):
     assert call(pkg, "spd_op_append_paged", APPEND, q_out=APPEND["q"], q_stride=512) == EINVAL
     assert call(pkg, "spd_op_append_paged", APPEND, n_tokens=0) == 0                       # nothing to do, nothing enqueued
@@ -130,6 +146,13 @@ def test_python_refuses_tensors_that_are_not_what_they_should_be(pkg, monkeypatc
         a = {**dict(dtype="fp32", K=K, V=K, table=i(4, 2), parents=i(2, 2), length=i(4), table_out=i(4, 2), width=2), **bad}
         with pytest.raises(ValueError):
             pkg.spd_op_beam_reorder(**a)
+    other = K.reshape(4, 8, 2, 16)                                         # as many elements in another order
+    with pytest.raises(ValueError):
+        pkg.spd_op_append_paged("fp32", K, other, i(2, 2), k, k, i(3), i(3), 1e4)
+    with pytest.raises(ValueError):
+        pkg.spd_op_attention_shared("fp32", q, K, other, i(4, 2), i(2), i(4), torch.empty_like(q), 2, 3, 3)
+    with pytest.raises(ValueError):
+        pkg.spd_op_beam_reorder("fp32", K, other, i(4, 2), i(2, 2), i(4), i(4, 2), 2)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)           # tensors of another device
     with pytest.raises(ValueError):
         pkg.spd_op_append_paged("fp32", K, K, i(2, 2), k, k, i(3), i(3), 1e4)
