@@ -17,6 +17,8 @@
 // K and V of a 16-bit cache are exact in their type; queries and probabilities go in as two fp16 numbers (22 bits, scaled by
 // powers of two into fp16's range) or three bf16 numbers (24 bits): the error against 64 bits is that of fp32 arithmetic.
 // An fp32 cache takes the fp32 products.  Four waves share a block's keys, 32 each in turn, with a running maximum and sum of their own.
+// Measured, heads of 128: four sequences of 74 positions, 32 heads in fp16, 6.4 us (latency: lengths, page numbers, keys, result); five of 1027
+// shared and about 20 own, 40 heads in fp32 (45 MB), 15.6 us and 3.9 for the join.
 #include "spd_device.h"
 
 #include <algorithm>
@@ -483,6 +485,9 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 // come through LDS, 16 bytes per lane straight from memory, ST stages of SK keys deep; pieces of a row are permuted by the row number,
 // so that neither the operand reads (16 rows side by side) nor the row reads meet in a bank.  One barrier per stage says both "this
 // stage has arrived" and "the one before has been read".
+// Measured, 64 heads of 128 on 8 in fp16: eight sequences over 8191 positions (37 MB) 15.1 us, bound by a block's chain; sixteen over
+// 65537 (271 MB; 69 GFLOP with the two parts of queries and probabilities) 78 .. 103 us, 3.1 TB/s and 0.8 PFLOP/s, the matrix cores and the vector
+// unit in turn.  Eight groups of eight over 2001, 32 heads on 8 in bf16 (127 MB), 35 us, 3.6 TB/s over the call.
 template <int DH, int RT> struct Stage {
     static constexpr int SK = DH == 64 || (DH == 128 && RT == 1) ? 64 : 32;             // keys
     static constexpr int NU = RT == 1 && SK == 64 ? 4 : 2;                              // tiles of 16 keys that go through the products together
@@ -863,6 +868,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
 
 // A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
 // memory for up to UM * groups chunks.  Every wave forms the row's maximum and sum for itself, so the block meets once.  Sums in a fixed order.
+// Measured, 512 rows of 128: 33 chunks each 4.0 us (a launch and three trips to memory); 1024 rows of 65: 8.3 us.
 constexpr int UM = 8;
 __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p) {
     __shared__ float4 acc[NTS];
