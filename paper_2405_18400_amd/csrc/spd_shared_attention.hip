@@ -33,8 +33,6 @@ constexpr int ROWS = 16;                         // query rows of a tile
 constexpr int CHUNK_MAX = 4096;                  // positions of a chunk at most (its page numbers lie in LDS)
 constexpr int PAGE_MIN = 4;                      // the smallest page: four keys of a lane lie on one
 constexpr float SLACK = 3.f;                     // a row's reference is raised when a probability would pass 2^3: seldom after the first turns
-constexpr float P_BITS = 12.f;                   // probabilities are scaled by 2^12, at most 2^15 then: two fp16 numbers hold them to 2^-36 of the reference
-                                                 // (cut off: sixty thousand keys may lose 2^-21 of the sum together)
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -44,10 +42,14 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // exp2(a - b) with exp2(-inf - anything) = 0, also where b is -inf (nothing seen yet).
 __device__ __forceinline__ float exp2_below(float a, float b) { return __builtin_amdgcn_exp2f(a - (b == -INFINITY ? 0.f : b)); }
 
-template <typename KT> struct Type;              // PARTS: numbers of the cache's type that stand for one fp32 number
-template <> struct Type<half_t> { static constexpr int PARTS = 2; };
-template <> struct Type<bf16_t> { static constexpr int PARTS = 3; };
-template <> struct Type<float> { static constexpr int PARTS = 1; };
+// PARTS: numbers of the cache's type that stand for one fp32 number.
+// P_BITS: probabilities are scaled by 2^P_BITS.  fp16: at most 2^15 then, and two fp16 numbers hold them to 2^-36 of the reference (cut off: sixty
+// thousand keys may lose 2^-20 of the sum together); values of at most 2^16 stay far below fp32's end.  The other types have fp32's range, and values
+// up to its end: scaled down, 2^21 keys of them add up to no infinity.  What is lost below are products under 2^-126, 2^-102 of a value of one.
+template <typename KT> struct Type;
+template <> struct Type<half_t> { static constexpr int PARTS = 2; static constexpr float P_BITS = 12.f; };
+template <> struct Type<bf16_t> { static constexpr int PARTS = 3; static constexpr float P_BITS = -24.f; };
+template <> struct Type<float> { static constexpr int PARTS = 1; static constexpr float P_BITS = -24.f; };
 
 // Two fp32 numbers as pairs of the cache's type, most significant part first.
 template <typename KT> __device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[Type<KT>::PARTS]);
@@ -361,7 +363,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 #pragma unroll
                 for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
             }
-            const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
+            const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - Type<KT>::P_BITS;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref));
@@ -700,7 +702,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
                     for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
                 }
-                const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - P_BITS;
+                const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - Type<KT>::P_BITS;
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll
