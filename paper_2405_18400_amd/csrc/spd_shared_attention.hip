@@ -33,6 +33,7 @@ constexpr int ROWS = 16;                         // query rows of a tile
 constexpr int CHUNK_MAX = 4096;                  // positions of a chunk at most (its page numbers lie in LDS)
 constexpr int PAGE_MIN = 4;                      // the smallest page: four keys of a lane lie on one
 constexpr float SLACK = 3.f;                     // a row's reference is raised when a probability would pass 2^3: seldom after the first turns
+constexpr float FAR = 0x1p20f;                   // scores (base 2) from which on an exponent is formed from the rounded score
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -68,6 +69,18 @@ template <> __device__ __forceinline__ void parts_of<bf16_t>(float x, float y, u
         x -= __uint_as_float(a & 0xFFFF0000u);
         y -= __uint_as_float(b & 0xFFFF0000u);
     }
+}
+
+// Scores of rows whose reference m is far from zero.  Where an fp32 number's step is one or more, the product in fma(score, scale, -reference) is not the one
+// that the reference was rounded from, and a probability passes every bound.  Formed from the rounded product, the largest exponent is the
+// reference's own and the difference is exact.  Leaves exponents, over scale, so that the reference is zero from there on.
+template <typename KT, int NU>
+__device__ __forceinline__ void far_scores(f32x4v (&s)[NU], float scale, float m) {
+    const float inv = __builtin_amdgcn_rcpf(scale), from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[u][r] = fabsf(m) > FAR ? ((s[u][r] * scale - from) + Type<KT>::P_BITS) * inv : s[u][r];
 }
 
 // The power of two that takes a row whose largest value is `top` to the upper end of fp16's range, and its inverse.
@@ -353,7 +366,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 #pragma unroll
                 for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
             mx *= scale[rt];
-            if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
+            if (__any(mx > m[rt] + SLACK || fabsf(m[rt]) > FAR)) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));    // the lane groups hold different keys of the same rows
                 mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
                 mx = fmaxf(mx, m[rt]);
@@ -362,8 +375,9 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
                 l[rt] *= corr;
 #pragma unroll
                 for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
+                far_scores<KT>(st[rt], scale[rt], mx);
             }
-            const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - Type<KT>::P_BITS;
+            const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref));
@@ -692,7 +706,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
                     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
                 mx *= scale[rt];
-                if (__any(mx > m[rt] + (m[rt] == -INFINITY ? 0.f : SLACK))) {
+                if (__any(mx > m[rt] + SLACK || fabsf(m[rt]) > FAR)) {
                     mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
                     mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
                     mx = fmaxf(mx, m[rt]);
@@ -701,8 +715,9 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                     l[rt] *= corr;
 #pragma unroll
                     for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
+                    far_scores<KT>(st[rt], scale[rt], mx);
                 }
-                const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) - Type<KT>::P_BITS;
+                const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import batch_reference as R
-from test_gpu_batch_ops import attend, attention_case, close
+from test_gpu_batch_ops import attend, attention_case, close, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +31,23 @@ def test_attention_of_values_as_large_as_the_type_holds(dtype, heads, kv, shared
     most = 65504.0 if dtype == "fp16" else 2.0 ** 128 * (1 - 2.0 ** -8)
     got, _ = attend(dtype, q, K, torch.where(V.isnan(), V, torch.full_like(V, most)), table, *rest, width)
     assert ((got.double() / most - 1.0).abs() < 1e-6).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@by_path
+def test_attention_of_scores_far_from_zero(dtype, heads, kv, shared, lengths, width):
+    """Scores of 2^19 to 2^37, all of them exact numbers whose next neighbours are 2^12 and more away: the best key takes all, equal best ones share."""
+    q, K, V, table, *rest = attention_case(dtype, heads, kv, 64, 16, shared, lengths, width, seed=22)
+    g = gen(23)
+    K = torch.where(K.isnan(), K, torch.randint(-100, 101, K.shape, generator=g).to(K.dtype))
+    q = torch.zeros_like(q)
+    q[..., 0] = torch.tensor([2.0 ** 15, 2.0 ** 22, -(2.0 ** 26), 2.0 ** 33]).repeat(heads // 4)     # over sqrt(64): steps of 2^12 and more
+    got, err = attend(dtype, q, K, V, table, *rest, width)
+    assert err == 0
+    close(got, R.attention(q, K, V, table, *rest, width), 1e-6)             # a handful of equal weights: some 2^-22
+    # all scores far below zero, and near one another: the definition's weights to a few steps of the scores (2^-3 at 2^21: compared where they are exact)
+    K[..., 0] = torch.where(K[..., 0].isnan(), K[..., 0], -120.0 - (K[..., 0] > 0).to(K.dtype) * 8)
+    q[..., 0] = 2.0 ** 20
+    got, err = attend(dtype, q, K, V, table, *rest, width)
+    assert err == 0
+    close(got, R.attention(q, K, V, table, *rest, width), 1e-5)
