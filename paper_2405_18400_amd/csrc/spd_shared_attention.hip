@@ -44,13 +44,14 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ float exp2_below(float a, float b) { return __builtin_amdgcn_exp2f(a - (b == -INFINITY ? 0.f : b)); }
 
 // PARTS: numbers of the cache's type that stand for one fp32 number.
-// P_BITS: probabilities are scaled by 2^P_BITS.  fp16: at most 2^15 then, and two fp16 numbers hold them to 2^-36 of the reference (cut off: sixty
-// thousand keys may lose 2^-20 of the sum together); values of at most 2^16 stay far below fp32's end.  The other types have fp32's range, and values
-// up to its end: scaled down, 2^21 keys of them add up to no infinity.  What is lost below are products under 2^-126, 2^-102 of a value of one.
+// Probabilities are exp2(score - reference + P_BITS) P_SCALE.  fp16: at most 2^15 then, and two fp16 numbers hold them to 2^-36 of the reference (cut off: sixty
+// thousand keys may lose 2^-20 of the sum together); values of at most 2^16 stay far below fp32's end.  (The exponent of some twelve is off by 2^-21: a
+// factor behind the exponential would be one instruction of ten per key.)  The other types have fp32's range, and values up to its end: scaled down, 2^21 keys of
+// them add up to no infinity, and what is lost below are products under 2^-126, 2^-102 of a value of one.
 template <typename KT> struct Type;
-template <> struct Type<half_t> { static constexpr int PARTS = 2; static constexpr float P_BITS = 12.f; };
-template <> struct Type<bf16_t> { static constexpr int PARTS = 3; static constexpr float P_BITS = -24.f; };
-template <> struct Type<float> { static constexpr int PARTS = 1; static constexpr float P_BITS = -24.f; };
+template <> struct Type<half_t> { static constexpr int PARTS = 2; static constexpr float P_BITS = 12.f, P_SCALE = 1.f; };
+template <> struct Type<bf16_t> { static constexpr int PARTS = 3; static constexpr float P_BITS = 0.f, P_SCALE = 0x1p-24f; };
+template <> struct Type<float> { static constexpr int PARTS = 1; static constexpr float P_BITS = 0.f, P_SCALE = 0x1p-24f; };
 
 // Two fp32 numbers as pairs of the cache's type, most significant part first.
 template <typename KT> __device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[Type<KT>::PARTS]);
@@ -366,7 +367,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 #pragma unroll
                 for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
             mx *= scale[rt];
-            if (__any(mx > m[rt] + SLACK || fabsf(m[rt]) > FAR)) {
+            if (__any((mx > m[rt] + SLACK) | (fabsf(m[rt]) > FAR))) {
                 mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));    // the lane groups hold different keys of the same rows
                 mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
                 mx = fmaxf(mx, m[rt]);
@@ -375,12 +376,12 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
                 l[rt] *= corr;
 #pragma unroll
                 for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
-                far_scores<KT>(st[rt], scale[rt], mx);
+                if (__any((fabsf(mx) > FAR) & (mx != -INFINITY))) far_scores<KT>(st[rt], scale[rt], mx);
             }
             const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref));
+                pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref)) * Type<KT>::P_SCALE;
                 l[rt] += pf[rt][i];
             }
             if constexpr (!F32) {
@@ -706,7 +707,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
                     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
                 mx *= scale[rt];
-                if (__any(mx > m[rt] + SLACK || fabsf(m[rt]) > FAR)) {
+                if (__any((mx > m[rt] + SLACK) | (fabsf(m[rt]) > FAR))) {
                     mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
                     mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
                     mx = fmaxf(mx, m[rt]);
@@ -715,14 +716,15 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
                     l[rt] *= corr;
 #pragma unroll
                     for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
-                    far_scores<KT>(st[rt], scale[rt], mx);
+                    if (__any((fabsf(mx) > FAR) & (mx != -INFINITY))) far_scores<KT>(st[rt], scale[rt], mx);
                 }
                 const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll
                     for (int r = 0; r < 4; r += 2) {
-                        const float p0 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r], scale[rt], -ref)), p1 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r + 1], scale[rt], -ref));
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r], scale[rt], -ref)) * Type<KT>::P_SCALE;
+                        const float p1 = __builtin_amdgcn_exp2f(fmaf(st[rt][u][r + 1], scale[rt], -ref)) * Type<KT>::P_SCALE;
                         l[rt] += p0 + p1;
                         uint32_t part[PARTS];
                         parts_of<KT>(p0, p1, part);

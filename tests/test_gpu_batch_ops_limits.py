@@ -1,5 +1,4 @@
 """The operators of several sequences over one paged cache at the limits of what their arguments may hold."""
-import math
 
 import pytest
 import torch
