@@ -44,8 +44,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ float exp2_below(float a, float b) { return __builtin_amdgcn_exp2f(a - (b == -INFINITY ? 0.f : b)); }
 
 // PARTS: numbers of the cache's type that stand for one fp32 number.
-// Probabilities are exp2(score - reference + P_BITS) P_SCALE.  fp16: at most 2^15 then, and two fp16 numbers hold them to 2^-36 of the reference (cut off: sixty
-// thousand keys may lose 2^-20 of the sum together); values of at most 2^16 stay far below fp32's end.  (The exponent of some twelve is off by 2^-21: a
+// Probabilities are exp2(score - reference + P_BITS) P_SCALE.  fp16: at most 2^15 then, and two fp16 numbers hold them to 2^-37 of the reference (sixty
+// thousand keys may be off by 2^-21 of the sum together); values of at most 2^16 stay far below fp32's end.  (The exponent of some twelve is off by 2^-21: a
 // factor behind the exponential would be one instruction of ten per key.)  The other types have fp32's range, and values up to its end: scaled down, 2^21 keys of
 // them add up to no infinity, and what is lost below are products under 2^-126, 2^-102 of a value of one.
 template <typename KT> struct Type;
@@ -53,22 +53,40 @@ template <> struct Type<half_t> { static constexpr int PARTS = 2; static constex
 template <> struct Type<bf16_t> { static constexpr int PARTS = 3; static constexpr float P_BITS = 0.f, P_SCALE = 0x1p-24f; };
 template <> struct Type<float> { static constexpr int PARTS = 1; static constexpr float P_BITS = 0.f, P_SCALE = 0x1p-24f; };
 
-// Two fp32 numbers as pairs of the cache's type, most significant part first.
+// Two fp32 numbers as pairs of the cache's type, most significant part first.  Every part is rounded to nearest and what it leaves has a sign, so two fp16 numbers
+// hold 24 bits and three bf16 numbers all of them; and where a sum is so large that small parts are lost in it, they are lost to either side.  (Cut off,
+// sixty thousand small weights beside a large one added up to 4e-5 less than they are over a bf16 cache.)
+typedef float f32x2v __attribute__((ext_vector_type(2)));
 template <typename KT> __device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[Type<KT>::PARTS]);
 template <> __device__ __forceinline__ void parts_of<half_t>(float x, float y, uint32_t (&out)[2]) {
-    out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    out[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), pair));
     float rx, ry;                                // x - hi, y - hi, in one instruction each (as two they are a sixth of a turn's vector instructions)
     asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rx) : "v"(out[0]), "v"(x));
     asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(ry) : "v"(out[0]), "v"(y));
-    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(rx, ry));
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{rx, ry}), pair));
 }
 template <> __device__ __forceinline__ void parts_of<bf16_t>(float x, float y, uint32_t (&out)[3]) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {                // eight bits each, cut off: the remainders are exact
-        const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-        out[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        x -= __uint_as_float(a & 0xFFFF0000u);
-        y -= __uint_as_float(b & 0xFFFF0000u);
+    for (int p = 0; p < 3; ++p) {
+        out[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), pair));
+        x -= __uint_as_float(out[p] << 16);
+        y -= __uint_as_float(out[p] & 0xFFFF0000u);
+    }
+}
+// The same for queries, which in bf16 may be as large as fp32's largest number: rounded, that would be an infinity.  Three times eight bits cut off are
+// all of them.
+template <typename KT> __device__ __forceinline__ void query_parts(float x, float y, uint32_t (&out)[Type<KT>::PARTS]) {
+    if constexpr (Type<KT>::PARTS == 2) parts_of<KT>(x, y, out);
+    else {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+            out[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            x -= __uint_as_float(a & 0xFFFF0000u);
+            y -= __uint_as_float(b & 0xFFFF0000u);
+        }
     }
 }
 
@@ -218,7 +236,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
             } else {
                 uint32_t part[4][PARTS];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) parts_of<KT>(x[i][e] * up, x[i][e + 1] * up, part[e / 2]);
+                for (int e = 0; e < 8; e += 2) query_parts<KT>(x[i][e] * up, x[i][e + 1] * up, part[e / 2]);
 #pragma unroll
                 for (int q = 0; q < PARTS; ++q)
                     to[(((q_row / ROWS) * NJ + piece / 4) * PARTS + q) * WAVE + (piece % 4) * ROWS + q_row % ROWS] = u32x4{part[0][q], part[1][q], part[2][q], part[3][q]};
@@ -611,7 +629,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
                 uint32_t part[PARTS];
-                parts_of<KT>(x[rt][j][e] * up, x[rt][j][e + 1] * up, part);
+                query_parts<KT>(x[rt][j][e] * up, x[rt][j][e + 1] * up, part);
 #pragma unroll
                 for (int q2 = 0; q2 < PARTS; ++q2) Q[rt][j][q2][e / 2] = part[q2];
             }

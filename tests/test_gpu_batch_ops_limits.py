@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import batch_reference as R
-from test_gpu_batch_ops import attend, attention_case, close, gen
+from test_gpu_batch_ops import attend, attention_case, close, gen, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,56 @@ def test_attention_of_scores_far_from_zero(dtype, heads, kv, shared, lengths, wi
     got, err = attend(dtype, q, K, V, table, *rest, width)
     assert err == 0
     close(got, R.attention(q, K, V, table, *rest, width), 1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_attention_weights_of_many_small_ones_add_up_to_one(dtype):
+    """Where a wave keeps one reference over many keys: a sequence of 60000 positions that ends inside a longer shared part, the first key 2^20 above the others.
+    Values of one come out as one: a weight is off by 2^-37 of the largest at most, to either side, and the many together by 60000 x 2^-37 = 4e-7.  The sums: a
+    lane adds 3750 weights and a wave's product 1875 partial sums to what the first key left there, each rounded to 2^-24 of it at most, a uniform error:
+    sqrt(3750 + 1875) 2^-24 / sqrt(3) = 2.6e-6 as one standard deviation."""
+    n, d = 60_000, 64
+    q = torch.zeros(2, 4, d)
+    q[..., 0] = 8.0
+    pages = (n + 200) // 16 + 1
+    K = torch.zeros(pages, 1, 16, d)
+    K[..., 0] = 0.25 * torch.rand(pages, 1, 16, generator=gen(25))
+    K[0, 0, 0, 0] = 14.0                                     # 8 x 14 / 8 = 14 = 20.2 log 2
+    V = torch.ones(pages, 1, 16, d)
+    table = torch.arange(pages, dtype=torch.int32).expand(2, -1).contiguous()
+    got, err = attend(dtype, q, K.to(R.TORCH[dtype]), V.to(R.TORCH[dtype]), table, ints([n + 100]), ints([n, n - 1]), 2, max_own=1)
+    assert err == 0 and (got - 1.0).abs().max() < 8e-6, (got - 1.0).abs().max()       # three standard deviations
+
+
+def balanced(dtype, g, rows, d=128):
+    """Queries of some units with all 24 bits in use, and two keys for each whose scores differ by little, but come about from quite different products."""
+    q = torch.randn(rows, d, generator=g, dtype=torch.float64) * 4
+    q = q.float().double()
+    k = torch.randn(rows, 2, d, generator=g, dtype=torch.float64) * 4
+    k -= (k @ q[:, :, None]) / (q * q).sum(-1)[:, None, None] * q[:, None]
+    return q.float(), k.to(R.TORCH[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("heads,width,bound", [(4, 1, 0), (64, 1, 0), (4, 2, 600), (64, 2, 600)], ids=["alone", "alone-many", "few", "many"])
+def test_attention_uses_all_bits_of_its_queries(dtype, heads, width, bound):
+    """Of two keys the first has the value one, the other's is zero: the result is a weight p, off by p (1 - p) <= 1/4 of the scores' error.  A score of 128 products of
+    some 16 / sqrt(128): twelve steps of 32 products, each rounded to 2^-25 of a partial sum (at most some 16 in all), 6e-6 at worst, 2e-6 of the weight, and the
+    exponential's 2^-22.  A query without its last eight bits (2^-16 of 4, over 128 keys of 4, / sqrt(128), random signs) moves a score by some 1e-4."""
+    g = gen(26)
+    n_kv, n_seq, page = 2, 16, 4
+    q, K = torch.zeros(n_seq, heads, 128), torch.zeros(n_seq, n_kv, page, 128, dtype=R.TORCH[dtype])
+    V = torch.zeros_like(K)
+    for s in range(0, n_seq, width):
+        qq, kk = balanced(dtype, g, n_kv)
+        q[s:s + width], K[s, :, :2] = qq.repeat_interleave(heads // n_kv, 0), kk
+    V[:, :, 0] = 1.0
+    table = torch.full((n_seq, 150), -1, dtype=torch.int32)
+    table[:, 0] = torch.arange(n_seq)
+    rest = (K, V, table, ints([2] * (n_seq // width)), ints([2] * n_seq))
+    got, err = attend(dtype, q, *rest, width, max_shared=max(bound, 2))     # (a bound of 600: blocks of their own for the shared positions)
+    want = R.attention(q, *rest, width)
+    assert err == 0 and 0.2 < want[..., 0].mean() < 0.8 and (got - want).abs().max() < 4e-6, (got - want).abs().max()
+    if dtype != "fp32":                                      # what the bound has to see: queries of fewer bits, in the oracle
+        cut = (q.view(torch.int32) & ~(0xFF if dtype == "bf16" else 0x1FFF)).view(torch.float32)
+        assert (R.attention(cut, *rest, width) - want).abs().max() > 8e-6
