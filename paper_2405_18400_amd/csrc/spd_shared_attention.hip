@@ -136,15 +136,18 @@ template <int B> __device__ __forceinline__ void load_words(const char *p, uint3
 // instructions, and a block of a short call has little else to do).
 __device__ __forceinline__ int over(int n, const Divisor &d) { return (int)(__umulhi(2u * (uint32_t)n, d.mul) >> d.shift); }
 
-// Whether any thread of the block found something bad, by one barrier, which also says that the pages' places have been written.
-__device__ __forceinline__ bool block_any(bool bad, int *flags) {
-    const bool mine = __any(bad);
-    if ((threadIdx.x & (WAVE - 1)) == 0) flags[threadIdx.x / WAVE] = mine;
-    __syncthreads();
+// The bits that any thread of the block has set (N of them), by one barrier, which also says that the pages' places have been written.
+template <int N>
+__device__ __forceinline__ int block_any(int bits, int *flags) {
     int all = 0;
 #pragma unroll
+    for (int i = 0; i < N; ++i) all |= __any((bits >> i) & 1) ? 1 << i : 0;
+    if ((threadIdx.x & (WAVE - 1)) == 0) flags[threadIdx.x / WAVE] = all;
+    __syncthreads();
+    all = 0;
+#pragma unroll
     for (int v = 0; v < NWS; ++v) all |= flags[v];
-    return all != 0;
+    return all;
 }
 
 // A stretch of positions read through one row of the table.
@@ -272,7 +275,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
         pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
-    const bool any_bad = block_any(bad, flags);
+    const bool any_bad = block_any<1>(bad, flags) != 0;
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) scale[rt] = row_scale[rt * ROWS + col];
@@ -540,7 +543,7 @@ __device__ __forceinline__ void to_lds16(const char *from, char *to) {
 #endif
 }
 
-// False: none of the chunk's positions is there.
+// False: none of the chunk's positions is there, or no row needs them.
 template <typename KT, int DH, int RT>
 __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit &un, char *lds, u64 *pages, int *flags) {
     constexpr int PARTS = Type<KT>::PARTS, NJ = DH / 32, FV = DH / 16, VW = FV / 2;
@@ -576,14 +579,18 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
     if ((to < 0 || to > p.max_shared) && p.err && tid == 0) *as_global(p.err) = 1;
     if (hi <= lo || to > p.max_shared) return false;
     const int n_pages = ((hi - 1) >> shift) - first + 1;     // (at most the row's entries: max_shared is)
-    bool bad = false;
+    bool bad = false, on = false;                // (on: a sequence of these rows reaches behind the shared positions, and so needs all of them)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) on = on || (len[rt] >= to && seq_fits(p, to, len[rt]));
     for (int i = tid; i < n_pages; i += NTS) {
         if (i != tid) page = as_global(entries)[i];
         const bool ok = (unsigned)page < (unsigned)p.c.n_pages;
         pages[i] = ok ? (u64)page * page_bytes : 0;          // (a page that is none: its keys are masked)
         bad = bad || !ok;
     }
-    const bool any_bad = block_any(bad, flags);
+    const int found = block_any<2>((int)bad | (int)on << 1, flags);
+    if (!(found & 2)) return false;
+    const bool any_bad = found & 1;
     if (any_bad && tid == 0 && p.err) *as_global(p.err) = 1;
 
     const int base = lo & ~3, stages = (hi - base + SK - 1) / SK;
@@ -859,16 +866,19 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
         } else {
             const auto resolve = [&](Unit &u) {
                 int to = as_global(p.shared)[g];
+                bool on = true;                  // a sequence of these rows reaches behind the shared positions: others have blocks of their own
                 if (p.width == 1) {              // nothing is shared: the whole sequence
                     const int len = as_global(p.len)[g];
                     to = seq_fits(p, to, len) ? len : -1;
                 } else {
                     if (to > p.max_shared) to = -1;
                     u.shared = to;
+                    const int row = min((int)(threadIdx.x & (WAVE - 1)), u.n_rows - 1), len = as_global(p.len)[u.seq + over(u.r0 + row, p.by_group)];
+                    on = __any(len >= to && seq_fits(p, to, len));       // (every wave looks at all rows)
                 }
                 if (to < 0 && p.err && threadIdx.x == 0) *as_global(p.err) = 1;
                 u.a = Stretch{u.seq, c * p.shared_chunk, min((c + 1) * p.shared_chunk, to)};
-                return u.a.hi > u.a.lo;
+                return on && u.a.hi > u.a.lo;
             };
             if (!attend<KT, DH, RT>(p, un, resolve, lds, pages, flags, lds_m, lds_l, row_scale))
                 for (int r = threadIdx.x; r < un.n_rows; r += NTS) nothing(p, un, r);

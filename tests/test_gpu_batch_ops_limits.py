@@ -53,6 +53,23 @@ def test_attention_of_scores_far_from_zero(dtype, heads, kv, shared, lengths, wi
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("heads", [4, 16])
+def test_attention_reports_pages_that_a_sequence_needs_alone(dtype, heads):
+    """Shared positions with blocks of their own: entries behind every sequence of a group may hold anything, also where shared[g] reaches over them."""
+    q, K, V, table, shared, length = attention_case(dtype, heads, 2, 64, 16, [700, 650, 700], [300, 17, 0, 290, 651, 700, 650, 20, 0, 0, 0, 0], 4, seed=24)
+    want = R.attention(q, K, V, table, shared, length, 4)
+    table[0, 300 // 16 + 1:], table[8] = -5, 1 << 30
+    for max_shared, max_own in ((700, 50), (704, 300)):
+        got, err = attend(dtype, q, K, V, table, shared, length, 4, max_shared=max_shared, max_own=max_own)
+        assert err == 0
+        close(got, want)
+    table[0, 300 // 16] = -5                                                # the last one that is needed
+    got, err = attend(dtype, q, K, V, table, shared, length, 4, max_shared=700, max_own=50)
+    assert err == 1
+    close(got, R.attention(q, K, V, table, shared, length, 4))
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
 def test_attention_weights_of_many_small_ones_add_up_to_one(dtype):
     """Where a wave keeps one reference over many keys: a sequence of 60000 positions that ends inside a longer shared part, the first key 2^20 above the others.
     Values of one come out as one: a weight is off by 2^-37 of the largest at most, to either side, and the many together by 60000 x 2^-37 = 4e-7.  The sums: a
