@@ -327,12 +327,13 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
  * [0, n_pages), a row of the table or a length out of range is never followed, and *err (DEVICE int32, may be NULL) is
  * set to 1 (and never cleared).  Calls do not synchronise and allocate nothing; those that need scratch take it from the caller, 256-byte
  * aligned and of the size the function beside them gives (0: none, NULL will do; SPD_EWORKSPACE if less), and leave nothing in it for a
- * later call: calls that may overlap need scratch of their own. */
+ * later call: calls that may overlap need scratch of their own.  What a call writes (results, scratch, the pools it appends to or copies in) lies apart from
+ * everything else that it is given, but where an operator says otherwise; SPD_EINVAL if not. */
 
 /* New tokens' keys and values into the cache, rotated on the way: token i, at position pos[i] of sequence seq[i] (DEVICE int32
  * [n_tokens]), has k and v rows DEVICE float [n_kv_heads, d_head] at k + i kv_stride, v + i kv_stride; k (and q) are rotated on adjacent
  * pairs by pos * rope_theta^(-2i/d_head).  q (may be NULL, then n_heads is 0): rows [n_heads, d_head] at q + i q_stride; q_out
- * [n_tokens, n_heads, d_head] gets them rotated, in fp32 (it may be q where q_stride is n_heads d_head; otherwise it lies apart from the rows of q, k and v).  Strides are in elements and
+ * [n_tokens, n_heads, d_head] gets them rotated, in fp32 (it may be q where q_stride is n_heads d_head).  Strides are in elements and
  * multiples of 4, so that the parts of one product's rows can be passed as they lie; pointers 16-byte aligned.  seq[i] < 0:
  * padding, nothing of that token is read or written.  A token whose position or page is out of range is left out whole, *err is set.  No two tokens of a
  * call may name the same position of the same page. */
@@ -343,7 +344,7 @@ int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_t *table, i
 
 /* One query per sequence and head: out[s][h] = softmax(q[s][h] . K / sqrt(d_head)) V over positions [0, len[s]) of
  * sequence s.  Positions below shared[g] are the same in all sequences of group g: they are read once, through the table of
- * the group's first sequence.  q, out DEVICE float [n_seq, n_heads, d_head]; shared DEVICE int32 [n_seq / width], len DEVICE int32 [n_seq]; out must not overlap q.
+ * the group's first sequence.  q, out DEVICE float [n_seq, n_heads, d_head]; shared DEVICE int32 [n_seq / width], len DEVICE int32 [n_seq].
  * max_shared >= every shared[g] and max_own >= every len[s] - shared[g] size the launch (host values; neither more than a row of
  * the table holds).  len[s] may be less than shared[g].  A sequence of length 0 gets zeros; so does one whose lengths are out of these bounds
  * (*err is set).  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result.  Nothing behind a sequence's last position gets into its result,
@@ -363,7 +364,7 @@ int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const 
  * unchanged; neither its logits nor those of an absent beam count.  Outputs DEVICE [n_groups, n_out], best first: scores, tokens (in
  * [0, vocab)), parents (in [0, n_in)) and, unless NULL, whether the beam has ended (its parent had, or the token is end_token).
  * Where there are fewer continuations, the others have score -inf, token 0, not ended, and as parent their own place (0 where that is no beam).  With
- * n_out = n_in an output may be the buffer of scores or ended; otherwise outputs lie apart from them. */
+ * n_out = n_in an output may be the buffer of scores or ended. */
 size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab);
 int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row_stride, int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab,
                        const float *scores, const int32_t *ended, int32_t end_token, float tau, float *out_scores, int32_t *out_tokens,
@@ -374,7 +375,7 @@ int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row_stride, in
  * row is the page being filled, which like those behind it must be the row's own.  A row's first child keeps the whole row; each
  * further child, in order, takes its parent's entries before e and, from e on, those of a row without a child (in order), into
  * whose page e the rows filled so far are copied in all n_layers (layer l's pools start l * layer_stride elements after K and V).  So
- * every beam has pages of its own to write into and none has to be found.  table_out [n_seq, table_stride] must not overlap table.
+ * every beam has pages of its own to write into and none has to be found.  table_out [n_seq, table_stride] is a table of its own.
  * A group with a parent outside [0, width), unequal lengths or, where a page is to be copied, a row whose page e is out of range or another
  * row's too is left as it was (its table copied unchanged) and *err is set. */
 int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,

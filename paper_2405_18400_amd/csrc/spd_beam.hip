@@ -486,14 +486,20 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
     if (ended && (end_token < 0 || end_token >= vocab)) return SPD_EINVAL;
     if (n_groups == 0) return SPD_OK;
     if (!logits || !scores || !out_scores || !out_tokens || !out_parents || (uintptr_t)logits % (dtype == SPD_DTYPE_FP32 ? 4 : 2)) return SPD_EINVAL;
-    // a group's outputs may take the place of its own inputs, not of another's
-    const size_t in_bytes = (size_t)n_groups * n_in * 4, out_bytes = (size_t)n_groups * n_out * 4;
-    for (const void *in : {(const void *)scores, (const void *)ended})
-        for (const void *out : {(const void *)out_scores, (const void *)out_tokens, (const void *)out_parents, (const void *)out_ended})
-            if (in && out && !(in == out && n_in == n_out) && spdk::overlap(in, in_bytes, out, out_bytes)) return SPD_EINVAL;
     const size_t need = spd_op_beam_select_scratch_bytes(n_groups, n_in, n_out, vocab);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;
+    // a group's outputs may take the place of its own scores or ended, and lie apart from everything else that is read or written
+    const size_t in_bytes = (size_t)n_groups * n_in * 4, out_bytes = (size_t)n_groups * n_out * 4;
+    const spdk::Span sz{logits, ((size_t)(n_groups * (size_t)n_in - 1) * row_stride + vocab) * (dtype == SPD_DTYPE_FP32 ? 4 : 2)}, sw{scratch, need}, ss{scores, in_bytes}, sd{ended, in_bytes},
+        outs[4] = {{out_scores, out_bytes}, {out_tokens, out_bytes}, {out_parents, out_bytes}, {out_ended, out_bytes}};
+    const auto unless_same = [&](const spdk::Span &in, const spdk::Span &out) { return in.p == out.p && n_in == n_out ? spdk::Span{} : in; };
+    for (int i = 0; i < 4; ++i) {
+        if (spdk::over_any(outs[i], {sz, sw, unless_same(ss, outs[i]), unless_same(sd, outs[i])})) return SPD_EINVAL;
+        for (int j = i + 1; j < 4; ++j)
+            if (spdk::over_any(outs[i], {outs[j]})) return SPD_EINVAL;
+    }
+    if (spdk::over_any(sw, {sz, ss, sd})) return SPD_EINVAL;
     const int ne = entries_per_lane((long long)n_groups * n_in, vocab, dtype == SPD_DTYPE_FP32 ? WAVES_FP32 : WAVES_16), slice = WAVE * ne;
     SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, 1.4426950408889634f / tau, 1.0 / (double)tau, out_scores, out_tokens, out_parents, out_ended,
                  (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};

@@ -318,6 +318,14 @@ namespace spdk {
 inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
+struct Span { const void *p; size_t bytes; };
+// Whether a result lies over any of what a call reads or writes besides (null: not given).
+inline bool over_any(Span out, std::initializer_list<Span> others) {
+    for (const Span &o : others)
+        if (out.p && o.p && out.bytes && o.bytes && overlap(out.p, out.bytes, o.p, o.bytes)) return true;
+    return false;
+}
+inline size_t pool_bytes(int dtype, const PagedCache &c) { return ((size_t)c.n_pages * c.n_kv_heads * c.d_head << c.page_shift) * (dtype == SPD_DTYPE_FP32 ? 4 : 2); }   // of one layer
 int paged_cache_status(int dtype, const PagedCache &c, int page_size);   // an spd_status
 PagedCache paged_cache(void *K, void *V, const int32_t *table, int n_pages, int n_kv_heads, int page_size, int d_head, int n_seq, int table_stride);
 hipError_t gemv(hipStream_t s, int dtype, int epi, const GemvArgs &a, int num_cu);
@@ -354,6 +362,7 @@ int attention_on_scratch(hipStream_t s, int dtype, const float *q, const void *K
 }  // namespace spdk
 
 // ---------------------------------------------------------------- host-side table builder
+#include <initializer_list>
 #include <string>
 #include <vector>
 struct NgramHostTable {

@@ -251,10 +251,12 @@ extern "C" int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_
     if ((q == nullptr) != (q_out == nullptr) || (q == nullptr) != (n_heads == 0)) return SPD_EINVAL;
     if (q && (q_stride < (int64_t)n_heads * d_head || q_stride % 4 || ((uintptr_t)q | (uintptr_t)q_out) % 16)) return SPD_EINVAL;
     if (q == q_out && q && q_stride != (int64_t)n_heads * d_head) return SPD_EINVAL;
-    // read by other blocks than those that write it
-    const size_t out_bytes = (size_t)n_tokens * n_heads * d_head * 4, kv_bytes = ((size_t)(n_tokens - 1) * kv_stride + (size_t)n_kv_heads * d_head) * 4;
-    if (q && (spdk::overlap(q_out, out_bytes, k, kv_bytes) || spdk::overlap(q_out, out_bytes, v, kv_bytes) ||
-              (q != q_out && spdk::overlap(q_out, out_bytes, q, ((size_t)(n_tokens - 1) * q_stride + (size_t)n_heads * d_head) * 4)))) return SPD_EINVAL;
+    // what is written lies apart from what other blocks read
+    const size_t out_bytes = (size_t)n_tokens * n_heads * d_head * 4, kv_bytes = ((size_t)(n_tokens - 1) * kv_stride + (size_t)n_kv_heads * d_head) * 4,
+                 q_bytes = q ? ((size_t)(n_tokens - 1) * q_stride + (size_t)n_heads * d_head) * 4 : 0, pool = spdk::pool_bytes(dtype, c), ids = (size_t)n_tokens * 4;
+    const spdk::Span sk{k, kv_bytes}, sv{v, kv_bytes}, sq{q, q_bytes}, st{table, (size_t)n_seq * table_stride * 4}, ss{seq, ids}, sp{pos, ids}, sK{K, pool}, sV{V, pool}, se{err, 4};
+    if (spdk::over_any(spdk::Span{q_out, out_bytes}, {sk, sv, q == q_out ? spdk::Span{} : sq, st, ss, sp, sK, sV, se}) || spdk::over_any(sK, {sV, sk, sv, sq, st, ss, sp, se}) ||
+        spdk::over_any(sV, {sk, sv, sq, st, ss, sp, se})) return SPD_EINVAL;
     AppendArgs a{c, q, k, v, q_stride, kv_stride, seq, pos, n_tokens, n_heads, 0, log2((double)rope_theta), q_out, err};
     hipStream_t s = (hipStream_t)hip_stream;
     const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_append<float>(s, a) : dtype == SPD_DTYPE_FP16 ? launch_append<half_t>(s, a) : launch_append<bf16_t>(s, a);
@@ -273,8 +275,10 @@ extern "C" int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_
     if (n_layers > 1 && (layer_stride < layer_elems || layer_stride % (16 / elem))) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
     if (!parents || !len || !table_out) return SPD_EINVAL;
-    const size_t table_bytes = (size_t)n_seq * table_stride * 4;
-    if (spdk::overlap(table_out, table_bytes, table, table_bytes)) return SPD_EINVAL;       // read while written
+    // what is written lies apart from what other blocks read
+    const size_t table_bytes = (size_t)n_seq * table_stride * 4, ids = (size_t)n_seq * 4, pools = (size_t)(n_layers - 1) * layer_stride * elem + spdk::pool_bytes(dtype, c);
+    const spdk::Span st{table, table_bytes}, sp{parents, ids}, sl{len, ids}, sK{K, pools}, sV{V, pools}, se{err, 4};
+    if (spdk::over_any(spdk::Span{table_out, table_bytes}, {st, sp, sl, sK, sV, se}) || spdk::over_any(sK, {sV, st, sp, sl, se}) || spdk::over_any(sV, {st, sp, sl, se})) return SPD_EINVAL;
     ReorderArgs a{c, parents, len, table_out, err, n_layers, width, n_seq / width, d_head * elem, 0, 0, (size_t)layer_stride * elem};
     // about 32 KB of keys and values per block
     a.heads_per_share = std::max(1, 16384 / (page_size * a.row_bytes));

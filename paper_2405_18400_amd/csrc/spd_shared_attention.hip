@@ -1091,10 +1091,14 @@ extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void
     if (n_seq == 0) return SPD_OK;
     if ((long long)n_seq * n_heads > (1 << 24)) return SPD_EINVAL;
     if (!q || !shared || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16) return SPD_EINVAL;
-    if (spdk::overlap(q, (size_t)n_seq * n_heads * d_head * 4, out, (size_t)n_seq * n_heads * d_head * 4)) return SPD_EINVAL;      // (blocks that share a head's queries)
     const size_t need = spd_op_attention_shared_scratch_bytes(n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
     if (scratch_bytes < need) return SPD_EWORKSPACE;
+    // what is written lies apart from what other blocks read (several share a head's queries)
+    const size_t rows = (size_t)n_seq * n_heads * d_head * 4, pool = spdk::pool_bytes(dtype, c);
+    const spdk::Span sq{q, rows}, so{out, rows}, sK{K, pool}, sV{V, pool}, st{table, (size_t)n_seq * table_stride * 4}, ss{shared, (size_t)(n_seq / width) * 4}, sl{len, (size_t)n_seq * 4},
+        se{err, 4}, sw{scratch, need};
+    if (spdk::over_any(so, {sq, sK, sV, st, ss, sl, se, sw}) || spdk::over_any(sw, {sq, sK, sV, st, ss, sl, se})) return SPD_EINVAL;
     const Cut cut = cut_for(dtype, n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
     SharedAttnArgs a{};
     a.c = c; a.q = q; a.out = out; a.shared = shared; a.len = len; a.err = err;

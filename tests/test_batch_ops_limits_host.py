@@ -1,0 +1,46 @@
+"""What the operators of several sequences over one paged cache refuse and how they cut their work, seen without a GPU (no status below follows a pointer)."""
+import pytest
+
+from test_batch_ops_host import A, APPEND, ATTEND, EINVAL, REORDER, SELECT, call, pkg  # noqa: F401
+
+
+def over(base, what, size, *others):
+    """Places of `what` (`size` bytes) over the beginning and the end of each of `others` (their bytes)."""
+    return [pytest.param(what, base[o] + at, id=f"{what}-{o}-{at}") for o, n in others for at in {4 - size, n - 4}]
+
+
+def aligned(places, by):
+    """The same, towards the middle, where an address has to be a multiple of `by`."""
+    return [pytest.param(p.values[0], (p.values[1] + (by - 1 if p.id.rsplit("-", 2)[1] == "" else 0)) // by * by, id=p.id) for p in places]
+
+
+POOL, TABLE = 40 * 2 * 16 * 64 * 2, 6 * 9 * 4
+LOGITS = (5 * 5000 + 5000) * 4
+
+
+@pytest.mark.parametrize("what,at", aligned(over(APPEND, "q_out", 6 * 256 * 4, ("table", TABLE), ("seq", 24), ("pos", 24), ("K", POOL), ("V", POOL)), 16)
+                         + aligned(over(APPEND, "K", POOL, ("V", POOL), ("q", 6 * 256 * 4), ("k", 6 * 128 * 4), ("v", 6 * 128 * 4), ("table", TABLE), ("seq", 24), ("pos", 24)), 16)
+                         + aligned(over(APPEND, "V", POOL, ("q", 6 * 256 * 4), ("k", 6 * 128 * 4), ("v", 6 * 128 * 4), ("table", TABLE), ("seq", 24), ("pos", 24)), 16))
+def test_append_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noqa: F811
+    assert call(pkg, "spd_op_append_paged", APPEND, **{what: at}) == EINVAL
+
+
+@pytest.mark.parametrize("what,at", aligned(over(ATTEND, "out", 6 * 4 * 64 * 4, ("K", POOL), ("V", POOL), ("table", 6 * 60 * 4), ("shared", 8), ("len", 24), ("scratch", 256)), 16)
+                         + aligned(over(ATTEND, "scratch", 256, ("K", POOL), ("V", POOL), ("q", 6 * 4 * 64 * 4), ("table", 6 * 60 * 4), ("shared", 8), ("len", 24)), 256))
+def test_attention_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noqa: F811
+    assert call(pkg, "spd_op_attention_shared", ATTEND, **{what: at}) == EINVAL
+
+
+@pytest.mark.parametrize("what,at", [p for o in ("out_scores", "out_tokens", "out_parents", "out_ended") for p in over(SELECT, o, 32, ("logits", LOGITS), ("scratch", 256))]
+                         + over(SELECT, "out_tokens", 32, ("out_scores", 32)) + over(SELECT, "out_parents", 32, ("out_scores", 32), ("out_tokens", 32))
+                         + over(SELECT, "out_ended", 32, ("out_scores", 32), ("out_tokens", 32), ("out_parents", 32))
+                         + aligned(over(SELECT, "scratch", 256, ("logits", LOGITS), ("scores", 24), ("ended", 24)), 256))
+def test_select_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noqa: F811
+    assert call(pkg, "spd_op_beam_select", SELECT, **{what: at}) == EINVAL
+
+
+@pytest.mark.parametrize("what,at", over(REORDER, "table_out", TABLE, ("parents", 24), ("len", 24), ("K", 2 * POOL), ("V", 2 * POOL))
+                         + aligned(over(REORDER, "K", 2 * POOL, ("V", 2 * POOL), ("table", TABLE), ("parents", 24), ("len", 24)), 16)
+                         + aligned(over(REORDER, "V", 2 * POOL, ("table", TABLE), ("parents", 24), ("len", 24)), 16))
+def test_reorder_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noqa: F811
+    assert call(pkg, "spd_op_beam_reorder", REORDER, **{what: at}) == EINVAL
