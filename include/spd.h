@@ -376,11 +376,21 @@ int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row_stride, in
  * further child, in order, takes its parent's entries before e and, from e on, those of a row without a child (in order), into
  * whose page e the rows filled so far are copied in all n_layers (layer l's pools start l * layer_stride elements after K and V).  So
  * every beam has pages of its own to write into and none has to be found.  table_out [n_seq, table_stride] is a table of its own.
- * A group with a parent outside [0, width), unequal lengths or, where a page is to be copied, a row whose page e is out of range or another
- * row's too is left as it was (its table copied unchanged) and *err is set. */
+ * A group with a parent outside [0, width), unequal lengths or, where a page is to be copied, a row whose page e is out of range or page e of another
+ * row of the group too is left as it was (its table copied unchanged) and *err is set.  That is all that is looked at: pages that are not a row's own in
+ * other ways (an entry of another group, or another entry of the same) are overwritten.
+ * Any row may come first afterwards.  So every row has to hold all positions up to len itself: also those that spd_op_attention_shared reads through a group's first
+ * row, whole pages of them by number, and on the page where they end, which is the row's own, as copies. */
 int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
                         int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
                         const int32_t *parents, const int32_t *len, int32_t *table_out, int32_t *err, void *hip_stream);
+
+/* The same where only a group's first row has to hold its shared positions (shared DEVICE int32 [n_seq / width], as for spd_op_attention_shared; those behind len do not
+ * count): all rows get its entries of whole pages of them, and where the first beam goes on from another row, the shared positions on the page where
+ * they end are copied to that row's page.  A group whose shared[g] is out of range, or one of these two pages where there is something to copy, is left as it was and *err is set. */
+int spd_op_beam_reorder_shared(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                               int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
+                               const int32_t *parents, const int32_t *len, const int32_t *shared, int32_t *table_out, int32_t *err, void *hip_stream);
 
 /* ---- test hooks for the error path of the persistent kernel's bounded waits ----
  * A wait of the persistent forward kernel that gives up (its grid was not co-resident) sets an

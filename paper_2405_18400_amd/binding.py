@@ -108,6 +108,7 @@ def lib():
             "spd_op_attention_shared": [i32, vp, vp, vp, vp] + [i32] * 6 + [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp, vp],
             "spd_op_beam_select": [i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
             "spd_op_beam_reorder": [i32, vp, vp, vp] + [i32] * 7 + [i64, i32, vp, vp, vp, vp, vp],
+            "spd_op_beam_reorder_shared": [i32, vp, vp, vp] + [i32] * 7 + [i64, i32, vp, vp, vp, vp, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -585,8 +586,9 @@ def spd_op_beam_select(dtype: str, logits, scores, out_scores, out_tokens, out_p
         raise SpdError(rc, where)
 
 
-def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, width: int, err=None):
-    """K, V [pages, ...] or [layers, pages, n_kv_heads, page_size, d_head]; parents int32 [n_seq / width, width], length int32 [n_seq]; table -> table_out."""
+def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, width: int, err=None, shared=None):
+    """K, V [pages, ...] or [layers, pages, n_kv_heads, page_size, d_head]; parents int32 [n_seq / width, width], length int32 [n_seq]; table -> table_out.
+    shared, int32 [n_seq / width]: positions that only a group's first row holds, as for the attention; without it every row has to hold all of its own (spd.h)."""
     torch, where = _torch(), "spd_op_beam_reorder"
     kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
     shape, rows = K.shape, table.shape
@@ -599,12 +601,14 @@ def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, wid
     if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and parents.dtype is i32 and length.dtype is i32 and table_out.dtype is i32 and V.shape == shape
             and parents.numel() == n_seq and length.numel() == n_seq and table_out.numel() == n_seq * entries and K.is_contiguous() and V.is_contiguous() and table.is_contiguous()
             and parents.is_contiguous() and length.is_contiguous() and table_out.is_contiguous() and K.get_device() == device and V.get_device() == device
-            and table.get_device() == device and parents.get_device() == device and length.get_device() == device and table_out.get_device() == device and err is None):
+            and table.get_device() == device and parents.get_device() == device and length.get_device() == device and table_out.get_device() == device
+            and shared is None and err is None):
         _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), parents=(parents, i32, groups), length=(length, i32, (n_seq,)),
-                table_out=(table_out, i32, rows), err=(err, i32, (1,)))
-    rc = lib().spd_op_beam_reorder(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
-                                   n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), table_out.data_ptr(),
-                                   None if err is None else err.data_ptr(), _stream_ptr(device))
+                table_out=(table_out, i32, rows), shared=(shared, i32, groups[:1]), err=(err, i32, (1,)))
+    name, of_group = (where, ()) if shared is None else (where + "_shared", (shared.data_ptr(),))
+    rc = getattr(lib(), name)(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
+                              n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), *of_group, table_out.data_ptr(),
+                              None if err is None else err.data_ptr(), _stream_ptr(device))
     if rc:
         raise SpdError(rc, where)
 

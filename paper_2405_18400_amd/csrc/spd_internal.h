@@ -280,8 +280,9 @@ struct AppendArgs {
 struct ReorderArgs {
     PagedCache c;                // layer 0's; layer l's pools start layer_bytes * l later
     const int32_t *parents, *len;
+    const int32_t *shared;       // per group, or null
     int32_t *table_out, *err;
-    int32_t n_layers, width, n_groups, row_bytes, shares, heads_per_share;
+    int32_t n_layers, width, n_groups, children, row_bytes, shares, heads_per_share;
     size_t layer_bytes;
 };
 struct Divisor { uint32_t mul; int32_t shift; };   // n / d = (2 n mul >> 32) >> shift for n < 2^31

@@ -156,7 +156,10 @@ __device__ __forceinline__ BeamRows beam_rows(const ReorderArgs &a, int g, int l
 // Measured: two further children of 32 layers x 32 heads x 10 rows x 128 in fp16, 10.5 MB read and as much written, 6.8 us (parents and
 // lengths, then page numbers, are two trips to memory before the copy's own); eight groups of five further children, 16 layers x 8 heads x some 40 rows x 128 in bf16,
 // 109 MB each way, 44 us (4.9 TB/s, a large copy's rate).
-// Blocks 0 .. groups - 1: a group's tables.  The others: (group, further child, layer, share of the key/value heads).
+// Blocks 0 .. groups - 1: a group's tables.  The others: (group, further child, layer, share of the key/value heads); where shared positions are
+// given, one child more stands for the rows of a page on which they end, which the group's first sequence has to have.  Those rows are written on the page of
+// its parent, the rows behind them are read from there and written elsewhere, and no page's rows in front are copied to: no block waits for another.
+template <bool SHARED>
 __global__ __launch_bounds__(NTP) void beam_reorder_kernel(const ReorderArgs a) {
     const int lane = threadIdx.x & (WAVE - 1), w = threadIdx.x / WAVE;
     const bool tables = (int)blockIdx.x < a.n_groups;
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(NTP) void beam_reorder_kernel(const ReorderArgs a) 
     rest /= a.shares;
     const int layer = rest % a.n_layers;
     rest /= a.n_layers;
-    const int child = tables ? 0 : rest % (a.width - 1), g = tables ? blockIdx.x : rest / (a.width - 1);
+    const int child = tables ? 0 : rest % a.children, g = tables ? blockIdx.x : rest / a.children;
     const int page_size = 1 << a.c.page_shift;
     BeamRows r = beam_rows(a, g, lane);
     const int len = as_global(a.len)[g * a.width];
@@ -182,22 +185,48 @@ __global__ __launch_bounds__(NTP) void beam_reorder_kernel(const ReorderArgs a) 
         }
         r.ok = !__any(!good);
     }
+    // shared positions: whole pages of them, and rows on the page where they end, which pages `have` and `want` hold for the first sequence so far and from now on
+    int whole = 0, tail = 0, have = 0, want = 0;
+    if constexpr (SHARED) {
+        const int shared = as_global(a.shared)[g], first = __shfl(r.parent, 0, WAVE);
+        if (shared < 0 || (long long)shared > (long long)a.c.table_stride << a.c.page_shift) r.ok = false;
+        if (r.ok) {
+            whole = min(shared, len) >> a.c.page_shift;
+            tail = min(shared, len) & (page_size - 1);
+            if (tail && first) {
+                have = as_global(table)[whole];
+                want = as_global(table)[(size_t)first * a.c.table_stride + whole];
+                r.ok = page_ok(a.c, have) && page_ok(a.c, want);
+            }
+        }
+    }
     if (tables) {
         if (!r.ok && threadIdx.x == 0) flag(a.err);
         int32_t *out = a.table_out + (size_t)g * a.width * a.c.table_stride;
         for (int j = w; j < a.width; j += NTP / WAVE) {
             const int parent = r.ok ? __shfl(r.parent, j, WAVE) : j, row = r.ok ? __shfl(r.row, j, WAVE) : j;
             for (int e = lane; e < a.c.table_stride; e += WAVE)
-                as_global(out)[(size_t)j * a.c.table_stride + e] = as_global(table)[(size_t)(e < entry ? parent : row) * a.c.table_stride + e];
+                as_global(out)[(size_t)j * a.c.table_stride + e] = as_global(table)[(size_t)(SHARED && r.ok && e < whole ? 0 : e < entry ? parent : row) * a.c.table_stride + e];
         }
         return;
     }
-    if (!r.ok || !filled || child >= __popc(r.further)) return;
-    const int j = nth_set_bit(r.further, child);
-    const size_t from = (size_t)__shfl(page, __shfl(r.parent, j, WAVE), WAVE), to = (size_t)__shfl(page, __shfl(r.row, j, WAVE), WAVE);
-    // 16-byte pieces: the filled rows of this share's heads, keys then values
+    if (!r.ok) return;
+    size_t from, to;
+    int row0 = 0, row1 = filled;                             // rows of the page that are copied
+    if (SHARED && child == a.width - 1) {
+        if (have == want) return;
+        from = (size_t)have; to = (size_t)want;
+        row1 = tail;
+    } else {
+        if (!filled || child >= __popc(r.further)) return;
+        const int j = nth_set_bit(r.further, child);
+        from = (size_t)__shfl(page, __shfl(r.parent, j, WAVE), WAVE); to = (size_t)__shfl(page, __shfl(r.row, j, WAVE), WAVE);
+        if (SHARED && whole == entry) row0 = tail;
+        if (SHARED && row0 >= row1) return;
+    }
+    // 16-byte pieces: the rows of this share's heads, keys then values
     const size_t head_bytes = (size_t)page_size * a.row_bytes, page_bytes = head_bytes * a.c.n_kv_heads;
-    const int per_head = filled * (a.row_bytes / 16), h0 = share * a.heads_per_share, h1 = min(a.c.n_kv_heads, h0 + a.heads_per_share);
+    const int per_head = (row1 - row0) * (a.row_bytes / 16), h0 = share * a.heads_per_share, h1 = min(a.c.n_kv_heads, h0 + a.heads_per_share);
     const int pieces = (h1 - h0) * per_head;
     const float by_head = 1.0f / (float)per_head;            // (at most 2^16 pieces: (p + 1/2) / per_head is never near a whole number)
     for (int i0 = threadIdx.x; i0 < 2 * pieces; i0 += COPIES * NTP) {
@@ -209,7 +238,7 @@ __global__ __launch_bounds__(NTP) void beam_reorder_kernel(const ReorderArgs a) 
             if (i >= 2 * pieces) break;
             const int p = i < pieces ? i : i - pieces, head = (int)(((float)p + 0.5f) * by_head);
             char *pool = (char *)(i < pieces ? a.c.K : a.c.V) + (size_t)layer * a.layer_bytes;
-            const size_t at = (size_t)(h0 + head) * head_bytes + 16 * (size_t)(p - head * per_head);
+            const size_t at = (size_t)(h0 + head) * head_bytes + (size_t)row0 * a.row_bytes + 16 * (size_t)(p - head * per_head);
             v[u] = global_load16(pool + from * page_bytes + at);
             to_at[u] = pool + to * page_bytes + at;
         }
@@ -263,9 +292,9 @@ extern "C" int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }
 
-extern "C" int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
-                                   int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
-                                   const int32_t *parents, const int32_t *len, int32_t *table_out, int32_t *err, void *hip_stream) {
+static int reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                   int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
+                   const int32_t *parents, const int32_t *len, const int32_t *shared, int32_t *table_out, int32_t *err, void *hip_stream) {
     const PagedCache c = spdk::paged_cache(K, V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride);
     const int rc = spdk::paged_cache_status(dtype, c, page_size);
     if (rc != SPD_OK) return rc;
@@ -277,14 +306,28 @@ extern "C" int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_
     if (!parents || !len || !table_out) return SPD_EINVAL;
     // what is written lies apart from what other blocks read
     const size_t table_bytes = (size_t)n_seq * table_stride * 4, ids = (size_t)n_seq * 4, pools = (size_t)(n_layers - 1) * layer_stride * elem + spdk::pool_bytes(dtype, c);
-    const spdk::Span st{table, table_bytes}, sp{parents, ids}, sl{len, ids}, sK{K, pools}, sV{V, pools}, se{err, 4};
-    if (spdk::over_any(spdk::Span{table_out, table_bytes}, {st, sp, sl, sK, sV, se}) || spdk::over_any(sK, {sV, st, sp, sl, se}) || spdk::over_any(sV, {st, sp, sl, se})) return SPD_EINVAL;
-    ReorderArgs a{c, parents, len, table_out, err, n_layers, width, n_seq / width, d_head * elem, 0, 0, (size_t)layer_stride * elem};
+    const spdk::Span st{table, table_bytes}, sp{parents, ids}, sl{len, ids}, sh{shared, (size_t)(n_seq / width) * 4}, sK{K, pools}, sV{V, pools}, se{err, 4};
+    if (spdk::over_any(spdk::Span{table_out, table_bytes}, {st, sp, sl, sh, sK, sV, se}) || spdk::over_any(sK, {sV, st, sp, sl, sh, se}) || spdk::over_any(sV, {st, sp, sl, sh, se})) return SPD_EINVAL;
+    ReorderArgs a{c, parents, len, shared, table_out, err, n_layers, width, n_seq / width, width == 1 ? 0 : width - 1 + (shared != nullptr), d_head * elem, 0, 0, (size_t)layer_stride * elem};
     // about 32 KB of keys and values per block
     a.heads_per_share = std::max(1, 16384 / (page_size * a.row_bytes));
     a.shares = (n_kv_heads + a.heads_per_share - 1) / a.heads_per_share;
-    const long long blocks = a.n_groups + (long long)a.n_groups * (width - 1) * n_layers * a.shares;
+    const long long blocks = a.n_groups + (long long)a.n_groups * a.children * n_layers * a.shares;
     if (blocks > INT32_MAX) return SPD_EINVAL;
-    hipLaunchKernelGGL(beam_reorder_kernel, dim3((unsigned)blocks), dim3(NTP), 0, (hipStream_t)hip_stream, a);
+    if (shared) hipLaunchKernelGGL(beam_reorder_kernel<true>, dim3((unsigned)blocks), dim3(NTP), 0, (hipStream_t)hip_stream, a);
+    else hipLaunchKernelGGL(beam_reorder_kernel<false>, dim3((unsigned)blocks), dim3(NTP), 0, (hipStream_t)hip_stream, a);
     return hipGetLastError() == hipSuccess ? SPD_OK : SPD_EHIP;
+}
+
+extern "C" int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                                   int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
+                                   const int32_t *parents, const int32_t *len, int32_t *table_out, int32_t *err, void *hip_stream) {
+    return reorder(dtype, K, V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride, n_layers, layer_stride, width, parents, len, nullptr, table_out, err, hip_stream);
+}
+
+extern "C" int spd_op_beam_reorder_shared(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                                          int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
+                                          const int32_t *parents, const int32_t *len, const int32_t *shared, int32_t *table_out, int32_t *err, void *hip_stream) {
+    if (!shared && n_seq > 0) return SPD_EINVAL;
+    return reorder(dtype, K, V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride, n_layers, layer_stride, width, parents, len, shared, table_out, err, hip_stream);
 }

@@ -1,7 +1,7 @@
 """What the operators of several sequences over one paged cache refuse and how they cut their work, seen without a GPU (no status below follows a pointer)."""
 import pytest
 
-from test_batch_ops_host import A, APPEND, ATTEND, EINVAL, REORDER, SELECT, call, pkg  # noqa: F401
+from test_batch_ops_host import A, APPEND, ATTEND, BAD_CACHE, EINVAL, REORDER, SELECT, call, pkg  # noqa: F401
 
 
 def over(base, what, size, *others):
@@ -44,3 +44,14 @@ def test_select_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noq
                          + aligned(over(REORDER, "V", 2 * POOL, ("table", TABLE), ("parents", 24), ("len", 24)), 16))
 def test_reorder_refuses_what_it_writes_over_what_it_reads(pkg, what, at):  # noqa: F811
     assert call(pkg, "spd_op_beam_reorder", REORDER, **{what: at}) == EINVAL
+
+
+REORDER_SHARED = {**{k: v for k, v in REORDER.items() if k not in ("table_out", "err", "stream")}, "shared": 7 * A, "table_out": 6 * A, "err": None, "stream": None}
+
+
+@pytest.mark.parametrize("what,at", BAD_CACHE + [("width", 0), ("width", 17), ("width", 4), ("n_layers", 0), ("layer_stride", 40 * 2 * 16 * 64 - 8), ("parents", None), ("len", None),
+                                                 ("table_out", None), ("table_out", 3 * A), ("shared", None)]
+                         + over(REORDER_SHARED, "table_out", TABLE, ("parents", 24), ("shared", 8)) + aligned(over(REORDER_SHARED, "K", 2 * POOL, ("shared", 8)), 16))
+def test_reorder_with_shared_positions_refuses(pkg, what, at):  # noqa: F811
+    assert call(pkg, "spd_op_beam_reorder_shared", REORDER_SHARED, **{what: at}) == EINVAL
+    assert call(pkg, "spd_op_beam_reorder_shared", REORDER_SHARED, n_seq=0, shared=None) == 0

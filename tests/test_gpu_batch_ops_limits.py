@@ -1,10 +1,12 @@
 """The operators of several sequences over one paged cache at the limits of what their arguments may hold."""
+import itertools
+import math
 
 import pytest
 import torch
 
 import batch_reference as R
-from test_gpu_batch_ops import attend, attention_case, close, gen, ints
+from test_gpu_batch_ops import Beams, P, attend, attention_case, close, gen, ints, reorder_case, say
 
 pytestmark = pytest.mark.gpu
 
@@ -120,3 +122,117 @@ def test_attention_uses_all_bits_of_its_queries(dtype, heads, width, bound):
     if dtype != "fp32":                                      # what the bound has to see: queries of fewer bits, in the oracle
         cut = (q.view(torch.int32) & ~(0xFF if dtype == "bf16" else 0x1FFF)).view(torch.float32)
         assert (R.attention(cut, *rest, width) - want).abs().max() > 8e-6
+
+
+def positions(K, V, table, shared, length, width):
+    """What each sequence's positions hold, [layers, kv, positions, 2 d] per sequence, read as the attention reads them."""
+    page = K.shape[3]
+    rows = []
+    for s, n in enumerate(length.tolist()):
+        p = torch.arange(n)
+        at = torch.where(p < shared[s // width], table[s - s % width, p // page], table[s, p // page]).long()
+        assert ((at >= 0) & (at < K.shape[1])).all()
+        rows.append(torch.cat([K[:, at, :, p % page], V[:, at, :, p % page]], -1))
+    return rows
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "fp32"])
+@pytest.mark.parametrize("page,shared,length", [(16, 37, 45), (16, 37, 61), (16, 37, 37), (16, 32, 40), (4, 3, 2), (8, 0, 9), (16, 37, 48), (4, 6, 7), (64, 33, 100)])
+def test_reorder_keeps_shared_positions_that_the_first_row_alone_holds(dtype, page, shared, length):
+    """All choices of three parents, on caches filled as for the attention: pages of NaN but for what counts, entries that no call needs out of range.  Every beam holds
+    its parent's positions, as the attention reads them, bit by bit; three times in a row, with the parents of another group each time."""
+    say("reorder", dtype, page, shared, length)
+    choices = list(itertools.product(range(3), repeat=3))
+    n = 3 * len(choices)
+    cases = [attention_case(dtype, 1, 2, 16, page, [shared] * len(choices), [length] * n, 3, seed=31 + l) for l in range(2)]
+    table = cases[0][3].clone()
+    order = torch.randperm(n * table.shape[1], generator=gen(31)).int().view(n, -1)     # (attention_case's own pages: rows have one to write on, filled or not)
+    e = length // page
+    K, V = (torch.full((2, n * table.shape[1], 2, page, 16), math.nan).to(R.TORCH[dtype]) for _ in range(2))
+    for s in range(n):
+        for i in range(table.shape[1]):
+            if table[s, i] >= 0:
+                for l, c in enumerate(cases):
+                    K[l, order[s, i]], V[l, order[s, i]] = c[1][cases[l][3][s, i]], c[2][cases[l][3][s, i]]
+                table[s, i] = order[s, i]
+            elif i >= min(e, min(shared, length) // page):
+                table[s, i] = order[s, i]
+    sh, ln = ints([shared] * len(choices)), ints([length] * n)
+    Kd, Vd, td = K.cuda(), V.cuda(), table.cuda()
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for step in range(3):
+        before = positions(Kd.cpu(), Vd.cpu(), td.cpu(), sh, ln, 3)
+        parents = ints(choices[step:] + choices[:step])
+        out = torch.full_like(td, -9)
+        P().spd_op_beam_reorder(dtype, Kd, Vd, td, parents.cuda(), ln.cuda(), out, 3, err=err, shared=sh.cuda())
+        assert int(err) == 0
+        after = positions(Kd.cpu(), Vd.cpu(), out.cpu(), sh, ln, 3)
+        for s in range(n):
+            was = before[s - s % 3 + int(parents[s // 3, s % 3])]
+            assert not was.isnan().any() and torch.equal(after[s], was), (step, s, parents[s // 3].tolist())
+        pages = out.cpu()[:, e:].sort().values if length < page * out.shape[1] else out.cpu()[:, :0]
+        assert len(set(pages.flatten().tolist())) == pages.numel()           # every beam has pages of its own to go on with
+        td = out
+
+
+def test_reorder_leaves_a_group_whose_shared_positions_make_no_sense_as_it_was():
+    K, V, table, length = reorder_case("fp16", 2, 2, 64, 16, [37, 40], 3, seed=32)
+    parents = ints([[2, 2, 0], [0, 1, 1]])
+    a, b, c = R.reorder(K, V, table, ints([[0, 1, 2], [0, 1, 1]]), length, 3)
+    for shared, entry, page in ((-1, None, 0), (16 * table.shape[1] + 1, None, 0), (20, (0, 1), -1), (20, (2, 1), len(K[0])), (35, (0, 2), 1 << 30), (35, (2, 2), -7)):
+        bad, want = table.clone(), c.clone()
+        if entry:
+            bad[entry] = page
+            want[entry] = page
+        Kd, Vd, out, err = K.cuda(), V.cuda(), torch.full_like(table, -9).cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        P().spd_op_beam_reorder("fp16", Kd, Vd, bad.cuda(), parents.cuda(), length.cuda(), out, 3, err=err, shared=ints([shared, 0]).cuda())
+        assert torch.equal(out.cpu(), want) and torch.equal(Kd.cpu(), a) and torch.equal(Vd.cpu(), b) and int(err) == 1, (shared, entry)
+
+
+class FirstRows(Beams):
+    """Prompts in each group's first row alone; the other rows' pages hold NaN there, and their entries in front of the page where a prompt ends are no pages."""
+
+    def start(self):
+        W = self.width
+        for s in range(len(self.prompts) * W):
+            if s % W:
+                self.table[s, :len(self.prompts[s // W]) // self.page] = -1
+        self.shared = ints([len(p) for p in self.prompts]).cuda()
+        prompts, self.prompts = self.prompts, [p if s % W == 0 else [] for p in self.prompts for s in range(W)]
+        self.width = 1                                          # (each row by itself, those without a prompt as padding)
+        n, logits = len(self.prompts), None
+        for t in range(max(map(len, self.prompts))):
+            on = [t < len(p) for p in self.prompts]
+            tokens = torch.tensor([p[t] if o else 0 for p, o in zip(self.prompts, on)]).cuda()
+            length = ints([t + 1 if o else 0 for o in on]).cuda()
+            z = self.forward(tokens, ints([s if o else -1 for s, o in enumerate(on)]).cuda(), ints([t] * n).cuda(), 1, self.table, torch.zeros(n, dtype=torch.int32, device="cuda"), length, 0,
+                             t + 1)
+            logits = z if logits is None else torch.where((length > 0)[:, None], z, logits)
+        self.prompts, self.width = prompts, W
+        self.length = ints([len(prompts[s // W]) for s in range(n)]).cuda()
+        return logits.view(len(prompts), W, -1)
+
+
+@pytest.mark.parametrize("dtype,bound", [("fp32", 1e-4), ("fp16", 5e-3), ("bf16", 4e-2)])
+def test_a_beam_search_over_prompts_that_the_first_rows_hold(dtype, bound):
+    """As test_a_beam_search, its bounds too, with prompts that end inside pages, at their ends and in front of the first page's."""
+    B = FirstRows(dtype, [[5, 17, 80, 3, 9, 2], [11], [1, 2, 3, 4, 5, 6, 7, 8]], seed=11)
+    G, W = len(B.prompts), B.width
+    z = B.start()[:, :1]
+    scores, ended = torch.zeros(G, 1, device="cuda"), torch.zeros(G, 1, dtype=torch.int32, device="cuda")
+    moved = 0
+    for step in range(9):
+        for g, texts in enumerate(B.texts):
+            for b, text in enumerate(texts):
+                want = B.logits64(text)
+                off = (z[g, b].cpu().double() - want).abs().max() / want.abs().max()
+                assert off < bound, (step, g, b, off)
+        s, t, p, e = (torch.empty(G, W, dtype=x, device="cuda") for x in (torch.float32, torch.int32, torch.int32, torch.int32))
+        P().spd_op_beam_select("fp32", z, scores, s, t, p, ended=ended, end_token=13, out_ended=e)
+        B.texts = [[B.texts[g][b] + [v] for b, v in zip(p[g].tolist(), t[g].tolist())] for g in range(G)]
+        moved += int((p[:, 0] != 0).sum())
+        P().spd_op_beam_reorder(dtype, B.K, B.V, B.table, p, B.length, B.spare, W, err=B.err, shared=B.shared)
+        B.table, B.spare, scores, ended = B.spare, B.table, s, e
+        pos, B.length = B.length, B.length + 1
+        z = B.forward(t.flatten(), ints(range(G * W)).cuda(), pos, W, B.table, B.shared, B.length, 8, 20).view(G, W, -1)
+    assert int(B.err) == 0 and moved > 0                        # (a first beam that goes on from another row)
