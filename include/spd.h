@@ -429,6 +429,12 @@ int spd_test_prefill_attention(int32_t kv_dtype, const float *q, const void *K, 
                                int32_t n_tokens, int32_t pos, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t cap_ctx,
                                void *hip_stream);
 
+/* ---- test hook of the attention over a paged cache ----
+ * How spd_op_attention_shared cuts a call (host only, no GPU): out[7] = chunks of the shared positions, positions of one, chunks of each sequence's own, query rows of a
+ * shared block, shared blocks in all, and where such a block's waves share out rows, keys of a stage and the stages that it holds (0, 0 elsewhere). */
+int spd_test_attention_shared_cut(int32_t dtype, int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared, int32_t max_own,
+                                  int32_t *out);
+
 const char *spd_last_error(const spd_ctx *ctx);
 const char *spd_strerror(int status);
 

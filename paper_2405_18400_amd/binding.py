@@ -96,6 +96,7 @@ def lib():
             "spd_test_state_status": [vp, sz],
             "spd_test_poke_err": [vp, i32],
             "spd_test_ngram_table": [C.POINTER(SpdNgramHostTables), i32, vp, sz, C.POINTER(i32)],
+            "spd_test_attention_shared_cut": [i32] * 8 + [vp],
             "spd_test_prefill_cut": [C.POINTER(SpdModelCfg), i32, i32, i32, vp],
             "spd_test_prefill_attention": [i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp],
             "spd_test_force_prefill_cut": [vp, i32, i32, i32, i32, vp],
@@ -643,6 +644,15 @@ def spd_test_prefill_cut(cfg: SpdModelCfg, num_cu: int, n_tokens: int, product: 
     if rc:
         raise SpdError(rc, "spd_test_prefill_cut")
     return int(out[0]), int(out[1]), int(out[2]), bool(out[3])
+
+
+def spd_test_attention_shared_cut(dtype: str, n_seq: int, width: int, n_heads: int, n_kv_heads: int, d_head: int, max_shared: int, max_own: int):
+    """-> (shared chunks, positions of one, own chunks, rows of a shared block, shared blocks, keys of a stage, stages)."""
+    out = np.zeros(7, np.int32)
+    rc = lib().spd_test_attention_shared_cut(SPD_DTYPE[dtype], n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own, _np_ptr(out))
+    if rc:
+        raise SpdError(rc, "spd_test_attention_shared_cut")
+    return tuple(int(x) for x in out)
 
 
 def spd_test_prefill_attention(kv_dtype: str, q, K, V, pos: int):

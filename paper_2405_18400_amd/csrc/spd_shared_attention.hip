@@ -978,17 +978,20 @@ __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs 
 struct Cut { int shared_chunks, shared_chunk, own_chunks; };
 constexpr int WHOLE = 512;                       // positions up to which a sequence's block takes shared and own ones in one go
 constexpr int CUS = 256, LONG = 768;
-// Rows of a shared block.
-int tile_rows(int dtype, int d_head, int rows) {
-    if (rows <= ROWS || (dtype == SPD_DTYPE_FP32 && d_head > 128)) return ROWS;
-    if (dtype == SPD_DTYPE_FP32 || d_head < 64) return 2 * ROWS;
+// Rows of a shared block; from 4 * ROWS on its waves share out rows, not keys.  (A sequence on its own may have a single chunk, whose block writes the output:
+// the kernel whose waves share out keys.)
+int tile_rows(int dtype, int d_head, int width, int group) {
+    const int rows = width * group;
+    const bool many = dtype != SPD_DTYPE_FP32 && d_head >= 64;
+    if (rows <= ROWS || (dtype == SPD_DTYPE_FP32 && d_head > 128) || (many && width == 1)) return ROWS;
+    if (!many) return 2 * ROWS;
     return rows > 4 * ROWS && d_head <= 128 && dtype == SPD_DTYPE_FP16 ? 8 * ROWS : 4 * ROWS;
 }
 Cut cut_for(int dtype, int n_seq, int width, int n_heads, int n_kv_heads, int d_head, int max_shared, int max_own) {
     const int groups = n_seq / width, group = n_heads / n_kv_heads;
     if (width > 1 && (long long)max_shared + max_own <= WHOLE) return Cut{0, 0, 1};
     const long long shared = std::max<long long>(1, width == 1 ? (long long)max_shared + max_own : max_shared);
-    const long long units = (long long)groups * n_kv_heads * ((width * group - 1) / tile_rows(dtype, d_head, width * group) + 1), own_units = (long long)n_seq * n_kv_heads;
+    const long long units = (long long)groups * n_kv_heads * ((width * group - 1) / tile_rows(dtype, d_head, width, group) + 1), own_units = (long long)n_seq * n_kv_heads;
     const auto cut = [&](long long positions, long long of, long long blocks) {
         const long long n = std::max<long long>(1, std::min(blocks / of, (positions + NWS * KEYS - 1) / (NWS * KEYS)));
         const long long chunk = ((positions + n - 1) / n + KEYS - 1) / KEYS * KEYS;
@@ -1039,11 +1042,9 @@ hipError_t launch_tiles(hipStream_t s, SharedAttnArgs a) {
 
 template <typename KT, int DH>
 hipError_t launch_rows(hipStream_t s, const SharedAttnArgs &a, int dtype) {
-    const int tile = tile_rows(dtype, a.c.d_head, a.shared_chunks ? a.width * (a.n_heads / a.c.n_kv_heads) : 1);
+    const int tile = a.shared_chunks ? tile_rows(dtype, a.c.d_head, a.width, a.n_heads / a.c.n_kv_heads) : ROWS;
     if (tile == ROWS) return launch_tiles<KT, DH, ROWS, false>(s, a);
     if constexpr (sizeof(KT) == 2 && DH >= 64) {
-        // (a sequence on its own may have a single chunk, whose block writes the output: the kernel whose waves share out keys)
-        if (a.width == 1) return launch_tiles<KT, DH, ROWS, false>(s, a);
         if constexpr (DH <= 128 && Type<KT>::PARTS == 2)
             if (tile == 8 * ROWS) return launch_tiles<KT, DH, 8 * ROWS, true>(s, a);
         return launch_tiles<KT, DH, 4 * ROWS, true>(s, a);
@@ -1076,6 +1077,22 @@ extern "C" size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t w
     }
     const size_t parts = (size_t)n_seq * n_heads * slots;
     return slots > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 0;
+}
+
+extern "C" int spd_test_attention_shared_cut(int32_t dtype, int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared, int32_t max_own,
+                                             int32_t *out) {
+    if (!out || n_seq <= 0 || width <= 0 || n_seq % width || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_shared < 0 || max_own < 0) return SPD_EINVAL;
+    const Cut c = cut_for(dtype, n_seq, width, n_heads, n_kv_heads, d_head, max_shared, max_own);
+    const int group = n_heads / n_kv_heads, tile = c.shared_chunks ? tile_rows(dtype, d_head, width, group) : ROWS;
+    out[0] = c.shared_chunks; out[1] = c.shared_chunk; out[2] = c.own_chunks; out[3] = tile;
+    out[4] = c.shared_chunks * (n_seq / width) * n_kv_heads * ((width * group + tile - 1) / tile);
+    out[5] = out[6] = 0;
+    if (tile >= 4 * ROWS) {
+        const bool two = tile == 8 * ROWS;
+        out[5] = d_head == 64 ? (two ? Stage<64, 2>::SK : Stage<64, 1>::SK) : d_head == 128 ? (two ? Stage<128, 2>::SK : Stage<128, 1>::SK) : Stage<256, 1>::SK;
+        out[6] = d_head == 64 ? (two ? Stage<64, 2>::ST : Stage<64, 1>::ST) : d_head == 128 ? (two ? Stage<128, 2>::ST : Stage<128, 1>::ST) : Stage<256, 1>::ST;
+    }
+    return SPD_OK;
 }
 
 extern "C" int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,

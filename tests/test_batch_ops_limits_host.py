@@ -55,3 +55,18 @@ REORDER_SHARED = {**{k: v for k, v in REORDER.items() if k not in ("table_out", 
 def test_reorder_with_shared_positions_refuses(pkg, what, at):  # noqa: F811
     assert call(pkg, "spd_op_beam_reorder_shared", REORDER_SHARED, **{what: at}) == EINVAL
     assert call(pkg, "spd_op_beam_reorder_shared", REORDER_SHARED, n_seq=0, shared=None) == 0
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+def test_attention_plans_the_blocks_that_it_launches(pkg, dtype, d):  # noqa: F811
+    """Shared blocks: two per compute unit at most each a chunk of 128 positions or more (and 4096 at most), also for a sequence on its own with more query heads per
+    key/value head than a tile has rows."""
+    for group in (1, 4, 16, 17, 34, 64):
+        for width in (1, 2, 8, 33):
+            for positions in (600, 5000, 40_000):
+                chunks, chunk, own, rows, blocks, keys, stages = pkg.spd_test_attention_shared_cut(dtype, 2 * width, width, 2 * group, 2, d, positions, 100)
+                tiles = -(-width * group // rows)
+                assert blocks == chunks * 4 * tiles and chunks * chunk >= positions + 100 * (width == 1)
+                assert chunk == 4096 or (blocks <= 512 + 4 * tiles and (chunk <= 128 or blocks >= 128)), (group, width, positions, blocks)
+                assert (keys > 0) == (rows >= 64) and (rows < 64 or width > 1)
