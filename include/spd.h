@@ -435,6 +435,10 @@ int spd_test_prefill_attention(int32_t kv_dtype, const float *q, const void *K, 
 int spd_test_attention_shared_cut(int32_t dtype, int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared, int32_t max_own,
                                   int32_t *out);
 
+/* ---- test hook of the selection ----
+ * How spd_op_beam_select cuts a call (host only, no GPU): out[2] = logits per lane of a slice (0: one launch, no slices) and slices of a row. */
+int spd_test_beam_select_cut(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab, int32_t *out);
+
 const char *spd_last_error(const spd_ctx *ctx);
 const char *spd_strerror(int status);
 

@@ -97,6 +97,7 @@ def lib():
             "spd_test_poke_err": [vp, i32],
             "spd_test_ngram_table": [C.POINTER(SpdNgramHostTables), i32, vp, sz, C.POINTER(i32)],
             "spd_test_attention_shared_cut": [i32] * 8 + [vp],
+            "spd_test_beam_select_cut": [i32] * 4 + [vp],
             "spd_test_prefill_cut": [C.POINTER(SpdModelCfg), i32, i32, i32, vp],
             "spd_test_prefill_attention": [i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp],
             "spd_test_force_prefill_cut": [vp, i32, i32, i32, i32, vp],
@@ -653,6 +654,15 @@ def spd_test_attention_shared_cut(dtype: str, n_seq: int, width: int, n_heads: i
     if rc:
         raise SpdError(rc, "spd_test_attention_shared_cut")
     return tuple(int(x) for x in out)
+
+
+def spd_test_beam_select_cut(n_groups: int, n_in: int, n_out: int, vocab: int):
+    """-> (logits per lane of a slice, 0 where there is one launch; slices of a row)."""
+    out = np.zeros(2, np.int32)
+    rc = lib().spd_test_beam_select_cut(n_groups, n_in, n_out, vocab, _np_ptr(out))
+    if rc:
+        raise SpdError(rc, "spd_test_beam_select_cut")
+    return int(out[0]), int(out[1])
 
 
 def spd_test_prefill_attention(kv_dtype: str, q, K, V, pos: int):

@@ -20,9 +20,9 @@ typedef unsigned long long u64;
 constexpr int NTB = 256, NWB = NTB / WAVE;       // slices: threads and waves per block
 constexpr int NTM = 1024;                        // merge: a wave per row
 constexpr int EM = 8;                            // keys per lane and turn there
-// Waves that slices are made longer for: six per SIMD in fp32, three in 16 bits, whose loads bring twice the entries (us, three / six: 128 rows
-// of 50258 in fp32 11.7 / 8.9, 64 of 131072 in bf16 9.7 / 11.0).
-constexpr int WAVES_FP32 = 6600, WAVES_16 = 3300;
+// Waves of the first kernel that the GPU holds at once, for each number of entries per lane: 256 compute units of four SIMDs, by the registers.
+constexpr int CUS = 256;
+constexpr int waves_per_simd(int ne) { return ne <= 16 ? 8 : ne == 32 ? 3 : 2; }
 
 // Order of fp32 numbers as unsigned ones.
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -192,7 +192,7 @@ template <typename LT, int VEC> __device__ __forceinline__ void load_logits(cons
 
 // A wave per slice of 64 NE entries; lane l's vector j holds entries VEC (64 j + l) ...
 template <typename LT, int NE, int VEC>
-__global__ __launch_bounds__(NTB) void beam_slice_kernel(const SelectArgs a) {
+__global__ __launch_bounds__(NTB, waves_per_simd(NE)) void beam_slice_kernel(const SelectArgs a) {
     __shared__ u64 list[NWB][WAVE], best[NWB][SPD_K_MAX];
     const int lane = threadIdx.x & (WAVE - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int part = blockIdx.x * NWB + w, row = part / a.slices, slice = part - row * a.slices;
@@ -434,11 +434,23 @@ __global__ __launch_bounds__(NTM) void beam_small_kernel(const SelectArgs a) {
     rank_group(a, s, g);
 }
 
-// Entries per lane of a slice: as few as that many waves allow (a wave's first word comes after one trip to memory whatever it holds).
-int entries_per_lane(long long rows, int vocab, int waves) {
-    for (int ne = 8; ne < 64; ne *= 2)
-        if (rows * ((vocab + WAVE * ne - 1) / (WAVE * ne)) <= waves) return ne;
-    return 64;
+// Entries per lane of a slice.  The first kernel takes a round for as many waves as the GPU holds, some 1.5 us and 0.05 per entry; the second a turn for every EM * 64 keys
+// that a row's slices leave, 2 us and, where many of them are kept, more, and 10 us more where more than a wave's worth of keys come from so few slices that a
+// lane holds half a slice's and the first halves alone are fewer than n_out.  So, counted in entries, rounds * (32 + entries) + 96 * turns + 200 there, and the least of it.
+// Measured over 160 calls of 1 to 512 rows of 5000 to 256000, fp32 and bf16, n_out 4 to 16: on (geometric) average 1.3% over each call's best, 12% under a
+// bound on the waves alone (of single calls 35% less to 14% more); 16 or 64 in place of 32, 32 or 64 in place of 96, 100 or 300 in place of 200 are within half a percent.
+// us at 8 / 16 / 32 / 64 entries: 128 rows of 32000 in fp32 14.0 / 13.3 / 13.5 / 14.5, 16 of 131072 17.5 / 13.5 / 11.5 / 12.3, 512 of 16000 in bf16
+// 17.9 / 15.4 / 19.4 / 21.7; 64 of 5000, 16 of each kept, 26 / 27 / 14.5 / 15.8.
+int entries_per_lane(long long rows, int vocab, int n_out) {
+    int best = 0;
+    long long least = 0;
+    for (int ne = 8; ne <= 64; ne *= 2) {
+        const long long slices = (vocab + WAVE * ne - 1) / (WAVE * ne), places = CUS * 4 * waves_per_simd(ne), keys = slices * n_out;
+        const bool halves = n_out > EM && keys > WAVE && slices <= n_out;
+        const long long cost = (rows * slices + places - 1) / places * (32 + ne) + (keys + EM * WAVE - 1) / (EM * WAVE) * 96 + (halves ? 200 : 0);
+        if (best == 0 || cost < least) { best = ne; least = cost; }
+    }
+    return best;
 }
 
 template <typename LT, int VEC>
@@ -472,9 +484,16 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 extern "C" size_t spd_op_beam_select_scratch_bytes(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab) {
     if (n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= SMALL) return 0;
     const long long rows = (long long)n_groups * n_in;
-    const int slice = WAVE * entries_per_lane(rows, vocab, WAVES_FP32);       // (the shorter slices, whatever the type)
+    const int slice = WAVE * entries_per_lane(rows, vocab, n_out);
     const size_t parts = (size_t)rows * (((size_t)vocab + slice - 1) / slice);
     return up256(parts * n_out * 8) + 2 * up256(parts * 4);
+}
+
+extern "C" int spd_test_beam_select_cut(int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab, int32_t *out) {
+    if (!out || n_groups <= 0 || n_in <= 0 || n_out <= 0 || vocab <= 0) return SPD_EINVAL;
+    out[0] = vocab <= SMALL ? 0 : entries_per_lane((long long)n_groups * n_in, vocab, n_out);
+    out[1] = vocab <= SMALL ? 1 : (vocab + WAVE * out[0] - 1) / (WAVE * out[0]);
+    return SPD_OK;
 }
 
 extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row_stride, int32_t n_groups, int32_t n_in, int32_t n_out, int32_t vocab,
@@ -500,7 +519,7 @@ extern "C" int spd_op_beam_select(int32_t dtype, const void *logits, int64_t row
             if (spdk::over_any(outs[i], {outs[j]})) return SPD_EINVAL;
     }
     if (spdk::over_any(sw, {sz, ss, sd})) return SPD_EINVAL;
-    const int ne = entries_per_lane((long long)n_groups * n_in, vocab, dtype == SPD_DTYPE_FP32 ? WAVES_FP32 : WAVES_16), slice = WAVE * ne;
+    const int ne = entries_per_lane((long long)n_groups * n_in, vocab, n_out), slice = WAVE * ne;
     SelectArgs a{logits, row_stride, n_groups, n_in, n_out, vocab, scores, ended, end_token, 1.4426950408889634f / tau, 1.0 / (double)tau, out_scores, out_tokens, out_parents, out_ended,
                  (vocab + slice - 1) / slice, nullptr, nullptr, nullptr};
     const long long parts = (long long)n_groups * n_in * a.slices;

@@ -70,3 +70,31 @@ def test_attention_plans_the_blocks_that_it_launches(pkg, dtype, d):  # noqa: F8
                 assert blocks == chunks * 4 * tiles and chunks * chunk >= positions + 100 * (width == 1)
                 assert chunk == 4096 or (blocks <= 512 + 4 * tiles and (chunk <= 128 or blocks >= 128)), (group, width, positions, blocks)
                 assert (keys > 0) == (rows >= 64) and (rows < 64 or width > 1)
+
+
+# Selections of 16 (groups, beams, vocabulary) and the logits per lane that each takes: every instance of the first kernel, rows on the grid of 16 bytes and off it, last slices
+# that are not full.  (The GPU tests run these.)
+SELECTIONS = [((16, 16, 9001), 8), ((1, 16, 16_002), 8), ((16, 16, 50_258), 16), ((40, 16, 33_003), 16), ((1, 16, 50_000), 32), ((4, 16, 5003), 32), ((4, 16, 131_072), 64),
+              ((4, 16, 131_070), 64), ((2, 16, 100_003), 64)]
+
+
+@pytest.mark.parametrize("shape,entries", SELECTIONS)
+def test_select_slices(pkg, shape, entries):  # noqa: F811
+    assert pkg.spd_test_beam_select_cut(*shape[:2], 16, shape[2]) == (entries, -(-shape[2] // (64 * entries)))
+
+
+def test_select_slices_follow_what_the_gpu_holds(pkg):  # noqa: F811
+    """As many entries per lane as make for the least of rounds of waves and turns of the second kernel; a vocabulary of one launch has no slices."""
+    assert pkg.spd_test_beam_select_cut(3, 2, 4, 4096) == (0, 1)
+    places = {8: 8192, 16: 8192, 32: 3072, 64: 2048}                       # 256 x 4 SIMDs x 8, 8, 3, 2 waves
+
+    def cost(rows, n_out, vocab, ne):
+        slices = -(-vocab // (64 * ne))
+        halves = n_out > 8 and slices * n_out > 64 and slices <= n_out
+        return -(-rows * slices // places[ne]) * (32 + ne) + -(-slices * n_out // 512) * 96 + 200 * halves
+
+    for rows in (1, 7, 64, 200, 3000):
+        for n_out in (1, 5, 16):
+            for vocab in (4097, 10_000, 50_258, 131_072, 1_000_001):
+                entries, slices = pkg.spd_test_beam_select_cut(rows, 1, n_out, vocab)
+                assert slices == -(-vocab // (64 * entries)) and cost(rows, n_out, vocab, entries) == min(cost(rows, n_out, vocab, ne) for ne in places)

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import batch_reference as R
+from test_batch_ops_limits_host import SELECTIONS
 from test_gpu_batch_ops import Beams, P, attend, attention_case, close, gen, ints, reorder_case, say
 
 pytestmark = pytest.mark.gpu
@@ -122,6 +123,31 @@ def test_attention_uses_all_bits_of_its_queries(dtype, heads, width, bound):
     if dtype != "fp32":                                      # what the bound has to see: queries of fewer bits, in the oracle
         cut = (q.view(torch.int32) & ~(0xFF if dtype == "bf16" else 0x1FFF)).view(torch.float32)
         assert (R.attention(cut, *rest, width) - want).abs().max() > 8e-6
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("groups,n_in,vocab", [shape for shape, _ in SELECTIONS])
+def test_select_with_slices_of_every_length(dtype, groups, n_in, vocab):
+    """Ties inside and across slices, a last slice that is not full, in every instance of the first kernel."""
+    say("select", dtype, groups, n_in, vocab)
+    g = gen(vocab + groups)
+    logits = (torch.randn(groups, n_in, vocab, generator=g) * 3).to(R.TORCH[dtype])
+    top = logits[:, :, :512].float().amax(-1, keepdim=True).to(logits.dtype) + 2
+    for at in (0, 511, 513, 1023, 4097, vocab - 1, vocab - 2):              # equal logits here and there, the last entries among them
+        logits[:, ::2, at] = top[:, ::2, 0]
+    logits[0, 1], logits[-1, 2] = 0.5, logits[-1, 0]                        # a row all alike; two equal rows
+    scores = -torch.rand(groups, n_in, generator=g) * 4
+    scores[-1, 2] = scores[-1, 0]
+    few = sorted({0, groups // 2, groups - 1})
+    out = [torch.empty(groups, 16, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)]
+    P().spd_op_beam_select(dtype, logits.cuda(), scores.cuda(), *out, tau=0.9)
+    s, t, p = (x.cpu() for x in out)
+    for i in few:
+        want = R.select(logits[i].float(), scores[i], 16, 0.9)
+        assert t[i].tolist() == [c[1] for c in want] and p[i].tolist() == [c[2] for c in want], i
+        score = torch.tensor([c[0] for c in want], dtype=torch.float64)
+        # as in the test of random logits: the sum of exponentials 1e-6 of itself, arguments of up to 30 / tau rounded at 2^-23
+        assert ((s[i] - score).abs() <= 5e-6 + score.abs() * 2.0 ** -24).all()
 
 
 def positions(K, V, table, shared, length, width):
