@@ -972,12 +972,14 @@ __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs 
 
 // How a call is cut: chunks of shared and of own positions per unit, and the positions of a shared chunk.
 // A block costs 5 us whatever its chunk (three trips to memory before its first product, its results' way back), and each chunk
-// a partial result per row, so short calls take one block per compute unit; where that leaves a block more than LONG positions, two run
-// beside each other and fill each other's waits.  us, one / two blocks per compute unit: 64 rows x 8191 positions x 8 heads 17.8 / 22.2; eight
-// groups of 32 rows x 2001 x 8 38.1 / 41.2; 128 rows x 65537 x 8 93.0 / 87.6.
+// a partial result per row, so a call takes one block per compute unit; where that leaves a block more than LONG positions, two run
+// beside each other and fill each other's waits.  Measured both ways over 299 calls (seven head layouts, the three types, 2 to 64 sequences over 1024 to 65536 shared positions):
+// at 192 to 832 positions of a block two take 13% longer on average, at 1024 5% (from 20% longer to 7% shorter), at 2048 they are even (from 14% shorter, mostly
+// tiles of 128 rows, to 12% longer, mostly where a compute unit holds one block anyway: d_head 256, fp32).  us, one / two: 64 rows x 16384 positions x 8 heads x 128 in fp16
+// 23.8 / 27.7; eight groups of 32 rows x 4096 x 8 37.1 / 44.4, x 8192 66.1 / 68.8; 128 rows x 32768 x 8 56.2 / 55.8, x 65536 98.7 / 86.3.
 struct Cut { int shared_chunks, shared_chunk, own_chunks; };
 constexpr int WHOLE = 512;                       // positions up to which a sequence's block takes shared and own ones in one go
-constexpr int CUS = 256, LONG = 768;
+constexpr int CUS = 256, LONG = 1536;
 // Rows of a shared block; from 4 * ROWS on its waves share out rows, not keys.  (A sequence on its own may have a single chunk, whose block writes the output:
 // the kernel whose waves share out keys.)
 int tile_rows(int dtype, int d_head, int width, int group) {
