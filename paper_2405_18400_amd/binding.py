@@ -448,21 +448,9 @@ def spd_op_attention_static(dtype: str, q, K, V, out, n_ctx: int):
 # ---- several sequences over one prompt, on a paged cache: K, V [pages, n_kv_heads, page_size, d_head], table int32 [n_seq, entries].
 # Nothing here waits for the GPU; `err`, an int32 tensor of one element, is set to 1 by what only the kernels can see (spd.h).
 # A decoding step makes a few such calls per layer, so each looks its arguments over in one expression and names what is wrong
-# only where something is (append / attention / selection / reordering: 15.7 / 13.7 / 13.1 / 8.9 us of host time per call with
-# a check per tensor, 9.1 / 10.2 / 9.7 / 6.4 now).
-def _refuse(where, device, **tensors):
-    """Says what is wrong with tensors given as (tensor, type, shape): they have to be whole, on `device`, and of as many elements (None: not looked at)."""
-    for name, (t, dtype, shape) in tensors.items():
-        if t is None:
-            continue
-        if t.get_device() != device:
-            raise ValueError(f"{where}: {name} is not on the current device")
-        if t.dtype is not dtype:
-            raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
-        if not t.is_contiguous():
-            raise ValueError(f"{where}: {name} is not contiguous")
-        if shape is not None and (t.numel() != math.prod(shape) or (name == "V" and t.shape != shape)):
-            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+# only where something is (append / attention / selection / reordering: 4.8 / 4.2 / 5.0 / 3.5 us of host time in front of a call's
+# launch, 0.2 to 0.3 more with err; with a check per tensor 2.1 to 2.6 us more).
+_INT32 = 2 ** 31 - 1      # (ctypes cuts larger numbers off without a word)
 
 
 def _kv_type(where, torch, dtype):
@@ -499,7 +487,7 @@ def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: flo
     if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n
             and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
             and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
-            and err is None):
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
         _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), err=(err, i32, (1,)))
     if k.shape != (n, n_kv, d) or v.shape != (n, n_kv, d):
         raise ValueError(f"{where}: k and v have to be [{n}, {n_kv}, {d}]")
@@ -535,11 +523,14 @@ def spd_op_attention_shared(dtype: str, q, K, V, table, shared, length, out, wid
     if width < 1 or n_seq % width:
         raise ValueError(f"{where}: {n_seq} sequences are no groups of {width}")
     groups = n_seq // width
+    if max_shared > _INT32 or max_own > _INT32:
+        raise ValueError(f"{where}: max_shared or max_own is no 32-bit number")
     if not (q.dtype is f32 and out.dtype is f32 and K.dtype is kv and V.dtype is kv and table.dtype is i32 and shared.dtype is i32 and length.dtype is i32 and q_d == d
             and out.numel() == q.numel() and V.shape == shape and table.numel() == n_seq * entries and shared.numel() == groups and length.numel() == n_seq
             and q.is_contiguous() and out.is_contiguous() and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and shared.is_contiguous()
             and length.is_contiguous() and q.get_device() == device and out.get_device() == device and K.get_device() == device and V.get_device() == device
-            and table.get_device() == device and shared.get_device() == device and length.get_device() == device and err is None):
+            and table.get_device() == device and shared.get_device() == device and length.get_device() == device
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
         _refuse(where, device, q=(q, f32, (n_seq, heads, d)), K=(K, kv, None), V=(V, kv, shape), table=(table, i32, (n_seq, entries)), shared=(shared, i32, (groups,)),
                 length=(length, i32, (n_seq,)), out=(out, f32, (n_seq, heads, d)), err=(err, i32, (1,)))
     L = lib()
@@ -561,6 +552,8 @@ def spd_op_beam_select(dtype: str, logits, scores, out_scores, out_tokens, out_p
     groups, n_in, vocab = logits.shape
     n_out = out_scores.shape[-1]
     n = groups * n_out
+    if not -_INT32 <= end_token <= _INT32:
+        raise ValueError(f"{where}: end_token is no 32-bit number")
     if logits.dtype is not kind:
         raise ValueError(f"{where}: logits are {logits.dtype}, not {dtype}")
     of_group, of_row, of_entry = logits.stride()
@@ -595,6 +588,8 @@ def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, wid
     kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
     shape, rows = K.shape, table.shape
     n_pages, n_kv, page_size, d = shape[-4:]
+    if len(shape) > 5:
+        raise ValueError(f"{where}: K has shape {tuple(shape)}, not [(layers,) pages, heads, page size, d_head]")
     layers = shape[0] if len(shape) == 5 else 1
     n_seq, entries = rows
     if width < 1 or n_seq % width:
@@ -604,7 +599,8 @@ def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, wid
             and parents.numel() == n_seq and length.numel() == n_seq and table_out.numel() == n_seq * entries and K.is_contiguous() and V.is_contiguous() and table.is_contiguous()
             and parents.is_contiguous() and length.is_contiguous() and table_out.is_contiguous() and K.get_device() == device and V.get_device() == device
             and table.get_device() == device and parents.get_device() == device and length.get_device() == device and table_out.get_device() == device
-            and shared is None and err is None):
+            and (shared is None or (shared.dtype is i32 and shared.numel() == groups[0] and shared.is_contiguous() and shared.get_device() == device))
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
         _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), parents=(parents, i32, groups), length=(length, i32, (n_seq,)),
                 table_out=(table_out, i32, rows), shared=(shared, i32, groups[:1]), err=(err, i32, (1,)))
     name, of_group = (where, ()) if shared is None else (where + "_shared", (shared.data_ptr(),))

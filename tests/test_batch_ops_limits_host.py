@@ -98,3 +98,64 @@ def test_select_slices_follow_what_the_gpu_holds(pkg):  # noqa: F811
             for vocab in (4097, 10_000, 50_258, 131_072, 1_000_001):
                 entries, slices = pkg.spd_test_beam_select_cut(rows, 1, n_out, vocab)
                 assert slices == -(-vocab // (64 * entries)) and cost(rows, n_out, vocab, entries) == min(cost(rows, n_out, vocab, ne) for ne in places)
+
+
+class Enqueued(Exception):
+    pass
+
+
+def test_python_looks_arguments_over_once_with_err_as_without(pkg, monkeypatch):  # noqa: F811
+    """A good call reaches the library without the check of each tensor that says what is wrong with one; a bad err or shared is still refused."""
+    import torch
+
+    from paper_2405_18400_amd import binding
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda device=None: None)
+
+    class Library:
+        spd_op_attention_shared_scratch_bytes = spd_op_beam_select_scratch_bytes = staticmethod(lambda *a: 0)
+
+        def __getattr__(self, name):
+            def enqueue(*args):
+                raise Enqueued(name)
+            return enqueue
+
+    monkeypatch.setattr(binding, "lib", Library)
+    refused = []
+    says = binding._refuse
+    monkeypatch.setattr(binding, "_refuse", lambda *a, **k: (refused.append(a), says(*a, **k)))
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    K, V, q, k = torch.zeros(4, 2, 8, 16), torch.zeros(4, 2, 8, 16), torch.zeros(4, 2, 16), torch.zeros(3, 2, 16)
+    calls = [lambda **c: pkg.spd_op_append_paged("fp32", K, V, i(2, 2), k, k, i(3), i(3), 1e4, **c),
+             lambda **c: pkg.spd_op_attention_shared("fp32", q, K, V, i(4, 2), i(2), i(4), torch.empty_like(q), 2, 3, 3, **c),
+             lambda **c: pkg.spd_op_beam_reorder("fp32", K, V, i(4, 2), i(2, 2), i(4), i(4, 2), 2, **c)]
+    for f in calls:
+        for good in ({}, {"err": i(1)}):
+            with pytest.raises(Enqueued):
+                f(**good)
+        assert not refused
+        for bad in (i(2), i(1).long(), torch.zeros(1)):
+            with pytest.raises(ValueError):
+                f(err=bad)
+        refused.clear()
+    with pytest.raises(Enqueued, match="spd_op_beam_reorder_shared"):
+        calls[2](shared=i(2), err=i(1))
+    assert not refused
+    for bad in (i(3), i(2).long(), torch.zeros(4, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            calls[2](shared=bad)
+
+
+def test_python_refuses_numbers_and_pools_that_would_be_cut_off(pkg, monkeypatch):  # noqa: F811
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    K, V, q = torch.zeros(4, 2, 8, 16), torch.zeros(4, 2, 8, 16), torch.zeros(4, 2, 16)
+    for bounds in ((1 << 32, 3), (3, 1 << 31), ((1 << 32) + 3, 3)):
+        with pytest.raises(ValueError):
+            pkg.spd_op_attention_shared("fp32", q, K, V, i(4, 2), i(2), i(4), torch.empty_like(q), 2, *bounds)
+    for end in (1 << 32, (1 << 32) + 2, -(1 << 32)):
+        with pytest.raises(ValueError):
+            pkg.spd_op_beam_select("fp32", torch.zeros(2, 3, 50), torch.zeros(2, 3), torch.zeros(2, 4), i(2, 4), i(2, 4), ended=i(2, 3), end_token=end)
+    with pytest.raises(ValueError):
+        pkg.spd_op_beam_reorder("fp32", K[None, None], V[None, None], i(4, 2), i(2, 2), i(4), i(4, 2), 2)
