@@ -450,6 +450,21 @@ def spd_op_attention_static(dtype: str, q, K, V, out, n_ctx: int):
 # A decoding step makes a few such calls per layer, so each looks its arguments over in one expression and names what is wrong
 # only where something is (append / attention / selection / reordering: 4.8 / 4.2 / 5.0 / 3.5 us of host time in front of a call's
 # launch, 0.2 to 0.3 more with err; with a check per tensor 2.1 to 2.6 us more).
+def _refuse(where, device, **tensors):
+    """Says what is wrong with tensors given as (tensor, type, shape): they have to be whole, on `device`, and of as many elements (None: not looked at)."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.get_device() != device:
+            raise ValueError(f"{where}: {name} is not on the current device")
+        if t.dtype is not dtype:
+            raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{where}: {name} is not contiguous")
+        if shape is not None and (t.numel() != math.prod(shape) or (name == "V" and t.shape != shape)):
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+
+
 _INT32 = 2 ** 31 - 1      # (ctypes cuts larger numbers off without a word)
 
 
