@@ -159,3 +159,21 @@ def test_python_refuses_numbers_and_pools_that_would_be_cut_off(pkg, monkeypatch
             pkg.spd_op_beam_select("fp32", torch.zeros(2, 3, 50), torch.zeros(2, 3), torch.zeros(2, 4), i(2, 4), i(2, 4), ended=i(2, 3), end_token=end)
     with pytest.raises(ValueError):
         pkg.spd_op_beam_reorder("fp32", K[None, None], V[None, None], i(4, 2), i(2, 2), i(4), i(4, 2), 2)
+
+
+# Calls whose shared blocks share out rows and go through their stages in LDS more than twice over: (dtype, heads, kv, d_head, page, groups, width, shared, own), then keys of a stage,
+# stages and rows of a block.  (The GPU tests run these.)
+RINGS = [(("fp16", 16, 2, 64, 16, 16, 4, 6001, 40), (64, 4, 64)), (("bf16", 16, 2, 64, 16, 16, 10, 6001, 40), (64, 4, 64)), (("fp16", 16, 2, 64, 16, 16, 10, 6001, 40), (64, 4, 128)),
+         (("fp16", 8, 2, 128, 32, 8, 5, 6007, 33), (64, 2, 64)), (("bf16", 32, 2, 128, 16, 8, 6, 5003, 33), (64, 2, 64)), (("fp16", 32, 2, 128, 16, 8, 6, 5003, 33), (32, 4, 128)),
+         (("fp16", 8, 2, 256, 16, 8, 5, 4100, 9), (32, 3, 64)), (("bf16", 16, 1, 256, 8, 8, 5, 9001, 9), (32, 3, 64)),
+         (("fp16", 32, 4, 64, 4, 16, 3, 5003, 21), (64, 4, 64)),            # more page numbers of a chunk than a block has threads
+         (("fp16", 16, 2, 128, 16, 8, 17, 5001, 33), (32, 4, 128))]         # 136 rows: a second tile of eight
+
+
+@pytest.mark.parametrize("case,cut", RINGS)
+def test_rings_go_round(pkg, case, cut):  # noqa: F811
+    dtype, heads, kv, d, page, groups, width, shared, own = case
+    chunks, chunk, _, rows, _, keys, stages = pkg.spd_test_attention_shared_cut(dtype, groups * width, width, heads, kv, d, shared, own)
+    assert (keys, stages, rows) == cut and chunks > 1 and chunk > 2 * stages * keys
+    if page == 4:
+        assert chunk // page > 256

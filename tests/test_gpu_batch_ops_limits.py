@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import batch_reference as R
-from test_batch_ops_limits_host import SELECTIONS
+from test_batch_ops_limits_host import RINGS, SELECTIONS
 from test_gpu_batch_ops import Beams, P, attend, attention_case, close, gen, ints, reorder_case, say
 
 pytestmark = pytest.mark.gpu
@@ -262,3 +262,58 @@ def test_a_beam_search_over_prompts_that_the_first_rows_hold(dtype, bound):
         pos, B.length = B.length, B.length + 1
         z = B.forward(t.flatten(), ints(range(G * W)).cuda(), pos, W, B.table, B.shared, B.length, 8, 20).view(G, W, -1)
     assert int(B.err) == 0 and moved > 0                        # (a first beam that goes on from another row)
+
+
+def on_gpu(dtype, heads, kv, d, page, groups, width, shared, own, seed):
+    """A larger case, made on the GPU: every row has pages of its own in random order, those of shared positions count in a group's first row alone.  Lengths behind the shared
+    positions, at their end, inside them and none."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = groups * width
+    shareds = [shared - 3 * i for i in range(groups)]
+    lengths = [shareds[s // width] + own - s % (own + 1) for s in range(n)]
+    lengths[1], lengths[width], lengths[-1] = shareds[0] - 5, shareds[1], 0
+    entries = (max(max(lengths), shared) - 1) // page + 1
+    table = torch.randperm(n * entries, generator=g, device="cuda").int().view(n, entries)
+    K, V = (torch.empty(n * entries, kv, page, d, device="cuda", dtype=R.TORCH[dtype]).normal_(generator=g) for _ in range(2))
+    q = torch.empty(n, heads, d, device="cuda").normal_(generator=g)
+    return q, K, V, table, ints(shareds).cuda(), ints(lengths).cuda()
+
+
+def in_64_bits(q, K, V, table, shared, length, width):
+    """batch_reference.attention with a sequence's heads at once, on the GPU."""
+    n, heads, d = q.shape
+    pages, kv, page, _ = K.shape
+    out = torch.zeros(n, heads, d, dtype=torch.float64, device="cuda")
+    for s, m in enumerate(length.tolist()):
+        p = torch.arange(m, device="cuda")
+        at = torch.where(p < shared[s // width], table[s - s % width, p // page], table[s, p // page]).long()
+        there = (at >= 0) & (at < pages)
+        at, p = at[there], p[there]
+        if len(p):
+            k, v = (x[at, :, p % page].double().transpose(0, 1).contiguous() for x in (K, V))
+            z = torch.matmul(q[s].double().view(kv, heads // kv, d), k.transpose(1, 2).contiguous()) / math.sqrt(d)
+            out[s] = torch.matmul(z.softmax(-1), v).view(heads, d)
+    return out
+
+
+def attend_on_gpu(dtype, q, K, V, table, shared, length, width, max_own):
+    out, err = torch.full_like(q, math.nan), torch.zeros(1, dtype=torch.int32, device="cuda")
+    P().spd_op_attention_shared(dtype, q, K, V, table, shared, length, out, width, int(shared.max()), max_own, err=err)
+    return out, int(err)
+
+
+@pytest.mark.parametrize("case", [c for c, _ in RINGS], ids=lambda c: "-".join(map(str, c)))
+def test_attention_through_stages_that_are_filled_again(case):
+    """Blocks whose waves share out rows, over chunks of more than twice the stages that LDS holds; then with a page that is none late in a chunk."""
+    say("ring", *case)
+    dtype, heads, kv, d, page, groups, width, shared, own = case
+    q, K, V, table, *rest = on_gpu(*case, seed=d + width)
+    got, err = attend_on_gpu(dtype, q, K, V, table, *rest, width, own)
+    assert err == 0
+    close(got, in_64_bits(q, K, V, table, *rest, width))
+    chunk = P().spd_test_attention_shared_cut(dtype, groups * width, width, heads, kv, d, shared, own)[1]
+    table[width, (2 * chunk - 40) // page] = -1              # of the second group, in the last stages of the second chunk
+    table[0, (chunk - 70) // page] = len(K)
+    got, err = attend_on_gpu(dtype, q, K, V, table, *rest, width, own)
+    assert err == 1
+    close(got, in_64_bits(q, K, V, table, *rest, width))
