@@ -317,3 +317,55 @@ def test_attention_through_stages_that_are_filled_again(case):
     got, err = attend_on_gpu(dtype, q, K, V, table, *rest, width, own)
     assert err == 1
     close(got, in_64_bits(q, K, V, table, *rest, width))
+
+
+@pytest.mark.parametrize("heads", [4, 16])
+def test_shared_positions_in_a_graph(heads):
+    """Attention cut into chunks and a reordering that keeps shared positions, captured once and replayed with other lengths, shared parts and parents: sequences that end before
+    the shared positions do, groups without any, none at all.  Every replay equals the eager calls; err is set by the one that has a reason."""
+    g = gen(41)
+    W, G, kv, d, page, entries = 3, 3, 2, 64, 16, 50
+    n = W * G
+    K0, V0 = (torch.randn(2, n * entries, kv, page, d, generator=g).half().cuda() for _ in range(2))
+    table = torch.randperm(n * entries, generator=g).int().view(n, entries).cuda()
+    q = torch.randn(n, heads, d, generator=g).cuda()
+    # shared, lengths (the same within a group: they are reordered), parents, err
+    runs = [([600, 40, 700], [640, 50, 655], [[1, 1, 0], [0, 1, 2], [2, 0, 2]], 0), ([600, 700, 0], [599, 0, 33], [[2, 2, 2], [1, 0, 2], [0, 0, 0]], 0),
+            ([0, 0, 0], [0, 0, 0], [[1, 2, 0]] * 3, 0), ([-1, 650, 700], [640, 650, 703], [[1, 1, 0], [2, 1, 1], [0, 1, 2]], 1), ([597, 33, 700], [640, 50, 701], [[2, 1, 0], [1, 1, 1], [2, 2, 1]], 0)]
+
+    class Step:
+        def __init__(self):
+            self.K, self.V, self.out, self.table = K0.clone(), V0.clone(), torch.empty_like(q), torch.empty_like(table)
+            self.shared, self.length, self.parents = ints([0] * G).cuda(), ints([0] * n).cuda(), torch.zeros(G, W, dtype=torch.int32, device="cuda")
+            self.err = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+        def load(self, run):
+            self.K.copy_(K0), self.V.copy_(V0), self.err.zero_()
+            self.shared.copy_(ints(run[0])), self.length.copy_(ints([x for x in run[1] for _ in range(W)])), self.parents.copy_(ints(run[2]))
+
+        def run(self):
+            P().spd_op_attention_shared("fp16", q, self.K[0], self.V[0], table, self.shared, self.length, self.out, W, 700, 60, err=self.err)
+            P().spd_op_beam_reorder("fp16", self.K, self.V, table, self.parents, self.length, self.table, W, err=self.err, shared=self.shared)
+
+        def results(self):
+            return [x.clone() for x in (self.K, self.V, self.out, self.table, self.err)]
+
+    eager, step = Step(), Step()
+    step.load(runs[0])
+    step.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.run()
+    for i in (0, 1, 2, 3, 4, 1, 0):
+        eager.load(runs[i])
+        eager.run()
+        want = eager.results()
+        step.load(runs[i])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(step.results(), want)), i
+        assert int(want[4]) == runs[i][3], i
+        if not runs[i][3]:
+            close(want[2], in_64_bits(q, K0[0], V0[0], table, eager.shared, eager.length, W))
