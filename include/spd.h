@@ -314,10 +314,11 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
                             int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t n_ctx,
                             int32_t cap_ctx, void *hip_stream);
 
-/* ---- several sequences over one prompt: the step of k independent passes or of a beam search ----
+/* ---- several sequences over one prompt: operators of the step of k independent passes or of a beam search ----
  * Section 4.3 holds Superposed Decoding against k independent passes and against beam search: n_seq sequences that
  * agree in their first positions.  These operators take such a batch through a step on a PAGED cache, for programs
- * that run those decoders' products themselves:
+ * that run those decoders' products themselves (and, for k independent passes, sample from several rows themselves).  No operator here
+ * attends from several new tokens of one sequence: a prompt goes through the step token by token, or its keys and values, come by elsewhere, go in with one append.
  *   K, V   DEVICE [n_pages, n_kv_heads, page_size, d_head] in `dtype` (fp32, fp16 or bf16), 16-byte aligned; page_size a
  *          power of two from 4 to 1024, d_head a power of two from 8 to 256;
  *   table  DEVICE int32 [n_seq, table_stride]: position p of sequence s is row p % page_size of page
@@ -346,7 +347,10 @@ int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_t *table, i
  * sequence s.  Positions below shared[g] are the same in all sequences of group g: they are read once, through the table of
  * the group's first sequence.  q, out DEVICE float [n_seq, n_heads, d_head]; shared DEVICE int32 [n_seq / width], len DEVICE int32 [n_seq].
  * max_shared >= every shared[g] and max_own >= every len[s] - shared[g] size the launch (host values; neither more than a row of
- * the table holds).  len[s] may be less than shared[g].  A sequence of length 0 gets zeros; so does one whose lengths are out of these bounds
+ * the table holds): the call is cut by these bounds, not by the lengths, so one whose bounds are far above them costs the launch of what they might need
+ * (a step of 74 positions 7.3 us at bounds of 64 + 10, 10.8 at 8192 + 2048).  len[s] may be less than shared[g]; such a sequence is read by
+ * itself, in as many pieces as max_own is cut into (sixteen over 65537 positions, one of them a position shorter: 1009 us at a max_own of 33, 317 at 1024, 157 at
+ * 65537, where all behind them take 91, 90 and 103).  A sequence of length 0 gets zeros; so does one whose lengths are out of these bounds
  * (*err is set).  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result.  Nothing behind a sequence's last position gets into its result,
  * whatever it holds. */
 size_t spd_op_attention_shared_scratch_bytes(int32_t n_seq, int32_t width, int32_t n_heads, int32_t n_kv_heads, int32_t d_head, int32_t max_shared,
@@ -357,7 +361,8 @@ int spd_op_attention_shared(int32_t dtype, const float *q, const void *K, const 
                             int32_t *err, void *hip_stream);
 
 /* The n_out best continuations of each group's n_in beams (both 1..SPD_K_MAX; n_in 1 at a search's first step): continuation (b, v)
- * scores scores[g][b] + log softmax(logits[g][b] / tau)[v], and the lower b, then the lower v goes first among equals.  logits
+ * scores scores[g][b] + log softmax(logits[g][b] / tau)[v], and the lower b, then the lower v goes first among equals.  (The sum of
+ * exponentials is an fp32 sum, which is some 1e-7 in a score: continuations of different beams that are nearer to each other than that may change places.)  logits
  * DEVICE [n_groups n_in rows of row_stride elements] in `dtype` (a logit that is no number counts as -inf, +inf as the largest finite
  * number; -inf is no continuation); scores DEVICE float [n_groups, n_in] (-inf or no number: no such beam).  ended (DEVICE int32
  * [n_groups, n_in], may be NULL): a beam with a value other than 0 has one continuation, itself, with token end_token and its score

@@ -4,11 +4,14 @@
 // score move all of them alike.  So one pass over the logits leaves, per slice of a row, the
 // n_out best (sort keys, exact) with the slice's maximum and sum of exponentials, and a second,
 // small kernel puts a row's slices together and ranks what is left of a group, at most n_in * n_out
-// continuations, by score in 64 bits.
+// continuations.  Scores are put together and compared in 64 bits, but a row's sum of exponentials is an fp32 sum of
+// the hardware's exponentials (2^-23 of each) and its logarithm fp32 (2^-24): some 1e-7 in a score, a fifth of the rounding of its
+// result at a score of ten.  Within a row it changes nothing; equal rows have equal sums; continuations of different rows that are nearer to each other may
+// change places.  Exponentials in 64 bits would cost several times the eight instructions that a logit takes now.
 // A wave has a slice to itself, all of it in registers, NE entries per lane: no barrier anywhere, and the selection is paid once per
-// wave.  128 rows of 50258 (22.5 MB read of 112 of them, 4.7 us at a large copy's rate): 18.7 us with 64-bit keys for every
-// entry, 8.9 with keys for those alone that can be among the best; 64 rows of 131072 in bf16 22.8 -> 9.7.  The second kernel, a chain of
-// dependent steps in one block per group: 15.5 -> 6.3 and 34 -> 9.6 us.
+// wave.  128 rows of 50258 (22.5 MB read of 112 of them, 3.6 us at a large read's rate): 18.7 us with 64-bit keys for every
+// entry, 9.2 with keys for those alone that can be among the best; 64 rows of 131072 in bf16 22.8 -> 9.9.  The second kernel, a chain of
+// dependent steps in one block per group: 15.5 -> 6.6 and 34 -> 9.8 us.
 #include "spd_device.h"
 
 using namespace spdd;

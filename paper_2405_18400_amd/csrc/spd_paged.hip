@@ -53,7 +53,7 @@ __device__ __forceinline__ float2 rotation(int pos, int i, double log2_theta, in
     return make_float2(q == 1 || q == 2 ? -cs : cs, q >= 2 ? -sn : sn);
 }
 
-// Measured: four tokens of 32 + 2 x 32 heads of 128 3.3 us (latency); 4099 tokens of 64 + 2 x 8 heads, 319 MB in all, 60.9 us, 5.2 TB/s
+// Measured: four tokens of 32 + 2 x 32 heads of 128 3.3 us (latency); 4099 tokens of 64 + 2 x 8 heads, 319 MB in all, 61 us, 5.2 TB/s
 // (a large copy: 4.8).
 // One block: part `part` of one token's pieces of four elements, q heads first, then k, then v.  U pieces per thread are
 // asked for before the position, the page and the angles are known.
@@ -153,7 +153,7 @@ __device__ __forceinline__ BeamRows beam_rows(const ReorderArgs &a, int g, int l
     return r;
 }
 
-// Measured: two further children of 32 layers x 32 heads x 10 rows x 128 in fp16, 10.5 MB read and as much written, 6.8 us (parents and
+// Measured: two further children of 32 layers x 32 heads x 10 rows x 128 in fp16, 10.5 MB read and as much written, 6.9 us (parents and
 // lengths, then page numbers, are two trips to memory before the copy's own); eight groups of five further children, 16 layers x 8 heads x some 40 rows x 128 in bf16,
 // 109 MB each way, 44 us (4.9 TB/s, a large copy's rate).
 // Blocks 0 .. groups - 1: a group's tables.  The others: (group, further child, layer, share of the key/value heads); where shared positions are

@@ -14,11 +14,11 @@
 //   * S^T's accumulator holds keys 16 u + 4 kk + r (kk: the lane's group of 16) of one row, which is P^T's operand layout
 //     when the eight k indices of a lane stand for those keys, so probabilities never leave their registers;
 //   * a lane fetches DH / 16 features of each of those eight keys of V, 16 lanes a whole row, and turns them round in registers.
-// K and V of a 16-bit cache are exact in their type; queries and probabilities go in as two fp16 numbers (22 bits, scaled by
+// K and V of a 16-bit cache are exact in their type; queries and probabilities go in as two fp16 numbers (24 bits, scaled by
 // powers of two into fp16's range) or three bf16 numbers (24 bits): the error against 64 bits is that of fp32 arithmetic.
 // An fp32 cache takes the fp32 products.  Four waves share a block's keys, 32 each in turn, with a running maximum and sum of their own.
-// Measured, heads of 128: four sequences of 74 positions, 32 heads in fp16, 6.4 us (latency: lengths, page numbers, keys, result); five of 1027
-// shared and about 20 own, 40 heads in fp32 (45 MB), 15.6 us and 3.9 for the join.
+// Measured, heads of 128: four sequences of 74 positions, 32 heads in fp16, 6.5 us (latency: lengths, page numbers, keys, result); five of 1027
+// shared and about 20 own, 40 heads in fp32 (45 MB), 16.1 us and 3.9 for the join.
 #include "spd_device.h"
 
 #include <algorithm>
@@ -523,9 +523,9 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 // come through LDS, 16 bytes per lane straight from memory, ST stages of SK keys deep; pieces of a row are permuted by the row number,
 // so that neither the operand reads (16 rows side by side) nor the row reads meet in a bank.  One barrier per stage says both "this
 // stage has arrived" and "the one before has been read".
-// Measured, 64 heads of 128 on 8 in fp16: eight sequences over 8191 positions (37 MB) 15.1 us, bound by a block's chain; sixteen over
-// 65537 (271 MB; 69 GFLOP with the two parts of queries and probabilities) 78 .. 103 us, 3.1 TB/s and 0.8 PFLOP/s, the matrix cores and the vector
-// unit in turn.  Eight groups of eight over 2001, 32 heads on 8 in bf16 (127 MB), 35 us, 3.6 TB/s over the call.
+// Measured, 64 heads of 128 on 8 in fp16: eight sequences over 8191 positions (37 MB) 15.3 us, bound by a block's chain; sixteen over
+// 65537 (271 MB; 69 GFLOP with the two parts of queries and probabilities) 80 .. 97 us, 3.4 TB/s and 0.85 PFLOP/s at best, the matrix cores busy for 34% of it and the
+// vector unit for 39%, in turn.  Eight groups of eight over 2001, 32 heads on 8 in bf16 (127 MB), 34.5 us, 3.7 TB/s (17% and 25%).
 template <int DH, int RT> struct Stage {
     static constexpr int SK = DH == 64 || (DH == 128 && RT == 1) ? 64 : 32;             // keys
     static constexpr int NU = RT == 1 && SK == 64 ? 4 : 2;                              // tiles of 16 keys that go through the products together
@@ -915,7 +915,7 @@ __global__ __launch_bounds__(NTS, (MANY && DH <= 128) || (sizeof(KT) * DH <= 512
 
 // A block per (sequence, query head).  A thread's first chunks are asked for together with all maxima and sums: one trip to
 // memory for up to UM * groups chunks.  Every wave forms the row's maximum and sum for itself, so the block meets once.  Sums in a fixed order.
-// Measured, 512 rows of 128: 33 chunks each 4.0 us (a launch and three trips to memory); 1024 rows of 65: 8.3 us.
+// Measured, 512 rows of 128: 33 chunks each 4.0 us (a launch and three trips to memory); 1024 rows of 64: 8.0 us.
 constexpr int UM = 8;
 __global__ __launch_bounds__(NTS) void shared_merge_kernel(const SharedAttnArgs p) {
     __shared__ float4 acc[NTS];
