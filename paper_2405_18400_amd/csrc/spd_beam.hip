@@ -448,7 +448,7 @@ int entries_per_lane(long long rows, int vocab, int n_out) {
     int best = 0;
     long long least = 0;
     for (int ne = 8; ne <= 64; ne *= 2) {
-        const long long slices = (vocab + WAVE * ne - 1) / (WAVE * ne), places = CUS * 4 * waves_per_simd(ne), keys = slices * n_out;
+        const long long slices = ((long long)vocab + WAVE * ne - 1) / (WAVE * ne), places = CUS * 4 * waves_per_simd(ne), keys = slices * n_out;
         const bool halves = n_out > EM && keys > WAVE && slices <= n_out;
         const long long cost = (rows * slices + places - 1) / places * (32 + ne) + (keys + EM * WAVE - 1) / (EM * WAVE) * 96 + (halves ? 200 : 0);
         if (best == 0 || cost < least) { best = ne; least = cost; }

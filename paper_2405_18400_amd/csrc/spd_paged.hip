@@ -292,6 +292,13 @@ extern "C" int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }
 
+// Whether any layer of a pool (pool bytes each, `apart` from one to the next) lies over o: the first layer that ends behind its beginning does, or none.
+static bool over_layers(const void *base, size_t pool, size_t apart, int n_layers, const spdk::Span &o) {
+    const uintptr_t b = (uintptr_t)base, at = (uintptr_t)o.p;
+    const size_t l = at < b + pool ? 0 : (at - b - pool) / apart + 1;
+    return l < (size_t)n_layers && spdk::overlap((const void *)(b + l * apart), pool, o.p, o.bytes);
+}
+
 static int reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
                    int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
                    const int32_t *parents, const int32_t *len, const int32_t *shared, int32_t *table_out, int32_t *err, void *hip_stream) {
@@ -304,10 +311,15 @@ static int reorder(int32_t dtype, void *K, void *V, const int32_t *table, int32_
     if (n_layers > 1 && (layer_stride < layer_elems || layer_stride % (16 / elem))) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
     if (!parents || !len || !table_out) return SPD_EINVAL;
-    // what is written lies apart from what other blocks read
-    const size_t table_bytes = (size_t)n_seq * table_stride * 4, ids = (size_t)n_seq * 4, pools = (size_t)(n_layers - 1) * layer_stride * elem + spdk::pool_bytes(dtype, c);
-    const spdk::Span st{table, table_bytes}, sp{parents, ids}, sl{len, ids}, sh{shared, (size_t)(n_seq / width) * 4}, sK{K, pools}, sV{V, pools}, se{err, 4};
-    if (spdk::over_any(spdk::Span{table_out, table_bytes}, {st, sp, sl, sh, sK, sV, se}) || spdk::over_any(sK, {sV, st, sp, sl, sh, se}) || spdk::over_any(sV, {st, sp, sl, sh, se})) return SPD_EINVAL;
+    // what is written lies apart from what other blocks read (layers may lie in turn: a layer's keys, its values, the next layer's keys, other things between them)
+    const size_t table_bytes = (size_t)n_seq * table_stride * 4, ids = (size_t)n_seq * 4, pool = spdk::pool_bytes(dtype, c), apart = n_layers > 1 ? (size_t)layer_stride * elem : pool;
+    const spdk::Span st{table, table_bytes}, sp{parents, ids}, sl{len, ids}, sh{shared, (size_t)(n_seq / width) * 4}, so{table_out, table_bytes}, se{err, 4};
+    if (spdk::over_any(so, {st, sp, sl, sh, se})) return SPD_EINVAL;
+    for (const void *p : {(const void *)K, (const void *)V})
+        for (const spdk::Span &o : {st, sp, sl, sh, so, se})
+            if (o.p && over_layers(p, pool, apart, n_layers, o)) return SPD_EINVAL;
+    const uintptr_t kp = (uintptr_t)K, vp = (uintptr_t)V;
+    if (over_layers((const void *)std::min(kp, vp), pool, apart, n_layers, spdk::Span{(const void *)std::max(kp, vp), pool})) return SPD_EINVAL;      // (the others of its layers lie alike)
     ReorderArgs a{c, parents, len, shared, table_out, err, n_layers, width, n_seq / width, width == 1 ? 0 : width - 1 + (shared != nullptr), d_head * elem, 0, 0, (size_t)layer_stride * elem};
     // about 32 KB of keys and values per block
     a.heads_per_share = std::max(1, 16384 / (page_size * a.row_bytes));

@@ -177,3 +177,19 @@ def test_rings_go_round(pkg, case, cut):  # noqa: F811
     assert (keys, stages, rows) == cut and chunks > 1 and chunk > 2 * stages * keys
     if page == 4:
         assert chunk // page > 256
+
+
+@pytest.mark.parametrize("layers,stride,off", [(2, POOL, POOL - 16), (2, POOL, 16), (4, 2 * POOL, POOL - 16), (4, 2 * POOL, POOL + 16), (4, 2 * POOL, 7 * POOL - 16), (4, 2 * POOL, 5 * POOL + 16),
+                                               (4, 3 * POOL, 2 * POOL + 16), (3, POOL + 16, POOL)])
+@pytest.mark.parametrize("first", ["K", "V"])
+def test_reorder_refuses_pools_whose_layers_meet(pkg, layers, stride, off, first):  # noqa: F811
+    other = "V" if first == "K" else "K"
+    assert call(pkg, "spd_op_beam_reorder", REORDER, n_layers=layers, layer_stride=stride // 2, **{first: 64 * A, other: 64 * A + off}) == EINVAL
+
+
+@pytest.mark.parametrize("at", [-16, POOL - 16, 2 * POOL - 16, 3 * POOL - 16, 7 * POOL - 16])
+def test_reorder_refuses_tables_over_a_layer(pkg, at):  # noqa: F811
+    """Keys and values in turn, a pool's room between them."""
+    pools = dict(K=64 * A, V=64 * A + 2 * POOL, n_layers=3, layer_stride=4 * POOL // 2)
+    for what in ("table_out", "table", "parents", "len"):
+        assert call(pkg, "spd_op_beam_reorder", REORDER, **pools, **{what: 64 * A + at}) == EINVAL

@@ -369,3 +369,22 @@ def test_shared_positions_in_a_graph(heads):
         assert int(want[4]) == runs[i][3], i
         if not runs[i][3]:
             close(want[2], in_64_bits(q, K0[0], V0[0], table, eager.shared, eager.length, W))
+
+
+def test_reorder_of_layers_that_lie_in_turn():
+    """A layer's keys, its values and room for something else, then the next layer's: the C entry takes the distance between layers; the tables lie in that room."""
+    K, V, table, length = reorder_case("fp16", 3, 2, 64, 16, [37, 10], 4, seed=51)
+    parents = ints([[2, 2, 0, 2], [1, 0, 0, 3]])
+    one = K[0].numel()
+    store = torch.full((3, 3, one), 7.0, dtype=torch.float16, device="cuda")
+    store[:, 0], store[:, 2] = K.flatten(1).cuda(), V.flatten(1).cuda()
+    room = store[1, 1].view(torch.int32)
+    sizes = [table.numel(), table.numel(), parents.numel(), length.numel()]
+    t, out, p, n = room[:sum(sizes)].split(sizes)
+    t.copy_(table.flatten()), p.copy_(parents.flatten()), n.copy_(length)
+    rc = P().lib().spd_op_beam_reorder(2, store[0, 0].data_ptr(), store[0, 2].data_ptr(), t.data_ptr(), K.shape[1], 2, 16, 64, 8, table.shape[1], 3, 3 * one, 4, p.data_ptr(), n.data_ptr(),
+                                       out.data_ptr(), None, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    a, b, c = R.reorder(K, V, table, parents, length, 4)
+    assert torch.equal(out.cpu().view(table.shape), c) and torch.equal(store[:, 0].cpu().view(K.shape), a) and torch.equal(store[:, 2].cpu().view(V.shape), b)
+    assert (store[0, 1] == 7.0).all() and (store[2, 1] == 7.0).all()
