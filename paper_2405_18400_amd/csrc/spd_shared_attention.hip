@@ -102,6 +102,41 @@ __device__ __forceinline__ void far_scores(f32x4v (&s)[NU], float scale, float m
         for (int r = 0; r < 4; ++r) s[u][r] = fabsf(m) > FAR ? ((s[u][r] * scale - from) + Type<KT>::P_BITS) * inv : s[u][r];
 }
 
+// One turn's scores of a lane's row against its reference m: what the exponents are taken from.  Where a probability would pass 2^SLACK in any row (or a reference is far from
+// zero) the references are raised, and sums and results so far follow.
+template <typename KT, int NU, int FV>
+__device__ __forceinline__ float raised(f32x4v (&s)[NU], f32x4v (&o)[FV], float scale, float &m, float &l) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[u][r]);
+    mx *= scale;
+    if (__any((mx > m + SLACK) | (fabsf(m) > FAR))) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));            // the lane groups hold different keys of the same rows
+        mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
+        mx = fmaxf(mx, m);
+        const float corr = exp2_below(m, mx);
+        m = mx;
+        l *= corr;
+#pragma unroll
+        for (int e = 0; e < FV; ++e) o[e] *= corr;
+        if (__any((fabsf(mx) > FAR) & (mx != -INFINITY))) far_scores<KT>(s, scale, mx);
+    }
+    return fabsf(m) > FAR ? 0.f : m - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
+}
+
+// Two features of eight keys (word i of each), turned round: eight keys of each feature.
+template <int VW>
+__device__ __forceinline__ void turned(const uint32_t (&v)[2][4][VW], int i, u32x4 &even, u32x4 &odd) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t x = v[k / 2][2 * (k % 2)][i], y = v[k / 2][2 * (k % 2) + 1][i];
+        even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    }
+}
+
 // The power of two that takes a row whose largest value is `top` to the upper end of fp16's range, and its inverse.
 __device__ __forceinline__ void scaling(float top, float &up, float &down) {
     int ex = 15;
@@ -382,24 +417,7 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             if (rt >= tiles) break;
-            float mx = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
-            mx *= scale[rt];
-            if (__any((mx > m[rt] + SLACK) | (fabsf(m[rt]) > FAR))) {
-                mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));    // the lane groups hold different keys of the same rows
-                mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
-                mx = fmaxf(mx, m[rt]);
-                const float corr = exp2_below(m[rt], mx);
-                m[rt] = mx;
-                l[rt] *= corr;
-#pragma unroll
-                for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
-                if (__any((fabsf(mx) > FAR) & (mx != -INFINITY))) far_scores<KT>(st[rt], scale[rt], mx);
-            }
-            const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
+            const float ref = raised<KT>(st[rt], o[rt], scale[rt], m[rt], l[rt]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 pf[rt][i] = __builtin_amdgcn_exp2f(fmaf(st[rt][i / 4][i % 4], scale[rt], -ref)) * Type<KT>::P_SCALE;
@@ -426,16 +444,10 @@ __device__ __forceinline__ bool attend(const SharedAttnArgs &p, Unit &un, F &&re
                         o[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i / 4][i % 4][e]), pf[rt][i], o[rt][e], 0, 0, 0);
             }
         } else {
-            // two features of eight keys at a time, turned round: eight keys of each
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
                 u32x4 even, odd;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t x = vf[k / 2][2 * (k % 2)][i], y = vf[k / 2][2 * (k % 2) + 1][i];
-                    even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                    odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                }
+                turned(vf, i, even, odd);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     if (rt >= tiles) break;
@@ -726,24 +738,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
             u32x4 pt[RT][NU / 2][PARTS];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < NU; ++u)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[rt][u][r]);
-                mx *= scale[rt];
-                if (__any((mx > m[rt] + SLACK) | (fabsf(m[rt]) > FAR))) {
-                    mx = fmaxf(mx, __shfl_xor(mx, 16, WAVE));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
-                    mx = fmaxf(mx, m[rt]);
-                    const float corr = exp2_below(m[rt], mx);
-                    m[rt] = mx;
-                    l[rt] *= corr;
-#pragma unroll
-                    for (int e = 0; e < FV; ++e) o[rt][e] *= corr;
-                    if (__any((fabsf(mx) > FAR) & (mx != -INFINITY))) far_scores<KT>(st[rt], scale[rt], mx);
-                }
-                const float ref = fabsf(m[rt]) > FAR ? 0.f : m[rt] - Type<KT>::P_BITS;      // (-inf: nothing seen yet, no score)
+                const float ref = raised<KT>(st[rt], o[rt], scale[rt], m[rt], l[rt]);
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -772,12 +767,7 @@ __device__ __forceinline__ bool attend_many(const SharedAttnArgs &p, const Unit 
 #pragma unroll
                 for (int i = 0; i < VW; ++i) {
                     u32x4 even, odd;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t x = vf[h][k / 2][2 * (k % 2)][i], y = vf[h][k / 2][2 * (k % 2) + 1][i];
-                        even[k] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                        odd[k] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                    }
+                    turned(vf[h], i, even, odd);
 #pragma unroll
                     for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
