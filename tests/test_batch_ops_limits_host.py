@@ -86,7 +86,7 @@ def test_select_slices(pkg, shape, entries):  # noqa: F811
 def test_select_slices_follow_what_the_gpu_holds(pkg):  # noqa: F811
     """As many entries per lane as make for the least of rounds of waves and turns of the second kernel; a vocabulary of one launch has no slices."""
     assert pkg.spd_test_beam_select_cut(3, 2, 4, 4096) == (0, 1)
-    places = {8: 8192, 16: 8192, 32: 3072, 64: 2048}                       # 256 x 4 SIMDs x 8, 8, 3, 2 waves
+    places = {8: 1024 * 8, 16: 1024 * 8, 32: 1024 * 3, 64: 1024 * 2}       # SIMDs and the waves that each holds
 
     def cost(rows, n_out, vocab, ne):
         slices = -(-vocab // (64 * ne))
