@@ -52,7 +52,10 @@ typedef enum {
     SPD_EHIP = -6           /* a HIP runtime call failed                                 */
 } spd_status;
 
-typedef enum { SPD_DTYPE_FP32 = 0, SPD_DTYPE_BF16 = 1, SPD_DTYPE_FP16 = 2 /* key/value cache only */ } spd_dtype;
+typedef enum {
+    SPD_DTYPE_FP32 = 0, SPD_DTYPE_BF16 = 1, SPD_DTYPE_FP16 = 2 /* key/value cache only */,
+    SPD_DTYPE_INT8 = 3 /* paged cache of codes and scales only, where an operator says so */
+} spd_dtype;
 
 /* Decoder-only transformer f_theta: RMSNorm, rotary on adjacent pairs (x_2i, x_2i+1) with
  * angle pos * rope_theta^(-2i/d_head), causal attention scaled by 1/sqrt(d_head), SwiGLU
@@ -317,8 +320,8 @@ int spd_op_attention_static(int32_t dtype, const float *q, const void *K, const 
 /* ---- several sequences over one prompt: operators of the step of k independent passes or of a beam search ----
  * Section 4.3 holds Superposed Decoding against k independent passes and against beam search: n_seq sequences that
  * agree in their first positions.  These operators take such a batch through a step on a PAGED cache, for programs
- * that run those decoders' products themselves (and, for k independent passes, sample from several rows themselves).  No operator here
- * attends from several new tokens of one sequence: a prompt goes through the step token by token, or its keys and values, come by elsewhere, go in with one append.
+ * that run those decoders' products themselves (and, for k independent passes, sample from several rows themselves).  The attention here
+ * takes one new token per sequence; several at once (a prompt, drafts) are the next section's.
  *   K, V   DEVICE [n_pages, n_kv_heads, page_size, d_head] in `dtype` (fp32, fp16 or bf16), 16-byte aligned; page_size a
  *          power of two from 4 to 1024, d_head a power of two from 8 to 256;
  *   table  DEVICE int32 [n_seq, table_stride]: position p of sequence s is row p % page_size of page
@@ -396,6 +399,59 @@ int spd_op_beam_reorder(int32_t dtype, void *K, void *V, const int32_t *table, i
 int spd_op_beam_reorder_shared(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
                                int32_t d_head, int32_t n_seq, int32_t table_stride, int32_t n_layers, int64_t layer_stride, int32_t width,
                                const int32_t *parents, const int32_t *len, const int32_t *shared, int32_t *table_out, int32_t *err, void *hip_stream);
+
+/* ---- chunks of new tokens: prompts and drafted tokens through a paged cache ----
+ * A step of a program that runs a model's products itself feeds sequence s the new tokens first[s] .. first[s + 1] - 1 of a call's n_tokens (first DEVICE
+ * int32 [n_seq + 1], ascending): a piece of its prompt, one token, or its newest token and drafts of the next ones (those that Superposed Decoding keeps, for
+ * one).  Their keys and values go into the cache, their queries attend over it, and of drafts it is found out which stand.  The cache is the paged one of
+ * the operators above, with their conventions (device-side lengths, *err, scratch, overlaps, nothing synchronised or allocated), and may also hold 8 bits per value:
+ *   K, V              DEVICE int8 [n_pages, n_kv_heads, page_size, d_head], SPD_DTYPE_INT8;
+ *   K_scale, V_scale  DEVICE float [n_pages, n_kv_heads, page_size], 16-byte aligned: a value is its code times its row's scale.
+ * Both are NULL for the other types.  (spd_op_append_paged, spd_op_attention_shared and spd_op_beam_reorder take no 8-bit cache.) */
+
+/* spd_op_append_paged into a cache of 8 bits: scale = fp32(max |x| / 127) over the d_head values x of a row, rotated where they are keys, and code = x / scale rounded
+ * to the nearest whole number, to even between two; rotation, scale and code are formed in 64 bits.  A row of zeros has scale 0.  A k or v that is no number counts as 0, an
+ * infinite one as the largest finite number. */
+int spd_op_append_paged_q8(int8_t *K, int8_t *V, float *K_scale, float *V_scale, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                           int32_t d_head, int32_t n_seq, int32_t table_stride, const float *q, int64_t q_stride, const float *k, const float *v, int64_t kv_stride,
+                           const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t n_heads, float rope_theta, float *q_out, int32_t *err, void *hip_stream);
+
+/* Cached rows back: k_out, v_out [n_tokens, n_kv_heads, d_head] in `out_dtype` (fp32, fp16 or bf16), 16-byte aligned, get the keys (as cached: rotated) and values at
+ * position pos[i] of sequence seq[i] of a cache in `dtype` (fp32, fp16, bf16 or int8: code x scale in fp32), rounded to nearest.  seq[i] < 0: padding, the row is left as it was; so is one whose position or
+ * page is out of range (*err is set).  The same position may be named more than once. */
+int spd_op_read_paged(int32_t dtype, const void *K, const void *V, const float *K_scale, const float *V_scale, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
+                      int32_t page_size, int32_t d_head, int32_t n_seq, int32_t table_stride, const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t out_dtype,
+                      void *k_out, void *v_out, int32_t *err, void *hip_stream);
+
+/* Causal attention of the new tokens: len[s] (DEVICE int32 [n_seq]) positions of sequence s are cached, its n new ones, appended before, among them.  The query of its j-th new token sits at
+ * position p = len[s] - n + j: out[t][h] = softmax(q[t][h] . K / sqrt(d_head)) V over positions 0 .. p.  Cache in `dtype` (fp32, fp16, bf16 or int8).  q rows [n_heads,
+ * d_head] at q + t q_stride (elements; a multiple of 8) and out [n_tokens, n_heads, d_head] in `io_dtype`: fp32, or the cache's own type, or with an int8 cache
+ * fp16 or bf16.  In fp32 queries and probabilities go into the products with 24 bits, in 16 bits with those of the type.  max_len >= every len[s] (a host
+ * value; no more than a row of the table holds) and max_new, the most new tokens of a sequence, size the launch: a sequence with more of them is taken as well, only slower.
+ * A sequence whose first and len do not fit (first descends or passes n_tokens, len below its new tokens or over max_len) gets zeros for the rows that it has, *err is set.  Rows that are no
+ * sequence's are left as they were.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
+ * sequence's last position, or behind a token's own, gets into its result. */
+size_t spd_op_attention_paged_scratch_bytes(int32_t dtype, int32_t io_dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                            int32_t max_new, int32_t max_len);
+int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64_t q_stride, const void *K, const void *V, const float *K_scale, const float *V_scale,
+                           const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size, int32_t d_head, int32_t n_seq, int32_t table_stride, const int32_t *first,
+                           const int32_t *len, int32_t n_tokens, int32_t n_heads, int32_t max_new, int32_t max_len, void *out, void *scratch, size_t scratch_bytes,
+                           int32_t *err, void *hip_stream);
+
+/* Which drafted tokens stand.  tokens (DEVICE int32 [n_tokens]): of sequence s its newest token, at first[s], then its m = first[s + 1] - first[s] - 1 >= 0 drafts.  Row t of logits
+ * (DEVICE, `dtype` fp32, fp16 or bf16, rows of row_stride elements) is what the target model expects behind token t, p = softmax(logits / tau); row t of draft_logits (draft_stride) what
+ * the drafter drew token t + 1 from, q = softmax(draft_logits / draft_tau), not looked at for a sequence's last token.  draft_logits NULL: drafts that were chosen, not drawn, q
+ * is 1 at the draft.  u (DEVICE float [n_tokens], in [0, 1), the caller's draws): draft x behind token t stands if all before it do and u[t] q(x) < p(x); so a text has the target's distribution whatever
+ * the drafter's is.  Behind the drafts that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0) at the
+ * first that does not (from p where that is zero everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  Sums and what is compared are formed in 64 bits.
+ * A logit that is no number counts as -inf, +inf as the largest finite number.  A draft outside [0, vocab) does not stand; *err is set.
+ * Outputs, DEVICE: out_accepted int32 [n_seq], the number a of drafts that stand; at first[s] .. first[s] + a of out_tokens int32 [n_tokens] those drafts and the token
+ * behind them, and of out_logprobs float [n_tokens] their log p; -1 and 0 at the sequence's other tokens.  A row without a finite logit gives token 0 with log p = -inf, *err is set.  A
+ * sequence without tokens, or whose first does not fit, has a = 0 and nothing else written (*err is set in the second case); rows that are no sequence's are left as they were. */
+size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_tokens, int32_t vocab);
+int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t row_stride, const void *draft_logits, int64_t draft_stride, const int32_t *tokens, const int32_t *first,
+                         const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, float tau, float draft_tau, int32_t *out_tokens, float *out_logprobs,
+                         int32_t *out_accepted, void *scratch, size_t scratch_bytes, int32_t *err, void *hip_stream);
 
 /* ---- test hooks for the error path of the persistent kernel's bounded waits ----
  * A wait of the persistent forward kernel that gives up (its grid was not co-resident) sets an

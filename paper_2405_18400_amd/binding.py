@@ -15,7 +15,7 @@ import numpy as np
 HERE = os.path.dirname(os.path.abspath(__file__))
 SPD_K_MAX, SPD_TAIL, SPD_N_ORDERS = 16, 5, 5
 SPD_EHIP = -6
-SPD_DTYPE = {"fp32": 0, "bf16": 1, "fp16": 2}   # fp16: key/value cache only
+SPD_DTYPE = {"fp32": 0, "bf16": 1, "fp16": 2, "int8": 3}   # fp16: key/value cache only; int8: paged cache of chunks of new tokens only
 _lib = None
 
 
@@ -111,6 +111,10 @@ def lib():
             "spd_op_beam_select": [i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, vp, sz, vp],
             "spd_op_beam_reorder": [i32, vp, vp, vp] + [i32] * 7 + [i64, i32, vp, vp, vp, vp, vp],
             "spd_op_beam_reorder_shared": [i32, vp, vp, vp] + [i32] * 7 + [i64, i32, vp, vp, vp, vp, vp, vp],
+            "spd_op_append_paged_q8": [vp] * 5 + [i32] * 6 + [vp, i64, vp, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp],
+            "spd_op_read_paged": [i32] + [vp] * 5 + [i32] * 6 + [vp, vp, i32, i32, vp, vp, vp, vp],
+            "spd_op_attention_paged": [i32, i32, vp, i64] + [vp] * 5 + [i32] * 6 + [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp, vp],
+            "spd_op_verify_drafts": [i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp, vp, vp, sz, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -120,6 +124,8 @@ def lib():
         L.spd_strerror.argtypes, L.spd_strerror.restype = [C.c_int], C.c_char_p
         L.spd_op_attention_scratch_bytes.argtypes, L.spd_op_attention_scratch_bytes.restype = [i32, i32, i32], sz
         L.spd_op_attention_shared_scratch_bytes.argtypes, L.spd_op_attention_shared_scratch_bytes.restype = [i32] * 7, sz
+        L.spd_op_attention_paged_scratch_bytes.argtypes, L.spd_op_attention_paged_scratch_bytes.restype = [i32] * 9, sz
+        L.spd_op_verify_drafts_scratch_bytes.argtypes, L.spd_op_verify_drafts_scratch_bytes.restype = [i32] * 3, sz
         L.spd_op_beam_select_scratch_bytes.argtypes, L.spd_op_beam_select_scratch_bytes.restype = [i32] * 4, sz
         L.hipStreamSynchronize.argtypes, L.hipStreamSynchronize.restype = [vp], C.c_int   # (the runtime that libspd is linked to)
         _lib = L
@@ -491,19 +497,8 @@ def _scratch(torch, n_bytes, like):
     return torch.empty(n_bytes, dtype=torch.uint8, device=like.device)
 
 
-def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: float, q=None, q_out=None, err=None):
-    """k, v [tokens, n_kv_heads, d_head] (and q [tokens, n_heads, d_head] -> q_out), rotated by pos, to the rows of their sequences; seq < 0: padding."""
-    torch, where = _torch(), "spd_op_append_paged"
-    kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
-    shape = K.shape
-    n_pages, n_kv, page_size, d = shape
-    n_seq, entries = table.shape
-    n = seq.numel()
-    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n
-            and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
-            and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
-            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
-        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), err=(err, i32, (1,)))
+def _new_rows(where, torch, device, k, v, q, q_out, n, n_kv, d):
+    """The rows of n new tokens: k, v [n, n_kv, d] and q [n, heads, d] -> q_out."""
     if k.shape != (n, n_kv, d) or v.shape != (n, n_kv, d):
         raise ValueError(f"{where}: k and v have to be [{n}, {n_kv}, {d}]")
     kv_stride, q_stride, heads, q_ptr, out_ptr = _rows(where, device, "k", k, n_kv, d, torch), 0, 0, None, None
@@ -520,6 +515,23 @@ def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: flo
         raise ValueError(f"{where}: q_out comes with q")
     if n <= 1:                          # (a single token's stride may be anything)
         kv_stride, q_stride = n_kv * d, heads * d
+    return kv_stride, q_ptr, q_stride, heads, out_ptr
+
+
+def spd_op_append_paged(dtype: str, K, V, table, k, v, seq, pos, rope_theta: float, q=None, q_out=None, err=None):
+    """k, v [tokens, n_kv_heads, d_head] (and q [tokens, n_heads, d_head] -> q_out), rotated by pos, to the rows of their sequences; seq < 0: padding."""
+    torch, where = _torch(), "spd_op_append_paged"
+    kv, i32, device = _kv_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
+    shape = K.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, entries = table.shape
+    n = seq.numel()
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n
+            and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
+            and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
+        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), err=(err, i32, (1,)))
+    kv_stride, q_ptr, q_stride, heads, out_ptr = _new_rows(where, torch, device, k, v, q, q_out, n, n_kv, d)
     rc = lib().spd_op_append_paged(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, q_ptr, q_stride,
                                    k.data_ptr(), v.data_ptr(), kv_stride, seq.data_ptr(), pos.data_ptr(), n, heads, rope_theta, out_ptr,
                                    None if err is None else err.data_ptr(), _stream_ptr(device))
@@ -622,6 +634,145 @@ def spd_op_beam_reorder(dtype: str, K, V, table, parents, length, table_out, wid
     rc = getattr(lib(), name)(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, layers,
                               n_pages * n_kv * page_size * d, width, parents.data_ptr(), length.data_ptr(), *of_group, table_out.data_ptr(),
                               None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
+
+
+# ---- chunks of new tokens through a paged cache, which may hold codes of 8 bits with a scale per row: K, V int8 [pages, n_kv_heads, page_size, d_head], scales float32
+# [pages, n_kv_heads, page_size].  Sequence s has the new tokens first[s] .. first[s + 1] - 1.
+def _cache_type(where, torch, dtype):
+    return torch.int8 if dtype == "int8" else _kv_type(where, torch, dtype)
+
+
+def _io_type(where, torch, dtype):
+    kind = "fp32" if dtype is torch.float32 else "fp16" if dtype is torch.float16 else "bf16" if dtype is torch.bfloat16 else None
+    if kind is None:
+        raise ValueError(f"{where}: rows are {dtype}, not float32, float16 or bfloat16")
+    return kind
+
+
+def _scales(where, torch, dtype, device, shape, K_scale, V_scale):
+    """Addresses of an 8-bit cache's scales (None, None for other caches)."""
+    if (K_scale is not None) != (dtype == "int8") or (V_scale is not None) != (dtype == "int8"):
+        raise ValueError(f"{where}: an int8 cache comes with K_scale and V_scale, others without")
+    if K_scale is None:
+        return None, None
+    f32, rows = torch.float32, shape[:3]
+    if not (K_scale.dtype is f32 and V_scale.dtype is f32 and K_scale.shape == rows and V_scale.shape == rows and K_scale.is_contiguous() and V_scale.is_contiguous()
+            and K_scale.get_device() == device and V_scale.get_device() == device):
+        _refuse(where, device, K_scale=(K_scale, f32, rows), V_scale=(V_scale, f32, rows))
+        raise ValueError(f"{where}: scales have to be {tuple(rows)}")
+    return K_scale.data_ptr(), V_scale.data_ptr()
+
+
+def spd_op_append_paged_q8(K, V, K_scale, V_scale, table, k, v, seq, pos, rope_theta: float, q=None, q_out=None, err=None):
+    """spd_op_append_paged into an int8 cache: codes to K and V, a scale per row to K_scale and V_scale."""
+    torch, where = _torch(), "spd_op_append_paged_q8"
+    i8, i32, device = torch.int8, torch.int32, torch.cuda.current_device()
+    shape = K.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, entries = table.shape
+    n = seq.numel()
+    if not (K.dtype is i8 and V.dtype is i8 and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n
+            and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous() and pos.is_contiguous()
+            and K.get_device() == device and V.get_device() == device and table.get_device() == device and seq.get_device() == device and pos.get_device() == device
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
+        _refuse(where, device, K=(K, i8, None), V=(V, i8, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), err=(err, i32, (1,)))
+    scales = _scales(where, torch, "int8", device, shape, K_scale, V_scale)
+    kv_stride, q_ptr, q_stride, heads, out_ptr = _new_rows(where, torch, device, k, v, q, q_out, n, n_kv, d)
+    rc = lib().spd_op_append_paged_q8(K.data_ptr(), V.data_ptr(), *scales, table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, q_ptr, q_stride, k.data_ptr(),
+                                      v.data_ptr(), kv_stride, seq.data_ptr(), pos.data_ptr(), n, heads, rope_theta, out_ptr, None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
+
+
+def spd_op_read_paged(dtype: str, K, V, table, seq, pos, k_out, v_out, K_scale=None, V_scale=None, err=None):
+    """Cached rows back: k_out, v_out [tokens, n_kv_heads, d_head], float32, float16 or bfloat16; seq < 0: padding."""
+    torch, where = _torch(), "spd_op_read_paged"
+    kv, i32, device = _cache_type(where, torch, dtype), torch.int32, torch.cuda.current_device()
+    shape = K.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, entries = table.shape
+    n, kind = seq.numel(), k_out.dtype
+    if not (K.dtype is kv and V.dtype is kv and table.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and V.shape == shape and pos.numel() == n and v_out.dtype is kind
+            and k_out.numel() == n * n_kv * d and v_out.numel() == n * n_kv * d and K.is_contiguous() and V.is_contiguous() and table.is_contiguous() and seq.is_contiguous()
+            and pos.is_contiguous() and k_out.is_contiguous() and v_out.is_contiguous() and K.get_device() == device and V.get_device() == device and table.get_device() == device
+            and seq.get_device() == device and pos.get_device() == device and k_out.get_device() == device and v_out.get_device() == device
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
+        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), seq=(seq, i32, (n,)), pos=(pos, i32, (n,)), k_out=(k_out, kind, (n, n_kv, d)),
+                v_out=(v_out, kind, (n, n_kv, d)), err=(err, i32, (1,)))
+    scales = _scales(where, torch, dtype, device, shape, K_scale, V_scale)
+    rc = lib().spd_op_read_paged(SPD_DTYPE[dtype], K.data_ptr(), V.data_ptr(), *scales, table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, seq.data_ptr(), pos.data_ptr(),
+                                 n, SPD_DTYPE[_io_type(where, torch, kind)], k_out.data_ptr(), v_out.data_ptr(), None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
+
+
+def spd_op_attention_paged(dtype: str, q, K, V, table, first, length, out, max_new: int, max_len: int, K_scale=None, V_scale=None, err=None):
+    """q [tokens, n_heads, d_head] (tokens may lie apart) -> out, both float32 or both the cache's type (int8 cache: float16 or bfloat16); first int32 [n_seq + 1], length int32 [n_seq]."""
+    torch, where = _torch(), "spd_op_attention_paged"
+    kv, i32, device, kind = _cache_type(where, torch, dtype), torch.int32, torch.cuda.current_device(), q.dtype
+    shape = K.shape
+    n_pages, n_kv, page_size, d = shape
+    n_seq, entries = table.shape
+    n, heads, q_d = q.shape
+    q_stride, between, within = q.stride()
+    if n <= 1:                          # (a single token's stride may be anything)
+        q_stride = heads * d
+    if max_new > _INT32 or max_len > _INT32:
+        raise ValueError(f"{where}: max_new or max_len is no 32-bit number")
+    if q_d != d or within != 1 or (between != d and heads > 1) or q.get_device() != device:
+        raise ValueError(f"{where}: q has to be [tokens, heads, {d}] on the current device, a token's heads one behind the other")
+    if not (out.dtype is kind and K.dtype is kv and V.dtype is kv and table.dtype is i32 and first.dtype is i32 and length.dtype is i32 and out.numel() == n * heads * d
+            and V.shape == shape and first.numel() == n_seq + 1 and length.numel() == n_seq and out.is_contiguous() and K.is_contiguous() and V.is_contiguous()
+            and table.is_contiguous() and first.is_contiguous() and length.is_contiguous() and out.get_device() == device and K.get_device() == device and V.get_device() == device
+            and table.get_device() == device and first.get_device() == device and length.get_device() == device
+            and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
+        _refuse(where, device, K=(K, kv, None), V=(V, kv, shape), table=(table, i32, None), first=(first, i32, (n_seq + 1,)), length=(length, i32, (n_seq,)), out=(out, kind, (n, heads, d)),
+                err=(err, i32, (1,)))
+    scales = _scales(where, torch, dtype, device, shape, K_scale, V_scale)
+    L, kinds = lib(), (SPD_DTYPE[dtype], SPD_DTYPE[_io_type(where, torch, kind)])
+    n_bytes, scratch = L.spd_op_attention_paged_scratch_bytes(*kinds, n_seq, n, heads, n_kv, d, max_new, max_len), None
+    if n_bytes:
+        buf = _scratch(torch, n_bytes, q)
+        scratch = buf.data_ptr()
+    rc = L.spd_op_attention_paged(*kinds, q.data_ptr(), q_stride, K.data_ptr(), V.data_ptr(), *scales, table.data_ptr(), n_pages, n_kv, page_size, d, n_seq, entries, first.data_ptr(),
+                                  length.data_ptr(), n, heads, max_new, max_len, out.data_ptr(), scratch, n_bytes, None if err is None else err.data_ptr(), _stream_ptr(device))
+    if rc:
+        raise SpdError(rc, where)
+
+
+def spd_op_verify_drafts(dtype: str, logits, tokens, first, u, out_tokens, out_logprobs, out_accepted, tau: float = 1.0, draft_logits=None, draft_tau: float = 1.0, err=None):
+    """logits, draft_logits [tokens, vocab] (rows may lie apart), tokens int32 and u float32 [tokens], first int32 [n_seq + 1] -> out_tokens, out_logprobs [tokens], out_accepted [n_seq]."""
+    torch, where = _torch(), "spd_op_verify_drafts"
+    kind, i32, f32, device = _kv_type(where, torch, dtype), torch.int32, torch.float32, torch.cuda.current_device()
+    n, vocab = logits.shape
+    n_seq = first.numel() - 1
+
+    def rows(name, t):
+        stride, within = t.stride()
+        if t.dtype is not kind or t.shape != (n, vocab) or (within != 1 and vocab > 1) or t.get_device() != device:
+            raise ValueError(f"{where}: {name} has to be {dtype} [{n}, {vocab}] on the current device, whole rows")
+        return stride if n > 1 else vocab
+
+    stride, draft_stride = rows("logits", logits), rows("draft_logits", draft_logits) if draft_logits is not None else 0
+    if not (tokens.dtype is i32 and first.dtype is i32 and u.dtype is f32 and out_tokens.dtype is i32 and out_logprobs.dtype is f32 and out_accepted.dtype is i32 and n_seq >= 0
+            and tokens.numel() == n and u.numel() == n and out_tokens.numel() == n and out_logprobs.numel() == n and out_accepted.numel() == n_seq
+            and tokens.is_contiguous() and first.is_contiguous() and u.is_contiguous() and out_tokens.is_contiguous() and out_logprobs.is_contiguous() and out_accepted.is_contiguous()
+            and tokens.get_device() == device and first.get_device() == device and u.get_device() == device and out_tokens.get_device() == device
+            and out_logprobs.get_device() == device and out_accepted.get_device() == device and (err is None or (err.dtype is i32 and err.numel() == 1 and err.get_device() == device))):
+        if n_seq < 0:
+            raise ValueError(f"{where}: first has one element more than there are sequences")
+        _refuse(where, device, tokens=(tokens, i32, (n,)), first=(first, i32, None), u=(u, f32, (n,)), out_tokens=(out_tokens, i32, (n,)), out_logprobs=(out_logprobs, f32, (n,)),
+                out_accepted=(out_accepted, i32, (n_seq,)), err=(err, i32, (1,)))
+    L = lib()
+    n_bytes, scratch = L.spd_op_verify_drafts_scratch_bytes(n_seq, n, vocab), None
+    if n_bytes:
+        buf = _scratch(torch, n_bytes, logits)
+        scratch = buf.data_ptr()
+    rc = L.spd_op_verify_drafts(SPD_DTYPE[dtype], logits.data_ptr(), stride, None if draft_logits is None else draft_logits.data_ptr(), draft_stride, tokens.data_ptr(), first.data_ptr(),
+                                u.data_ptr(), n_seq, n, vocab, tau, draft_tau, out_tokens.data_ptr(), out_logprobs.data_ptr(), out_accepted.data_ptr(), scratch, n_bytes,
+                                None if err is None else err.data_ptr(), _stream_ptr(device))
     if rc:
         raise SpdError(rc, where)
 

@@ -277,6 +277,19 @@ struct AppendArgs {
     float *q_out;                // [n_tokens, n_heads, d_head]
     int32_t *err;
 };
+struct AppendQ8Args {
+    AppendArgs a;                // K and V hold codes
+    float *k_scale, *v_scale;    // [n_pages, n_kv_heads, page size]
+    double log2_theta_low;       // what log2_theta leaves of the logarithm
+};
+struct ReadArgs {
+    PagedCache c;
+    const float *k_scale, *v_scale;
+    const int32_t *seq, *pos;
+    int32_t n_tokens;
+    void *k_out, *v_out;         // [n_tokens, n_kv_heads, d_head]
+    int32_t *err;
+};
 struct ReorderArgs {
     PagedCache c;                // layer 0's; layer l's pools start layer_bytes * l later
     const int32_t *parents, *len;
@@ -298,6 +311,27 @@ struct SharedAttnArgs {
     int32_t group;               // query heads per key/value head
     Divisor by_group, by_kv_heads, by_width, by_row_tiles, by_own_tiles, by_shared_chunks, by_own_chunks;
     float *part_ml, *part;       // scratch, [n_seq, n_heads, slots]: maximum and sum; O [.., d_head]
+};
+struct PagedAttnArgs {
+    PagedCache c;
+    const float *k_scale, *v_scale;  // int8 cache
+    const void *q;               // rows [n_heads, d_head] at q + t q_stride
+    int64_t q_stride;
+    void *out;                   // [n_tokens, n_heads, d_head]
+    const int32_t *first, *len;  // [n_seq + 1], [n_seq]
+    int32_t *err;
+    int32_t n_tokens, n_heads, group, max_len;
+};
+struct VerifyArgs {
+    const void *logits, *draft_logits;   // rows; draft_logits may be null
+    int64_t row_stride, draft_stride;    // elements
+    const int32_t *tokens, *first;       // [n_tokens], [n_seq + 1]
+    const float *u;                      // [n_tokens]
+    int32_t n_seq, n_tokens, vocab;
+    double by_tau, by_draft_tau;
+    int32_t *out_tokens;
+    float *out_logprobs;
+    int32_t *out_accepted, *err;
 };
 struct SelectArgs {
     const void *logits;
@@ -326,7 +360,12 @@ inline bool over_any(Span out, std::initializer_list<Span> others) {
         if (out.p && o.p && out.bytes && o.bytes && overlap(out.p, out.bytes, o.p, o.bytes)) return true;
     return false;
 }
-inline size_t pool_bytes(int dtype, const PagedCache &c) { return ((size_t)c.n_pages * c.n_kv_heads * c.d_head << c.page_shift) * (dtype == SPD_DTYPE_FP32 ? 4 : 2); }   // of one layer
+inline size_t pool_bytes(int dtype, const PagedCache &c) {   // of one layer
+    return ((size_t)c.n_pages * c.n_kv_heads * c.d_head << c.page_shift) * (dtype == SPD_DTYPE_FP32 ? 4 : dtype == SPD_DTYPE_INT8 ? 1 : 2);
+}
+inline size_t scale_bytes(const PagedCache &c) { return ((size_t)c.n_pages * c.n_kv_heads << c.page_shift) * 4; }
+// paged_cache_status for operators that take 8 bits too: scales with an int8 cache, and only with one.
+int paged_cache_status(int dtype, const PagedCache &c, int page_size, const float *k_scale, const float *v_scale);
 int paged_cache_status(int dtype, const PagedCache &c, int page_size);   // an spd_status
 PagedCache paged_cache(void *K, void *V, const int32_t *table, int n_pages, int n_kv_heads, int page_size, int d_head, int n_seq, int table_stride);
 hipError_t gemv(hipStream_t s, int dtype, int epi, const GemvArgs &a, int num_cu);

@@ -106,18 +106,182 @@ __global__ __launch_bounds__(NTP) void append_paged_kernel(const AppendArgs a) {
     }
 }
 
-template <typename KT>
-hipError_t launch_append(hipStream_t s, AppendArgs a) {
+// few tokens: one piece per thread, so that many blocks share the way to memory; many: four, so that angles and page
+// numbers are formed for more of them
+long long append_blocks(AppendArgs &a, bool &few) {
     const long long pieces = (long long)(a.n_heads + 2 * a.c.n_kv_heads) * (a.c.d_head / 4);
-    // few tokens: one piece per thread, so that many blocks share the way to memory; many: four, so that angles and page
-    // numbers are formed for more of them
-    const bool few = pieces * a.n_tokens < 4LL * NTP * 1024;
+    few = pieces * a.n_tokens < 4LL * NTP * 1024;
     const int u = few ? 1 : 4;
     a.parts = (int)((pieces + u * NTP - 1) / (u * NTP));
-    const long long blocks = (long long)a.n_tokens * a.parts;
+    return (long long)a.n_tokens * a.parts;
+}
+
+template <typename KT>
+hipError_t launch_append(hipStream_t s, AppendArgs a) {
+    bool few;
+    const long long blocks = append_blocks(a, few);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     if (few) hipLaunchKernelGGL((append_paged_kernel<KT, 1>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
     else hipLaunchKernelGGL((append_paged_kernel<KT, 4>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
+    return hipGetLastError();
+}
+
+// ---- eight bits per value ----
+
+struct q8_t { int8_t b; };
+
+// cos and sin of pos * theta^(-2i / d_head) in 64 bits: a key's place between two codes hangs on them.  2i / d_head is exact, so the logarithm's two parts times it
+// are off by 2^-106 of it, and the frequency by the last place of exp2.  The angle is reduced to a quarter turn as in rotation(); the rest of at most
+// pi / 4 goes through the Taylor series, whose first terms left out are below 2^-57.
+__device__ __forceinline__ double2 rotation64(int pos, int i, double log2_theta, double log2_theta_low, int d_head) {
+    const double part = -2.0 * i / d_head, y = part * log2_theta, low = fma(part, log2_theta, -y) + part * log2_theta_low;
+    const double f = exp2(y), angle = (double)pos * fma(f, 0.69314718055994530942 * low, f);
+    const double quarters = rint(angle * 0.63661977236758134308);                    // 2 / pi
+    double r = fma(-quarters, 1.57079632679489655800, angle);                        // pi / 2 in two parts
+    r = fma(-quarters, 6.12323399573676603587e-17, r);
+    const double z = r * r;
+    double s = 1.0, c = 1.0;
+#pragma unroll
+    for (int k = 8; k >= 1; --k) {                                                   // x - x^3/3! + .. + x^17/17!, 1 - x^2/2! + .. + x^16/16!
+        s = fma(s, -z * (1.0 / (2.0 * k * (2.0 * k + 1.0))), 1.0);
+        c = fma(c, -z * (1.0 / (2.0 * k * (2.0 * k - 1.0))), 1.0);
+    }
+    s *= r;
+    const int q = (int)((long long)quarters & 3);
+    const double cs = (q & 1) ? s : c, sn = (q & 1) ? c : s;
+    return make_double2(q == 1 || q == 2 ? -cs : cs, q >= 2 ? -sn : sn);
+}
+
+__device__ __forceinline__ float finite(float x) { return x != x ? 0.f : fminf(fmaxf(x, -3.402823466e38f), 3.402823466e38f); }
+
+// The code of x: x / scale, whose rounding to 64 bits is the nearest (a product with the inverse and one correction), to the nearest whole number.
+__device__ __forceinline__ int code_of(double x, double scale, double inv) {
+    double n = x * inv;
+    n = fma(fma(-n, scale, x), inv, n);
+    return min(max((int)rint(n), -127), 127);
+}
+
+// append_paged_kernel into codes and scales.  A row's d_head / 4 threads lie in one wave, next to each other, and find its largest value by exchanging theirs.
+template <int U>
+__global__ __launch_bounds__(NTP) void append_q8_kernel(const AppendQ8Args p) {
+    const AppendArgs &a = p.a;
+    __shared__ double2 turn[128];
+    const int tid = threadIdx.x, t = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const int d = a.c.d_head, per_head = d / 4;
+    const int q_end = a.n_heads * per_head, k_end = q_end + a.c.n_kv_heads * per_head, end = k_end + a.c.n_kv_heads * per_head;
+    const int seq = as_global(a.seq)[t], pos = as_global(a.pos)[t];
+    if (seq < 0) return;                                                              // padding
+    float4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = (part * U + u) * NTP + tid;
+        x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at < q_end) x[u] = global_load_float4(a.q + (size_t)t * a.q_stride + 4 * at);
+        else if (at < k_end) x[u] = global_load_float4(a.k + (size_t)t * a.kv_stride + 4 * (at - q_end));
+        else if (at < end) x[u] = global_load_float4(a.v + (size_t)t * a.kv_stride + 4 * (at - k_end));
+    }
+    if (seq >= a.c.n_seq || pos < 0 || (pos >> a.c.page_shift) >= a.c.table_stride) {
+        if (tid == 0) flag(a.err);
+        return;
+    }
+    const int page = as_global(a.c.table)[(size_t)seq * a.c.table_stride + (pos >> a.c.page_shift)];
+    if (tid < d / 2) turn[tid] = rotation64(pos, tid, a.log2_theta, p.log2_theta_low, d);
+    __syncthreads();
+    if (!page_ok(a.c, page)) {
+        if (tid == 0) flag(a.err);
+        return;
+    }
+    const int page_size = 1 << a.c.page_shift, row = pos & (page_size - 1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = (part * U + u) * NTP + tid;               // (threads past the end stay for the exchange)
+        const bool is_q = at < q_end, turned = at < k_end;
+        double y[4];
+        const float in[4] = {is_q ? x[u].x : finite(x[u].x), is_q ? x[u].y : finite(x[u].y), is_q ? x[u].z : finite(x[u].z), is_q ? x[u].w : finite(x[u].w)};
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            const double2 c = turn[2 * (at % per_head) + e / 2];
+            y[e] = turned ? fma((double)in[e], c.x, -((double)in[e + 1] * c.y)) : (double)in[e];
+            y[e + 1] = turned ? fma((double)in[e], c.y, (double)in[e + 1] * c.x) : (double)in[e + 1];
+        }
+        if (is_q) store_four<float>(a.q_out, (size_t)t * q_end * 4 + 4 * at, make_float4((float)y[0], (float)y[1], (float)y[2], (float)y[3]));
+        double top = fmax(fmax(fabs(y[0]), fabs(y[1])), fmax(fabs(y[2]), fabs(y[3])));
+        for (int o = 1; o < per_head; o <<= 1) top = fmax(top, __shfl_xor(top, o, WAVE));
+        if (is_q || at >= end) continue;
+        const float scale = (float)(top / 127.0);
+        const double inv = scale > 0.f ? 1.0 / (double)scale : 0.0;
+        const int of = turned ? at - q_end : at - k_end, head = of / per_head;
+        const size_t place = ((size_t)page * a.c.n_kv_heads + head) * page_size + row;
+        uint32_t codes = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) codes |= (uint32_t)(code_of(y[e], (double)scale, inv) & 0xFF) << (8 * e);
+        *(uint32_t __attribute__((address_space(1))) *)((int8_t *)(turned ? a.c.K : a.c.V) + place * d + 4 * (of % per_head)) = codes;
+        if (of % per_head == 0) as_global(turned ? p.k_scale : p.v_scale)[place] = scale;
+    }
+}
+
+hipError_t launch_append_q8(hipStream_t s, AppendQ8Args p) {
+    bool few;
+    const long long blocks = append_blocks(p.a, few);
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (few) hipLaunchKernelGGL((append_q8_kernel<1>), dim3((unsigned)blocks), dim3(NTP), 0, s, p);
+    else hipLaunchKernelGGL((append_q8_kernel<4>), dim3((unsigned)blocks), dim3(NTP), 0, s, p);
+    return hipGetLastError();
+}
+
+// Eight elements of a row, as fp32 numbers.
+template <typename KT> __device__ __forceinline__ void load_eight(const void *p, size_t i, float (&x)[8]) {
+    const u32x4 v = global_load16((const KT *)p + i);
+    Store<KT>::unpack(v, x);
+}
+template <> __device__ __forceinline__ void load_eight<float>(const void *p, size_t i, float (&x)[8]) {
+    const float4 a = global_load_float4((const float *)p + i), b = global_load_float4((const float *)p + i + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+template <> __device__ __forceinline__ void load_eight<q8_t>(const void *p, size_t i, float (&x)[8]) {
+    const u32x2 v = *(const u32x2 __attribute__((address_space(1))) *)((const int8_t *)p + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)((e < 4 ? v.x : v.y) >> (8 * (e % 4)));
+}
+
+// A thread: eight elements of one row of one token, keys in front, then values.
+template <typename KT, typename OT>
+__global__ __launch_bounds__(NTP) void read_paged_kernel(const ReadArgs a) {
+    const int d = a.c.d_head, row_pieces = a.c.n_kv_heads * d / 8;
+    const long long i = (long long)blockIdx.x * NTP + threadIdx.x;
+    const int t = (int)(i / (2 * row_pieces)), in_token = (int)(i % (2 * row_pieces));
+    if (t >= a.n_tokens) return;
+    const int seq = as_global(a.seq)[t], pos = as_global(a.pos)[t];
+    if (seq < 0) return;
+    if (seq >= a.c.n_seq || pos < 0 || (pos >> a.c.page_shift) >= a.c.table_stride) { flag(a.err); return; }
+    const int page = as_global(a.c.table)[(size_t)seq * a.c.table_stride + (pos >> a.c.page_shift)];
+    if (!page_ok(a.c, page)) { flag(a.err); return; }
+    const bool is_v = in_token >= row_pieces;
+    const int at = 8 * (is_v ? in_token - row_pieces : in_token), head = at / d, page_size = 1 << a.c.page_shift;
+    const size_t place = ((size_t)page * a.c.n_kv_heads + head) * page_size + (pos & (page_size - 1));
+    float x[8];
+    load_eight<KT>(is_v ? a.c.V : a.c.K, place * d + at % d, x);
+    if constexpr (sizeof(KT) == 1) {
+        const float scale = as_global(is_v ? a.v_scale : a.k_scale)[place];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] *= scale;
+            asm("" : "+v"(x[e]));                // (an fp32 number: a value is the same whatever type it is read in.  Product and conversion as one instruction round once)
+        }
+    }
+    void *out = is_v ? a.v_out : a.k_out;
+    const size_t to = (size_t)t * a.c.n_kv_heads * d + at;
+    store_four<OT>(out, to, make_float4(x[0], x[1], x[2], x[3]));
+    store_four<OT>(out, to + 4, make_float4(x[4], x[5], x[6], x[7]));
+}
+
+template <typename KT>
+hipError_t launch_read(hipStream_t s, const ReadArgs &a, int out_dtype) {
+    const long long pieces = (long long)a.n_tokens * 2 * (a.c.n_kv_heads * a.c.d_head / 8), blocks = (pieces + NTP - 1) / NTP;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (out_dtype == SPD_DTYPE_FP32) hipLaunchKernelGGL((read_paged_kernel<KT, float>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
+    else if (out_dtype == SPD_DTYPE_FP16) hipLaunchKernelGGL((read_paged_kernel<KT, half_t>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
+    else hipLaunchKernelGGL((read_paged_kernel<KT, bf16_t>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
     return hipGetLastError();
 }
 
@@ -261,34 +425,82 @@ int paged_cache_status(int dtype, const PagedCache &c, int page_size) {
     return SPD_OK;
 }
 
+int paged_cache_status(int dtype, const PagedCache &c, int page_size, const float *k_scale, const float *v_scale) {
+    const bool q8 = dtype == SPD_DTYPE_INT8;
+    if ((k_scale != nullptr) != q8 || (v_scale != nullptr) != q8 || ((uintptr_t)k_scale | (uintptr_t)v_scale) % 16) return SPD_EINVAL;
+    return paged_cache_status(q8 ? SPD_DTYPE_FP32 : dtype, c, page_size);
+}
+
 PagedCache paged_cache(void *K, void *V, const int32_t *table, int n_pages, int n_kv_heads, int page_size, int d_head, int n_seq, int table_stride) {
     return PagedCache{K, V, table, n_pages, n_kv_heads, page_size > 0 ? __builtin_ctz((unsigned)page_size) : 0, d_head, n_seq, table_stride};
 }
 
 }  // namespace spdk
 
+// What the two append operators look at: the arguments, and that what is written lies apart from what other blocks read.  (n_tokens 0: SPD_OK too, nothing to do.)
+static int append_status(const AppendArgs &a, size_t pool, spdk::Span k_scale, spdk::Span v_scale, float rope_theta) {
+    const PagedCache &c = a.c;
+    const int64_t heads = (int64_t)a.n_heads * c.d_head, kv_heads = (int64_t)c.n_kv_heads * c.d_head;
+    if (a.n_tokens < 0 || !(rope_theta > 0.f) || !(rope_theta < INFINITY) || a.n_heads < 0 || heads > (1 << 24) || kv_heads > (1 << 24)) return SPD_EINVAL;
+    if (a.n_tokens == 0) return SPD_OK;
+    if (!a.k || !a.v || !a.seq || !a.pos || a.kv_stride < kv_heads || a.kv_stride % 4 || ((uintptr_t)a.k | (uintptr_t)a.v) % 16) return SPD_EINVAL;
+    if ((a.q == nullptr) != (a.q_out == nullptr) || (a.q == nullptr) != (a.n_heads == 0)) return SPD_EINVAL;
+    if (a.q && (a.q_stride < heads || a.q_stride % 4 || ((uintptr_t)a.q | (uintptr_t)a.q_out) % 16)) return SPD_EINVAL;
+    if (a.q == a.q_out && a.q && a.q_stride != heads) return SPD_EINVAL;
+    const size_t out_bytes = (size_t)a.n_tokens * heads * 4, kv_bytes = ((size_t)(a.n_tokens - 1) * a.kv_stride + (size_t)kv_heads) * 4,
+                 q_bytes = a.q ? ((size_t)(a.n_tokens - 1) * a.q_stride + (size_t)heads) * 4 : 0, ids = (size_t)a.n_tokens * 4;
+    const spdk::Span sk{a.k, kv_bytes}, sv{a.v, kv_bytes}, sq{a.q, q_bytes}, st{c.table, (size_t)c.n_seq * c.table_stride * 4}, ss{a.seq, ids}, sp{a.pos, ids}, sK{c.K, pool}, sV{c.V, pool}, se{a.err, 4};
+    if (spdk::over_any(spdk::Span{a.q_out, out_bytes}, {sk, sv, a.q == a.q_out ? spdk::Span{} : sq, st, ss, sp, sK, sV, k_scale, v_scale, se})) return SPD_EINVAL;
+    if (spdk::over_any(sK, {sV, k_scale, v_scale, sk, sv, sq, st, ss, sp, se}) || spdk::over_any(sV, {k_scale, v_scale, sk, sv, sq, st, ss, sp, se})) return SPD_EINVAL;
+    if (spdk::over_any(k_scale, {v_scale, sk, sv, sq, st, ss, sp, se}) || spdk::over_any(v_scale, {sk, sv, sq, st, ss, sp, se})) return SPD_EINVAL;
+    return SPD_OK;
+}
+
 extern "C" int spd_op_append_paged(int32_t dtype, void *K, void *V, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
                                    int32_t d_head, int32_t n_seq, int32_t table_stride, const float *q, int64_t q_stride, const float *k, const float *v,
                                    int64_t kv_stride, const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t n_heads, float rope_theta,
                                    float *q_out, int32_t *err, void *hip_stream) {
     const PagedCache c = spdk::paged_cache(K, V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride);
-    const int rc = spdk::paged_cache_status(dtype, c, page_size);
+    int rc = spdk::paged_cache_status(dtype, c, page_size);
     if (rc != SPD_OK) return rc;
-    if (n_tokens < 0 || !(rope_theta > 0.f) || !(rope_theta < INFINITY) || n_heads < 0 || (long long)n_heads * d_head > (1 << 24) || (long long)n_kv_heads * d_head > (1 << 24)) return SPD_EINVAL;
-    if (n_tokens == 0) return SPD_OK;
-    if (!k || !v || !seq || !pos || kv_stride < (int64_t)n_kv_heads * d_head || kv_stride % 4 || ((uintptr_t)k | (uintptr_t)v) % 16) return SPD_EINVAL;
-    if ((q == nullptr) != (q_out == nullptr) || (q == nullptr) != (n_heads == 0)) return SPD_EINVAL;
-    if (q && (q_stride < (int64_t)n_heads * d_head || q_stride % 4 || ((uintptr_t)q | (uintptr_t)q_out) % 16)) return SPD_EINVAL;
-    if (q == q_out && q && q_stride != (int64_t)n_heads * d_head) return SPD_EINVAL;
-    // what is written lies apart from what other blocks read
-    const size_t out_bytes = (size_t)n_tokens * n_heads * d_head * 4, kv_bytes = ((size_t)(n_tokens - 1) * kv_stride + (size_t)n_kv_heads * d_head) * 4,
-                 q_bytes = q ? ((size_t)(n_tokens - 1) * q_stride + (size_t)n_heads * d_head) * 4 : 0, pool = spdk::pool_bytes(dtype, c), ids = (size_t)n_tokens * 4;
-    const spdk::Span sk{k, kv_bytes}, sv{v, kv_bytes}, sq{q, q_bytes}, st{table, (size_t)n_seq * table_stride * 4}, ss{seq, ids}, sp{pos, ids}, sK{K, pool}, sV{V, pool}, se{err, 4};
-    if (spdk::over_any(spdk::Span{q_out, out_bytes}, {sk, sv, q == q_out ? spdk::Span{} : sq, st, ss, sp, sK, sV, se}) || spdk::over_any(sK, {sV, sk, sv, sq, st, ss, sp, se}) ||
-        spdk::over_any(sV, {sk, sv, sq, st, ss, sp, se})) return SPD_EINVAL;
-    AppendArgs a{c, q, k, v, q_stride, kv_stride, seq, pos, n_tokens, n_heads, 0, log2((double)rope_theta), q_out, err};
+    const AppendArgs a{c, q, k, v, q_stride, kv_stride, seq, pos, n_tokens, n_heads, 0, log2((double)rope_theta), q_out, err};
+    rc = append_status(a, spdk::pool_bytes(dtype, c), {}, {}, rope_theta);
+    if (rc != SPD_OK || n_tokens == 0) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
     const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_append<float>(s, a) : dtype == SPD_DTYPE_FP16 ? launch_append<half_t>(s, a) : launch_append<bf16_t>(s, a);
+    return e == hipSuccess ? SPD_OK : SPD_EHIP;
+}
+
+extern "C" int spd_op_append_paged_q8(int8_t *K, int8_t *V, float *K_scale, float *V_scale, const int32_t *table, int32_t n_pages, int32_t n_kv_heads, int32_t page_size,
+                                      int32_t d_head, int32_t n_seq, int32_t table_stride, const float *q, int64_t q_stride, const float *k, const float *v, int64_t kv_stride,
+                                      const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t n_heads, float rope_theta, float *q_out, int32_t *err, void *hip_stream) {
+    const PagedCache c = spdk::paged_cache(K, V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride);
+    int rc = spdk::paged_cache_status(SPD_DTYPE_INT8, c, page_size, K_scale, V_scale);
+    if (rc != SPD_OK) return rc;
+    const double log2_theta = log2((double)rope_theta);
+    AppendQ8Args p{{c, q, k, v, q_stride, kv_stride, seq, pos, n_tokens, n_heads, 0, log2_theta, q_out, err}, K_scale, V_scale, (double)(log2l((long double)rope_theta) - (long double)log2_theta)};
+    const size_t scales = spdk::scale_bytes(c);
+    rc = append_status(p.a, spdk::pool_bytes(SPD_DTYPE_INT8, c), {K_scale, scales}, {V_scale, scales}, rope_theta);
+    if (rc != SPD_OK || n_tokens == 0) return rc;
+    return launch_append_q8((hipStream_t)hip_stream, p) == hipSuccess ? SPD_OK : SPD_EHIP;
+}
+
+extern "C" int spd_op_read_paged(int32_t dtype, const void *K, const void *V, const float *K_scale, const float *V_scale, const int32_t *table, int32_t n_pages, int32_t n_kv_heads,
+                                 int32_t page_size, int32_t d_head, int32_t n_seq, int32_t table_stride, const int32_t *seq, const int32_t *pos, int32_t n_tokens, int32_t out_dtype,
+                                 void *k_out, void *v_out, int32_t *err, void *hip_stream) {
+    const PagedCache c = spdk::paged_cache((void *)K, (void *)V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride);
+    const int rc = spdk::paged_cache_status(dtype, c, page_size, K_scale, V_scale);
+    if (rc != SPD_OK) return rc;
+    if (n_tokens < 0 || (out_dtype != SPD_DTYPE_FP32 && out_dtype != SPD_DTYPE_FP16 && out_dtype != SPD_DTYPE_BF16) || (int64_t)n_kv_heads * d_head > (1 << 24)) return SPD_EINVAL;
+    if (n_tokens == 0) return SPD_OK;
+    if (!seq || !pos || !k_out || !v_out || ((uintptr_t)k_out | (uintptr_t)v_out) % 16) return SPD_EINVAL;
+    const size_t pool = spdk::pool_bytes(dtype, c), scales = spdk::scale_bytes(c), out = (size_t)n_tokens * n_kv_heads * d_head * (out_dtype == SPD_DTYPE_FP32 ? 4 : 2), ids = (size_t)n_tokens * 4;
+    const spdk::Span so{k_out, out}, sw{v_out, out}, sK{K, pool}, sV{V, pool}, sk{K_scale, scales}, sv{V_scale, scales}, st{table, (size_t)n_seq * table_stride * 4}, ss{seq, ids}, sp{pos, ids}, se{err, 4};
+    if (spdk::over_any(so, {sw, sK, sV, sk, sv, st, ss, sp, se}) || spdk::over_any(sw, {sK, sV, sk, sv, st, ss, sp, se})) return SPD_EINVAL;
+    const ReadArgs a{c, K_scale, V_scale, seq, pos, n_tokens, k_out, v_out, err};
+    hipStream_t s = (hipStream_t)hip_stream;
+    const hipError_t e = dtype == SPD_DTYPE_FP32 ? launch_read<float>(s, a, out_dtype) : dtype == SPD_DTYPE_FP16 ? launch_read<half_t>(s, a, out_dtype)
+                         : dtype == SPD_DTYPE_BF16 ? launch_read<bf16_t>(s, a, out_dtype) : launch_read<q8_t>(s, a, out_dtype);
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }
 
