@@ -245,7 +245,8 @@ def _own_read(s):
 def _own_attend(s):
     import paper_2405_18400_amd as pkg
     c = s["c"]
-    pkg.spd_op_attention_paged(c["dtype"], s["q"], s["K"], s["V"], s["table"], s["first"], s["length"], s["out"], max(_news(c)), c["past"] + max(_news(c)),
+    news = _news(c)
+    pkg.spd_op_attention_paged(c["dtype"], s["q"], s["K"], s["V"], s["table"], s["first"], s["length"], s["out"], max(news), max(p + n for p, n in zip(_pasts(c), news)),
                                K_scale=s.get("K_scale"), V_scale=s.get("V_scale"))
     return s["out"]
 
