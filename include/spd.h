@@ -428,8 +428,8 @@ int spd_op_read_paged(int32_t dtype, const void *K, const void *V, const float *
  * d_head] at q + t q_stride (elements; a multiple of 8) and out [n_tokens, n_heads, d_head] in `io_dtype`: fp32, or the cache's own type, or with an int8 cache
  * fp16 or bf16.  In fp32 queries and probabilities go into the products with 24 bits, in 16 bits with those of the type.  max_len >= every len[s] (a host
  * value; no more than a row of the table holds) and max_new, the most new tokens of a sequence, size the launch: a sequence with more of them is taken as well, only slower.
- * A sequence whose first and len do not fit (first descends or passes n_tokens, len below its new tokens or over max_len) gets zeros for the rows that it has, *err is set.  Rows that are no
- * sequence's are left as they were.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
+ * A sequence whose first and len do not fit (first negative or past n_tokens, len below its new tokens or over max_len) gets zeros for the rows that it has; where first descends anywhere no row
+ * is written; *err is set.  Rows that are no sequence's are left as they were.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
  * sequence's last position, or behind a token's own, gets into its result. */
 size_t spd_op_attention_paged_scratch_bytes(int32_t dtype, int32_t io_dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                             int32_t max_new, int32_t max_len);
@@ -447,7 +447,8 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * A logit that is no number counts as -inf, +inf as the largest finite number.  A draft outside [0, vocab) does not stand; *err is set.
  * Outputs, DEVICE: out_accepted int32 [n_seq], the number a of drafts that stand; at first[s] .. first[s] + a of out_tokens int32 [n_tokens] those drafts and the token
  * behind them, and of out_logprobs float [n_tokens] their log p; -1 and 0 at the sequence's other tokens.  A row without a finite logit gives token 0 with log p = -inf, *err is set.  A
- * sequence without tokens, or whose first does not fit, has a = 0 and nothing else written (*err is set in the second case); rows that are no sequence's are left as they were. */
+ * sequence without tokens, or whose first is negative or past n_tokens, has a = 0 and nothing else written (*err is set in the second case); so have all where first descends anywhere.  Rows that
+ * are no sequence's are left as they were. */
 size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_tokens, int32_t vocab);
 int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t row_stride, const void *draft_logits, int64_t draft_stride, const int32_t *tokens, const int32_t *first,
                          const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, float tau, float draft_tau, int32_t *out_tokens, float *out_logprobs,

@@ -321,6 +321,9 @@ struct PagedAttnArgs {
     const int32_t *first, *len;  // [n_seq + 1], [n_seq]
     int32_t *err;
     int32_t n_tokens, n_heads, group, max_len;
+    int32_t n_tiles, splits, chunk;   // tiles of rows at most; chunks of positions, and the positions of one
+    Divisor by_group, by_kv_heads, by_splits;
+    float *part_ml, *part;       // scratch, [n_tokens, n_heads, splits]: reference and sum; O over that sum [.., d_head]
 };
 struct VerifyArgs {
     const void *logits, *draft_logits;   // rows; draft_logits may be null

@@ -1,107 +1,687 @@
 // Causal attention of every sequence's new tokens over a paged cache.
 //
-// One wave per (token, query head): 64 keys at a time, one per lane, with a running maximum and sum; then the lanes share out the
-// features.  Sums in 64 bits.
-#include "spd_device.h"
+// Rows of a key/value head: its query heads of all new tokens of a sequence, token by token.  A block owns (64 or 128 rows of a
+// sequence, key/value head, chunk of positions); rows share every key that they meet, so the tile's rows are what a cached byte is used for.  Both
+// products run on the matrix cores, S^T [key, row] = K Q^T and O^T [feature, row] = V^T P^T, in tiles of 32 keys or features by 32 rows:
+//   * S^T's accumulator holds, of one row, keys 8 i + 4 h + r (h: the lane's half, r < 4, i < 4), which is P^T's operand layout when a lane's eight k indices
+//     stand for keys 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3: probabilities never leave their registers;
+//   * V^T's operand for those keys is two reads of four keys each that LDS turns round on the way (16-bit types; fp32 values go in one by one).
+// Keys and values come through LDS in stages of 64 positions, two deep, 16 bytes per lane straight from memory; codes of 8 bits come through registers and
+// lie in LDS as fp16 numbers, which they are exactly: a key's scale multiplies its scores, a value's its probability.  Pieces of a row are permuted by the row's
+// number, so that the operand reads meet in no bank.  One barrier per stage.
+// The four waves of a block of 128 rows share out rows; of 64, rows and the stage's halves.  Where there are few tiles the positions are cut into chunks, and a second
+// kernel puts a row's chunks together in order.
+#include "spd_attention.h"
 
 #include <algorithm>
 
 using namespace spdd;
+using namespace spda;
 
 namespace {
 
-struct q8_t { int8_t b; };
+constexpr int NT = 256, NW = NT / WAVE;
+constexpr int TR = 32;                           // rows (and keys, features) of a matrix product
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-template <typename KT> __device__ __forceinline__ float element(const void *p, size_t i) {
-    if constexpr (sizeof(KT) == 1) return (float)as_global((const int8_t *)p)[i];
-    else return Store<KT>::load1(p, i);
+struct q8_t { int8_t b; };                       // codes: fp16 numbers in the products
+template <typename KT> struct InLds { typedef KT type; };
+template <> struct InLds<q8_t> { typedef half_t type; };
+
+// Queries and probabilities are PARTS numbers of the cache's type each: all 24 bits where rows are fp32, one number where they are of 16 bits.
+// P: exp2(score - reference + P_BITS) P_SCALE, as for Type.
+template <typename KT, typename IO> struct Kind {
+    typedef typename InLds<KT>::type LT;
+    static constexpr bool F32 = sizeof(KT) == 4, Q8 = sizeof(KT) == 1;
+    static constexpr int PARTS = sizeof(IO) == 4 ? Type<LT>::PARTS : 1;
+    static constexpr float P_BITS = Type<LT>::P_BITS, P_SCALE = Type<LT>::P_SCALE;
+};
+
+template <typename KT, typename IO, int DH, int RW> struct Shape {
+    typedef Kind<KT, IO> T;
+    static constexpr int KW = NW / RW, ROWS = RW * TR;                                  // waves that share out keys; rows of a block
+    static constexpr int ROWB = DH * (T::F32 ? 4 : 2), PIECES = ROWB / 16;              // bytes and 16-byte pieces of a row in LDS
+    static constexpr int SK = T::F32 && DH == 256 ? 32 : 64, NU = SK / (TR * KW);       // keys of a stage; tiles of keys of a wave
+    static constexpr int HALF = SK * ROWB, BYTES = 2 * HALF, LOADS = HALF / 16 / NT;    // K, then V; pieces per thread, of K as of V
+    static constexpr int ST = 2, LDS = ST * BYTES;
+    static constexpr int PER_CU = LDS <= 80 * 1024 && DH <= 128 && T::PARTS < 3 && !T::F32 ? 2 : 1;   // blocks side by side: 256 or 512 registers
+};
+
+// Where piece `piece` of row `key` lies.  K: 16 rows side by side are read at one piece.  V: four rows by four pieces (fp32: two rows, four apart, by eight).
+template <int PIECES> __device__ __forceinline__ int k_place(int key, int piece) {
+    return PIECES >= 16 ? piece ^ (key & 15) : PIECES == 8 ? piece ^ ((key >> 1) & 7) : piece ^ ((key >> 2) & 3);
+}
+template <int PIECES, bool F32> __device__ __forceinline__ int v_place(int key, int piece) {
+    if (F32) return PIECES >= 16 ? piece ^ (((key >> 2) & 1) << 3) : piece;
+    return PIECES >= 16 ? piece ^ ((key & 3) << 2) : PIECES == 8 ? piece ^ (((key >> 1) & 1) << 2) : piece;
 }
 
-// The sequence that token t belongs to: behind all that end before it.  (Bounded whatever `first` holds.)
-__device__ __forceinline__ int sequence_of(const int32_t *first, int n_seq, int t, int lane) {
-    int before = 0;
-    for (int i = lane; i < n_seq; i += WAVE) before += as_global(first)[i + 1] <= t;
-    for (int o = 1; o < WAVE; o <<= 1) before += __shfl_xor(before, o, WAVE);
-    return before;
+template <typename LT> __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c);
+template <> __device__ __forceinline__ f32x16 mfma32<half_t>(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 mfma32<bf16_t>(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-template <typename KT, typename IO>
-__global__ __launch_bounds__(WAVE) void paged_attn_kernel(const PagedAttnArgs p) {
-    __shared__ float q[256];
-    const int lane = threadIdx.x, t = blockIdx.x / p.n_heads, h = blockIdx.x % p.n_heads, d = p.c.d_head, kvh = h / p.group;
-    if (blockIdx.x == 0)                         // what no token may show
-        for (int i = lane; i < p.c.n_seq; i += WAVE)
-            if ((as_global(p.first)[i] < 0 || as_global(p.first)[i] > as_global(p.first)[i + 1] || as_global(p.first)[i + 1] > p.n_tokens) && p.err) *as_global(p.err) = 1;
-    const int s = sequence_of(p.first, p.c.n_seq, t, lane);
-    if (s >= p.c.n_seq) return;
-    const int a = as_global(p.first)[s], b = as_global(p.first)[s + 1], len = as_global(p.len)[s];
-    if (t < a || t >= b) return;
-    const size_t row = ((size_t)t * p.n_heads + h) * d;
-    const bool fits = a >= 0 && b <= p.n_tokens && len >= b - a && len <= p.max_len && (long long)len <= (long long)p.c.table_stride << p.c.page_shift;
-    if (!fits && p.err && lane == 0) *as_global(p.err) = 1;
-    const int n = fits ? len - (b - a) + (t - a) + 1 : 0;
-    for (int i = lane; i < d; i += WAVE) q[i] = Store<IO>::load1(p.q, (size_t)t * p.q_stride + (size_t)h * d + i);
-    __syncthreads();
-    float m = -INFINITY;
-    double l = 0.0, o[4] = {0.0, 0.0, 0.0, 0.0};
-    const float scale = 1.4426950408889634f / sqrtf((float)d);
-    const int page_size = 1 << p.c.page_shift;
-    for (int k0 = 0; k0 < n; k0 += WAVE) {
-        const int pos = k0 + lane;
-        size_t place = 0;
-        bool in = pos < n;
-        if (in) {
-            const int page = as_global(p.c.table)[(size_t)s * p.c.table_stride + (pos >> p.c.page_shift)];
-            in = (unsigned)page < (unsigned)p.c.n_pages;
-            if (!in && p.err) *as_global(p.err) = 1;
-            else place = ((size_t)page * p.c.n_kv_heads + kvh) * page_size + (pos & (page_size - 1));
-        }
-        float z = -INFINITY, vs = 1.f;
-        if (in) {
-            z = 0.f;
-            for (int i = 0; i < d; ++i) z = fmaf(q[i], element<KT>(p.c.K, place * d + i), z);
-            if constexpr (sizeof(KT) == 1) {
-                z *= as_global(p.k_scale)[place];
-                vs = as_global(p.v_scale)[place];
-            }
-            z *= scale;
-        }
-        const float mx = fmaxf(m, wave_max(z));
-        if (mx == -INFINITY && !__any(z != z)) continue;
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx), e = __builtin_amdgcn_exp2f(z - mx);
-        m = mx;
-        l = l * f + e;
-        for (int i = 0; i < 4; ++i) o[i] *= f;
-        for (int k = 0; k < WAVE; ++k) {
-            const float w = __shfl(e, k, WAVE) * __shfl(vs, k, WAVE);
-            const size_t from = (size_t)__shfl((unsigned long long)place, k, WAVE) * d;
-            if (w == 0.f) continue;
-            for (int i = 0; i < 4; ++i)
-                if (lane + i * WAVE < d) o[i] += (double)w * element<KT>(p.c.V, from + lane + i * WAVE);
+// Four rows of four 16-bit numbers per lane, turned round among 16 lanes: lane i gets four rows of column i.
+__device__ __forceinline__ u32x2 turned_read(const char *p) {
+    u32x2 v{0, 0};
+#if defined(__HIP_DEVICE_COMPILE__)
+    v = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+#endif
+    return v;
+}
+
+// Four codes as four fp16 numbers: 1024 + 128 + code, less 1152.
+__device__ __forceinline__ void codes_to_half(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+    const uint32_t x = codes ^ 0x80808080u;
+    const f16x2 off{(_Float16)-1152.f, (_Float16)-1152.f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u)) + off);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u)) + off);
+}
+
+// Two fp32 numbers as pairs of LT, PARTS of them; one: rounded to nearest.
+template <typename LT, int PARTS> __device__ __forceinline__ void probability_parts(float x, float y, uint32_t (&out)[PARTS]) {
+    if constexpr (PARTS > 1) parts_of<LT>(x, y, out);
+    else if constexpr (sizeof(LT) == 2) {
+        typedef _Float16 hpair __attribute__((ext_vector_type(2)));
+        typedef __bf16 bpair __attribute__((ext_vector_type(2)));
+        if constexpr (Type<LT>::PARTS == 2) out[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), hpair));
+        else out[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), bpair));
+    }
+}
+
+// Whether any of the 16 bytes' numbers is infinite or none.
+template <int BYTES> __device__ __forceinline__ bool not_finite(u32x4 v, bool bf) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (BYTES == 4) bad |= (v[i] & 0x7F800000u) == 0x7F800000u;
+        else {
+            const uint32_t e = bf ? 0x7F80u : 0x7C00u;
+            bad |= ((v[i] & e) == e) | (((v[i] >> 16) & e) == e);
         }
     }
-    for (int i = 1; i < WAVE; i <<= 1) l += __shfl_xor(l, i, WAVE);
-    for (int i = 0; i < 4; ++i)
-        if (lane + i * WAVE < d) Store<IO>::store1(p.out, row + lane + i * WAVE, l == 0.0 ? 0.f : (float)(o[i] / l));
+    return bad;
 }
 
-template <typename KT, typename IO>
-hipError_t launch(hipStream_t s, const PagedAttnArgs &a) {
-    hipLaunchKernelGGL((paged_attn_kernel<KT, IO>), dim3((unsigned)(a.n_tokens * a.n_heads)), dim3(WAVE), 0, s, a);
+// Which sequence a tile of rows belongs to.  Tiles are numbered so that sequence s has those from over(first[s]) + s on (over: whole tiles of its rows in front), which needs no sum over
+// sequences.  False: none, or first descends somewhere (then there is no telling whose rows are whose).
+struct Whose { int seq, a, b, tile; };
+__device__ __forceinline__ bool whose(const PagedAttnArgs &p, int tile, int log2_rows, int lane, Whose &w, bool &descends) {
+    int s = 0;
+    bool bad = false;
+    const auto start = [&](int i, int f) { return (int)(((unsigned)min(max(f, 0), p.n_tokens) * (unsigned)p.group) >> log2_rows) + i; };
+    for (int i0 = 0; i0 < p.c.n_seq; i0 += WAVE) {
+        const int i = min(i0 + lane, p.c.n_seq - 1), a = as_global(p.first)[i], b = as_global(p.first)[i + 1];
+        bad = bad || b < a;
+        s += __popcll(__ballot(i0 + lane < p.c.n_seq && start(i + 1, b) <= tile));
+    }
+    descends = __any(bad);
+    if (descends || s >= p.c.n_seq) return false;
+    w.seq = s;
+    w.a = as_global(p.first)[s];
+    w.b = as_global(p.first)[s + 1];
+    w.tile = tile - start(s, w.a);
+    return w.tile >= 0;
+}
+
+template <typename IO> __device__ __forceinline__ void store_rows(void *p, size_t i, float4 v) {
+    if constexpr (sizeof(IO) == 4) *(f32x4 __attribute__((address_space(1))) *)((float *)p + i) = f32x4{v.x, v.y, v.z, v.w};
+    else {
+        uint32_t lo[1], hi[1];
+        probability_parts<IO, 1>(v.x, v.y, lo);
+        probability_parts<IO, 1>(v.z, v.w, hi);
+        *(u32x2 __attribute__((address_space(1))) *)((uint16_t *)p + i) = u32x2{lo[0], hi[0]};
+    }
+}
+
+template <typename KT, typename IO, int DH, int RW>
+__global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_attn_kernel(const PagedAttnArgs p) {
+    typedef Kind<KT, IO> T;
+    typedef Shape<KT, IO, DH, RW> S;
+    typedef typename T::LT LT;
+    constexpr bool F32 = T::F32, Q8 = T::Q8;
+    constexpr int PARTS = T::PARTS, KW = S::KW, ROWS = S::ROWS, ROWB = S::ROWB, PIECES = S::PIECES, SK = S::SK, NU = S::NU, HALF = S::HALF, BYTES = S::BYTES, LOADS = S::LOADS;
+    constexpr int NJ = F32 ? DH / 8 : DH / 16, NF = DH / TR, PIECE_EL = F32 ? 4 : 8, LOG2_ROWS = RW == 4 ? 7 : 6;
+    extern __shared__ __align__(1024) char lds[];
+    __shared__ int bad_stage[2], odd_stage[2];               // the stage, + 1, that has a key on no page, a value that is no finite number
+    __shared__ __align__(16) float k_sc[2][SK], v_sc[2][SK];
+    __shared__ int v_exp[2];
+    __shared__ float join_m[RW][WAVE], join_l[RW][WAVE];
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane & (TR - 1), h = lane / TR, rw = wv % RW, kw = wv / RW;
+    const int d = p.c.d_head, shift = p.c.page_shift, in_page = (1 << shift) - 1, group = p.group;
+    // which rows, which positions
+    const int rest = over(blockIdx.x, p.by_kv_heads), kvh = blockIdx.x - rest * p.c.n_kv_heads, tile_r = over(rest, p.by_splits), split = rest - tile_r * p.splits;
+    Whose own;
+    bool descends;
+    const bool found = whose(p, p.n_tiles - 1 - tile_r, LOG2_ROWS, lane, own, descends);     // (late tiles see the most keys: they start first)
+    if (descends && blockIdx.x == 0 && tid == 0 && p.err) *as_global(p.err) = 1;
+    if (!found) return;
+    const int r0 = own.tile * ROWS, n = own.b - own.a, from = max(own.a, 0), n_rows = min(((min(own.b, p.n_tokens) - from) * group) - r0, ROWS);
+    if (n_rows <= 0) return;
+    const int len = as_global(p.len)[own.seq];
+    if (own.a < 0 || own.b > p.n_tokens || len < n || len > p.max_len || (long long)len > (long long)p.c.table_stride << shift) {
+        if (tid == 0 && p.err) *as_global(p.err) = 1;
+        if (split == 0)
+            for (int i = tid; i < n_rows * d / 4; i += NT) {
+                const int r = r0 + i / (d / 4), tok = over(r, p.by_group);
+                store_rows<IO>(p.out, ((size_t)(from + tok) * p.n_heads + kvh * group + r - tok * group) * d + 4 * (i % (d / 4)), make_float4(0.f, 0.f, 0.f, 0.f));
+            }
+        return;
+    }
+    const int pos0 = len - n, pos_min = pos0 + over(r0, p.by_group), pos_max = pos0 + over(r0 + n_rows - 1, p.by_group);
+    const int lo = split * p.chunk, hi = min(pos_max + 1, lo + p.chunk);
+    if (lo >= hi) return;
+    const int stages = (hi - lo + SK - 1) / SK;
+    const int r = r0 + min(rw * TR + col, n_rows - 1), tok = over(r, p.by_group), pos = pos0 + tok;       // (rows past the last repeat it)
+    const bool active = rw * TR < n_rows;
+    const int wave_lo = __builtin_amdgcn_readfirstlane(pos), wave_hi = __builtin_amdgcn_readlane(pos, TR - 1);
+    const size_t row_at = (size_t)(own.a + tok) * p.n_heads + kvh * group + r - tok * group;
+
+    const int row_bytes = d * (int)sizeof(KT);
+    const u64 head_bytes = (u64)row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
+    const char *Kh = (const char *)p.c.K + (size_t)kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)kvh * head_bytes;
+    const int32_t *entries = p.c.table + (size_t)own.seq * p.c.table_stride;
+    if (tid < 2) bad_stage[tid] = odd_stage[tid] = 0;
+    if constexpr (DH == 32) {                                // heads narrower than the tile: nothing is ever put behind their ends
+        for (int i = tid; i < S::LDS / 16; i += NT) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    // Page numbers are asked for a stage ahead of the keys on them.
+    int page[LOADS], scale_page = 0;
+    const auto ask = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) page[i] = as_global(entries)[min(lo + t * SK + (tid + i * NT) / PIECES, hi - 1) >> shift];
+        if constexpr (Q8)
+            if (tid < 2 * SK) scale_page = as_global(entries)[min(lo + t * SK + tid % SK, hi - 1) >> shift];
+    };
+    u32x2 kc[LOADS], vc[LOADS];                              // Q8: a stage's codes and scales on their way
+    float scale_in = 0.f;
+    int drop = 0, drop_next = 0, v_top = -200;               // (drop: bit i: this thread's piece i of the stage is of a key that does not count)
+    const auto fetch = [&](int t) {
+        char *to = lds + (t % 2) * BYTES + wv * (WAVE * 16);
+        drop_next = 0;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int key = (tid + i * NT) / PIECES, slot = (tid + i * NT) % PIECES, at = lo + t * SK + key, pos = min(at, hi - 1);
+            const bool ok = (unsigned)page[i] < (unsigned)p.c.n_pages;
+            bad = bad || !ok;
+            drop_next |= (int)(!ok || at >= hi) << i;
+            const u64 row = (ok ? (u64)page[i] : 0) * page_bytes + (uint32_t)((pos & in_page) * row_bytes);
+            const int kp = k_place<PIECES>(key, slot), vp = v_place<PIECES, F32>(key, slot);
+            if constexpr (Q8) {
+                if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(Kh + row + 8 * kp);
+                if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(Vh + row + 8 * vp);
+            } else {
+                if (DH > 32 || PIECE_EL * kp < d) to_lds16(Kh + row + 16 * kp, to + i * (NT * 16));
+                if (DH > 32 || PIECE_EL * vp < d) to_lds16(Vh + row + 16 * vp, to + HALF + i * (NT * 16));
+            }
+        }
+        if constexpr (Q8) {
+            if (tid < 2 * SK) {
+                const int at = lo + t * SK + tid % SK, pos = min(at, hi - 1);
+                const bool ok = (unsigned)scale_page < (unsigned)p.c.n_pages;
+                scale_in = 0.f;
+                if (ok && at < hi) scale_in = as_global(tid < SK ? p.k_scale : p.v_scale)[((((size_t)scale_page * p.c.n_kv_heads + kvh) << shift) + (pos & in_page))];
+            }
+        }
+        if (bad) {
+            bad_stage[t % 2] = t + 1;
+            if (p.err) *as_global(p.err) = 1;
+        }
+    };
+    const auto put = [&](int t) {                            // Q8: codes and scales to LDS
+        char *to = lds + (t % 2) * BYTES;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int slot = (tid + i * NT) % PIECES, key = (tid + i * NT) / PIECES;
+            u32x4 x;
+            uint32_t a, b;
+            codes_to_half(kc[i].x, a, b); x.x = a; x.y = b;
+            codes_to_half(kc[i].y, a, b); x.z = a; x.w = b;
+            if (DH > 32 || 8 * k_place<PIECES>(key, slot) < d) *(u32x4 *)(to + (tid + i * NT) * 16) = x;
+            codes_to_half(vc[i].x, a, b); x.x = a; x.y = b;
+            codes_to_half(vc[i].y, a, b); x.z = a; x.w = b;
+            if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + (tid + i * NT) * 16) = x;
+        }
+        if (wv == 0) k_sc[t % 2][tid] = scale_in;
+        if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
+            const float size = fabsf(scale_in);
+            int ex = -200;
+            if (size > 0.f && size < INFINITY) (void)frexpf(size, &ex);
+#pragma unroll
+            for (int o = 1; o < WAVE; o <<= 1) ex = max(ex, __shfl_xor(ex, o, WAVE));
+            v_top = max(v_top, ex);
+            v_sc[t % 2][tid - SK] = ldexpf(scale_in, -v_top);
+            if (lane == 0) v_exp[t % 2] = v_top;
+        }
+    };
+
+    ask(0);
+    // this lane's query: its row's features 16 j + 8 h .. + 7 (fp32: 8 j + 4 h .. + 3)
+    u32x4 Q[NJ][PARTS];
+    float scale = 1.4426950408889634f / sqrtf((float)d);     // to logarithms of base 2
+    {
+        const size_t q_at = (size_t)(own.a + tok) * p.q_stride + (size_t)(kvh * group + r - tok * group) * d;
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int f = 8 * j + 4 * h;
+                const float4 x = DH > 32 || f < d ? global_load_float4((const float *)p.q + q_at + f) : make_float4(0.f, 0.f, 0.f, 0.f);
+                Q[j][0] = u32x4{__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z), __float_as_uint(x.w)};
+            }
+        } else {
+            float x[NJ][8];
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int f = 16 * j + 8 * h;
+                const bool in = DH > 32 || f < d;
+                if constexpr (sizeof(IO) == 4) {
+                    const float4 a = in ? global_load_float4((const float *)p.q + q_at + f) : make_float4(0.f, 0.f, 0.f, 0.f), b = in ? global_load_float4((const float *)p.q + q_at + f + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    x[j][0] = a.x; x[j][1] = a.y; x[j][2] = a.z; x[j][3] = a.w; x[j][4] = b.x; x[j][5] = b.y; x[j][6] = b.z; x[j][7] = b.w;
+                } else {
+                    Q[j][0] = in ? global_load16((const uint16_t *)p.q + q_at + f) : u32x4{0, 0, 0, 0};
+                    Store<IO>::unpack(Q[j][0], x[j]);
+                }
+            }
+            if constexpr (!(sizeof(IO) == 2 && Type<IO>::PARTS == Type<LT>::PARTS)) {        // (rows of the products' own type go in as they are)
+                float up = 1.f, down = 1.f;
+                if constexpr (Type<LT>::PARTS == 2) {
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
+                    top = fmaxf(top, __shfl_xor(top, TR, WAVE));
+                    scaling(top, up, down);
+                }
+                scale *= down;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        uint32_t part[PARTS];
+                        if constexpr (PARTS > 1) query_parts<LT>(x[j][e] * up, x[j][e + 1] * up, part);
+                        else probability_parts<LT, 1>(x[j][e] * up, x[j][e + 1] * up, part);
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) Q[j][q][e / 2] = part[q];
+                    }
+            }
+        }
+    }
+    f32x16 o[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[f][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    int o_exp = -200;                                        // Q8: O is held by this power of two
+    __syncthreads();                                         // (the stages' marks)
+    fetch(0);
+    drop = drop_next;
+    if (stages > 1) ask(1);
+    if constexpr (Q8) put(0);
+
+    for (int t = 0; t < stages; ++t) {
+        const int stage0 = lo + t * SK;
+        char *const k_tile = lds + (t % 2) * BYTES, *const v_tile = k_tile + HALF;
+        if constexpr (!Q8) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // Values that do not count are zero; one that some rows see and others do not must not be what zero times it is not zero.
+            if (drop) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i)
+                    if ((drop >> i) & 1) *(u32x4 *)(v_tile + (tid + i * NT) * 16) = u32x4{0, 0, 0, 0};
+            }
+            if (stage0 + SK - 1 > pos_min) {
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) odd = odd || not_finite<sizeof(LT)>(*(const u32x4 *)(v_tile + (tid + i * NT) * 16), Type<LT>::PARTS == 3);
+                if (odd) odd_stage[t % 2] = t + 1;
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 1 < stages) {
+            fetch(t + 1);
+            if (t + 2 < stages) ask(t + 2);
+        }
+        const bool any_bad = bad_stage[t % 2] == t + 1;
+        const int tb = stage0 + kw * (TR * NU), key_base = kw * (TR * NU);
+        if (!Q8 && odd_stage[t % 2] == t + 1) {              // seldom: rows that see such a value get no number at its feature, and it counts as zero from here on
+            if (active)
+                for (int key = key_base; key < key_base + TR * NU; ++key) {
+                    const bool seen = stage0 + key <= pos;
+#pragma unroll
+                    for (int f = 0; f < NF; ++f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int feature = TR * f + 8 * (i / 4) + 4 * h + i % 4;
+                            const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(key, feature / PIECE_EL) + feature % PIECE_EL * (int)sizeof(LT);
+                            bool odd;
+                            if constexpr (F32) odd = (*(const uint32_t *)at & 0x7F800000u) == 0x7F800000u;
+                            else {
+                                const uint32_t e = Type<LT>::PARTS == 3 ? 0x7F80u : 0x7C00u;
+                                odd = (*(const uint16_t *)at & e) == e;
+                            }
+                            if (odd && seen) o[f][i] = NAN;
+                        }
+                }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                u32x4 *at = (u32x4 *)(v_tile + (tid + i * NT) * 16);
+                u32x4 x = *at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (F32) x[e] = (x[e] & 0x7F800000u) == 0x7F800000u ? 0 : x[e];
+                    else {
+                        const uint32_t ex = Type<LT>::PARTS == 3 ? 0x7F80u : 0x7C00u;
+                        if ((x[e] & ex) == ex) x[e] &= 0xFFFF0000u;
+                        if (((x[e] >> 16) & ex) == ex) x[e] &= 0xFFFFu;
+                    }
+                }
+                *at = x;
+            }
+            __syncthreads();
+        }
+        if (active && tb <= wave_hi) {
+            f32x16 st[NU];
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[u][i] = 0.f;
+                const int key = key_base + TR * u + col;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const u32x4 k = *(const u32x4 *)(k_tile + key * ROWB + 16 * k_place<PIECES>(key, 2 * j + h));
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) st[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[c]), __uint_as_float(Q[j][0][c]), st[u], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int q = PARTS - 1; q >= 0; --q) st[u] = mfma32<LT>(k, Q[j][q], st[u]);
+                    }
+                }
+                if constexpr (Q8) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 s = *(const float4 *)&k_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
+                        st[u][i] *= s.x; st[u][i + 1] *= s.y; st[u][i + 2] *= s.z; st[u][i + 3] *= s.w;
+                    }
+                }
+            }
+            const bool masked = tb + TR * NU - 1 > wave_lo || any_bad;
+            if (masked) {                                    // keys behind a row's own position, or on no page: no score
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int at = tb + TR * u + 2 * i + 4 * h;          // (four keys lie on one page)
+                        const bool ok = !any_bad || (unsigned)as_global(entries)[min(at, hi - 1) >> shift] < (unsigned)p.c.n_pages;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) st[u][i + e] = ok && at + e <= pos ? st[u][i + e] : -INFINITY;
+                    }
+            }
+            // The reference is raised where a probability would pass 2^SLACK; only that row's, so that a row's result hangs on nothing but itself.
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[u][i]);
+            mx *= scale;
+            if (__any((mx > m + SLACK) | (fabsf(m) > FAR))) {
+                mx = fmaxf(mx, __shfl_xor(mx, TR, WAVE));    // the lane's halves hold different keys of the same rows
+                mx = mx > m + SLACK ? mx : m;
+                const float corr = exp2_below(m, mx);
+                m = mx;
+                l *= corr;
+#pragma unroll
+                for (int f = 0; f < NF; ++f)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[f][i] *= corr;
+                if (__any((fabsf(m) > FAR) & (m != -INFINITY))) {        // far from zero, an exponent is formed from the rounded score
+                    const float inv = __builtin_amdgcn_rcpf(scale);
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) st[u][i] = fabsf(m) > FAR && m != -INFINITY ? ((st[u][i] * scale - m) + T::P_BITS) * inv : st[u][i];
+                }
+            }
+            const float ref = fabsf(m) > FAR ? 0.f : m - T::P_BITS;      // (-inf, nothing seen yet: no score either)
+            if constexpr (Q8) {
+                const int ex = v_exp[t % 2];
+                if (ex != o_exp) {
+                    const float f0 = ldexpf(1.f, o_exp - ex);
+                    o_exp = ex;
+#pragma unroll
+                    for (int f = 0; f < NF; ++f)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[f][i] *= f0;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                if constexpr (F32) {
+                    float pf[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        pf[i] = __builtin_amdgcn_exp2f(fmaf(st[u][i], scale, -ref)) * T::P_SCALE;
+                        l += pf[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = key_base + TR * u + 8 * (i / 4) + 4 * h + i % 4;
+#pragma unroll
+                        for (int f = 0; f < NF; ++f) {
+                            const float v = *(const float *)(v_tile + key * ROWB + 16 * v_place<PIECES, F32>(key, 8 * f + col / 4) + 4 * (col % 4));
+                            o[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pf[i], o[f], 0, 0, 0);
+                        }
+                    }
+                } else {
+                    u32x4 pt[2][PARTS];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        float pf[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            pf[e] = __builtin_amdgcn_exp2f(fmaf(st[u][i + e], scale, -ref));
+                            if (T::P_SCALE != 1.f) pf[e] *= T::P_SCALE;
+                        }
+                        l += (pf[0] + pf[1]) + (pf[2] + pf[3]);
+                        if constexpr (Q8) {
+                            const float4 s = *(const float4 *)&v_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
+                            const float by[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) pf[e] = masked && pf[e] == 0.f ? 0.f : pf[e] * by[e];
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            uint32_t part[PARTS];
+                            probability_parts<LT, PARTS>(pf[e], pf[e + 1], part);
+#pragma unroll
+                            for (int q = 0; q < PARTS; ++q) pt[i / 8][q][(i % 8) / 2 + e / 2] = part[q];
+                        }
+                    }
+                    const int t4 = (lane % 16) / 4, fg = (lane / 16) % 2;
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const int key = key_base + TR * u + 16 * g + 4 * h + t4;
+#pragma unroll
+                        for (int f = 0; f < NF; ++f) {
+                            const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(t4, 4 * f + 2 * fg + (lane % 4) / 2) + 8 * (lane % 2);     // (a place hangs on key % 4 alone)
+                            const u32x2 x = turned_read(at), y = turned_read(at + 8 * ROWB);
+                            const u32x4 v{x.x, x.y, y.x, y.y};
+#pragma unroll
+                            for (int q = PARTS - 1; q >= 0; --q) o[f] = mfma32<LT>(v, pt[g][q], o[f]);
+                        }
+                    }
+                }
+            }
+        }
+        if constexpr (Q8)
+            if (t + 1 < stages) put(t + 1);
+        drop = drop_next;
+    }
+    l += __shfl_xor(l, TR, WAVE);
+    if constexpr (KW > 1) {                                  // two waves have shared out the keys of the same rows
+        __syncthreads();
+        float *O = (float *)lds + rw * (NF * 16) * WAVE + lane;
+        if (kw == 1) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) O[(f * 16 + i) * WAVE] = o[f][i];
+            join_m[rw][lane] = m;
+            join_l[rw][lane] = l;
+            if (Q8 && lane == 0) v_sc[0][rw] = (float)o_exp;
+        }
+        __syncthreads();
+        if (kw == 1) return;
+        const float m1 = join_m[rw][lane], M = fmaxf(m, m1);
+        float f0 = exp2_below(m, M), f1 = exp2_below(m1, M);
+        l = l * f0 + join_l[rw][lane] * f1;
+        if constexpr (Q8) {                                  // (a wave with no key to see in the last stages has not followed their scales)
+            const int ex1 = (int)v_sc[0][rw], ex = max(o_exp, ex1);
+            f0 = ldexpf(f0, o_exp - ex);
+            f1 = ldexpf(f1, ex1 - ex);
+            o_exp = ex;
+        }
+        m = M;
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[f][i] = o[f][i] * f0 + O[(f * 16 + i) * WAVE] * f1;
+    }
+    if (!active || rw * TR + col >= n_rows) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;              // (nothing seen: zeros)
+    const size_t at = p.splits > 1 ? row_at * p.splits + split : row_at;
+    if (p.splits > 1 && h == 0) {
+        as_global(p.part_ml)[2 * at] = m;
+        as_global(p.part_ml)[2 * at + 1] = l;
+    }
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int feature = TR * f + 2 * i + 4 * h;
+            if (DH == 32 && feature >= d) continue;
+            float4 y = make_float4(o[f][i] * inv, o[f][i + 1] * inv, o[f][i + 2] * inv, o[f][i + 3] * inv);
+            if constexpr (Q8) y = make_float4(ldexpf(y.x, o_exp), ldexpf(y.y, o_exp), ldexpf(y.z, o_exp), ldexpf(y.w, o_exp));
+            if (p.splits > 1) store_rows<float>(p.part, at * d + feature, y);
+            else store_rows<IO>(p.out, at * d + feature, y);
+        }
+}
+
+// A wave per row puts its chunks together: d_head / 4 lanes a chunk, chunks side by side, sums in a fixed order.
+constexpr int SPLITS_MAX = WAVE;
+template <typename IO>
+__global__ __launch_bounds__(NT) void paged_merge_kernel(const PagedAttnArgs p) {
+    const int lane = threadIdx.x & (WAVE - 1), d = p.c.d_head, per = d / 4, side = WAVE / per;
+    const int row = blockIdx.x * NW + threadIdx.x / WAVE, t = row / p.n_heads;
+    if (t >= p.n_tokens) return;
+    int s = 0;
+    bool bad = false;
+    for (int i0 = 0; i0 < p.c.n_seq; i0 += WAVE) {
+        const int i = min(i0 + lane, p.c.n_seq - 1), a = as_global(p.first)[i], b = as_global(p.first)[i + 1];
+        bad = bad || b < a;
+        s += __popcll(__ballot(i0 + lane < p.c.n_seq && b <= t));
+    }
+    if (__any(bad) || s >= p.c.n_seq) return;
+    const int a = as_global(p.first)[s], b = as_global(p.first)[s + 1], len = as_global(p.len)[s], n = b - a;
+    if (t < a || a < 0 || b > p.n_tokens || len < n || len > p.max_len || (long long)len > (long long)p.c.table_stride << p.c.page_shift) return;    // (not theirs, or zeros already)
+    const int chunks = (len - n + t - a) / p.chunk + 1;
+    const size_t at = (size_t)row * p.splits;
+    float m = -INFINITY, l = 0.f;
+    if (lane < chunks) {
+        m = as_global(p.part_ml)[2 * (at + lane)];
+        l = as_global(p.part_ml)[2 * (at + lane) + 1];
+    }
+    float M = m;
+#pragma unroll
+    for (int o = 1; o < WAVE; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, WAVE));
+    l *= exp2_below(m, M);
+    float L = l;
+#pragma unroll
+    for (int o = 1; o < WAVE; o <<= 1) L += __shfl_xor(L, o, WAVE);
+    l = L == 0.f ? 0.f : l / L;                              // a chunk's share
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < chunks; c0 += side) {
+        const int c = c0 + lane / per;
+        const float f = __shfl(l, min(c, WAVE - 1), WAVE);
+        if (c >= chunks || f == 0.f) continue;
+        const float4 x = global_load_float4(p.part + (at + c) * d + 4 * (lane % per));
+        y.x += f * x.x; y.y += f * x.y; y.z += f * x.z; y.w += f * x.w;
+    }
+    for (int o = per; o < WAVE; o <<= 1) {
+        y.x += __shfl_xor(y.x, o, WAVE); y.y += __shfl_xor(y.y, o, WAVE); y.z += __shfl_xor(y.z, o, WAVE); y.w += __shfl_xor(y.w, o, WAVE);
+    }
+    if (lane < per) store_rows<IO>(p.out, (size_t)row * d + 4 * lane, y);
+}
+
+// How a call is cut.
+struct Cut { int rows, splits, chunk; };
+constexpr int CUS = 256, CHUNK_MIN = 256;
+Cut cut_for(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int d_head, int max_new, int max_len) {
+    const long long group = n_heads / n_kv_heads;
+    Cut c;
+    c.rows = std::max(1, max_new) * group <= 64 && !(dtype == SPD_DTYPE_FP32 && d_head == 256) ? 64 : 128;
+    const long long blocks = std::max<long long>(n_seq, (n_tokens * group + c.rows - 1) / c.rows) * n_kv_heads;
+    const int positions = std::max(1, max_len);
+    long long n = std::min<long long>(std::max<long long>(1, 2 * CUS / blocks), (positions + CHUNK_MIN - 1) / CHUNK_MIN);
+    n = std::min<long long>(n, SPLITS_MAX);
+    c.chunk = (int)(((positions + n - 1) / n + 63) / 64 * 64);
+    c.splits = (positions + c.chunk - 1) / c.chunk;
+    return c;
+}
+
+template <typename KT, typename IO, int DH, int RW>
+hipError_t launch_rows(hipStream_t s, PagedAttnArgs a) {
+    typedef Shape<KT, IO, DH, RW> S;
+    a.n_tiles = (int)((long long)a.n_tokens * a.group / S::ROWS + a.c.n_seq);
+    const long long blocks = (long long)a.n_tiles * a.c.n_kv_heads * a.splits;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    if (S::LDS > 60 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void *)paged_attn_kernel<KT, IO, DH, RW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((paged_attn_kernel<KT, IO, DH, RW>), dim3((unsigned)blocks), dim3(NT), S::LDS, s, a);
+    if (a.splits > 1) hipLaunchKernelGGL(paged_merge_kernel<IO>, dim3((unsigned)(((long long)a.n_tokens * a.n_heads + NW - 1) / NW)), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
 
+template <typename KT, typename IO>
+hipError_t launch(hipStream_t s, const PagedAttnArgs &a, int rows) {
+    const int d = a.c.d_head;
+    if (rows == 64) {
+        if (d <= 32) return launch_rows<KT, IO, 32, 2>(s, a);
+        if (d == 64) return launch_rows<KT, IO, 64, 2>(s, a);
+        if (d == 128) return launch_rows<KT, IO, 128, 2>(s, a);
+        if constexpr (sizeof(KT) != 4) return launch_rows<KT, IO, 256, 2>(s, a);
+    }
+    if (d <= 32) return launch_rows<KT, IO, 32, 4>(s, a);
+    if (d == 64) return launch_rows<KT, IO, 64, 4>(s, a);
+    if (d == 128) return launch_rows<KT, IO, 128, 4>(s, a);
+    return launch_rows<KT, IO, 256, 4>(s, a);
+}
+
 bool io_fits(int dtype, int io) {
-    if (io == SPD_DTYPE_FP32) return true;
-    return dtype == SPD_DTYPE_INT8 ? io == SPD_DTYPE_FP16 || io == SPD_DTYPE_BF16 : dtype == io;
+    if (io == SPD_DTYPE_FP32) return dtype >= SPD_DTYPE_FP32 && dtype <= SPD_DTYPE_INT8;
+    return dtype == SPD_DTYPE_INT8 ? io == SPD_DTYPE_FP16 || io == SPD_DTYPE_BF16 : dtype == io && io != SPD_DTYPE_INT8;
 }
 
 }  // namespace
 
 extern "C" size_t spd_op_attention_paged_scratch_bytes(int32_t dtype, int32_t io_dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                                        int32_t max_new, int32_t max_len) {
-    (void)dtype; (void)io_dtype; (void)n_seq; (void)n_tokens; (void)n_heads; (void)n_kv_heads; (void)d_head; (void)max_new; (void)max_len;
-    return 0;
+    if (!io_fits(dtype, io_dtype) || n_seq <= 0 || n_tokens <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || d_head <= 0 || max_new < 0 || max_len < 0) return 0;
+    const Cut c = cut_for(dtype, n_seq, n_tokens, n_heads, n_kv_heads, d_head, max_new, max_len);
+    const size_t parts = (size_t)n_tokens * n_heads * c.splits;
+    return c.splits > 1 ? up256(parts * 8) + up256(parts * d_head * 4) : 0;
 }
 
 extern "C" int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64_t q_stride, const void *K, const void *V, const float *K_scale, const float *V_scale,
@@ -125,12 +705,15 @@ extern "C" int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const voi
     const spdk::Span sq{q, q_bytes}, so{out, rows}, sK{K, pool}, sV{V, pool}, sk{K_scale, scales}, sv{V_scale, scales}, st{table, (size_t)n_seq * table_stride * 4},
         sf{first, (size_t)(n_seq + 1) * 4}, sl{len, (size_t)n_seq * 4}, se{err, 4}, sw{scratch, need};
     if (spdk::over_any(so, {sq, sK, sV, sk, sv, st, sf, sl, se, sw}) || spdk::over_any(sw, {sq, sK, sV, sk, sv, st, sf, sl, se})) return SPD_EINVAL;
-    PagedAttnArgs a{c, K_scale, V_scale, q, q_stride, out, first, len, err, n_tokens, n_heads, n_heads / n_kv_heads, max_len};
+    const Cut cut = cut_for(dtype, n_seq, n_tokens, n_heads, n_kv_heads, d_head, max_new, max_len);
+    const int group = n_heads / n_kv_heads;
+    PagedAttnArgs a{c, K_scale, V_scale, q, q_stride, out, first, len, err, n_tokens, n_heads, group, max_len, 0, cut.splits, cut.chunk, divisor(group), divisor(n_kv_heads), divisor(cut.splits),
+                    (float *)scratch, (float *)((char *)scratch + up256((size_t)n_tokens * n_heads * cut.splits * 8))};
     hipStream_t s = (hipStream_t)hip_stream;
-    hipError_t e = hipErrorInvalidValue;
-    if (dtype == SPD_DTYPE_FP32) e = launch<float, float>(s, a);
-    else if (dtype == SPD_DTYPE_FP16) e = io_dtype == SPD_DTYPE_FP32 ? launch<half_t, float>(s, a) : launch<half_t, half_t>(s, a);
-    else if (dtype == SPD_DTYPE_BF16) e = io_dtype == SPD_DTYPE_FP32 ? launch<bf16_t, float>(s, a) : launch<bf16_t, bf16_t>(s, a);
-    else e = io_dtype == SPD_DTYPE_FP32 ? launch<q8_t, float>(s, a) : io_dtype == SPD_DTYPE_FP16 ? launch<q8_t, half_t>(s, a) : launch<q8_t, bf16_t>(s, a);
+    hipError_t e;
+    if (dtype == SPD_DTYPE_FP32) e = launch<float, float>(s, a, cut.rows);
+    else if (dtype == SPD_DTYPE_FP16) e = io_dtype == SPD_DTYPE_FP32 ? launch<half_t, float>(s, a, cut.rows) : launch<half_t, half_t>(s, a, cut.rows);
+    else if (dtype == SPD_DTYPE_BF16) e = io_dtype == SPD_DTYPE_FP32 ? launch<bf16_t, float>(s, a, cut.rows) : launch<bf16_t, bf16_t>(s, a, cut.rows);
+    else e = io_dtype == SPD_DTYPE_FP32 ? launch<q8_t, float>(s, a, cut.rows) : io_dtype == SPD_DTYPE_FP16 ? launch<q8_t, half_t>(s, a, cut.rows) : launch<q8_t, bf16_t>(s, a, cut.rows);
     return e == hipSuccess ? SPD_OK : SPD_EHIP;
 }

@@ -50,7 +50,9 @@ __global__ __launch_bounds__(NTV) void verify_kernel(const VerifyArgs a) {
     __shared__ int chosen;
     const int s = blockIdx.x, tid = threadIdx.x;
     const int lo = as_global(a.first)[s], hi = as_global(a.first)[s + 1];
-    const bool fits = lo >= 0 && lo <= hi && hi <= a.n_tokens;
+    int descends = 0;
+    for (int i = tid; i < a.n_seq; i += NTV) descends |= as_global(a.first)[i + 1] < as_global(a.first)[i];
+    const bool fits = !__syncthreads_or(descends) && lo >= 0 && hi <= a.n_tokens;
     if (!fits || lo == hi) {
         if (tid == 0) {
             as_global(a.out_accepted)[s] = 0;
