@@ -36,14 +36,16 @@ template <typename KT, typename IO> struct Kind {
     typedef typename InLds<KT>::type LT;
     static constexpr bool F32 = sizeof(KT) == 4, Q8 = sizeof(KT) == 1;
     static constexpr int PARTS = sizeof(IO) == 4 ? Type<LT>::PARTS : 1;
-    static constexpr float P_BITS = Type<LT>::P_BITS, P_SCALE = Type<LT>::P_SCALE;
+    // (one number of 16 bits: an exponent that is off by 2^-20 does not show, and the factor would be an instruction per key)
+    static constexpr bool IN_EXPONENT = PARTS == 1 && !F32;
+    static constexpr float P_SCALE = IN_EXPONENT ? 1.f : Type<LT>::P_SCALE, P_BITS = Type<LT>::PARTS == 2 ? Type<LT>::P_BITS : IN_EXPONENT ? -24.f : 0.f;
 };
 
 template <typename KT, typename IO, int DH, int RW> struct Shape {
     typedef Kind<KT, IO> T;
     static constexpr int KW = NW / RW, ROWS = RW * TR;                                  // waves that share out keys; rows of a block
     static constexpr int ROWB = DH * (T::F32 ? 4 : 2), PIECES = ROWB / 16;              // bytes and 16-byte pieces of a row in LDS
-    static constexpr int SK = T::F32 && DH == 256 ? 32 : 64, NU = SK / (TR * KW);       // keys of a stage; tiles of keys of a wave
+    static constexpr int SK = DH == 256 && KW == 1 ? 32 : 64, NU = SK / (TR * KW);       // keys of a stage; tiles of keys of a wave
     static constexpr int HALF = SK * ROWB, BYTES = 2 * HALF, LOADS = HALF / 16 / NT;    // K, then V; pieces per thread, of K as of V
     static constexpr int ST = 2, LDS = ST * BYTES;
     static constexpr int PER_CU = LDS <= 80 * 1024 && DH <= 128 && T::PARTS < 3 && !T::F32 ? 2 : 1;   // blocks side by side: 256 or 512 registers
@@ -92,6 +94,17 @@ template <typename LT, int PARTS> __device__ __forceinline__ void probability_pa
         if constexpr (Type<LT>::PARTS == 2) out[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), hpair));
         else out[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{x, y}), bpair));
     }
+}
+
+// Adds the two numbers of a pair.
+template <typename LT> __device__ __forceinline__ float pair_sum(uint32_t pair, float sum) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __bf16 bpair __attribute__((ext_vector_type(2)));
+    if constexpr (Type<LT>::PARTS == 2) return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bpair, pair), __builtin_bit_cast(bpair, 0x3F803F80u), sum, false);
+#else
+    return sum;
+#endif
 }
 
 // Whether any of the 16 bytes' numbers is infinite or none.
@@ -182,52 +195,71 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const int wave_lo = __builtin_amdgcn_readfirstlane(pos), wave_hi = __builtin_amdgcn_readlane(pos, TR - 1);
     const size_t row_at = (size_t)(own.a + tok) * p.n_heads + kvh * group + r - tok * group;
 
-    const int row_bytes = d * (int)sizeof(KT);
-    const u64 head_bytes = (u64)row_bytes << shift, page_bytes = head_bytes * p.c.n_kv_heads;
-    const char *Kh = (const char *)p.c.K + (size_t)kvh * head_bytes, *Vh = (const char *)p.c.V + (size_t)kvh * head_bytes;
+    const int row_bytes = d * (int)sizeof(KT), row_shift = 31 - __builtin_clz((unsigned)row_bytes), head_shift = row_shift + shift;
+    const char *K = (const char *)p.c.K, *V = (const char *)p.c.V;
     const int32_t *entries = p.c.table + (size_t)own.seq * p.c.table_stride;
     if (tid < 2) bad_stage[tid] = odd_stage[tid] = 0;
     if constexpr (DH == 32) {                                // heads narrower than the tile: nothing is ever put behind their ends
         for (int i = tid; i < S::LDS / 16; i += NT) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
-    // Page numbers are asked for a stage ahead of the keys on them.
+    // A wave's piece i of a stage is KEYS keys side by side, which lie on one page (but where a page is shorter than that): page numbers, asked for a stage ahead of the keys on them, and
+    // addresses are the wave's, a lane's part of them stays the same.
+    constexpr int KEYS = WAVE / PIECES;
+    const bool whole = KEYS <= 4 || KEYS <= 1 << shift;
     int page[LOADS], scale_page = 0;
     const auto ask = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) page[i] = as_global(entries)[min(lo + t * SK + (tid + i * NT) / PIECES, hi - 1) >> shift];
+        for (int i = 0; i < LOADS; ++i) {
+            const int key = (wv * WAVE + i * NT) / PIECES;
+            page[i] = as_global(entries)[whole ? min(lo + t * SK + key, (hi - 1) & ~(KEYS - 1)) >> shift : min(lo + t * SK + key + lane / PIECES, hi - 1) >> shift];
+        }
         if constexpr (Q8)
-            if (tid < 2 * SK) scale_page = as_global(entries)[min(lo + t * SK + tid % SK, hi - 1) >> shift];
+            if (wv < 2) scale_page = as_global(entries)[min(lo + t * SK + lane % SK, hi - 1) >> shift];
     };
     u32x2 kc[LOADS], vc[LOADS];                              // Q8: a stage's codes and scales on their way
     float scale_in = 0.f;
     int drop = 0, drop_next = 0, v_top = -200;               // (drop: bit i: this thread's piece i of the stage is of a key that does not count)
     const auto fetch = [&](int t) {
         char *to = lds + (t % 2) * BYTES + wv * (WAVE * 16);
+        const bool end = lo + (t + 1) * SK > hi;
         drop_next = 0;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int key = (tid + i * NT) / PIECES, slot = (tid + i * NT) % PIECES, at = lo + t * SK + key, pos = min(at, hi - 1);
-            const bool ok = (unsigned)page[i] < (unsigned)p.c.n_pages;
-            bad = bad || !ok;
-            drop_next |= (int)(!ok || at >= hi) << i;
-            const u64 row = (ok ? (u64)page[i] : 0) * page_bytes + (uint32_t)((pos & in_page) * row_bytes);
+            const int key0 = (wv * WAVE + i * NT) / PIECES, key = key0 + lane / PIECES, slot = lane % PIECES, at = lo + t * SK + key;
             const int kp = k_place<PIECES>(key, slot), vp = v_place<PIECES, F32>(key, slot);
-            if constexpr (Q8) {
-                if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(Kh + row + 8 * kp);
-                if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(Vh + row + 8 * vp);
+            const char *k_row, *v_row;                       // the wave's first row, or (short pages) the lane's
+            uint32_t off;
+            bool ok;
+            if (whole) {
+                const int pg = __builtin_amdgcn_readfirstlane(page[i]), pos0 = min(lo + t * SK + key0, (hi - 1) & ~(KEYS - 1));
+                ok = (unsigned)pg < (unsigned)p.c.n_pages;
+                const u64 row = ((u64)(uint32_t)((ok ? pg : 0) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(pos0 & in_page) << row_shift);
+                k_row = K + row; v_row = V + row;
+                off = (uint32_t)(lane / PIECES) << row_shift;
             } else {
-                if (DH > 32 || PIECE_EL * kp < d) to_lds16(Kh + row + 16 * kp, to + i * (NT * 16));
-                if (DH > 32 || PIECE_EL * vp < d) to_lds16(Vh + row + 16 * vp, to + HALF + i * (NT * 16));
+                ok = (unsigned)page[i] < (unsigned)p.c.n_pages;
+                const u64 row = ((u64)(uint32_t)((ok ? page[i] : 0) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(min(at, hi - 1) & in_page) << row_shift);
+                k_row = K + row; v_row = V + row;
+                off = 0;
+            }
+            bad = bad || !ok;
+            if (end || !ok) drop_next |= (int)(!ok || at >= hi) << i;
+            if constexpr (Q8) {
+                if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
+                if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
+            } else {
+                if (DH > 32 || PIECE_EL * kp < d) to_lds16(k_row + (off + 16 * kp), to + i * (NT * 16));
+                if (DH > 32 || PIECE_EL * vp < d) to_lds16(v_row + (off + 16 * vp), to + HALF + i * (NT * 16));
             }
         }
         if constexpr (Q8) {
-            if (tid < 2 * SK) {
-                const int at = lo + t * SK + tid % SK, pos = min(at, hi - 1);
+            if (wv < 2) {
+                const int at = lo + t * SK + lane % SK;
                 const bool ok = (unsigned)scale_page < (unsigned)p.c.n_pages;
                 scale_in = 0.f;
-                if (ok && at < hi) scale_in = as_global(tid < SK ? p.k_scale : p.v_scale)[((((size_t)scale_page * p.c.n_kv_heads + kvh) << shift) + (pos & in_page))];
+                if (ok && at < hi) scale_in = as_global(wv == 0 ? p.k_scale : p.v_scale)[((size_t)(uint32_t)(scale_page * p.c.n_kv_heads + kvh) << shift) + (at & in_page)];
             }
         }
         if (bad) {
@@ -249,7 +281,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             codes_to_half(vc[i].y, a, b); x.z = a; x.w = b;
             if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + (tid + i * NT) * 16) = x;
         }
-        if (wv == 0) k_sc[t % 2][tid] = scale_in;
+        if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in;
         if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
             const float size = fabsf(scale_in);
             int ex = -200;
@@ -257,7 +289,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
 #pragma unroll
             for (int o = 1; o < WAVE; o <<= 1) ex = max(ex, __shfl_xor(ex, o, WAVE));
             v_top = max(v_top, ex);
-            v_sc[t % 2][tid - SK] = ldexpf(scale_in, -v_top);
+            if (lane < SK) v_sc[t % 2][lane] = ldexpf(scale_in, -v_top);
             if (lane == 0) v_exp[t % 2] = v_top;
         }
     };
@@ -314,6 +346,10 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             }
         }
     }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) asm volatile("" : "+v"(Q[j][q]));      // (queries are waited for here: else the products of every stage would wait for whatever has been asked for since)
     f32x16 o[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f)
@@ -356,11 +392,13 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             if (active)
                 for (int key = key_base; key < key_base + TR * NU; ++key) {
                     const bool seen = stage0 + key <= pos;
+                    int half = h;
+                    asm volatile("" : "+v"(half));           // (or all these places would be formed ahead of the stages, and kept)
 #pragma unroll
                     for (int f = 0; f < NF; ++f)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int feature = TR * f + 8 * (i / 4) + 4 * h + i % 4;
+                            const int feature = TR * f + 8 * (i / 4) + 4 * half + i % 4;
                             const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(key, feature / PIECE_EL) + feature % PIECE_EL * (int)sizeof(LT);
                             bool odd;
                             if constexpr (F32) odd = (*(const uint32_t *)at & 0x7F800000u) == 0x7F800000u;
@@ -492,7 +530,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                             pf[e] = __builtin_amdgcn_exp2f(fmaf(st[u][i + e], scale, -ref));
                             if (T::P_SCALE != 1.f) pf[e] *= T::P_SCALE;
                         }
-                        l += (pf[0] + pf[1]) + (pf[2] + pf[3]);
+                        if constexpr (PARTS > 1 || Q8) l += (pf[0] + pf[1]) + (pf[2] + pf[3]);
                         if constexpr (Q8) {
                             const float4 s = *(const float4 *)&v_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
                             const float by[4] = {s.x, s.y, s.z, s.w};
@@ -503,6 +541,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                         for (int e = 0; e < 4; e += 2) {
                             uint32_t part[PARTS];
                             probability_parts<LT, PARTS>(pf[e], pf[e + 1], part);
+                            if constexpr (PARTS == 1 && !Q8) l = pair_sum<LT>(part[0], l);       // (of what they weigh, one instruction for two)
 #pragma unroll
                             for (int q = 0; q < PARTS; ++q) pt[i / 8][q][(i % 8) / 2 + e / 2] = part[q];
                         }
@@ -691,8 +730,8 @@ extern "C" int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const voi
     const PagedCache c = spdk::paged_cache((void *)K, (void *)V, table, n_pages, n_kv_heads, page_size, d_head, n_seq, table_stride);
     const int rc = spdk::paged_cache_status(dtype, c, page_size, K_scale, V_scale);
     if (rc != SPD_OK) return rc;
-    if (!io_fits(dtype, io_dtype) || n_tokens < 0 || n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_len < 0 || max_len > (long long)table_stride * page_size || max_len > INT32_MAX / 2)
-        return SPD_EINVAL;
+    if (!io_fits(dtype, io_dtype) || n_tokens < 0 || n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_len < 0 || max_len > (long long)table_stride * page_size || max_len > INT32_MAX / 2 ||
+        (long long)n_pages * n_kv_heads > INT32_MAX) return SPD_EINVAL;
     if (n_tokens == 0 || n_seq == 0) return SPD_OK;
     if ((long long)n_tokens * n_heads > (1 << 24) || n_seq > (1 << 20)) return SPD_EINVAL;
     const int io_bytes = io_dtype == SPD_DTYPE_FP32 ? 4 : 2;
