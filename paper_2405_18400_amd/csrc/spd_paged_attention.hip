@@ -47,6 +47,9 @@ template <typename KT, typename IO, int DH, int RW> struct Shape {
     static constexpr int ROWB = DH * (T::F32 ? 4 : 2), PIECES = ROWB / 16;              // bytes and 16-byte pieces of a row in LDS
     static constexpr int SK = DH == 256 && KW == 1 ? 32 : 64, NU = SK / (TR * KW);       // keys of a stage; tiles of keys of a wave
     static constexpr int HALF = SK * ROWB, BYTES = 2 * HALF, LOADS = HALF / 16 / NT;    // K, then V; pieces per thread, of K as of V
+    // Heads of 256 with 24 bits over bf16 or fp32: queries and results together are more than a wave's registers, so a block takes half of the features of the values (its scores are formed
+    // twice).
+    static constexpr int FS = DH == 256 && (T::F32 || T::PARTS == 3) ? 2 : 1;
     static constexpr int ST = 2, LDS = ST * BYTES;
     static constexpr int PER_CU = LDS <= 80 * 1024 && DH <= 128 && T::PARTS < 3 && !T::F32 ? 2 : 1;   // blocks side by side: 256 or 512 registers
 };
@@ -66,6 +69,21 @@ template <> __device__ __forceinline__ f32x16 mfma32<half_t>(u32x4 a, u32x4 b, f
 }
 template <> __device__ __forceinline__ f32x16 mfma32<bf16_t>(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// 16 bytes per lane straight into LDS, `to` + 16 lane on.  Written out, because the compiler, which knows the instruction, lets every turned read wait for all of them; they are
+// waited for once per stage.  (No vector register is written; M0, which these kernels use for nothing else, is set right before its use.)
+__device__ __forceinline__ void stage16(const char *from, uint32_t off, const char *to) {     // (from + off, off per lane)
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)to), "v"(off), "s"(from) : "memory");
+#endif
+}
+
+// All loads have arrived, in registers (the compiler knows) and in LDS.
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
+    asm volatile("" ::: "memory");
 }
 
 // Four rows of four 16-bit numbers per lane, turned round among 16 lanes: lane i gets four rows of column i.
@@ -121,10 +139,47 @@ template <int BYTES> __device__ __forceinline__ bool not_finite(u32x4 v, bool bf
     return bad;
 }
 
-// Which sequence a tile of rows belongs to.  Tiles are numbered so that sequence s has those from over(first[s]) + s on (over: whole tiles of its rows in front), which needs no sum over
-// sequences.  False: none, or first descends somewhere (then there is no telling whose rows are whose).
-struct Whose { int seq, a, b, tile; };
-__device__ __forceinline__ bool whose(const PagedAttnArgs &p, int tile, int log2_rows, int lane, Whose &w, bool &descends) {
+// The tile of rows that is the block's: of the launch's x-th, the tiles farthest behind their sequence's beginning first (they see the most keys; a call whose last blocks are its
+// longest ones waits for them: three prompts of 2999 tokens in the order of their rows 54 us).  Up to 64 sequences are looked at by one wave at once, one trip to memory: sequences with more than T tiles each have one at
+// every height below T, so x is found by going down from the tallest.  More sequences: tiles in the order of rows, sequence s's from over(first[s]) + s on (over: whole tiles in front), which
+// needs no sum over sequences; late ones first.  False: none, or first descends somewhere (then there is no telling whose rows are whose).
+struct Whose { int seq, a, b, len, tile; };
+__device__ __forceinline__ bool whose(const PagedAttnArgs &p, int x, int log2_rows, int lane, Whose &w, bool &descends) {
+    if (p.c.n_seq <= WAVE) {
+        const int i = min(lane, p.c.n_seq - 1), a = as_global(p.first)[i], b = as_global(p.first)[i + 1], len = as_global(p.len)[i];
+        descends = __any(b < a);
+        if (descends) return false;
+        const int tokens = max(min(b, p.n_tokens) - max(a, 0), 0);
+        const int tiles = lane < p.c.n_seq ? (tokens * p.group + (1 << log2_rows) - 1) >> log2_rows : 0;
+        const auto tallest = [&](int below) { return (int)__int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(tiles < below ? (float)tiles : 0.f)), WAVE - 1)); };
+        for (int top = tallest(INT32_MAX); top > 0;) {
+            const u64 with = __ballot(tiles >= top);
+            const int next = tallest(top), n = __popcll(with), of = n * (top - next);
+            if (x >= of) {
+                x -= of;
+                top = next;
+                continue;
+            }
+            int down = 0;
+            if (n > 1)
+                while (x >= n) { x -= n; ++down; }
+            else {
+                down = x;
+                x = 0;
+            }
+            u64 left = with;
+            for (; x > 0; --x) left &= left - 1;
+            const int s = __builtin_ctzll(left);
+            w.seq = s;
+            w.a = __builtin_amdgcn_readlane(a, s);
+            w.b = __builtin_amdgcn_readlane(b, s);
+            w.len = __builtin_amdgcn_readlane(len, s);
+            w.tile = top - 1 - down;
+            return true;
+        }
+        return false;
+    }
+    const int tile = p.n_tiles - 1 - x;
     int s = 0;
     bool bad = false;
     const auto start = [&](int i, int f) { return (int)(((unsigned)min(max(f, 0), p.n_tokens) * (unsigned)p.group) >> log2_rows) + i; };
@@ -136,10 +191,11 @@ __device__ __forceinline__ bool whose(const PagedAttnArgs &p, int tile, int log2
     descends = __any(bad);
     if (descends || s >= p.c.n_seq) return false;
     w.seq = s;
-    w.a = as_global(p.first)[s];
-    w.b = as_global(p.first)[s + 1];
+    w.a = __builtin_amdgcn_readfirstlane(as_global(p.first)[s]);
+    w.b = __builtin_amdgcn_readfirstlane(as_global(p.first)[s + 1]);
+    w.len = __builtin_amdgcn_readfirstlane(as_global(p.len)[s]);
     w.tile = tile - start(s, w.a);
-    return w.tile >= 0;
+    return true;
 }
 
 template <typename IO> __device__ __forceinline__ void store_rows(void *p, size_t i, float4 v) {
@@ -159,7 +215,8 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     typedef typename T::LT LT;
     constexpr bool F32 = T::F32, Q8 = T::Q8;
     constexpr int PARTS = T::PARTS, KW = S::KW, ROWS = S::ROWS, ROWB = S::ROWB, PIECES = S::PIECES, SK = S::SK, NU = S::NU, HALF = S::HALF, BYTES = S::BYTES, LOADS = S::LOADS;
-    constexpr int NJ = F32 ? DH / 8 : DH / 16, NF = DH / TR, PIECE_EL = F32 ? 4 : 8, LOG2_ROWS = RW == 4 ? 7 : 6;
+    constexpr bool LEAN = DH == 256 || Q8;                   // registers are scarce
+    constexpr int FS = S::FS, NJ = F32 ? DH / 8 : DH / 16, NF = DH / TR / FS, PIECE_EL = F32 ? 4 : 8, LOG2_ROWS = RW == 4 ? 7 : 6;
     extern __shared__ __align__(1024) char lds[];
     __shared__ int bad_stage[2], odd_stage[2];               // the stage, + 1, that has a key on no page, a value that is no finite number
     __shared__ __align__(16) float k_sc[2][SK], v_sc[2][SK];
@@ -168,18 +225,18 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane & (TR - 1), h = lane / TR, rw = wv % RW, kw = wv / RW;
     const int d = p.c.d_head, shift = p.c.page_shift, in_page = (1 << shift) - 1, group = p.group;
     // which rows, which positions
-    const int rest = over(blockIdx.x, p.by_kv_heads), kvh = blockIdx.x - rest * p.c.n_kv_heads, tile_r = over(rest, p.by_splits), split = rest - tile_r * p.splits;
+    const int block = blockIdx.x / FS, share = blockIdx.x % FS, rest = over(block, p.by_kv_heads), kvh = block - rest * p.c.n_kv_heads, tile_r = over(rest, p.by_splits), split = rest - tile_r * p.splits;
     Whose own;
     bool descends;
-    const bool found = whose(p, p.n_tiles - 1 - tile_r, LOG2_ROWS, lane, own, descends);     // (late tiles see the most keys: they start first)
+    const bool found = whose(p, tile_r, LOG2_ROWS, lane, own, descends);
     if (descends && blockIdx.x == 0 && tid == 0 && p.err) *as_global(p.err) = 1;
     if (!found) return;
     const int r0 = own.tile * ROWS, n = own.b - own.a, from = max(own.a, 0), n_rows = min(((min(own.b, p.n_tokens) - from) * group) - r0, ROWS);
     if (n_rows <= 0) return;
-    const int len = as_global(p.len)[own.seq];
+    const int len = own.len;
     if (own.a < 0 || own.b > p.n_tokens || len < n || len > p.max_len || (long long)len > (long long)p.c.table_stride << shift) {
         if (tid == 0 && p.err) *as_global(p.err) = 1;
-        if (split == 0)
+        if (split == 0 && share == 0)
             for (int i = tid; i < n_rows * d / 4; i += NT) {
                 const int r = r0 + i / (d / 4), tok = over(r, p.by_group);
                 store_rows<IO>(p.out, ((size_t)(from + tok) * p.n_heads + kvh * group + r - tok * group) * d + 4 * (i % (d / 4)), make_float4(0.f, 0.f, 0.f, 0.f));
@@ -203,6 +260,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         for (int i = tid; i < S::LDS / 16; i += NT) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
+    const auto of_share = [&](int i) { return FS == 1 || (tid + i * NT) % PIECES / (PIECES / 2) == share; };      // (places are permuted within halves of a row)
     // A wave's piece i of a stage is KEYS keys side by side, which lie on one page (but where a page is shorter than that): page numbers, asked for a stage ahead of the keys on them, and
     // addresses are the wave's, a lane's part of them stays the same.
     constexpr int KEYS = WAVE / PIECES;
@@ -223,36 +281,43 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const auto fetch = [&](int t) {
         char *to = lds + (t % 2) * BYTES + wv * (WAVE * 16);
         const bool end = lo + (t + 1) * SK > hi;
+        int lane = tid & (WAVE - 1);
+        if constexpr (LEAN) asm volatile("" : "+v"(lane));
         drop_next = 0;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key0 = (wv * WAVE + i * NT) / PIECES, key = key0 + lane / PIECES, slot = lane % PIECES, at = lo + t * SK + key;
             const int kp = k_place<PIECES>(key, slot), vp = v_place<PIECES, F32>(key, slot);
-            const char *k_row, *v_row;                       // the wave's first row, or (short pages) the lane's
-            uint32_t off;
+            const auto issue = [&](const char *k_row, const char *v_row, uint32_t off) {
+                if constexpr (Q8) {
+                    if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
+                    if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
+                } else {
+                    if (DH > 32 || PIECE_EL * kp < d) stage16(k_row, off + 16 * kp, to + i * (NT * 16));
+                    if ((DH > 32 || PIECE_EL * vp < d) && of_share(i)) stage16(v_row, off + 16 * vp, to + HALF + i * (NT * 16));
+                }
+            };
             bool ok;
-            if (whole) {
+            if (whole) {                                     // the wave's first row, and the lane's behind it
                 const int pg = __builtin_amdgcn_readfirstlane(page[i]), pos0 = min(lo + t * SK + key0, (hi - 1) & ~(KEYS - 1));
                 ok = (unsigned)pg < (unsigned)p.c.n_pages;
                 const u64 row = ((u64)(uint32_t)((ok ? pg : 0) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(pos0 & in_page) << row_shift);
-                k_row = K + row; v_row = V + row;
-                off = (uint32_t)(lane / PIECES) << row_shift;
-            } else {
+                issue(K + row, V + row, (uint32_t)(lane / PIECES) << row_shift);
+            } else {                                         // short pages: page by page, each for its own lanes
                 ok = (unsigned)page[i] < (unsigned)p.c.n_pages;
-                const u64 row = ((u64)(uint32_t)((ok ? page[i] : 0) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(min(at, hi - 1) & in_page) << row_shift);
-                k_row = K + row; v_row = V + row;
-                off = 0;
+                const int pos0 = min(at, hi - 1);
+                u64 left = __ballot(true);
+                while (left) {
+                    const int first = __builtin_ctzll(left), pg = __builtin_amdgcn_readlane(page[i], first), pos1 = __builtin_amdgcn_readlane(pos0, first) & ~in_page;
+                    const bool mine = (pos0 & ~in_page) == pos1;
+                    left &= ~__ballot(mine);
+                    const u64 row = (u64)(uint32_t)(((unsigned)pg < (unsigned)p.c.n_pages ? pg : 0) * p.c.n_kv_heads + kvh) << head_shift;
+                    if (mine) issue(K + row, V + row, (uint32_t)(pos0 & in_page) << row_shift);
+                }
             }
             bad = bad || !ok;
             if (end || !ok) drop_next |= (int)(!ok || at >= hi) << i;
-            if constexpr (Q8) {
-                if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
-                if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
-            } else {
-                if (DH > 32 || PIECE_EL * kp < d) to_lds16(k_row + (off + 16 * kp), to + i * (NT * 16));
-                if (DH > 32 || PIECE_EL * vp < d) to_lds16(v_row + (off + 16 * vp), to + HALF + i * (NT * 16));
-            }
         }
         if constexpr (Q8) {
             if (wv < 2) {
@@ -346,10 +411,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             }
         }
     }
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int q = 0; q < PARTS; ++q) asm volatile("" : "+v"(Q[j][q]));      // (queries are waited for here: else the products of every stage would wait for whatever has been asked for since)
+    wait_loads();                                            // (queries are waited for here: else the products of every stage would wait for whatever has been asked for since)
     f32x16 o[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f)
@@ -367,7 +429,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         const int stage0 = lo + t * SK;
         char *const k_tile = lds + (t % 2) * BYTES, *const v_tile = k_tile + HALF;
         if constexpr (!Q8) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            wait_loads();
             // Values that do not count are zero; one that some rows see and others do not must not be what zero times it is not zero.
             if (drop) {
 #pragma unroll
@@ -377,7 +439,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             if (stage0 + SK - 1 > pos_min) {
                 bool odd = false;
 #pragma unroll
-                for (int i = 0; i < LOADS; ++i) odd = odd || not_finite<sizeof(LT)>(*(const u32x4 *)(v_tile + (tid + i * NT) * 16), Type<LT>::PARTS == 3);
+                for (int i = 0; i < LOADS; ++i) odd = odd || (of_share(i) && not_finite<sizeof(LT)>(*(const u32x4 *)(v_tile + (tid + i * NT) * 16), Type<LT>::PARTS == 3));
                 if (odd) odd_stage[t % 2] = t + 1;
             }
         }
@@ -398,7 +460,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                     for (int f = 0; f < NF; ++f)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int feature = TR * f + 8 * (i / 4) + 4 * half + i % 4;
+                            const int feature = share * (DH / 2) + TR * f + 8 * (i / 4) + 4 * half + i % 4;
                             const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(key, feature / PIECE_EL) + feature % PIECE_EL * (int)sizeof(LT);
                             bool odd;
                             if constexpr (F32) odd = (*(const uint32_t *)at & 0x7F800000u) == 0x7F800000u;
@@ -429,22 +491,42 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         }
         if (active && tb <= wave_hi) {
             f32x16 st[NU];
+            // pieces of keys are asked for KD ahead of their products
+            constexpr int KD = NJ < 4 ? NJ : DH == 256 && (F32 || PARTS == 3) ? 2 : LEAN ? 4 : NJ < 8 ? NJ : 8, STEPS = NU * NJ;
+            int k_off = 16 * k_place<PIECES>(key_base + col, h);             // (piece 2 j + h lies where piece h does, but for the bits of 2 j)
+            if constexpr (LEAN) asm volatile("" : "+v"(k_off));              // (formed from here on in every stage: kept, the places of all pieces are a register each)
+            const char *k_row = k_tile + (key_base + col) * ROWB;
+            const auto key_piece = [&](int i) { return *(const u32x4 *)(k_row + TR * (i / NJ) * ROWB + (k_off ^ 32 * (i % NJ))); };
+            u32x4 k[KD];
+#pragma unroll
+            for (int i = 0; i < KD; ++i) k[i] = key_piece(i);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int u = i / NJ, j = i % NJ;
+                if (j == 0)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) st[u][e] = 0.f;
+                if constexpr (F32) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) st[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[i % KD][c]), __uint_as_float(Q[j][0][c]), st[u], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int q = PARTS - 1; q >= 0; --q) st[u] = mfma32<LT>(k[i % KD], Q[j][q], st[u]);
+                }
+                if (i + KD < STEPS) k[i % KD] = key_piece(i + KD);
+            }
+            if constexpr (DH >= 64) {                        // in this order: reads from LDS (0x100), products (0x8)
+                constexpr int EACH = F32 ? 4 : PARTS;
+                __builtin_amdgcn_sched_group_barrier(0x100, KD, 0);
+#pragma unroll
+                for (int i = 0; i < STEPS - KD; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x8, KD * EACH, 0);
+            }
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[u][i] = 0.f;
-                const int key = key_base + TR * u + col;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const u32x4 k = *(const u32x4 *)(k_tile + key * ROWB + 16 * k_place<PIECES>(key, 2 * j + h));
-                    if constexpr (F32) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) st[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[c]), __uint_as_float(Q[j][0][c]), st[u], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int q = PARTS - 1; q >= 0; --q) st[u] = mfma32<LT>(k, Q[j][q], st[u]);
-                    }
-                }
                 if constexpr (Q8) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
@@ -506,6 +588,9 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             for (int u = 0; u < NU; ++u) {
                 if constexpr (F32) {
                     float pf[16];
+                    int half = h;
+                    if constexpr (LEAN) asm volatile("" : "+v"(half));
+                    const char *v_row = v_tile + (key_base + 4 * half) * ROWB;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         pf[i] = __builtin_amdgcn_exp2f(fmaf(st[u][i], scale, -ref)) * T::P_SCALE;
@@ -513,10 +598,9 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                     }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int key = key_base + TR * u + 8 * (i / 4) + 4 * h + i % 4;
 #pragma unroll
                         for (int f = 0; f < NF; ++f) {
-                            const float v = *(const float *)(v_tile + key * ROWB + 16 * v_place<PIECES, F32>(key, 8 * f + col / 4) + 4 * (col % 4));
+                            const float v = *(const float *)(v_row + (TR * u + 8 * (i / 4) + i % 4) * ROWB + 16 * v_place<PIECES, F32>(4 * half, 8 * f) + 4 * col + share * (ROWB / 2));
                             o[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, pf[i], o[f], 0, 0, 0);
                         }
                     }
@@ -546,13 +630,15 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                             for (int q = 0; q < PARTS; ++q) pt[i / 8][q][(i % 8) / 2 + e / 2] = part[q];
                         }
                     }
-                    const int t4 = (lane % 16) / 4, fg = (lane / 16) % 2;
+                    int at4 = lane % 16;
+                    if constexpr (LEAN) asm volatile("" : "+v"(at4));
+                    const int t4 = at4 / 4, fg = (lane / 16) % 2;
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
                         const int key = key_base + TR * u + 16 * g + 4 * h + t4;
 #pragma unroll
                         for (int f = 0; f < NF; ++f) {
-                            const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(t4, 4 * f + 2 * fg + (lane % 4) / 2) + 8 * (lane % 2);     // (a place hangs on key % 4 alone)
+                            const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(t4, 4 * f + 2 * fg + (lane % 4) / 2) + 8 * (lane % 2) + share * (ROWB / 2);     // (a place hangs on key % 4 alone)
                             const u32x2 x = turned_read(at), y = turned_read(at + 8 * ROWB);
                             const u32x4 v{x.x, x.y, y.x, y.y};
 #pragma unroll
@@ -599,7 +685,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     if (!active || rw * TR + col >= n_rows) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;              // (nothing seen: zeros)
     const size_t at = p.splits > 1 ? row_at * p.splits + split : row_at;
-    if (p.splits > 1 && h == 0) {
+    if (p.splits > 1 && h == 0 && share == 0) {
         as_global(p.part_ml)[2 * at] = m;
         as_global(p.part_ml)[2 * at + 1] = l;
     }
@@ -607,7 +693,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     for (int f = 0; f < NF; ++f)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const int feature = TR * f + 2 * i + 4 * h;
+            const int feature = share * (DH / 2) + TR * f + 2 * i + 4 * h;
             if (DH == 32 && feature >= d) continue;
             float4 y = make_float4(o[f][i] * inv, o[f][i + 1] * inv, o[f][i + 2] * inv, o[f][i + 3] * inv);
             if constexpr (Q8) y = make_float4(ldexpf(y.x, o_exp), ldexpf(y.y, o_exp), ldexpf(y.z, o_exp), ldexpf(y.w, o_exp));
@@ -682,7 +768,7 @@ template <typename KT, typename IO, int DH, int RW>
 hipError_t launch_rows(hipStream_t s, PagedAttnArgs a) {
     typedef Shape<KT, IO, DH, RW> S;
     a.n_tiles = (int)((long long)a.n_tokens * a.group / S::ROWS + a.c.n_seq);
-    const long long blocks = (long long)a.n_tiles * a.c.n_kv_heads * a.splits;
+    const long long blocks = (long long)a.n_tiles * a.c.n_kv_heads * a.splits * S::FS;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     if (S::LDS > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)paged_attn_kernel<KT, IO, DH, RW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
