@@ -331,10 +331,20 @@ struct VerifyArgs {
     const int32_t *tokens, *first;       // [n_tokens], [n_seq + 1]
     const float *u;                      // [n_tokens]
     int32_t n_seq, n_tokens, vocab;
-    double by_tau, by_draft_tau;
+    double by_tau, by_draft_tau;         // log2(e) / tau
     int32_t *out_tokens;
     float *out_logprobs;
     int32_t *out_accepted, *err;
+    int32_t slices;
+    double *sum, *rest;                  // scratch: [rows of logits, then of draft_logits; slices] sum of exp((logit - largest) / tau); [n_seq, slices] what a draft that does not stand leaves
+    float *top;                          // scratch, as sum: largest logit of a slice
+    struct VerifyPick *pick;             // scratch, [n_seq]
+};
+// The row of a sequence that its last token is drawn from.
+struct VerifyPick {
+    double inv, draft_inv;               // 1 / sum of exp((logit - top) / tau), 0 where no logit is finite
+    float top, draft_top;
+    int32_t row, token, refused, pad;    // -1: nothing to draw; the draft that does not stand, if one was refused
 };
 struct SelectArgs {
     const void *logits;
