@@ -336,15 +336,15 @@ struct VerifyArgs {
     float *out_logprobs;
     int32_t *out_accepted, *err;
     int32_t slices;
-    double *sum, *rest;                  // scratch: [rows of logits, then of draft_logits; slices] sum of exp((logit - largest) / tau); [n_seq, slices] what a draft that does not stand leaves
-    float *top;                          // scratch, as sum: largest logit of a slice
+    float *top, *sum;                    // scratch: [rows of logits, then of draft_logits; slices] largest logit, sum of exp((logit - that) / tau) in fp32
+    double *exact, *rest;                // scratch: [2, n_seq, pieces] the same sums of a sequence's last row, in 64 bits; [n_seq, pieces] what a draft that does not stand leaves of it
+    int32_t pieces;                      // of a row: several to a slice
     struct VerifyPick *pick;             // scratch, [n_seq]
 };
 // The row of a sequence that its last token is drawn from.
 struct VerifyPick {
-    double inv, draft_inv;               // 1 / sum of exp((logit - top) / tau), 0 where no logit is finite
-    float top, draft_top;
-    int32_t row, token, refused, pad;    // -1: nothing to draw; the draft that does not stand, if one was refused
+    float top, draft_top;                // largest logits
+    int32_t row, token, refused;         // -1: nothing to draw; the draft that does not stand, if one was refused
 };
 struct SelectArgs {
     const void *logits;

@@ -1,11 +1,13 @@
 // Verification of drafted tokens against the target's probabilities, and the draw of the token behind those that stand.
 //
 // Bound: every row of logits is read once, whatever stands (which rows count hangs on the rows before them), and the one row that a sequence's last token
-// is drawn from once or twice more.  Three launches:
-//   * slices of all rows: largest logit and sum of exponentials;
-//   * a block per slice and sequence puts its sequence's rows together, finds the first draft that does not stand, and sums its slice of what that leaves, max(p - q, 0);
+// is drawn from three times more.  Four launches:
+//   * slices of all rows: largest logit and sum of exponentials, in fp32;
+//   * a block per slice and sequence puts its sequence's rows together, finds the first draft that does not stand, and sums its slice of that row again, in 64 bits;
+//   * the same blocks sum what that row leaves, max(p - q, 0);
 //   * a block per sequence finds the slice where the draw falls, and the token in it.
-// Exponentials and sums are in 64 bits: of a hundred thousand borders between tokens, one in a thousand draws meets one that sums of fp32 exponentials have moved.
+// Whether a draft stands is one comparison, which an error of 1e-8 hardly ever turns.  The draw falls between as many borders as there are tokens: of a hundred thousand, one in a
+// thousand draws meets one that sums of fp32 exponentials have moved.  So that row is in 64 bits; all rows in 64 bits took 61 us where fp32 takes what reading takes.
 #include "spd_attention.h"
 
 #include <algorithm>
@@ -20,15 +22,18 @@ constexpr int NTV = 256, NWV = NTV / WAVE;
 // A logit as it counts: no number is -inf, +inf the largest finite number.
 __device__ __forceinline__ float logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f); }
 
-// 2^x for x <= 0: x to the nearest whole number and a rest of at most 1/2, whose exponential is ten terms of its series; the next one is 2e-13.
-__device__ __forceinline__ double exp2_64(double x) {
-    x = fmax(x, -2000.0);
-    const double k = rint(x), f = x - k;
-    constexpr double L = 0.69314718055994530942;
-    double y = 1.0;
+// exp((z - top) / tau), c = log2(e) / tau, z <= top, in 64 bits: to the nearest power of two by adding 1.5 2^52, which leaves the whole number in the low bits, and a rest of at most 1/2, whose
+// exponential is ten terms of its series; the next one is 2e-13.  (As conversions and ldexp these steps take the time of twice as many products.)  What is below 2^-900 counts as that.
+__device__ __forceinline__ double exp_64(float z, float top, double c) {
+    constexpr double MAGIC = 6755399441055744.0, L = 0.69314718055994530942;
+    constexpr double C[11] = {1.0, L, L * L / 2, L * L * L / 6, L * L * L * L / 24, L * L * L * L * L / 120, L * L * L * L * L * L / 720, L * L * L * L * L * L * L / 5040,
+                              L * L * L * L * L * L * L * L / 40320, L * L * L * L * L * L * L * L * L / 362880, L * L * L * L * L * L * L * L * L * L / 3628800};
+    const double d = fmax((double)z - (double)top, -900.0 / c), t = fma(d, c, MAGIC), f = fma(d, c, -(t - MAGIC));
+    double y = C[10];
 #pragma unroll
-    for (int n = 10; n >= 1; --n) y = fma(y, f * (L / n), 1.0);
-    return ldexp(y, (int)k);
+    for (int n = 9; n >= 0; --n) y = fma(y, f, C[n]);
+    const u64 bits = __builtin_bit_cast(u64, y) + ((u64)(uint32_t)__builtin_bit_cast(u64, t) << 52);       // (the exponent's place: modulo 2^12)
+    return z > -INFINITY ? __builtin_bit_cast(double, bits) : 0.0;
 }
 
 // Sums over the block, the same in all threads.
@@ -43,6 +48,18 @@ __device__ __forceinline__ double block_add(double v, double *red) {
     if (threadIdx.x % WAVE == 0) red[threadIdx.x / WAVE] = v;
     __syncthreads();
     return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// N numbers' sums over the block, each by one thread to `out`.
+template <int N> __device__ __forceinline__ void block_adds(const double (&v)[N], double (*red)[NWV], double *out) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const double x = wave_add(v[i]);
+        if (threadIdx.x % WAVE == 0) red[i][threadIdx.x / WAVE] = x;
+    }
+    __syncthreads();
+    if (threadIdx.x < N) out[threadIdx.x] = (red[threadIdx.x][0] + red[threadIdx.x][1]) + (red[threadIdx.x][2] + red[threadIdx.x][3]);
 }
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;      // on no grid but that of the elements
@@ -68,8 +85,7 @@ template <typename T> __device__ __forceinline__ const void *row_of(const void *
 template <typename T, int E>
 __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T), PIECES = E / VEC;
-    __shared__ float tops[NWV];
-    __shared__ double red[NWV];
+    __shared__ float tops[NWV], red[NWV];
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
     const bool draft = r >= a.n_tokens;
     const int t = draft ? r - a.n_tokens : r;
@@ -78,11 +94,11 @@ __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
     for (int i = lane; i <= a.n_seq; i += WAVE) {
         const int f = as_global(a.first)[i];
         last = last || f == t + 1;
-        inside = inside || (i == 0 && f <= t) ;
+        inside = inside || (i == 0 && f <= t);
     }
     if (!__any(inside) || t >= as_global(a.first)[a.n_seq] || (draft && __any(last))) return;
     const void *row = draft ? row_of<T>(a.draft_logits, a.draft_stride, t) : row_of<T>(a.logits, a.row_stride, t);
-    const double c = draft ? a.by_draft_tau : a.by_tau;
+    const float c = (float)(draft ? a.by_draft_tau : a.by_tau);
     float z[PIECES][VEC], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) load_logits<T, VEC>(row, (slice * PIECES + i) * NTV * VEC + tid * VEC, a.vocab, z[i]);
@@ -94,66 +110,59 @@ __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
     if (lane == 0) tops[tid / WAVE] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    double sum = 0.0;
-    if (top > -INFINITY)
+    const float from = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
+    for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += exp2_64(((double)z[i][e] - (double)top) * c);
-    sum = block_add(sum, red);
+        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((z[i][e] - from) * c);
+    sum = wave_sum(sum);
+    if (lane == 0) red[tid / WAVE] = sum;
+    __syncthreads();
     if (tid == 0) {
         as_global(a.top)[blockIdx.x] = top;
-        as_global(a.sum)[blockIdx.x] = sum;
+        as_global(a.sum)[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
     }
 }
 
-// A row's largest logit and the inverse of its sum, by a wave.
-__device__ __forceinline__ void whole_row(const VerifyArgs &a, int r, double c, int lane, float &top, double &inv) {
+// A row's largest logit, and its sum of exponentials to 1e-8, by 16 lanes.
+constexpr int ROWL = 16;
+__device__ __forceinline__ void whole_row(const VerifyArgs &a, int r, double c, int lane, float &top, double &sum) {
     const size_t at = (size_t)r * a.slices;
-    top = -INFINITY;
-    for (int i = lane; i < a.slices; i += WAVE) top = fmaxf(top, as_global(a.top)[at + i]);
-    top = wave_max(top);
-    double sum = 0.0;
-    for (int i = lane; i < a.slices; i += WAVE) {
-        const float m = as_global(a.top)[at + i];
-        if (m > -INFINITY) sum += as_global(a.sum)[at + i] * exp2_64(((double)m - (double)top) * c);
+    float m = -INFINITY, s = 0.f;                // the lane's slices so far
+    for (int i = lane; i < a.slices; i += ROWL) {
+        const float x = as_global(a.top)[at + i], y = as_global(a.sum)[at + i], up = fmaxf(m, x);
+        if (up == -INFINITY) continue;
+        s = s * __builtin_amdgcn_exp2f((m - up) * (float)c) + y * __builtin_amdgcn_exp2f((x - up) * (float)c);
+        m = up;
     }
-    sum = wave_add(sum);
-    inv = top > -INFINITY ? 1.0 / sum : 0.0;
+    top = m;
+#pragma unroll
+    for (int o = 1; o < ROWL; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
+    s = m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * (float)c);
+#pragma unroll
+    for (int o = 1; o < ROWL; o <<= 1) s += __shfl_xor(s, o, WAVE);
+    sum = s;
 }
-template <typename T> __device__ __forceinline__ double exponent(const void *row, int v, float top, double c) { return ((double)logit(Store<T>::load1(row, v)) - (double)top) * c; }
 
-// What a row leaves of VEC tokens from v0 on.
-template <typename T, int VEC>
-__device__ __forceinline__ void weights(const VerifyArgs &a, const VerifyPick &k, bool rest, int v0, double (&w)[VEC]) {
-    float z[VEC];
-    load_logits<T, VEC>(row_of<T>(a.logits, a.row_stride, k.row), v0, a.vocab, z);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) w[e] = k.inv == 0.0 ? 0.0 : exp2_64(((double)z[e] - (double)k.top) * a.by_tau) * k.inv;
-    if (!rest) return;
-    if (a.draft_logits) {
-        load_logits<T, VEC>(row_of<T>(a.draft_logits, a.draft_stride, k.row), v0, a.vocab, z);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] = fmax(w[e] - (k.draft_inv == 0.0 ? 0.0 : exp2_64(((double)z[e] - (double)k.draft_top) * a.by_draft_tau) * k.draft_inv), 0.0);
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] = v0 + e == k.token ? 0.0 : w[e];
-    }
+// Whether all of `first` ascends (every thread of the block looks at some of it).
+__device__ __forceinline__ bool ascends(const VerifyArgs &a) {
+    int descends = 0;
+    for (int i = threadIdx.x; i < a.n_seq; i += NTV) descends |= as_global(a.first)[i + 1] < as_global(a.first)[i];
+    return !__syncthreads_or(descends);
 }
 
 template <typename T, int E>
 __global__ __launch_bounds__(NTV) void verify_drafts_kernel(const VerifyArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T), PIECES = E / VEC;
     __shared__ int stop;
-    __shared__ double red[NWV];
-    __shared__ VerifyPick pick;
-    const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = tid / WAVE, s = blockIdx.x / a.slices, slice = blockIdx.x - s * a.slices;
-    int descends = 0;
-    for (int i = tid; i < a.n_seq; i += NTV) descends |= as_global(a.first)[i + 1] < as_global(a.first)[i];
+    __shared__ double red[PIECES][NWV];
+    __shared__ float last_top[2];
+    const int tid = threadIdx.x, s = blockIdx.x / a.slices, slice = blockIdx.x - s * a.slices, lane = tid % ROWL;
     if (tid == 0) stop = INT32_MAX;
-    const bool sorted = !__syncthreads_or(descends);
+    const bool sorted = ascends(a);
     const int lo = as_global(a.first)[s], hi = as_global(a.first)[s + 1];
-    const bool fits = sorted && lo >= 0 && hi <= a.n_tokens;
+    const bool fits = sorted && lo >= 0 && hi <= a.n_tokens, drawn = a.draft_logits != nullptr;
     if (!fits || lo == hi) {
         if (tid == 0 && slice == 0) {
             as_global(a.out_accepted)[s] = 0;
@@ -162,163 +171,201 @@ __global__ __launch_bounds__(NTV) void verify_drafts_kernel(const VerifyArgs a) 
         }
         return;
     }
-    // a wave per row: does its draft stand?  (Those behind the first that does not are looked at in vain.)
-    const bool drawn = a.draft_logits != nullptr;
-    for (int t = lo + wv; t < hi - 1; t += NWV) {
-        const int x = as_global(a.tokens)[t + 1];
+    // 16 lanes per row: does its draft stand?  (Those behind the first that does not are looked at in vain.)
+    for (int t0 = lo; t0 < hi - 1; t0 += NTV / ROWL) {
+        const int t = t0 + tid / ROWL, u = min(t, hi - 2), x = as_global(a.tokens)[u + 1];          // (all lanes take part in the exchange)
         const bool known = (unsigned)x < (unsigned)a.vocab;
-        float top;
-        double inv, p = 0.0, q = 1.0, e = 0.0;
-        whole_row(a, t, a.by_tau, lane, top, inv);
-        if (known && inv != 0.0) {
-            e = exponent<T>(row_of<T>(a.logits, a.row_stride, t), x, top, a.by_tau);
-            p = exp2_64(e) * inv;
+        float top, draft_top = -INFINITY;
+        double sum, draft_sum = 0.0;
+        whole_row(a, u, a.by_tau, lane, top, sum);
+        if (drawn) whole_row(a, a.n_tokens + u, a.by_draft_tau, lane, draft_top, draft_sum);
+        if (lane != 0 || t >= hi - 1) continue;
+        double p = 0.0, q = 1.0;
+        float z = -INFINITY;
+        if (known && top > -INFINITY) {
+            z = logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, t), x));
+            p = exp_64(z, top, a.by_tau) / sum;
         }
-        const double log2_p = e + log2(inv);
-        if (drawn) {
-            whole_row(a, a.n_tokens + t, a.by_draft_tau, lane, top, inv);
-            q = known && inv != 0.0 ? exp2_64(exponent<T>(row_of<T>(a.draft_logits, a.draft_stride, t), x, top, a.by_draft_tau)) * inv : 0.0;
-        }
-        const bool stands = (double)as_global(a.u)[t] * q < p;
-        if (lane == 0) {
-            if (!stands) atomicMin(&stop, t);
-            else if (slice == 0) {
-                as_global(a.out_tokens)[t] = x;
-                as_global(a.out_logprobs)[t] = (float)(log2_p * 0.69314718055994530942);
-            }
+        if (drawn) q = known && draft_top > -INFINITY ? exp_64(logit(Store<T>::load1(row_of<T>(a.draft_logits, a.draft_stride, t), x)), draft_top, a.by_draft_tau) / draft_sum : 0.0;
+        if (!((double)as_global(a.u)[t] * q < p)) atomicMin(&stop, t);
+        else if (slice == 0) {
+            as_global(a.out_tokens)[t] = x;
+            as_global(a.out_logprobs)[t] = (float)((((double)z - (double)top) * a.by_tau - log2(sum)) * 0.69314718055994530942);
         }
     }
     __syncthreads();
     const bool refused = stop < hi - 1;
     const int row = refused ? stop : hi - 1;
-    if (wv == 0) {
-        VerifyPick k{};
-        k.row = row;
-        k.refused = refused;
-        k.token = refused ? as_global(a.tokens)[row + 1] : -1;
-        whole_row(a, row, a.by_tau, lane, k.top, k.inv);
-        if (refused && drawn) whole_row(a, a.n_tokens + row, a.by_draft_tau, lane, k.draft_top, k.draft_inv);
-        if (lane == 0) {
-            pick = k;
-            if (slice == 0) {
-                a.pick[s] = k;
-                as_global(a.out_accepted)[s] = row - lo;
-                if (a.err && (k.inv == 0.0 || (refused && (unsigned)k.token >= (unsigned)a.vocab))) *as_global(a.err) = 1;
-            }
-        }
+    if (tid < 2 * ROWL) {                        // the largest logits of the last row, the target's and the drafter's
+        const bool draft = tid >= ROWL;
+        float top;
+        double sum;
+        whole_row(a, draft && refused && drawn ? a.n_tokens + row : row, draft ? a.by_draft_tau : a.by_tau, lane, top, sum);
+        if (lane == 0) last_top[draft] = top;
     }
     if (slice == 0)
         for (int i = row + 1 + tid; i < hi; i += NTV) {
             as_global(a.out_tokens)[i] = -1;
             as_global(a.out_logprobs)[i] = 0.f;
         }
-    if (!refused) return;                        // (the slices' sums are there)
     __syncthreads();
-    const VerifyPick k = pick;
-    double sum = 0.0;
-#pragma unroll 1
-    for (int i = 0; i < PIECES; ++i) {
-        double w[VEC];
-        weights<T, VEC>(a, k, true, (slice * PIECES + i) * NTV * VEC + tid * VEC, w);
+    if (slice == 0 && tid == 0) {
+        const int x = refused ? as_global(a.tokens)[row + 1] : -1;
+        a.pick[s] = VerifyPick{last_top[0], last_top[1], row, x, refused};
+        as_global(a.out_accepted)[s] = row - lo;
+        if (a.err && (last_top[0] == -INFINITY || (refused && (unsigned)x >= (unsigned)a.vocab))) *as_global(a.err) = 1;
+    }
+    // that row's sums, in 64 bits
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += w[e];
+    for (int d = 0; d < 2; ++d) {
+        if (d && !(refused && drawn)) break;
+        const void *z_row = d ? row_of<T>(a.draft_logits, a.draft_stride, row) : row_of<T>(a.logits, a.row_stride, row);
+        const double c = d ? a.by_draft_tau : a.by_tau;
+        const float top = last_top[d];
+        double sum[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            float z[VEC];
+            load_logits<T, VEC>(z_row, (slice * PIECES + i) * NTV * VEC + tid * VEC, a.vocab, z);
+            sum[i] = 0.0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[i] += top == -INFINITY ? 0.0 : exp_64(z[e], top, c);
+        }
+        block_adds<PIECES>(sum, red, a.exact + ((size_t)d * a.n_seq + s) * a.pieces + slice * PIECES);
+    }
+}
+
+// The inverses of a sequence's last row's sums (0 where no logit is finite), by the block: the target's, the drafter's.
+__device__ __forceinline__ void inverses(const VerifyArgs &a, const VerifyPick &k, int s, double *red, double &inv, double &draft_inv) {
+    double sum = 0.0, draft = 0.0;
+    for (int i = threadIdx.x; i < a.pieces; i += NTV) {
+        sum += a.exact[(size_t)s * a.pieces + i];
+        if (k.refused && a.draft_logits) draft += a.exact[((size_t)a.n_seq + s) * a.pieces + i];
     }
     sum = block_add(sum, red);
-    if (tid == 0) a.rest[(size_t)s * a.slices + slice] = sum;
+    draft = block_add(draft, red);
+    inv = sum > 0.0 ? 1.0 / sum : 0.0;
+    draft_inv = draft > 0.0 ? 1.0 / draft : 0.0;
+}
+
+// What a sequence's last row leaves of VEC tokens from v0 on.
+template <typename T, int VEC>
+__device__ __forceinline__ void weights(const VerifyArgs &a, const VerifyPick &k, double inv, double draft_inv, bool rest, int v0, double (&w)[VEC]) {
+    float z[VEC], y[VEC];
+    load_logits<T, VEC>(row_of<T>(a.logits, a.row_stride, k.row), v0, a.vocab, z);
+    const bool drawn = rest && a.draft_logits;
+    if (drawn) load_logits<T, VEC>(row_of<T>(a.draft_logits, a.draft_stride, k.row), v0, a.vocab, y);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) w[e] = inv == 0.0 ? 0.0 : exp_64(z[e], k.top, a.by_tau) * inv;
+    if (drawn && draft_inv != 0.0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] = fmax(w[e] - exp_64(y[e], k.draft_top, a.by_draft_tau) * draft_inv, 0.0);
+    }
+    if (rest && !drawn) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] = v0 + e == k.token ? 0.0 : w[e];
+    }
 }
 
 template <typename T, int E>
-__global__ __launch_bounds__(NTV) void verify_pick_kernel(const VerifyArgs a) {
+__global__ __launch_bounds__(NTV) void verify_rest_kernel(const VerifyArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T), PIECES = E / VEC;
-    __shared__ double red[NWV], before_slice;
-    __shared__ int found, last, in_slice;
+    __shared__ double red[NWV], reds[PIECES][NWV];
+    const int s = blockIdx.x / a.slices, slice = blockIdx.x - s * a.slices;
+    const VerifyPick k = a.pick[s];
+    if (k.row < 0 || !k.refused) return;         // (p itself: its sums are there)
+    double inv, draft_inv, sum[PIECES];
+    inverses(a, k, s, red, inv, draft_inv);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        double w[VEC];
+        weights<T, VEC>(a, k, inv, draft_inv, true, (slice * PIECES + i) * NTV * VEC + threadIdx.x * VEC, w);
+        sum[i] = 0.0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[i] += w[e];
+    }
+    block_adds<PIECES>(sum, reds, a.rest + (size_t)s * a.pieces + slice * PIECES);
+}
+
+template <typename T>
+__global__ __launch_bounds__(NTV) void verify_pick_kernel(const VerifyArgs a) {
+    constexpr int VEC = 16 / (int)sizeof(T);
+    __shared__ double red[NWV], part[NWV], before_piece;
+    __shared__ int found, last, in_piece;
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = tid / WAVE, s = blockIdx.x;
     const VerifyPick k = a.pick[s];
     if (k.row < 0) return;
     const double u = (double)as_global(a.u)[as_global(a.first)[s + 1] - 1];
-    if (tid == 0) { found = INT32_MAX; last = -1; in_slice = -1; }
-    // a slice's sum: what is left, or (all stand, or nothing is left) p itself
+    if (tid == 0) { found = INT32_MAX; last = -1; in_piece = -1; }
+    double inv, draft_inv;
+    inverses(a, k, s, red, inv, draft_inv);
+    // a piece's sum: what is left, or (all stand, or nothing is left) p itself
     bool rest = k.refused;
-    const auto slice_sum = [&](int i) {
-        if (rest) return a.rest[(size_t)s * a.slices + i];
-        const size_t at = (size_t)k.row * a.slices + i;
-        const float m = as_global(a.top)[at];
-        return m > -INFINITY ? as_global(a.sum)[at] * exp2_64(((double)m - (double)k.top) * a.by_tau) * k.inv : 0.0;
-    };
+    const auto piece_sum = [&](int i) { return rest ? a.rest[(size_t)s * a.pieces + i] : a.exact[(size_t)s * a.pieces + i] * inv; };
     double total;
     for (;;) {
         double sum = 0.0;
-        for (int i = tid; i < a.slices; i += NTV) sum += slice_sum(i);
+        for (int i = tid; i < a.pieces; i += NTV) sum += piece_sum(i);
         total = block_add(sum, red);
         if (total > 0.0 || !rest) break;
         rest = false;
     }
     const double bound = u * total;
-    if (wv == 0) {                               // the slice where the sums pass it; the last with a weight where none does
-        double before = 0.0;
-        int pick = -1;
-        double pick_before = 0.0;
-        for (int i0 = 0; i0 < a.slices; i0 += WAVE) {
-            const double mine = i0 + lane < a.slices ? slice_sum(i0 + lane) : 0.0;
-            double upto = mine;
+    const auto running = [&](double v) {         // sums up to and with each lane's
 #pragma unroll
-            for (int o = 1; o < WAVE; o <<= 1) {
-                const double x = __shfl_up(upto, o, WAVE);
-                if (lane >= o) upto += x;
-            }
+        for (int o = 1; o < WAVE; o <<= 1) {
+            const double x = __shfl_up(v, o, WAVE);
+            if (lane >= o) v += x;
+        }
+        return v;
+    };
+    if (wv == 0) {                               // the piece where the sums pass it; the last with a weight where none does
+        double before = 0.0, pick_before = 0.0;
+        int pick = -1;
+        for (int i0 = 0; i0 < a.pieces; i0 += WAVE) {
+            const double mine = i0 + lane < a.pieces ? piece_sum(i0 + lane) : 0.0, upto = running(mine);
             const u64 some = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && before + upto > bound);
-            if (past) {
-                pick = i0 + __builtin_ctzll(past);
-                pick_before = before + (__shfl(upto, pick - i0, WAVE) - __shfl(mine, pick - i0, WAVE));
-                break;
+            const int at = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : -1;
+            if (at >= 0) {
+                pick = i0 + at;
+                pick_before = before + (__shfl(upto, at, WAVE) - __shfl(mine, at, WAVE));
             }
-            if (some) {
-                pick = i0 + 63 - __builtin_clzll(some);
-                pick_before = before + (__shfl(upto, pick - i0, WAVE) - __shfl(mine, pick - i0, WAVE));
-            }
+            if (past) break;
             before += __shfl(upto, WAVE - 1, WAVE);
         }
-        if (lane == 0) { in_slice = pick; before_slice = pick_before; }
+        if (lane == 0) { in_piece = pick; before_piece = pick_before; }
     }
     __syncthreads();
-    double before = before_slice;
-    if (in_slice >= 0)
-#pragma unroll 1
-        for (int i = 0; i < PIECES; ++i) {
-            const int v0 = (in_slice * PIECES + i) * NTV * VEC + tid * VEC;
-            double w[VEC], mine = 0.0;
-            weights<T, VEC>(a, k, rest, v0, w);
+    if (in_piece >= 0) {                         // its tokens lie in the order of threads
+        const int v0 = in_piece * NTV * VEC + tid * VEC;
+        double w[VEC], mine = 0.0;
+        weights<T, VEC>(a, k, inv, draft_inv, rest, v0, w);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) mine += w[e];
-            double upto = mine;
+        for (int e = 0; e < VEC; ++e) mine += w[e];
+        const double upto = running(mine);
+        if (lane == WAVE - 1) part[wv] = upto;
+        __syncthreads();
+        double at = before_piece + (upto - mine);
+        for (int j = 0; j < wv; ++j) at += part[j];
+        int first_past = INT32_MAX, last_some = -1;
 #pragma unroll
-            for (int o = 1; o < WAVE; o <<= 1) {
-                const double x = __shfl_up(upto, o, WAVE);
-                if (lane >= o) upto += x;
+        for (int e = 0; e < VEC; ++e) {
+            at += w[e];
+            if (w[e] > 0.0) {
+                last_some = v0 + e;
+                if (at > bound) first_past = min(first_past, v0 + e);
             }
-            __syncthreads();
-            if (lane == WAVE - 1) red[wv] = upto;
-            __syncthreads();
-            double at = before + (upto - mine);
-            for (int j = 0; j < wv; ++j) at += red[j];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                at += w[e];
-                if (w[e] > 0.0) {
-                    atomicMax(&last, v0 + e);
-                    if (at > bound) { atomicMin(&found, v0 + e); break; }
-                }
-            }
-            before += (red[0] + red[1]) + (red[2] + red[3]);
-            __syncthreads();
-            if (found != INT32_MAX) break;
         }
+        if (first_past != INT32_MAX) atomicMin(&found, first_past);
+        if (last_some >= 0) atomicMax(&last, last_some);
+    }
     __syncthreads();
     if (tid == 0) {
         const int v = found != INT32_MAX ? found : last >= 0 ? last : 0;
         as_global(a.out_tokens)[k.row] = v;
-        const double e = k.inv == 0.0 ? 0.0 : exponent<T>(row_of<T>(a.logits, a.row_stride, k.row), v, k.top, a.by_tau);
-        as_global(a.out_logprobs)[k.row] = k.inv == 0.0 ? -INFINITY : (float)((e + log2(k.inv)) * 0.69314718055994530942);
+        float logp = -INFINITY;
+        if (inv != 0.0) logp = (float)((((double)logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, k.row), v)) - (double)k.top) * a.by_tau + log2(inv)) * 0.69314718055994530942);
+        as_global(a.out_logprobs)[k.row] = logp;
     }
 }
 
@@ -332,7 +379,8 @@ int slices_for(int n_tokens, int vocab) {
 template <typename T, int E> hipError_t launch_each(hipStream_t s, const VerifyArgs &a) {
     hipLaunchKernelGGL((verify_sums_kernel<T, E>), dim3((unsigned)(a.n_tokens * (a.draft_logits ? 2 : 1) * a.slices)), dim3(NTV), 0, s, a);
     hipLaunchKernelGGL((verify_drafts_kernel<T, E>), dim3((unsigned)(a.n_seq * a.slices)), dim3(NTV), 0, s, a);
-    hipLaunchKernelGGL((verify_pick_kernel<T, E>), dim3((unsigned)a.n_seq), dim3(NTV), 0, s, a);
+    hipLaunchKernelGGL((verify_rest_kernel<T, E>), dim3((unsigned)(a.n_seq * a.slices)), dim3(NTV), 0, s, a);
+    hipLaunchKernelGGL((verify_pick_kernel<T>), dim3((unsigned)a.n_seq), dim3(NTV), 0, s, a);
     return hipGetLastError();
 }
 template <typename T> hipError_t launch(hipStream_t s, const VerifyArgs &a) { return each_for(a.n_tokens, a.vocab) == 8 ? launch_each<T, 8>(s, a) : launch_each<T, 32>(s, a); }
@@ -342,7 +390,8 @@ template <typename T> hipError_t launch(hipStream_t s, const VerifyArgs &a) { re
 extern "C" size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_tokens, int32_t vocab) {
     if (n_seq <= 0 || n_tokens < 0 || vocab <= 0) return 0;
     const size_t slices = (size_t)slices_for(n_tokens, vocab), rows = 2 * (size_t)n_tokens * slices;
-    return up256(rows * 8) + up256(rows * 4) + up256(n_seq * slices * 8) + up256(n_seq * sizeof(VerifyPick));
+    const size_t pieces = slices * (each_for(n_tokens, vocab) / 4);            // (of fp32 logits: the most)
+    return 2 * up256(rows * 4) + up256(2 * n_seq * pieces * 8) + up256(n_seq * pieces * 8) + up256(n_seq * sizeof(VerifyPick));
 }
 
 extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t row_stride, const void *draft_logits, int64_t draft_stride, const int32_t *tokens, const int32_t *first,
@@ -369,9 +418,11 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
     char *w = (char *)scratch;
     VerifyArgs a{logits, draft_logits, row_stride, draft_stride, tokens, first, u, n_seq, n_tokens, vocab, log2e / tau, draft_logits ? log2e / draft_tau : 1.0, out_tokens, out_logprobs, out_accepted, err, slices};
     const size_t row_sums = 2 * (size_t)n_tokens * slices;
-    a.sum = (double *)w; w += up256(row_sums * 8);
     a.top = (float *)w; w += up256(row_sums * 4);
-    a.rest = (double *)w; w += up256((size_t)n_seq * slices * 8);
+    a.sum = (float *)w; w += up256(row_sums * 4);
+    a.pieces = slices * (each_for(n_tokens, vocab) / (16 / el));
+    a.exact = (double *)w; w += up256(2 * (size_t)n_seq * a.pieces * 8);
+    a.rest = (double *)w; w += up256((size_t)n_seq * a.pieces * 8);
     a.pick = (VerifyPick *)w;
     hipStream_t s = (hipStream_t)hip_stream;
     if (n_tokens == 0) {                         // (sequences without tokens: a = 0 each)
