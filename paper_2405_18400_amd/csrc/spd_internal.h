@@ -267,6 +267,7 @@ struct PagedCache {
     const int32_t *table;
     int32_t n_pages, n_kv_heads, page_shift, d_head, n_seq, table_stride;
 };
+struct Divisor { uint32_t mul; int32_t shift; };   // n / d = (2 n mul >> 32) >> shift for n < 2^31
 struct AppendArgs {
     PagedCache c;
     const float *q, *k, *v;      // [n_tokens] rows, strides in elements
@@ -289,6 +290,7 @@ struct ReadArgs {
     int32_t n_tokens;
     void *k_out, *v_out;         // [n_tokens, n_kv_heads, d_head]
     int32_t *err;
+    Divisor by_token;            // pieces of eight elements of a token, keys and values
 };
 struct ReorderArgs {
     PagedCache c;                // layer 0's; layer l's pools start layer_bytes * l later
@@ -298,7 +300,6 @@ struct ReorderArgs {
     int32_t n_layers, width, n_groups, children, row_bytes, shares, heads_per_share;
     size_t layer_bytes;
 };
-struct Divisor { uint32_t mul; int32_t shift; };   // n / d = (2 n mul >> 32) >> shift for n < 2^31
 struct SharedAttnArgs {
     PagedCache c;
     const float *q;              // [n_seq, n_heads, d_head]

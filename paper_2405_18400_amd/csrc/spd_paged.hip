@@ -5,11 +5,12 @@
 // little.  What they need besides the data itself -- page numbers, angles, which row a beam goes
 // on in -- is formed again by every block that uses it: it is a few dozen instructions, and a
 // kernel of its own would cost a launch.
-#include "spd_device.h"
+#include "spd_attention.h"
 
 #include <algorithm>
 
 using namespace spdd;
+using namespace spda;
 
 namespace {
 
@@ -37,6 +38,11 @@ __device__ __forceinline__ uint32_t bf16_of(float v) {
 }
 template <> __device__ __forceinline__ void store_four<bf16_t>(void *p, size_t i, const float4 v) {
     store_words(p, i, bf16_of(v.x) | bf16_of(v.y) << 16, bf16_of(v.z) | bf16_of(v.w) << 16);
+}
+
+template <typename OT> __device__ __forceinline__ uint32_t two_words(float x, float y) {
+    if constexpr (sizeof(OT) == 2 && Type<OT>::PARTS == 2) return Store<half_t>::bits(x) | (uint32_t)Store<half_t>::bits(y) << 16;
+    else return bf16_of(x) | bf16_of(y) << 16;
 }
 
 // cos and sin of pos * theta^(-2i / d_head).  The angle is formed and reduced to a quarter turn in 64 bits (at position
@@ -244,45 +250,85 @@ template <> __device__ __forceinline__ void load_eight<q8_t>(const void *p, size
     for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)((e < 4 ? v.x : v.y) >> (8 * (e % 4)));
 }
 
-// A thread: eight elements of one row of one token, keys in front, then values.
-template <typename KT, typename OT>
+// A thread: U pieces of eight elements of a row, a block's width apart; a token's keys in front, then its values.  Places, page numbers and rows are three trips to memory, each of them
+// asked for all pieces at once.
+template <typename KT, typename OT, int U>
 __global__ __launch_bounds__(NTP) void read_paged_kernel(const ReadArgs a) {
-    const int d = a.c.d_head, row_pieces = a.c.n_kv_heads * d / 8;
-    const long long i = (long long)blockIdx.x * NTP + threadIdx.x;
-    const int t = (int)(i / (2 * row_pieces)), in_token = (int)(i % (2 * row_pieces));
-    if (t >= a.n_tokens) return;
-    const int seq = as_global(a.seq)[t], pos = as_global(a.pos)[t];
-    if (seq < 0) return;
-    if (seq >= a.c.n_seq || pos < 0 || (pos >> a.c.page_shift) >= a.c.table_stride) { flag(a.err); return; }
-    const int page = as_global(a.c.table)[(size_t)seq * a.c.table_stride + (pos >> a.c.page_shift)];
-    if (!page_ok(a.c, page)) { flag(a.err); return; }
-    const bool is_v = in_token >= row_pieces;
-    const int at = 8 * (is_v ? in_token - row_pieces : in_token), head = at / d, page_size = 1 << a.c.page_shift;
-    const size_t place = ((size_t)page * a.c.n_kv_heads + head) * page_size + (pos & (page_size - 1));
-    float x[8];
-    load_eight<KT>(is_v ? a.c.V : a.c.K, place * d + at % d, x);
-    if constexpr (sizeof(KT) == 1) {
-        const float scale = as_global(is_v ? a.v_scale : a.k_scale)[place];
+    const int d = a.c.d_head, row_pieces = a.c.n_kv_heads * d / 8, page_size = 1 << a.c.page_shift, pieces = a.n_tokens * 2 * row_pieces, i0 = blockIdx.x * (NTP * U) + threadIdx.x;
+    int token[U], seq[U], pos[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] *= scale;
-            asm("" : "+v"(x[e]));                // (an fp32 number: a value is the same whatever type it is read in.  Product and conversion as one instruction round once)
+    for (int u = 0; u < U; ++u) {
+        token[u] = over(min(i0 + u * NTP, pieces - 1), a.by_token);
+        seq[u] = as_global(a.seq)[token[u]];
+        pos[u] = as_global(a.pos)[token[u]];
+    }
+    int page[U];
+    bool ok[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        ok[u] = (unsigned)seq[u] < (unsigned)a.c.n_seq && pos[u] >= 0 && (pos[u] >> a.c.page_shift) < a.c.table_stride;
+        page[u] = ok[u] ? as_global(a.c.table)[(size_t)seq[u] * a.c.table_stride + (pos[u] >> a.c.page_shift)] : -1;
+    }
+    float x[U][8], scale[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        ok[u] = page_ok(a.c, page[u]);
+        if (!ok[u]) {
+            if (seq[u] >= 0) flag(a.err);        // (negative: padding)
+            continue;
+        }
+        const int in_token = min(i0 + u * NTP, pieces - 1) - token[u] * 2 * row_pieces, at = 8 * (in_token >= row_pieces ? in_token - row_pieces : in_token);
+        const bool is_v = in_token >= row_pieces;
+        const size_t place = ((size_t)page[u] * a.c.n_kv_heads + at / d) * page_size + (pos[u] & (page_size - 1));
+        load_eight<KT>(is_v ? a.c.V : a.c.K, place * d + at % d, x[u]);
+        if constexpr (sizeof(KT) == 1) scale[u] = as_global(is_v ? a.v_scale : a.k_scale)[place];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!ok[u] || i0 + u * NTP >= pieces) continue;
+        if constexpr (sizeof(KT) == 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[u][e] *= scale[u];
+                asm("" : "+v"(x[u][e]));         // (an fp32 number: a value is the same whatever type it is read in.  Product and conversion as one instruction round once)
+            }
+        }
+        const int in_token = i0 + u * NTP - token[u] * 2 * row_pieces, at = 8 * (in_token >= row_pieces ? in_token - row_pieces : in_token);
+        void *out = in_token >= row_pieces ? a.v_out : a.k_out;
+        const size_t to = (size_t)token[u] * a.c.n_kv_heads * d + at;
+        if constexpr (sizeof(OT) == 2) {
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = two_words<OT>(x[u][2 * e], x[u][2 * e + 1]);
+            *(u32x4 __attribute__((address_space(1))) *)((uint16_t *)out + to) = w;
+        } else {
+            store_four<OT>(out, to, make_float4(x[u][0], x[u][1], x[u][2], x[u][3]));
+            store_four<OT>(out, to + 4, make_float4(x[u][4], x[u][5], x[u][6], x[u][7]));
         }
     }
-    void *out = is_v ? a.v_out : a.k_out;
-    const size_t to = (size_t)t * a.c.n_kv_heads * d + at;
-    store_four<OT>(out, to, make_float4(x[0], x[1], x[2], x[3]));
-    store_four<OT>(out, to + 4, make_float4(x[4], x[5], x[6], x[7]));
+}
+
+template <typename KT, typename OT>
+hipError_t launch_read_as(hipStream_t s, ReadArgs a) {
+    const int per_token = 2 * (a.c.n_kv_heads * a.c.d_head / 8), most = std::max(1, (1 << 30) / per_token), n = a.n_tokens;      // (pieces are counted in 31 bits)
+    const size_t token_bytes = (size_t)a.c.n_kv_heads * a.c.d_head * sizeof(OT);
+    a.by_token = divisor(per_token);
+    for (int t = 0; t < n; t += most) {
+        ReadArgs b = a;
+        b.n_tokens = std::min(most, n - t);
+        b.seq += t; b.pos += t;
+        b.k_out = (char *)a.k_out + (size_t)t * token_bytes; b.v_out = (char *)a.v_out + (size_t)t * token_bytes;
+        const long long pieces = (long long)b.n_tokens * per_token;
+        // few pieces: one per thread, so that many blocks share the way to memory
+        if (pieces < 4LL * NTP * 1024) hipLaunchKernelGGL((read_paged_kernel<KT, OT, 1>), dim3((unsigned)((pieces + NTP - 1) / NTP)), dim3(NTP), 0, s, b);
+        else hipLaunchKernelGGL((read_paged_kernel<KT, OT, 4>), dim3((unsigned)((pieces + 4 * NTP - 1) / (4 * NTP))), dim3(NTP), 0, s, b);
+    }
+    return hipGetLastError();
 }
 
 template <typename KT>
 hipError_t launch_read(hipStream_t s, const ReadArgs &a, int out_dtype) {
-    const long long pieces = (long long)a.n_tokens * 2 * (a.c.n_kv_heads * a.c.d_head / 8), blocks = (pieces + NTP - 1) / NTP;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    if (out_dtype == SPD_DTYPE_FP32) hipLaunchKernelGGL((read_paged_kernel<KT, float>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
-    else if (out_dtype == SPD_DTYPE_FP16) hipLaunchKernelGGL((read_paged_kernel<KT, half_t>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
-    else hipLaunchKernelGGL((read_paged_kernel<KT, bf16_t>), dim3((unsigned)blocks), dim3(NTP), 0, s, a);
-    return hipGetLastError();
+    return out_dtype == SPD_DTYPE_FP32 ? launch_read_as<KT, float>(s, a) : out_dtype == SPD_DTYPE_FP16 ? launch_read_as<KT, half_t>(s, a) : launch_read_as<KT, bf16_t>(s, a);
 }
 
 // What the beams of a group go on in, one lane per beam.  A row's first child keeps it; further children take the rows that
