@@ -14,6 +14,7 @@
 #include "spd_attention.h"
 
 #include <algorithm>
+#include <type_traits>
 
 using namespace spdd;
 using namespace spda;
@@ -51,6 +52,8 @@ template <typename KT, typename IO, int DH, int RW> struct Shape {
     // twice).
     static constexpr int FS = DH == 256 && (T::F32 || T::PARTS == 3) ? 2 : 1;
     static constexpr int ST = 2, LDS = ST * BYTES;
+    // 8 bits with few rows: codes are asked for two stages ahead of their products (half the bytes of a stage are under way where 16 bits have all)
+    static constexpr int DEPTH = T::Q8 && RW == 2 && DH <= 128 ? 2 : 1;
     static constexpr int PER_CU = LDS <= 80 * 1024 && DH <= 128 && T::PARTS < 3 && !T::F32 ? 2 : 1;   // blocks side by side: 256 or 512 registers
 };
 
@@ -216,11 +219,12 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     constexpr bool F32 = T::F32, Q8 = T::Q8;
     constexpr int PARTS = T::PARTS, KW = S::KW, ROWS = S::ROWS, ROWB = S::ROWB, PIECES = S::PIECES, SK = S::SK, NU = S::NU, HALF = S::HALF, BYTES = S::BYTES, LOADS = S::LOADS;
     constexpr bool LEAN = DH == 256 || Q8;                   // registers are scarce
-    constexpr int FS = S::FS, NJ = F32 ? DH / 8 : DH / 16, NF = DH / TR / FS, PIECE_EL = F32 ? 4 : 8, LOG2_ROWS = RW == 4 ? 7 : 6;
+    constexpr int DEPTH = S::DEPTH, FS = S::FS, NJ = F32 ? DH / 8 : DH / 16, NF = DH / TR / FS, PIECE_EL = F32 ? 4 : 8, LOG2_ROWS = RW == 4 ? 7 : 6;
     extern __shared__ __align__(1024) char lds[];
-    __shared__ int bad_stage[2], odd_stage[2];               // the stage, + 1, that has a key on no page, a value that is no finite number
+    __shared__ int bad_stage[4], odd_stage[2];               // the stage, + 1, that has a key on no page, a value that is no finite number
     __shared__ __align__(16) float k_sc[2][SK], v_sc[2][SK];
     __shared__ int v_exp[2];
+    __shared__ u64 odd_keys[2];
     __shared__ float join_m[RW][WAVE], join_l[RW][WAVE];
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane & (TR - 1), h = lane / TR, rw = wv % RW, kw = wv / RW;
     const int d = p.c.d_head, shift = p.c.page_shift, in_page = (1 << shift) - 1, group = p.group;
@@ -255,7 +259,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const int row_bytes = d * (int)sizeof(KT), row_shift = 31 - __builtin_clz((unsigned)row_bytes), head_shift = row_shift + shift;
     const char *K = (const char *)p.c.K, *V = (const char *)p.c.V;
     const int32_t *entries = p.c.table + (size_t)own.seq * p.c.table_stride;
-    if (tid < 2) bad_stage[tid] = odd_stage[tid] = 0;
+    if (tid < 4) bad_stage[tid] = odd_stage[tid % 2] = 0;
     if constexpr (DH == 32) {                                // heads narrower than the tile: nothing is ever put behind their ends
         for (int i = tid; i < S::LDS / 16; i += NT) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
@@ -265,20 +269,22 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     // addresses are the wave's, a lane's part of them stays the same.
     constexpr int KEYS = WAVE / PIECES;
     const bool whole = KEYS <= 4 || KEYS <= 1 << shift;
-    int page[LOADS], scale_page = 0;
-    const auto ask = [&](int t) {
+    int page[DEPTH][LOADS], scale_page[DEPTH];
+    const auto ask = [&](int t, auto set) {
+        constexpr int X = decltype(set)::value;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key = (wv * WAVE + i * NT) / PIECES;
-            page[i] = as_global(entries)[whole ? min(lo + t * SK + key, (hi - 1) & ~(KEYS - 1)) >> shift : min(lo + t * SK + key + lane / PIECES, hi - 1) >> shift];
+            page[X][i] = as_global(entries)[whole ? min(lo + t * SK + key, (hi - 1) & ~(KEYS - 1)) >> shift : min(lo + t * SK + key + lane / PIECES, hi - 1) >> shift];
         }
         if constexpr (Q8)
-            if (wv < 2) scale_page = as_global(entries)[min(lo + t * SK + lane % SK, hi - 1) >> shift];
+            if (wv < 2) scale_page[X] = as_global(entries)[min(lo + t * SK + lane % SK, hi - 1) >> shift];
     };
-    u32x2 kc[LOADS], vc[LOADS];                              // Q8: a stage's codes and scales on their way
-    float scale_in = 0.f;
+    u32x2 kc[DEPTH][LOADS], vc[DEPTH][LOADS];                // Q8: a stage's codes and scales on their way
+    float scale_in[DEPTH];
     int drop = 0, drop_next = 0, v_top = -200;               // (drop: bit i: this thread's piece i of the stage is of a key that does not count)
-    const auto fetch = [&](int t) {
+    const auto fetch = [&](int t, auto set) {
+        constexpr int X = decltype(set)::value;
         char *to = lds + (t % 2) * BYTES + wv * (WAVE * 16);
         const bool end = lo + (t + 1) * SK > hi;
         int lane = tid & (WAVE - 1);
@@ -291,8 +297,8 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             const int kp = k_place<PIECES>(key, slot), vp = v_place<PIECES, F32>(key, slot);
             const auto issue = [&](const char *k_row, const char *v_row, uint32_t off) {
                 if constexpr (Q8) {
-                    if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
-                    if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
+                    if (DH > 32 || 8 * kp < d) kc[X][i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
+                    if (DH > 32 || 8 * vp < d) vc[X][i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
                 } else {
                     if (DH > 32 || PIECE_EL * kp < d) stage16(k_row, off + 16 * kp, to + i * (NT * 16));
                     if ((DH > 32 || PIECE_EL * vp < d) && of_share(i)) stage16(v_row, off + 16 * vp, to + HALF + i * (NT * 16));
@@ -300,16 +306,16 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             };
             bool ok;
             if (whole) {                                     // the wave's first row, and the lane's behind it
-                const int pg = __builtin_amdgcn_readfirstlane(page[i]), pos0 = min(lo + t * SK + key0, (hi - 1) & ~(KEYS - 1));
+                const int pg = __builtin_amdgcn_readfirstlane(page[X][i]), pos0 = min(lo + t * SK + key0, (hi - 1) & ~(KEYS - 1));
                 ok = (unsigned)pg < (unsigned)p.c.n_pages;
                 const u64 row = ((u64)(uint32_t)((ok ? pg : 0) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(pos0 & in_page) << row_shift);
                 issue(K + row, V + row, (uint32_t)(lane / PIECES) << row_shift);
             } else {                                         // short pages: page by page, each for its own lanes
-                ok = (unsigned)page[i] < (unsigned)p.c.n_pages;
+                ok = (unsigned)page[X][i] < (unsigned)p.c.n_pages;
                 const int pos0 = min(at, hi - 1);
                 u64 left = __ballot(true);
                 while (left) {
-                    const int first = __builtin_ctzll(left), pg = __builtin_amdgcn_readlane(page[i], first), pos1 = __builtin_amdgcn_readlane(pos0, first) & ~in_page;
+                    const int first = __builtin_ctzll(left), pg = __builtin_amdgcn_readlane(page[X][i], first), pos1 = __builtin_amdgcn_readlane(pos0, first) & ~in_page;
                     const bool mine = (pos0 & ~in_page) == pos1;
                     left &= ~__ballot(mine);
                     const u64 row = (u64)(uint32_t)(((unsigned)pg < (unsigned)p.c.n_pages ? pg : 0) * p.c.n_kv_heads + kvh) << head_shift;
@@ -322,44 +328,51 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         if constexpr (Q8) {
             if (wv < 2) {
                 const int at = lo + t * SK + lane % SK;
-                const bool ok = (unsigned)scale_page < (unsigned)p.c.n_pages;
-                scale_in = 0.f;
-                if (ok && at < hi) scale_in = as_global(wv == 0 ? p.k_scale : p.v_scale)[((size_t)(uint32_t)(scale_page * p.c.n_kv_heads + kvh) << shift) + (at & in_page)];
+                const bool ok = (unsigned)scale_page[X] < (unsigned)p.c.n_pages;
+                scale_in[X] = 0.f;
+                if (ok && at < hi) scale_in[X] = as_global(wv == 0 ? p.k_scale : p.v_scale)[((size_t)(uint32_t)(scale_page[X] * p.c.n_kv_heads + kvh) << shift) + (at & in_page)];
             }
         }
         if (bad) {
-            bad_stage[t % 2] = t + 1;
+            bad_stage[t % 4] = t + 1;
             if (p.err) *as_global(p.err) = 1;
         }
     };
-    const auto put = [&](int t) {                            // Q8: codes and scales to LDS
+    const auto put = [&](int t, auto set) {                  // Q8: codes and scales to LDS
+        constexpr int X = decltype(set)::value;
         char *to = lds + (t % 2) * BYTES;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int slot = (tid + i * NT) % PIECES, key = (tid + i * NT) / PIECES;
             u32x4 x;
             uint32_t a, b;
-            codes_to_half(kc[i].x, a, b); x.x = a; x.y = b;
-            codes_to_half(kc[i].y, a, b); x.z = a; x.w = b;
+            codes_to_half(kc[X][i].x, a, b); x.x = a; x.y = b;
+            codes_to_half(kc[X][i].y, a, b); x.z = a; x.w = b;
             if (DH > 32 || 8 * k_place<PIECES>(key, slot) < d) *(u32x4 *)(to + (tid + i * NT) * 16) = x;
-            codes_to_half(vc[i].x, a, b); x.x = a; x.y = b;
-            codes_to_half(vc[i].y, a, b); x.z = a; x.w = b;
+            codes_to_half(vc[X][i].x, a, b); x.x = a; x.y = b;
+            codes_to_half(vc[X][i].y, a, b); x.z = a; x.w = b;
             if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + (tid + i * NT) * 16) = x;
         }
-        if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in;
+        if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in[X];
         if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
-            const float size = fabsf(scale_in);
+            const float size = fabsf(scale_in[X]);
             int ex = -200;
             if (size > 0.f && size < INFINITY) (void)frexpf(size, &ex);
 #pragma unroll
             for (int o = 1; o < WAVE; o <<= 1) ex = max(ex, __shfl_xor(ex, o, WAVE));
             v_top = max(v_top, ex);
-            if (lane < SK) v_sc[t % 2][lane] = ldexpf(scale_in, -v_top);
+            const bool odd = !(size < INFINITY);             // counts as zero; rows that see it get no number
+            if (lane < SK) v_sc[t % 2][lane] = odd ? 0.f : ldexpf(scale_in[X], -v_top);
+            const u64 keys = __ballot(odd && lane < SK);
+            if (keys && lane == 0) { odd_stage[t % 2] = t + 1; odd_keys[t % 2] = keys; }
             if (lane == 0) v_exp[t % 2] = v_top;
         }
     };
 
-    ask(0);
+    constexpr std::integral_constant<int, 0> EVEN{};
+    constexpr std::integral_constant<int, DEPTH - 1> ODD{};  // (which of the sets a stage's are)
+    ask(0, EVEN);
+    if (DEPTH == 2 && stages > 1) ask(1, ODD);
     // this lane's query: its row's features 16 j + 8 h .. + 7 (fp32: 8 j + 4 h .. + 3)
     u32x4 Q[NJ][PARTS];
     float scale = 1.4426950408889634f / sqrtf((float)d);     // to logarithms of base 2
@@ -420,12 +433,13 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     float m = -INFINITY, l = 0.f;
     int o_exp = -200;                                        // Q8: O is held by this power of two
     __syncthreads();                                         // (the stages' marks)
-    fetch(0);
+    fetch(0, EVEN);
     drop = drop_next;
-    if (stages > 1) ask(1);
-    if constexpr (Q8) put(0);
+    if (DEPTH == 2 && stages > 1) fetch(1, ODD);
+    if (stages > DEPTH) ask(DEPTH, EVEN);
+    if constexpr (Q8) put(0, EVEN);
 
-    for (int t = 0; t < stages; ++t) {
+    const auto stage = [&](int t, auto mine, auto other) {
         const int stage0 = lo + t * SK;
         char *const k_tile = lds + (t % 2) * BYTES, *const v_tile = k_tile + HALF;
         if constexpr (!Q8) {
@@ -444,11 +458,11 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + 1 < stages) {
-            fetch(t + 1);
-            if (t + 2 < stages) ask(t + 2);
+        if (t + DEPTH < stages) {
+            fetch(t + DEPTH, mine);
+            if (t + DEPTH + 1 < stages) ask(t + DEPTH + 1, other);
         }
-        const bool any_bad = bad_stage[t % 2] == t + 1;
+        const bool any_bad = bad_stage[t % 4] == t + 1;
         const int tb = stage0 + kw * (TR * NU), key_base = kw * (TR * NU);
         if (!Q8 && odd_stage[t % 2] == t + 1) {              // seldom: rows that see such a value get no number at its feature, and it counts as zero from here on
             if (active)
@@ -489,10 +503,18 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             }
             __syncthreads();
         }
+        if (Q8 && odd_stage[t % 2] == t + 1) {
+            bool seen = false;
+            for (u64 left = odd_keys[t % 2]; left; left &= left - 1) seen = seen || stage0 + __builtin_ctzll(left) <= pos;
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[f][i] = seen ? NAN : o[f][i];
+        }
         if (active && tb <= wave_hi) {
             f32x16 st[NU];
             // pieces of keys are asked for KD ahead of their products
-            constexpr int KD = NJ < 4 ? NJ : DH == 256 && (F32 || PARTS == 3) ? 2 : LEAN ? 4 : NJ < 8 ? NJ : 8, STEPS = NU * NJ;
+            constexpr int KD = NJ < 4 ? NJ : (DH == 256 && (F32 || PARTS == 3)) || (Q8 && PARTS == 2 && RW == 4) ? 2 : LEAN ? 4 : NJ < 8 ? NJ : 8, STEPS = NU * NJ;
             int k_off = 16 * k_place<PIECES>(key_base + col, h);             // (piece 2 j + h lies where piece h does, but for the bits of 2 j)
             if constexpr (LEAN) asm volatile("" : "+v"(k_off));              // (formed from here on in every stage: kept, the places of all pieces are a register each)
             const char *k_row = k_tile + (key_base + col) * ROWB;
@@ -605,36 +627,34 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                         }
                     }
                 } else {
-                    u32x4 pt[2][PARTS];
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        float pf[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            pf[e] = __builtin_amdgcn_exp2f(fmaf(st[u][i + e], scale, -ref));
-                            if (T::P_SCALE != 1.f) pf[e] *= T::P_SCALE;
-                        }
-                        if constexpr (PARTS > 1 || Q8) l += (pf[0] + pf[1]) + (pf[2] + pf[3]);
-                        if constexpr (Q8) {
-                            const float4 s = *(const float4 *)&v_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
-                            const float by[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) pf[e] = masked && pf[e] == 0.f ? 0.f : pf[e] * by[e];
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; e += 2) {
-                            uint32_t part[PARTS];
-                            probability_parts<LT, PARTS>(pf[e], pf[e + 1], part);
-                            if constexpr (PARTS == 1 && !Q8) l = pair_sum<LT>(part[0], l);       // (of what they weigh, one instruction for two)
-#pragma unroll
-                            for (int q = 0; q < PARTS; ++q) pt[i / 8][q][(i % 8) / 2 + e / 2] = part[q];
-                        }
-                    }
                     int at4 = lane % 16;
                     if constexpr (LEAN) asm volatile("" : "+v"(at4));
                     const int t4 = at4 / 4, fg = (lane / 16) % 2;
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
+                    for (int g = 0; g < 2; ++g) {            // 16 keys at a time
+                        u32x4 pt[PARTS];
+#pragma unroll
+                        for (int i = 8 * g; i < 8 * g + 8; i += 4) {
+                            float pf[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                pf[e] = __builtin_amdgcn_exp2f(fmaf(st[u][i + e], scale, -ref));
+                                if (T::P_SCALE != 1.f) pf[e] *= T::P_SCALE;
+                            }
+                            if constexpr (PARTS > 1 || Q8) l += (pf[0] + pf[1]) + (pf[2] + pf[3]);
+                            if constexpr (Q8) {
+                                const float4 s = *(const float4 *)&v_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
+                                pf[0] *= s.x; pf[1] *= s.y; pf[2] *= s.z; pf[3] *= s.w;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; e += 2) {
+                                uint32_t part[PARTS];
+                                probability_parts<LT, PARTS>(pf[e], pf[e + 1], part);
+                                if constexpr (PARTS == 1 && !Q8) l = pair_sum<LT>(part[0], l);       // (of what they weigh, one instruction for two)
+#pragma unroll
+                                for (int q = 0; q < PARTS; ++q) pt[q][(i % 8) / 2 + e / 2] = part[q];
+                            }
+                        }
                         const int key = key_base + TR * u + 16 * g + 4 * h + t4;
 #pragma unroll
                         for (int f = 0; f < NF; ++f) {
@@ -642,15 +662,19 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                             const u32x2 x = turned_read(at), y = turned_read(at + 8 * ROWB);
                             const u32x4 v{x.x, x.y, y.x, y.y};
 #pragma unroll
-                            for (int q = PARTS - 1; q >= 0; --q) o[f] = mfma32<LT>(v, pt[g][q], o[f]);
+                            for (int q = PARTS - 1; q >= 0; --q) o[f] = mfma32<LT>(v, pt[q], o[f]);
                         }
                     }
                 }
             }
         }
         if constexpr (Q8)
-            if (t + 1 < stages) put(t + 1);
+            if (t + 1 < stages) put(t + 1, other);
         drop = drop_next;
+    };
+    for (int t = 0; t < stages; t += DEPTH) {
+        stage(t, EVEN, ODD);
+        if (DEPTH == 2 && t + 1 < stages) stage(t + 1, ODD, EVEN);
     }
     l += __shfl_xor(l, TR, WAVE);
     if constexpr (KW > 1) {                                  // two waves have shared out the keys of the same rows
