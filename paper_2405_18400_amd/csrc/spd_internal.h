@@ -323,7 +323,7 @@ struct PagedAttnArgs {
     int32_t *err;
     int32_t n_tokens, n_heads, group, max_len;
     int32_t n_tiles, splits, chunk;   // tiles of rows at most; chunks of positions, and the positions of one
-    Divisor by_group, by_kv_heads, by_splits;
+    Divisor by_group, by_kv_heads, by_splits, by_heads, by_chunk;
     float *part_ml, *part;       // scratch, [n_tokens, n_heads, splits]: reference and sum; O over that sum [.., d_head]
 };
 struct VerifyArgs {
