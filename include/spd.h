@@ -429,7 +429,7 @@ int spd_op_read_paged(int32_t dtype, const void *K, const void *V, const float *
  * fp16 or bf16.  In fp32 queries and probabilities go into the products with 24 bits, in 16 bits with those of the type.  max_len >= every len[s] (a host
  * value; no more than a row of the table holds) and max_new, the most new tokens of a sequence, size the launch: a sequence with more of them is taken as well, only slower.
  * A sequence whose first and len do not fit (first negative or past n_tokens, len below its new tokens or over max_len) gets zeros for the rows that it has; where first descends anywhere no row
- * is written; *err is set.  Rows that are no sequence's are left as they were.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
+ * is written; *err is set.  Rows that are no sequence's are left as they were.  n_seq is at most 65536, n_tokens n_heads at most 2^24.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
  * sequence's last position, or behind a token's own, gets into its result. */
 size_t spd_op_attention_paged_scratch_bytes(int32_t dtype, int32_t io_dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                             int32_t max_new, int32_t max_len);
@@ -443,7 +443,8 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * the drafter drew token t + 1 from, q = softmax(draft_logits / draft_tau), not looked at for a sequence's last token.  draft_logits NULL: drafts that were chosen, not drawn, q
  * is 1 at the draft.  u (DEVICE float [n_tokens], in [0, 1), the caller's draws): draft x behind token t stands if all before it do and u[t] q(x) < p(x); so a text has the target's distribution whatever
  * the drafter's is.  Behind the drafts that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0) at the
- * first that does not (from p where that is zero everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  Sums and what is compared are formed in 64 bits.
+ * first that does not (from p where that is zero everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  u q(x) and p(x) are compared with
+ * sums of fp32 exponentials, off by about 1e-8 of themselves; the row that a token is drawn from is summed in 64 bits.  tau and draft_tau lie between 2^-100 and 2^100, n_seq is at most 65536.
  * A logit that is no number counts as -inf, +inf as the largest finite number.  A draft outside [0, vocab) does not stand; *err is set.
  * Outputs, DEVICE: out_accepted int32 [n_seq], the number a of drafts that stand; at first[s] .. first[s] + a of out_tokens int32 [n_tokens] those drafts and the token
  * behind them, and of out_logprobs float [n_tokens] their log p; -1 and 0 at the sequence's other tokens.  A row without a finite logit gives token 0 with log p = -inf, *err is set.  A

@@ -229,7 +229,6 @@ __global__ __launch_bounds__(NTP) void append_q8_kernel(const AppendQ8Args p) {
 hipError_t launch_append_q8(hipStream_t s, AppendQ8Args p) {
     bool few;
     const long long blocks = append_blocks(p.a, few);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     if (few) hipLaunchKernelGGL((append_q8_kernel<1>), dim3((unsigned)blocks), dim3(NTP), 0, s, p);
     else hipLaunchKernelGGL((append_q8_kernel<4>), dim3((unsigned)blocks), dim3(NTP), 0, s, p);
     return hipGetLastError();
@@ -528,6 +527,8 @@ extern "C" int spd_op_append_paged_q8(int8_t *K, int8_t *V, float *K_scale, floa
     const size_t scales = spdk::scale_bytes(c);
     rc = append_status(p.a, spdk::pool_bytes(SPD_DTYPE_INT8, c), {K_scale, scales}, {V_scale, scales}, rope_theta);
     if (rc != SPD_OK || n_tokens == 0) return rc;
+    bool few;
+    if (append_blocks(p.a, few) > UINT32_MAX / NTP) return SPD_EINVAL;           // (threads of a grid are counted in 32 bits)
     return launch_append_q8((hipStream_t)hip_stream, p) == hipSuccess ? SPD_OK : SPD_EHIP;
 }
 

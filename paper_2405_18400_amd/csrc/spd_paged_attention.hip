@@ -770,7 +770,7 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(const PagedAttnArgs p) 
 
 // How a call is cut.
 struct Cut { int rows, splits, chunk; };
-constexpr int CUS = 256, CHUNK_MIN = 256;
+constexpr int CUS = 256, CHUNK_MIN = 256, SEQS_MAX = 1 << 16;        // (every block looks through the sequences)
 Cut cut_for(int dtype, int io_dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int d_head, int max_new, int max_len) {
     const long long group = n_heads / n_kv_heads;
     Cut c;
@@ -790,7 +790,6 @@ hipError_t launch_rows(hipStream_t s, PagedAttnArgs a) {
     typedef Shape<KT, IO, DH, RW> S;
     a.n_tiles = (int)((long long)a.n_tokens * a.group / S::ROWS + a.c.n_seq);
     const long long blocks = (long long)a.n_tiles * a.c.n_kv_heads * a.splits * S::FS;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     if (S::LDS > 60 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void *)paged_attn_kernel<KT, IO, DH, RW>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
         if (e != hipSuccess) return e;
@@ -842,7 +841,7 @@ extern "C" int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const voi
     if (!io_fits(dtype, io_dtype) || n_tokens < 0 || n_heads < 1 || n_heads % n_kv_heads || max_new < 0 || max_len < 0 || max_len > (long long)table_stride * page_size || max_len > INT32_MAX / 2 ||
         (long long)n_pages * n_kv_heads > INT32_MAX) return SPD_EINVAL;
     if (n_tokens == 0 || n_seq == 0) return SPD_OK;
-    if ((long long)n_tokens * n_heads > (1 << 24) || n_seq > (1 << 20)) return SPD_EINVAL;
+    if ((long long)n_tokens * n_heads > (1 << 24) || n_seq > SEQS_MAX) return SPD_EINVAL;
     const int io_bytes = io_dtype == SPD_DTYPE_FP32 ? 4 : 2;
     if (!q || !first || !len || !out || ((uintptr_t)q | (uintptr_t)out) % 16 || q_stride < (int64_t)n_heads * d_head || q_stride % 8) return SPD_EINVAL;
     const size_t need = spd_op_attention_paged_scratch_bytes(dtype, io_dtype, n_seq, n_tokens, n_heads, n_kv_heads, d_head, max_new, max_len);
@@ -855,6 +854,7 @@ extern "C" int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const voi
     if (spdk::over_any(so, {sq, sK, sV, sk, sv, st, sf, sl, se, sw}) || spdk::over_any(sw, {sq, sK, sV, sk, sv, st, sf, sl, se})) return SPD_EINVAL;
     const Cut cut = cut_for(dtype, io_dtype, n_seq, n_tokens, n_heads, n_kv_heads, d_head, max_new, max_len);
     const int group = n_heads / n_kv_heads;
+    if (((long long)n_tokens * group / cut.rows + n_seq) * n_kv_heads * cut.splits * 2 > UINT32_MAX / NT) return SPD_EINVAL;       // (threads of a grid are counted in 32 bits)
     PagedAttnArgs a{c, K_scale, V_scale, q, q_stride, out, first, len, err, n_tokens, n_heads, group, max_len, 0, cut.splits, cut.chunk, divisor(group), divisor(n_kv_heads), divisor(cut.splits), divisor(n_heads), divisor(cut.chunk),
                     (float *)scratch, (float *)((char *)scratch + up256((size_t)n_tokens * n_heads * cut.splits * 8))};
     hipStream_t s = (hipStream_t)hip_stream;

@@ -369,6 +369,9 @@ __global__ __launch_bounds__(NTV) void verify_pick_kernel(const VerifyArgs a) {
     }
 }
 
+constexpr int SEQS_MAX = 1 << 16;                // (every block looks through the sequences)
+constexpr float TAU_MIN = 0x1p-100f;             // (and 1 / tau: what fp32 exponents hold)
+
 // Logits per thread of a slice: 32, or 8 where that leaves too few blocks to fill the GPU.
 int each_for(int n_tokens, int vocab) { return (long long)n_tokens * 2 * ((vocab + 32 * NTV - 1) / (32 * NTV)) < 512 ? 8 : 32; }
 int slices_for(int n_tokens, int vocab) {
@@ -399,9 +402,9 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
                                     int32_t *out_accepted, void *scratch, size_t scratch_bytes, int32_t *err, void *hip_stream) {
     if (dtype != SPD_DTYPE_FP32 && dtype != SPD_DTYPE_BF16 && dtype != SPD_DTYPE_FP16) return SPD_EINVAL;
     const int el = dtype == SPD_DTYPE_FP32 ? 4 : 2;
-    if (n_seq < 0 || n_tokens < 0 || vocab < 1 || vocab > (1 << 24) || !(tau > 0.f) || !(tau < INFINITY) || (draft_logits && (!(draft_tau > 0.f) || !(draft_tau < INFINITY)))) return SPD_EINVAL;
+    if (n_seq < 0 || n_tokens < 0 || vocab < 1 || vocab > (1 << 24) || !(tau >= TAU_MIN) || !(tau <= 1.f / TAU_MIN) || (draft_logits && (!(draft_tau >= TAU_MIN) || !(draft_tau <= 1.f / TAU_MIN)))) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
-    if (!first || !out_accepted || (n_tokens > 0 && (!logits || !tokens || !u || !out_tokens || !out_logprobs)) || n_seq > (1 << 20) || n_tokens > (1 << 20)) return SPD_EINVAL;
+    if (!first || !out_accepted || (n_tokens > 0 && (!logits || !tokens || !u || !out_tokens || !out_logprobs)) || n_seq > SEQS_MAX || n_tokens > (1 << 20)) return SPD_EINVAL;
     if (row_stride < vocab || (draft_logits && draft_stride < vocab) || ((uintptr_t)logits | (uintptr_t)draft_logits) % el) return SPD_EINVAL;
     const size_t need = spd_op_verify_drafts_scratch_bytes(n_seq, n_tokens, vocab);
     if (need && (!scratch || (uintptr_t)scratch % 256)) return SPD_EINVAL;
@@ -413,7 +416,7 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
     if (spdk::over_any(ot, {sz, sd, st, sf, su, ol, oa, se, sw}) || spdk::over_any(ol, {sz, sd, st, sf, su, oa, se, sw}) || spdk::over_any(oa, {sz, sd, st, sf, su, se, sw}) ||
         spdk::over_any(sw, {sz, sd, st, sf, su, se})) return SPD_EINVAL;
     const int slices = slices_for(n_tokens, vocab);
-    if ((long long)std::max(2 * n_tokens, n_seq) * slices > INT32_MAX) return SPD_EINVAL;
+    if ((long long)std::max(2 * n_tokens, n_seq) * slices > UINT32_MAX / NTV) return SPD_EINVAL;      // (threads of a grid are counted in 32 bits)
     const double log2e = 1.4426950408889634074;
     char *w = (char *)scratch;
     VerifyArgs a{logits, draft_logits, row_stride, draft_stride, tokens, first, u, n_seq, n_tokens, vocab, log2e / tau, draft_logits ? log2e / draft_tau : 1.0, out_tokens, out_logprobs, out_accepted, err, slices};

@@ -78,7 +78,8 @@ def test_scales_come_with_8_bits_alone(pkg, dtype):
 @pytest.mark.parametrize("what,value", BAD_POOLS + [("dtype", 4), ("dtype", -1), ("io_dtype", 3), ("io_dtype", -1), ("n_heads", 0), ("n_heads", 3), ("n_heads", -2), ("max_new", -1), ("max_len", -1), ("max_len", 961),
                                                     ("max_len", (1 << 31) - 1), ("n_tokens", -1), ("q", None), ("q", 6 * A + 8), ("out", None), ("out", 9 * A + 4), ("first", None), ("len", None), ("q_stride", 252),
                                                     ("q_stride", 260), ("q_stride", 255), ("scratch", 16 * A + 64), ("n_tokens", 1 << 24), ("out", 6 * A), ("out", 6 * A + 16), ("out", 6 * A + 29 * 1024),
-                                                    ("out", A), ("out", 3 * A), ("out", 5 * A), ("out", 7 * A), ("out", 8 * A), ("err", 9 * A + 4)])
+                                                    ("out", A), ("out", 3 * A), ("out", 5 * A), ("out", 7 * A), ("out", 8 * A), ("err", 9 * A + 4),
+                                                    ("n_seq", (1 << 16) + 1), ("n_pages", 1 << 30)])
 def test_attention_refuses(pkg, what, value):
     if what == "scratch" and not pkg.lib().spd_op_attention_paged_scratch_bytes(3, 0, 6, 30, 4, 2, 64, 9, 960):
         pytest.skip("this call takes no scratch")
@@ -107,7 +108,8 @@ def test_attention_scratch(pkg):
 @pytest.mark.parametrize("what,value", [("dtype", 3), ("dtype", -1), ("logits", None), ("logits", A + 2), ("draft_logits", 2 * A + 2), ("row_stride", 4999), ("draft_stride", 4999), ("tokens", None), ("first", None),
                                         ("u", None), ("n_seq", -1), ("n_tokens", -1), ("vocab", 0), ("vocab", -1), ("vocab", (1 << 24) + 1), ("tau", 0.0), ("tau", -1.0), ("tau", math.inf), ("tau", math.nan),
                                         ("draft_tau", 0.0), ("draft_tau", math.nan), ("out_tokens", None), ("out_logprobs", None), ("out_accepted", None), ("out_tokens", 3 * A), ("out_tokens", A + 4), ("out_logprobs", 5 * A),
-                                        ("out_logprobs", 6 * A + 4), ("out_accepted", 4 * A), ("out_accepted", 7 * A + 24), ("err", 8 * A + 8), ("out_tokens", 2 * A + 6 * 20000 + 19996)])
+                                        ("out_logprobs", 6 * A + 4), ("out_accepted", 4 * A), ("out_accepted", 7 * A + 24), ("err", 8 * A + 8), ("out_tokens", 2 * A + 6 * 20000 + 19996), ("n_seq", (1 << 16) + 1), ("n_tokens", (1 << 20) + 1), ("tau", 2.0 ** -101), ("tau", 2.0 ** 101),
+                                        ("draft_tau", 2.0 ** -101), ("draft_tau", 2.0 ** 101)])
 def test_verify_refuses(pkg, what, value):
     assert call(pkg, "spd_op_verify_drafts", VERIFY, **{what: value}) == EINVAL
 
@@ -123,6 +125,16 @@ def test_verify_of_nothing_and_scratch(pkg):
         assert call(pkg, "spd_op_verify_drafts", VERIFY, scratch=None) == EINVAL
         assert call(pkg, "spd_op_verify_drafts", VERIFY, scratch=9 * A + 64) == EINVAL
         assert call(pkg, "spd_op_verify_drafts", VERIFY, scratch=A) == EINVAL
+
+
+def test_grids_past_32_bits_are_refused(pkg):
+    """Calls whose threads pass 32 bits; nothing is launched."""
+    assert call(pkg, "spd_op_verify_drafts", VERIFY, logits=1 << 50, draft_logits=1 << 51, tokens=1 << 52, first=1 << 53, u=1 << 54, out_tokens=1 << 55, out_logprobs=1 << 56, out_accepted=1 << 57, scratch=1 << 58,
+                n_tokens=1 << 20, vocab=1 << 18, row_stride=1 << 18, draft_stride=1 << 18, scratch_bytes=1 << 50) == EINVAL
+    wide = dict(zip(("K", "V", "K_scale", "V_scale", "table", "q", "first", "len", "out"), (1 << n for n in range(48, 57))), scratch=1 << 58)
+    assert call(pkg, "spd_op_attention_paged", ATTEND, **wide, n_pages=1, n_kv_heads=1 << 10, n_heads=1 << 10, n_seq=1 << 16, n_tokens=1 << 14, q_stride=1 << 16) == EINVAL
+    wide = dict(zip(("K", "V", "K_scale", "V_scale", "table", "q", "k", "v", "seq", "pos", "q_out"), (1 << n for n in range(48, 59))))
+    assert call(pkg, "spd_op_append_paged_q8", WRITE, **wide, n_heads=1 << 14, q_stride=1 << 20, n_tokens=1 << 20) == EINVAL
 
 
 # ------------------------------------------------------------------ the references that the GPU tests go by

@@ -315,6 +315,32 @@ def test_attention_bounds_size_the_launch_alone(dtype, io, max_new, max_len):
     check(dtype, case, max_new=max_new, max_len=max_len)
 
 
+@pytest.mark.parametrize("dtype,io,heads,kv,d,page", [("fp16", "fp32", 2, 1, 64, 16), ("int8", "bf16", 8, 2, 128, 16), ("bf16", "bf16", 3, 3, 32, 8), ("fp32", "fp32", 4, 2, 64, 64)])
+@pytest.mark.parametrize("n_seq,long", [(64, 0), (65, 0), (130, 300), (200, 1700)])
+def test_attention_of_many_sequences(dtype, io, heads, kv, d, page, n_seq, long):
+    """One past what a wave looks at in one go, and many; no new tokens, one, a few and more than a tile of rows; long ones next to short ones."""
+    say("attention", dtype, io, heads, kv, d, page, n_seq, long)
+    g = gen(n_seq)
+    news = [int(x) for x in torch.randint(0, 4, (n_seq,), generator=g)]
+    pasts = [int(x) for x in torch.randint(0, 60, (n_seq,), generator=g)]
+    news[0], news[-1], news[n_seq // 2], pasts[3] = 0, 2, 90, long
+    check(dtype, attention_case(dtype, io, heads, kv, d, page, news, pasts, seed=n_seq, pad=3))
+
+
+@pytest.mark.parametrize("dtype,io", [("fp16", "fp16"), ("int8", "fp32")])
+def test_attention_of_many_sequences_with_firsts_and_lengths_out_of_range(dtype, io):
+    case = attention_case(dtype, io, 2, 2, 64, 16, [2] * 80, [30] * 80, seed=9, pad=1)
+    want, _ = attend(dtype, case)
+    for where, what, value, rows, left in [("first", 70, 100, slice(0, 161), 7.0), ("length", 75, 1, slice(150, 152), 0.0), ("length", 3, 33, slice(6, 8), 0.0), ("first", 80, 162, slice(158, 161), 0.0),
+                                           ("first", 0, -1, slice(0, 2), 0.0)]:
+        changed = case[where].clone()
+        changed[what] = value
+        got, err = attend(dtype, {**case, where: changed}, max_new=2, max_len=32)
+        keep = torch.ones(161, dtype=torch.bool)
+        keep[rows] = False
+        assert err == 1 and torch.equal(got[keep], want[keep]) and (got[rows] == left).all(), (where, what)
+
+
 def test_attention_of_nothing():
     out = torch.full((3, 4, 64), 7.0, device="cuda")
     pools = (torch.zeros(1, 2, 16, 64, dtype=torch.float16, device="cuda"),) * 2
