@@ -6,6 +6,8 @@ import pytest
 import torch
 
 import chunk_reference as R
+from test_batch_ops_host import APPEND, REORDER
+from test_batch_ops_host import ATTEND as SHARED
 
 EINVAL, EWORKSPACE = -1, -4
 A = 1 << 20          # an aligned address
@@ -135,6 +137,63 @@ def test_grids_past_32_bits_are_refused(pkg):
     assert call(pkg, "spd_op_attention_paged", ATTEND, **wide, n_pages=1, n_kv_heads=1 << 10, n_heads=1 << 10, n_seq=1 << 16, n_tokens=1 << 14, q_stride=1 << 16) == EINVAL
     wide = dict(zip(("K", "V", "K_scale", "V_scale", "table", "q", "k", "v", "seq", "pos", "q_out"), (1 << n for n in range(48, 59))))
     assert call(pkg, "spd_op_append_paged_q8", WRITE, **wide, n_heads=1 << 14, q_stride=1 << 20, n_tokens=1 << 20) == EINVAL
+
+
+@pytest.mark.parametrize("name", ["spd_op_append_paged", "spd_op_attention_shared", "spd_op_beam_reorder"])
+def test_operators_without_scales_take_no_8_bit_cache(pkg, name):
+    base = {"spd_op_append_paged": APPEND, "spd_op_attention_shared": SHARED, "spd_op_beam_reorder": REORDER}[name]
+    assert call(pkg, name, base, dtype=3) == EINVAL
+
+
+def test_python_refuses_tensors_that_are_not_what_they_should_be(pkg, monkeypatch):
+    """Shapes, types, strides and devices, before the library is asked; a good call gets there (stand-ins say which device is the current one, and that the library was asked)."""
+    from paper_2405_18400_amd import binding
+
+    class Enqueued(Exception):
+        pass
+
+    class Library:
+        spd_op_attention_paged_scratch_bytes = spd_op_verify_drafts_scratch_bytes = staticmethod(lambda *a: 0)
+
+        def __getattr__(self, name):
+            def enqueue(*args):
+                raise Enqueued(name)
+            return enqueue
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)          # (that of a CPU tensor)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda device=None: None)
+    monkeypatch.setattr(binding, "lib", Library)
+    i, f = lambda *s: torch.zeros(*s, dtype=torch.int32), torch.zeros  # noqa: E731
+    codes, scale, half, rows = f(4, 2, 8, 16, dtype=torch.int8), f(4, 2, 8), f(4, 2, 8, 16, dtype=torch.float16), f(3, 2, 16)
+    write = dict(K=codes, V=codes, K_scale=scale, V_scale=scale, table=i(2, 2), k=rows, v=rows, seq=i(3), pos=i(3), rope_theta=1e4)
+    read = dict(dtype="int8", K=codes, V=codes, table=i(2, 2), seq=i(3), pos=i(3), k_out=rows, v_out=rows, K_scale=scale, V_scale=scale)
+    attend = dict(dtype="int8", q=f(5, 4, 16), K=codes, V=codes, table=i(2, 2), first=i(3), length=i(2), out=f(5, 4, 16), max_new=3, max_len=9, K_scale=scale, V_scale=scale)
+    verify = dict(dtype="fp16", logits=f(5, 50).half(), tokens=i(5), first=i(3), u=f(5), out_tokens=i(5), out_logprobs=f(5), out_accepted=i(2), draft_logits=f(5, 50).half())
+    pools = [dict(K=codes[:2]), dict(V=codes.transpose(1, 2)), dict(K=half), dict(table=f(2, 2)), dict(table=i(2, 4)[:, ::2]), dict(K_scale=None), dict(V_scale=None), dict(K_scale=scale[:3]),
+             dict(V_scale=scale.double()), dict(K_scale=f(4, 8, 2).transpose(1, 2)), dict(err=i(2)), dict(err=f(1))]
+    for name, good, others, bad in [
+            ("spd_op_append_paged_q8", write, [dict(q=f(3, 4, 16), q_out=f(3, 4, 16)), dict(k=f(3, 6, 16)[:, :2], v=f(3, 6, 16)[:, 2:4])],
+             [dict(k=rows[:2]), dict(v=rows.half()), dict(q=f(3, 4, 16)), dict(q_out=f(3, 4, 16)), dict(k=f(3, 4, 16)[:, ::2], v=f(3, 4, 16)[:, ::2]), dict(seq=i(2)), dict(pos=i(3).long()),
+              dict(k=f(3, 6, 16)[:, :2]), dict(q=f(3, 4, 8), q_out=f(3, 4, 8)), dict(q=f(3, 4, 16), q_out=f(3, 4, 16).half())]),
+            ("spd_op_read_paged", read, [dict(k_out=rows.half(), v_out=rows.half()), dict(dtype="fp16", K=half, V=half, K_scale=None, V_scale=None)],
+             [dict(dtype="fp16"), dict(dtype="fp16", K=half, V=half), dict(dtype="fp8"), dict(k_out=rows.half()), dict(k_out=rows.double(), v_out=rows.double()), dict(k_out=rows[:2]), dict(seq=i(4)),
+              dict(v_out=f(3, 16, 2).transpose(1, 2))]),
+            ("spd_op_attention_paged", attend, [dict(q=f(5, 4, 16).half(), out=f(5, 4, 16).half()), dict(q=f(5, 9, 16)[:, :4]), dict(dtype="fp16", K=half, V=half, K_scale=None, V_scale=None)],
+             [dict(q=f(5, 4, 16).half()), dict(out=f(4, 4, 16)), dict(q=f(5, 4, 8)), dict(q=f(5, 16, 4).transpose(1, 2)), dict(q=f(5, 8, 16)[:, ::2]), dict(q=f(5, 4, 16).double(), out=f(5, 4, 16).double()),
+              dict(first=i(2)), dict(length=i(3)), dict(first=i(3).long()), dict(max_new=1 << 31), dict(max_len=1 << 32), dict(dtype="fp8"), dict(dtype="fp16")]),
+            ("spd_op_verify_drafts", verify, [dict(draft_logits=None), dict(logits=f(5, 60).half()[:, :50])],
+             [dict(logits=f(5, 50)), dict(draft_logits=f(5, 49).half()), dict(logits=f(50, 5).half().t()), dict(tokens=i(4)), dict(first=i(0)), dict(first=i(4)), dict(u=f(5).double()), dict(out_tokens=f(5)),
+              dict(out_logprobs=f(6)), dict(out_accepted=i(3)), dict(dtype="int8"), dict(err=i(2))])]:
+        for more in [{}, dict(err=i(1))] + others:
+            with pytest.raises(Enqueued, match=name):
+                getattr(pkg, name)(**{**good, **more})
+        for wrong in bad + (pools if "K" in good else []):
+            with pytest.raises(ValueError):
+                getattr(pkg, name)(**{**good, **wrong})
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)           # tensors of another device
+    for name, good in (("spd_op_append_paged_q8", write), ("spd_op_read_paged", read), ("spd_op_attention_paged", attend), ("spd_op_verify_drafts", verify)):
+        with pytest.raises(ValueError):
+            getattr(pkg, name)(**good)
 
 
 # ------------------------------------------------------------------ the references that the GPU tests go by
