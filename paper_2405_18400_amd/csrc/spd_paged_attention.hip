@@ -600,6 +600,22 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                         for (int i = 0; i < 16; ++i) o[f][i] *= f0;
                 }
             }
+            // pieces of values are asked for VD ahead of their products
+            constexpr int VD = NF < 4 ? NF : 4, VALUES = NU * 2 * NF;
+            int at4 = lane % 16;
+            if constexpr (LEAN) asm volatile("" : "+v"(at4));
+            const int t4 = at4 / 4, fg = (lane / 16) % 2;
+            const auto value_piece = [&](int i) {            // 16 keys, i / NF, by 32 features, i % NF
+                const int f = i % NF, key = key_base + 16 * (i / NF) + 4 * h + t4;
+                const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(t4, 4 * f + 2 * fg + (lane % 4) / 2) + 8 * (lane % 2) + share * (ROWB / 2);     // (a place hangs on key % 4 alone)
+                const u32x2 x = turned_read(at), y = turned_read(at + 8 * ROWB);
+                return u32x4{x.x, x.y, y.x, y.y};
+            };
+            u32x4 v[VD];
+            if constexpr (!F32) {
+#pragma unroll
+                for (int i = 0; i < VD; ++i) v[i] = value_piece(i);
+            }
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 if constexpr (F32) {
@@ -621,9 +637,6 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                         }
                     }
                 } else {
-                    int at4 = lane % 16;
-                    if constexpr (LEAN) asm volatile("" : "+v"(at4));
-                    const int t4 = at4 / 4, fg = (lane / 16) % 2;
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {            // 16 keys at a time
                         u32x4 pt[PARTS];
@@ -649,16 +662,24 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                                 for (int q = 0; q < PARTS; ++q) pt[q][(i % 8) / 2 + e / 2] = part[q];
                             }
                         }
-                        const int key = key_base + TR * u + 16 * g + 4 * h + t4;
 #pragma unroll
                         for (int f = 0; f < NF; ++f) {
-                            const char *at = v_tile + key * ROWB + 16 * v_place<PIECES, F32>(t4, 4 * f + 2 * fg + (lane % 4) / 2) + 8 * (lane % 2) + share * (ROWB / 2);     // (a place hangs on key % 4 alone)
-                            const u32x2 x = turned_read(at), y = turned_read(at + 8 * ROWB);
-                            const u32x4 v{x.x, x.y, y.x, y.y};
+                            const int i = (2 * u + g) * NF + f;
 #pragma unroll
-                            for (int q = PARTS - 1; q >= 0; --q) o[f] = mfma32<LT>(v, pt[q], o[f]);
+                            for (int q = PARTS - 1; q >= 0; --q) o[f] = mfma32<LT>(v[i % VD], pt[q], o[f]);
+                            if (i + VD < VALUES) v[i % VD] = value_piece(i + VD);
                         }
                     }
+                }
+            }
+            if constexpr (!F32 && DH >= 64) {                // (as above; Q8: and two reads of scales for every 16 keys)
+                constexpr int SCALES = Q8 ? 2 : 0;
+                __builtin_amdgcn_sched_group_barrier(0x100, 2 * VD + SCALES, 0);
+#pragma unroll
+                for (int i = 0; i < VALUES; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, PARTS, 0);
+                    if (i % NF == 0 && i + NF < VALUES) __builtin_amdgcn_sched_group_barrier(0x100, 2 + SCALES, 0);
+                    else if (i + VD < VALUES) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 }
             }
         }
