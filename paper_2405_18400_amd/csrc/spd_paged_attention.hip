@@ -83,6 +83,19 @@ __device__ __forceinline__ void stage16(const char *from, uint32_t off, const ch
 #endif
 }
 
+// The same for N pieces in a row (at most four), 1024 bytes apart in memory as in LDS: the offset of the instruction counts for both.
+template <int N> __device__ __forceinline__ void stage16_each(const char *from, const uint32_t (&off)[N], const char *to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t m = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)to;
+    if constexpr (N == 1) stage16(from, off[0], to);
+    else if constexpr (N == 2)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(m), "v"(off[0]), "v"(off[1]), "s"(from) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+                     "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(m), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory");
+#endif
+}
+
 // All loads have arrived, in registers (the compiler knows) and in LDS.
 __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
@@ -265,17 +278,23 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         for (int i = tid; i < S::LDS / 16; i += NT) ((u32x4 *)lds)[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
-    const auto of_share = [&](int i) { return FS == 1 || (tid + i * NT) % PIECES / (PIECES / 2) == share; };      // (places are permuted within halves of a row)
-    // A wave's piece i of a stage is KEYS keys side by side, which lie on one page (but where a page is shorter than that): page numbers, asked for a stage ahead of the keys on them, and
-    // addresses are the wave's, a lane's part of them stays the same.
-    constexpr int KEYS = WAVE / PIECES;
-    const bool whole = KEYS <= 4 || KEYS <= 1 << shift;
+    const auto of_share = [&]() { return FS == 1 || lane % PIECES / (PIECES / 2) == share; };      // (places are permuted within halves of a row)
+    // A wave's part of a stage is LOADS pieces of KEYS keys each, side by side.  Where they lie on one page, page number (asked for a stage ahead) and address are formed once, by the wave; a lane's part of
+    // the address stays the same, but for the permutation.  Shorter pages: piece by piece, or, where a piece lies on several, page by page.
+    // Measured, 2999 tokens of prompts over pages of 16: @ONE@
+    constexpr int KEYS = WAVE / PIECES, OWN = KEYS * LOADS;
+    const bool one = DH > 32 && OWN <= 1 << shift, whole = KEYS <= 4 || KEYS <= 1 << shift;
+    const auto place = [&](int i) { return ((wv * LOADS + i) * WAVE + lane) * 16; };          // of this thread's piece i in LDS
     int page[LOADS], scale_page = 0;
+    const auto entry = [&](int pos) { return ((const __attribute__((address_space(4))) int32_t *)entries)[pos >> shift]; };      // (of the wave: a scalar load)
     const auto ask = [&](int t) {
+        if (one) page[0] = entry(min(lo + t * SK + wv * OWN, (hi - 1) & ~(OWN - 1)));
+        else if (whole) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int key = (wv * WAVE + i * NT) / PIECES;
-            page[i] = as_global(entries)[whole ? min(lo + t * SK + key, (hi - 1) & ~(KEYS - 1)) >> shift : min(lo + t * SK + key + lane / PIECES, hi - 1) >> shift];
+            for (int i = 0; i < LOADS; ++i) page[i] = entry(min(lo + t * SK + wv * OWN + i * KEYS, (hi - 1) & ~(KEYS - 1)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) page[i] = as_global(entries)[min(lo + t * SK + wv * OWN + i * KEYS + lane / PIECES, hi - 1) >> shift];
         }
         if constexpr (Q8)
             if (wv < 2) scale_page = as_global(entries)[min(lo + t * SK + lane % SK, hi - 1) >> shift];
@@ -284,23 +303,58 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     float scale_in = 0.f;
     int drop = 0, drop_next = 0, v_top = -200;               // (drop: bit i: this thread's piece i of the stage is of a key that does not count)
     const auto fetch = [&](int t) {
-        char *to = lds + (t % 2) * BYTES + wv * (WAVE * 16);
+        char *to = lds + (t % 2) * BYTES + wv * (LOADS * WAVE * 16);
         const bool end = lo + (t + 1) * SK > hi;
         int lane = tid & (WAVE - 1);
         if constexpr (LEAN) asm volatile("" : "+v"(lane));
         drop_next = 0;
         bool bad = false;
+        if (one) {
+            constexpr int UNIT = Q8 ? 8 : 16;
+            const int pg = __builtin_amdgcn_readfirstlane(page[0]), pos0 = min(lo + t * SK + wv * OWN, (hi - 1) & ~(OWN - 1)), key = wv * OWN + lane / PIECES, slot = lane % PIECES;
+            bad = (unsigned)pg >= (unsigned)p.c.n_pages;
+            const u64 row = ((u64)(uint32_t)((bad ? 0 : pg) * p.c.n_kv_heads + kvh) << head_shift) + ((u64)(uint32_t)(pos0 & in_page) << row_shift);
+            const char *k_row = K + row, *v_row = V + row;
+            // a key's bits go into its row's places by exclusive or: piece i's by a constant
+            const uint32_t in_row = (uint32_t)(lane / PIECES) * (PIECES * UNIT), k_off = in_row + UNIT * k_place<PIECES>(key, slot), v_off = in_row + UNIT * v_place<PIECES, F32>(key, slot);
+            if constexpr (Q8) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + i * (WAVE * UNIT) + (k_off ^ UNIT * k_place<PIECES>(KEYS * i, 0)));
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + i * (WAVE * UNIT) + (v_off ^ UNIT * v_place<PIECES, F32>(KEYS * i, 0)));
+            } else {
+                constexpr int EACH = LOADS < 4 ? LOADS : 4;
+#pragma unroll
+                for (int i = 0; i < LOADS; i += EACH) {
+                    uint32_t off[EACH];
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) off[e] = k_off ^ UNIT * k_place<PIECES>(KEYS * (i + e), 0);
+                    stage16_each<EACH>(k_row + i * (WAVE * 16), off, to + i * (WAVE * 16));
+                }
+                if (of_share())
+#pragma unroll
+                    for (int i = 0; i < LOADS; i += EACH) {
+                        uint32_t off[EACH];
+#pragma unroll
+                        for (int e = 0; e < EACH; ++e) off[e] = v_off ^ UNIT * v_place<PIECES, F32>(KEYS * (i + e), 0);
+                        stage16_each<EACH>(v_row + i * (WAVE * 16), off, to + HALF + i * (WAVE * 16));
+                    }
+            }
+            if (end || bad)
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) drop_next |= (int)(bad || lo + t * SK + key + KEYS * i >= hi) << i;
+        } else
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int key0 = (wv * WAVE + i * NT) / PIECES, key = key0 + lane / PIECES, slot = lane % PIECES, at = lo + t * SK + key;
+            const int key0 = wv * OWN + i * KEYS, key = key0 + lane / PIECES, slot = lane % PIECES, at = lo + t * SK + key;
             const int kp = k_place<PIECES>(key, slot), vp = v_place<PIECES, F32>(key, slot);
             const auto issue = [&](const char *k_row, const char *v_row, uint32_t off) {
                 if constexpr (Q8) {
                     if (DH > 32 || 8 * kp < d) kc[i] = *(const u32x2 __attribute__((address_space(1))) *)(k_row + (off + 8 * kp));
                     if (DH > 32 || 8 * vp < d) vc[i] = *(const u32x2 __attribute__((address_space(1))) *)(v_row + (off + 8 * vp));
                 } else {
-                    if (DH > 32 || PIECE_EL * kp < d) stage16(k_row, off + 16 * kp, to + i * (NT * 16));
-                    if ((DH > 32 || PIECE_EL * vp < d) && of_share(i)) stage16(v_row, off + 16 * vp, to + HALF + i * (NT * 16));
+                    if (DH > 32 || PIECE_EL * kp < d) stage16(k_row, off + 16 * kp, to + i * (WAVE * 16));
+                    if ((DH > 32 || PIECE_EL * vp < d) && of_share()) stage16(v_row, off + 16 * vp, to + HALF + i * (WAVE * 16));
                 }
             };
             bool ok;
@@ -341,15 +395,15 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         char *to = lds + (t % 2) * BYTES;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int slot = (tid + i * NT) % PIECES, key = (tid + i * NT) / PIECES;
+            const int slot = lane % PIECES, key = wv * OWN + i * KEYS + lane / PIECES;
             u32x4 x;
             uint32_t a, b;
             codes_to_half(kc[i].x, a, b); x.x = a; x.y = b;
             codes_to_half(kc[i].y, a, b); x.z = a; x.w = b;
-            if (DH > 32 || 8 * k_place<PIECES>(key, slot) < d) *(u32x4 *)(to + (tid + i * NT) * 16) = x;
+            if (DH > 32 || 8 * k_place<PIECES>(key, slot) < d) *(u32x4 *)(to + place(i)) = x;
             codes_to_half(vc[i].x, a, b); x.x = a; x.y = b;
             codes_to_half(vc[i].y, a, b); x.z = a; x.w = b;
-            if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + (tid + i * NT) * 16) = x;
+            if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + place(i)) = x;
         }
         if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in;
         if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
@@ -442,12 +496,12 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             if (drop) {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i)
-                    if ((drop >> i) & 1) *(u32x4 *)(v_tile + (tid + i * NT) * 16) = u32x4{0, 0, 0, 0};
+                    if ((drop >> i) & 1) *(u32x4 *)(v_tile + place(i)) = u32x4{0, 0, 0, 0};
             }
             if (stage0 + SK - 1 > pos_min) {
                 bool odd = false;
 #pragma unroll
-                for (int i = 0; i < LOADS; ++i) odd = odd || (of_share(i) && not_finite<sizeof(LT)>(*(const u32x4 *)(v_tile + (tid + i * NT) * 16), Type<LT>::PARTS == 3));
+                for (int i = 0; i < LOADS; ++i) odd = odd || (of_share() && not_finite<sizeof(LT)>(*(const u32x4 *)(v_tile + place(i)), Type<LT>::PARTS == 3));
                 if (odd) odd_stage[t % 2] = t + 1;
             }
         }
@@ -482,7 +536,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                u32x4 *at = (u32x4 *)(v_tile + (tid + i * NT) * 16);
+                u32x4 *at = (u32x4 *)(v_tile + place(i));
                 u32x4 x = *at;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
