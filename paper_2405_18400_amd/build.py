@@ -42,9 +42,10 @@ def build_library(verbose: bool = False, out: str = LIB) -> str:
         if res.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + log)
         if usage in cmd:
-            scratch = [int(l.split("ScratchSize [bytes/lane]:")[1].split()[0]) for l in log.splitlines() if "ScratchSize [bytes/lane]:" in l]
-            if not scratch or any(scratch):
-                raise RuntimeError(f"spilled registers ({scratch} bytes per lane, kernel by kernel):\n" + " ".join(cmd))
+            for what in ("ScratchSize [bytes/lane]:", "VGPRs Spill:"):
+                spilled = [int(l.split(what)[1].split()[0]) for l in log.splitlines() if what in l]
+                if not spilled or any(spilled):
+                    raise RuntimeError(f"spilled registers ({what} {spilled}, kernel by kernel):\n" + " ".join(cmd))
             return
         logs.append(log)
 

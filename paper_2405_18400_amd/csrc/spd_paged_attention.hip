@@ -281,7 +281,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const auto of_share = [&]() { return FS == 1 || lane % PIECES / (PIECES / 2) == share; };      // (places are permuted within halves of a row)
     // A wave's part of a stage is LOADS pieces of KEYS keys each, side by side.  Where they lie on one page, page number (asked for a stage ahead) and address are formed once, by the wave; a lane's part of
     // the address stays the same, but for the permutation.  Shorter pages: piece by piece, or, where a piece lies on several, page by page.
-    // Measured, 2999 tokens of prompts over pages of 16: @ONE@
+    // Measured, 2999 tokens of prompts over pages of 16: a piece's address each and page numbers as vector loads 51.1 us, so 48.8.
     constexpr int KEYS = WAVE / PIECES, OWN = KEYS * LOADS;
     const bool one = DH > 32 && OWN <= 1 << shift, whole = KEYS <= 4 || KEYS <= 1 << shift;
     const auto place = [&](int i) { return ((wv * LOADS + i) * WAVE + lane) * 16; };          // of this thread's piece i in LDS
@@ -296,8 +296,6 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) page[i] = as_global(entries)[min(lo + t * SK + wv * OWN + i * KEYS + lane / PIECES, hi - 1) >> shift];
         }
-        if constexpr (Q8)
-            if (wv < 2) scale_page = as_global(entries)[min(lo + t * SK + lane % SK, hi - 1) >> shift];
     };
     u32x2 kc[LOADS], vc[LOADS];                              // Q8: a stage's codes and scales on their way
     float scale_in = 0.f;
@@ -309,6 +307,15 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         if constexpr (LEAN) asm volatile("" : "+v"(lane));
         drop_next = 0;
         bool bad = false;
+        if constexpr (Q8) {                                  // scales, and page numbers for the next stage's: in front of the codes (behind them they wait for room on the way to memory, 700 cycles)
+            if (wv < 2) {
+                const int at = lo + t * SK + lane % SK;
+                const bool ok = (unsigned)scale_page < (unsigned)p.c.n_pages;
+                scale_in = 0.f;
+                if (ok && at < hi) scale_in = as_global(wv == 0 ? p.k_scale : p.v_scale)[((size_t)(uint32_t)(scale_page * p.c.n_kv_heads + kvh) << shift) + (at & in_page)];
+                if (t + 1 < stages) scale_page = as_global(entries)[min(lo + (t + 1) * SK + lane % SK, hi - 1) >> shift];
+            }
+        }
         if (one) {
             constexpr int UNIT = Q8 ? 8 : 16;
             const int pg = __builtin_amdgcn_readfirstlane(page[0]), pos0 = min(lo + t * SK + wv * OWN, (hi - 1) & ~(OWN - 1)), key = wv * OWN + lane / PIECES, slot = lane % PIECES;
@@ -378,14 +385,6 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             bad = bad || !ok;
             if (end || !ok) drop_next |= (int)(!ok || at >= hi) << i;
         }
-        if constexpr (Q8) {
-            if (wv < 2) {
-                const int at = lo + t * SK + lane % SK;
-                const bool ok = (unsigned)scale_page < (unsigned)p.c.n_pages;
-                scale_in = 0.f;
-                if (ok && at < hi) scale_in = as_global(wv == 0 ? p.k_scale : p.v_scale)[((size_t)(uint32_t)(scale_page * p.c.n_kv_heads + kvh) << shift) + (at & in_page)];
-            }
-        }
         if (bad) {
             bad_stage[t % 2] = t + 1;
             if (p.err) *as_global(p.err) = 1;
@@ -408,11 +407,8 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in;
         if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
             const float size = fabsf(scale_in);
-            int ex = -200;
-            if (size > 0.f && size < INFINITY) (void)frexpf(size, &ex);
-#pragma unroll
-            for (int o = 1; o < WAVE; o <<= 1) ex = max(ex, __shfl_xor(ex, o, WAVE));
-            v_top = max(v_top, ex);
+            const float ex = size > 0.f && size < INFINITY ? (float)__builtin_amdgcn_frexp_expf(size) : -200.f;
+            v_top = max(v_top, (int)__int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(ex)), WAVE - 1)));
             const bool odd = !(size < INFINITY);             // counts as zero; rows that see it get no number
             if (lane < SK) v_sc[t % 2][lane] = odd ? 0.f : ldexpf(scale_in, -v_top);
             const u64 keys = __ballot(odd && lane < SK);
@@ -422,6 +418,8 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     };
 
     ask(0);
+    if constexpr (Q8)
+        if (wv < 2) scale_page = as_global(entries)[min(lo + lane % SK, hi - 1) >> shift];
     // this lane's query: its row's features 16 j + 8 h .. + 7 (fp32: 8 j + 4 h .. + 3)
     u32x4 Q[NJ][PARTS];
     float scale = 1.4426950408889634f / sqrtf((float)d);     // to logarithms of base 2
@@ -655,7 +653,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                 }
             }
             // pieces of values are asked for VD ahead of their products
-            constexpr int VD = NF < 4 ? NF : 4, VALUES = NU * 2 * NF;
+            constexpr int VD = NF < 4 ? NF : Q8 && PARTS == 2 && RW == 4 ? 2 : 4, VALUES = NU * 2 * NF;
             int at4 = lane % 16;
             if constexpr (LEAN) asm volatile("" : "+v"(at4));
             const int t4 = at4 / 4, fg = (lane / 16) % 2;
