@@ -168,8 +168,8 @@ __device__ __forceinline__ int code_of(double x, double scale, double inv) {
 }
 
 // append_paged_kernel into codes and scales.  A row's d_head / 4 threads lie in one wave, next to each other, and find its largest value by exchanging theirs.
-// Bound by memory, though half of the arithmetic is in 64 bits (vector unit 72% busy).  Measured: three tokens of 32 + 2 x 32 heads of 128 3.9 us (latency); 4099 tokens of 64 + 2 x 8
-// heads, 168 MB read and 145 written, 62 us, 5.0 TB/s, a large copy's rate.
+// Bound by memory, though half of the arithmetic is in 64 bits (vector unit 72% busy).  Measured: three tokens of 32 + 2 x 32 heads of 128 4.0 us (latency); 4099 tokens of 64 + 2 x 8
+// heads, 168 MB read and 145 written, 63 us, 5.0 TB/s, a large copy's rate.
 template <int U>
 __global__ __launch_bounds__(NTP) void append_q8_kernel(const AppendQ8Args p) {
     const AppendArgs &a = p.a;
@@ -253,7 +253,7 @@ template <> __device__ __forceinline__ void load_eight<q8_t>(const void *p, size
 
 // A thread: U pieces of eight elements of a row, a block's width apart; a token's keys in front, then its values.  Places, page numbers and rows are three trips to memory, each of them
 // asked for all pieces at once.  Measured: 60001 tokens of 2 x 8 heads of 128 from 8 to 16 bits, 404 MB in all, 88 us, 4.6 TB/s (a large copy: 5.0; one piece after the other, 1.4 times as long);
-// twenty tokens of 2 x 32 heads 2.9 us (latency).
+// twenty tokens of 2 x 32 heads 3.0 us (latency).
 template <typename KT, typename OT, int U>
 __global__ __launch_bounds__(NTP) void read_paged_kernel(const ReadArgs a) {
     const int d = a.c.d_head, row_pieces = a.c.n_kv_heads * d / 8, page_size = 1 << a.c.page_shift, pieces = a.n_tokens * 2 * row_pieces, i0 = blockIdx.x * (NTP * U) + threadIdx.x;

@@ -11,8 +11,8 @@
 // number, so that the operand reads meet in no bank.  One barrier per stage.
 // Bound: the matrix cores where there are many rows (and with all 24 bits of them two or three products for each), else the vector unit, which forms some 500 instructions per wave and stage
 // (masks, exponentials, parts of them, codes to numbers) in between: a wave's products and its exponentials follow one another, and two blocks per compute unit are what registers allow.
-// Measured (kernel alone; then what the bytes or products alone would take): 512 tokens of 64 heads on 8 behind 32257 positions in fp16, 24 bits, 0.95 ms = 1.15 PFLOP/s in two products each, the rate of a large
-// fp16 product; 2999 tokens of 32 heads in bf16 from their beginnings 55 us (23); 40 tokens of eight sequences over 4001 positions of 8 bits 32 us (9); four tokens behind 73 positions 9 us.
+// Measured (kernel alone; then what the bytes or products alone would take): 512 tokens of 64 heads on 8 behind 32257 positions in fp16, 24 bits, 0.94 ms = 1.16 PFLOP/s in two products each, the rate of a large
+// fp16 product; 2999 tokens of 32 heads in bf16 from their beginnings 51 us (23); 40 tokens of eight sequences over 4001 positions of 8 bits 31 us (9); four tokens behind 73 positions 9 us.
 // The four waves of a block of 128 rows share out rows; of 64, rows and the stage's halves.  Where there are few tiles the positions are cut into chunks, and a second
 // kernel puts a row's chunks together in order.
 #include "spd_attention.h"
@@ -157,7 +157,7 @@ template <int BYTES> __device__ __forceinline__ bool not_finite(u32x4 v, bool bf
 }
 
 // The tile of rows that is the block's: of the launch's x-th, the tiles farthest behind their sequence's beginning first (they see the most keys; a call whose last blocks are its
-// longest ones waits for them: prompts of 2999 tokens in the order of their rows 54 us, so 50).  Up to 64 sequences are looked at by one wave at once, one trip to memory: sequences with more than T tiles each have one at
+// longest ones waits for them: prompts of 2999 tokens in the order of their rows 54 us, so 50 at the time).  Up to 64 sequences are looked at by one wave at once, one trip to memory: sequences with more than T tiles each have one at
 // every height below T, so x is found by going down from the tallest.  More sequences: tiles in the order of rows, sequence s's from over(first[s]) + s on (over: whole tiles in front), which
 // needs no sum over sequences; late ones first.  False: none, or first descends somewhere (then there is no telling whose rows are whose).
 struct Whose { int seq, a, b, len, tile; };
@@ -846,7 +846,7 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(const PagedAttnArgs p) 
 }
 
 // How a call is cut.  Tiles of 128 rows use a key twice as often as those of 64, whose waves halve the keys of a stage instead: that pays where the rows of a sequence fill no more than one.  Chunks
-// of positions where there are fewer tiles than places for blocks, as many as fill these (two per compute unit where the second gains more than it costs), none of under 256 positions.  Measured, us (rows of a tile, chunks; the rule's own first):
+// of positions where there are fewer tiles than places for blocks, as many as fill these (two per compute unit where the second gains more than it costs), none of under 256 positions.  Measured before the last steps, which left the order as it is, us (rows of a tile, chunks; the rule's own first):
 //   2999 tokens of prompts, bf16:                 128: 51.4 | 64: 67.3
 //   708 tokens behind 2003 positions, 8 bits:     128, 2: 76.6 | 1: 96.0 | 3: 85.4 | 64, 1: 77.0
 //   40 tokens behind 4001 positions, 8 bits:      64, 8: 35.7 | 4: 46.0 | 6: 42.6 | 11: 42.0 | 16: 43.6 | 128, 8: 42.0

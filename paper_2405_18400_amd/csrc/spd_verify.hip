@@ -8,8 +8,8 @@
 //   * a block per sequence finds the slice where the draw falls, and the token in it.
 // Whether a draft stands is one comparison, which an error of 1e-8 hardly ever turns.  The draw falls between as many borders as there are tokens: of a hundred thousand, one in a
 // thousand draws meets one that sums of fp32 exponentials have moved.  So that row is in 64 bits; all rows in 64 bits took 61 us where fp32 takes what reading takes.
-// Measured, the four in turn: 32 sequences with 190 tokens, 131072 logits in bf16, 100 MB in all: 22.6 us (4.1 TB/s), 21.7 and 14.8 (vector unit 50% busy, exponentials in 64 bits), 12.1 (a block's chain of
-// trips and sums); one sequence of five tokens, 32000 logits in fp32: 3.3, 9.0, 5.1 and 8.9, chains all of them.
+// Measured, the four in turn: 32 sequences with 190 tokens, 131072 logits in bf16, 100 MB in all: 22.4 us (4.1 TB/s), 21.5 and 14.5 (vector unit 50% busy, exponentials in 64 bits), 12.0 (a block's chain of
+// trips and sums); one sequence of five tokens, 32000 logits in fp32: 3.3, 8.8, 5.1 and 8.9, chains all of them.
 #include "spd_attention.h"
 
 #include <algorithm>
