@@ -92,7 +92,7 @@ template <int N> __device__ __forceinline__ void stage16_each(const char *from, 
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(m), "v"(off[0]), "v"(off[1]), "s"(from) : "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(m), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory");
+                     "global_load_lds_dwordx4 %4, %5 offset:0xc00" ::"s"(m), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory");
 #endif
 }
 
