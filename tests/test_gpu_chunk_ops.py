@@ -307,6 +307,15 @@ def test_attention_of_long_parts_and_many_rows(dtype, io, heads, kv, d, page, ne
 
 
 @pytest.mark.parametrize("dtype,io", KINDS)
+@pytest.mark.parametrize("page", [4, 8, 16])
+@pytest.mark.parametrize("heads,kv,d,news,pasts", [(4, 2, 64, [3, 40], [70, 21]), (2, 2, 128, [5, 150], [601, 9]), (4, 1, 128, [2], [130]), (2, 1, 256, [90, 1], [33, 75]), (2, 2, 256, [2, 3], [61, 700])])
+def test_attention_over_pages_shorter_than_a_waves_part_of_a_stage(dtype, io, page, heads, kv, d, news, pasts):
+    """A wave brings 8 or 16 keys of a stage: on one page, on several, or several pages to one of its loads; tiles of 64 and 128 rows."""
+    say("attention", dtype, io, page, heads, kv, d, news, pasts)
+    check(dtype, attention_case(dtype, io, heads, kv, d, page, news, pasts, seed=d + page + 1, pad=1))
+
+
+@pytest.mark.parametrize("dtype,io", KINDS)
 @pytest.mark.parametrize("max_new,max_len", [(0, 1024), (1, 200), (1000, 173)])
 def test_attention_bounds_size_the_launch_alone(dtype, io, max_new, max_len):
     """Too small or too large a max_new, more room in max_len than there is: the same up to the order of sums."""
