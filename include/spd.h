@@ -444,7 +444,8 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * is 1 at the draft.  u (DEVICE float [n_tokens], in [0, 1), the caller's draws): draft x behind token t stands if all before it do and u[t] q(x) < p(x); so a text has the target's distribution whatever
  * the drafter's is.  Behind the drafts that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0) at the
  * first that does not (from p where that is zero everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  u q(x) and p(x) are compared with
- * sums of fp32 exponentials, off by about 1e-8 of themselves; the row that a token is drawn from is summed in 64 bits.  tau and draft_tau lie between 2^-100 and 2^100, n_seq is at most 65536.
+ * sums of fp32 exponentials, off by about 1e-8 of themselves; the row that a token is drawn from is summed in 64 bits.  tau and draft_tau, in 64 bits (the draw falls
+ * between as many borders as there are tokens, and a temperature rounded to 32 bits moves one in two thousand draws over 131072 logits to another token), lie between 2^-100 and 2^100; n_seq is at most 65536.
  * A logit that is no number counts as -inf, +inf as the largest finite number.  A draft outside [0, vocab) does not stand; *err is set.
  * Outputs, DEVICE: out_accepted int32 [n_seq], the number a of drafts that stand; at first[s] .. first[s] + a of out_tokens int32 [n_tokens] those drafts and the token
  * behind them, and of out_logprobs float [n_tokens] their log p; -1 and 0 at the sequence's other tokens.  A row without a finite logit gives token 0 with log p = -inf, *err is set.  A
@@ -452,7 +453,7 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * are no sequence's are left as they were. */
 size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_tokens, int32_t vocab);
 int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t row_stride, const void *draft_logits, int64_t draft_stride, const int32_t *tokens, const int32_t *first,
-                         const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, float tau, float draft_tau, int32_t *out_tokens, float *out_logprobs,
+                         const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, double tau, double draft_tau, int32_t *out_tokens, float *out_logprobs,
                          int32_t *out_accepted, void *scratch, size_t scratch_bytes, int32_t *err, void *hip_stream);
 
 /* ---- test hooks for the error path of the persistent kernel's bounded waits ----

@@ -114,7 +114,7 @@ def lib():
             "spd_op_append_paged_q8": [vp] * 5 + [i32] * 6 + [vp, i64, vp, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp],
             "spd_op_read_paged": [i32] + [vp] * 5 + [i32] * 6 + [vp, vp, i32, i32, vp, vp, vp, vp],
             "spd_op_attention_paged": [i32, i32, vp, i64] + [vp] * 5 + [i32] * 6 + [vp, vp, i32, i32, i32, i32, vp, vp, sz, vp, vp],
-            "spd_op_verify_drafts": [i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, f32, f32, vp, vp, vp, vp, sz, vp, vp],
+            "spd_op_verify_drafts": [i32, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, C.c_double, C.c_double, vp, vp, vp, vp, sz, vp, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)

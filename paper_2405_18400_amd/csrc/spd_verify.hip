@@ -372,7 +372,7 @@ __global__ __launch_bounds__(NTV) void verify_pick_kernel(const VerifyArgs a) {
 }
 
 constexpr int SEQS_MAX = 1 << 16;                // (every block looks through the sequences)
-constexpr float TAU_MIN = 0x1p-100f;             // (and 1 / tau: what fp32 exponents hold)
+constexpr double TAU_MIN = 0x1p-100;             // (and 1 / tau: what fp32 exponents hold)
 
 // Logits per thread of a slice: 32, or 8 where that leaves too few blocks to fill the GPU.
 int each_for(int n_tokens, int vocab) { return (long long)n_tokens * 2 * ((vocab + 32 * NTV - 1) / (32 * NTV)) < 512 ? 8 : 32; }
@@ -400,11 +400,11 @@ extern "C" size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_to
 }
 
 extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t row_stride, const void *draft_logits, int64_t draft_stride, const int32_t *tokens, const int32_t *first,
-                                    const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, float tau, float draft_tau, int32_t *out_tokens, float *out_logprobs,
+                                    const float *u, int32_t n_seq, int32_t n_tokens, int32_t vocab, double tau, double draft_tau, int32_t *out_tokens, float *out_logprobs,
                                     int32_t *out_accepted, void *scratch, size_t scratch_bytes, int32_t *err, void *hip_stream) {
     if (dtype != SPD_DTYPE_FP32 && dtype != SPD_DTYPE_BF16 && dtype != SPD_DTYPE_FP16) return SPD_EINVAL;
     const int el = dtype == SPD_DTYPE_FP32 ? 4 : 2;
-    if (n_seq < 0 || n_tokens < 0 || vocab < 1 || vocab > (1 << 24) || !(tau >= TAU_MIN) || !(tau <= 1.f / TAU_MIN) || (draft_logits && (!(draft_tau >= TAU_MIN) || !(draft_tau <= 1.f / TAU_MIN)))) return SPD_EINVAL;
+    if (n_seq < 0 || n_tokens < 0 || vocab < 1 || vocab > (1 << 24) || !(tau >= TAU_MIN) || !(tau <= 1.0 / TAU_MIN) || (draft_logits && (!(draft_tau >= TAU_MIN) || !(draft_tau <= 1.0 / TAU_MIN)))) return SPD_EINVAL;
     if (n_seq == 0) return SPD_OK;
     if (!first || !out_accepted || (n_tokens > 0 && (!logits || !tokens || !u || !out_tokens || !out_logprobs)) || n_seq > SEQS_MAX || n_tokens > (1 << 20)) return SPD_EINVAL;
     if (row_stride < vocab || (draft_logits && draft_stride < vocab) || ((uintptr_t)logits | (uintptr_t)draft_logits) % el) return SPD_EINVAL;
