@@ -24,19 +24,22 @@ constexpr int NTV = 256, NWV = NTV / WAVE;
 // A logit as it counts: no number is -inf, +inf the largest finite number.
 __device__ __forceinline__ float logit(float x) { return fminf(fmaxf(x, -INFINITY), 3.402823466e38f); }
 
-// exp((z - top) / tau), c = log2(e) / tau, z <= top, in 64 bits: to the nearest power of two by adding 1.5 2^52, which leaves the whole number in the low bits, and a rest of at most 1/2, whose
-// exponential is ten terms of its series; the next one is 2e-13.  (As conversions and ldexp these steps take the time of twice as many products.)  What is below 2^-900 counts as that.
-__device__ __forceinline__ double exp_64(float z, float top, double c) {
+// 2^(d c), d c < 1000, in 64 bits: to the nearest power of two by adding 1.5 2^52, which leaves the whole number in the low bits, and a rest of at most 1/2, whose
+// exponential is ten terms of its series; the next one is 2e-13.  (As conversions and ldexp these steps take the time of twice as many products.)  What is below 2^-1021 is 0.
+__device__ __forceinline__ double exp2_64(double d, double c) {
     constexpr double MAGIC = 6755399441055744.0, L = 0.69314718055994530942;
     constexpr double C[11] = {1.0, L, L * L / 2, L * L * L / 6, L * L * L * L / 24, L * L * L * L * L / 120, L * L * L * L * L * L / 720, L * L * L * L * L * L * L / 5040,
                               L * L * L * L * L * L * L * L / 40320, L * L * L * L * L * L * L * L * L / 362880, L * L * L * L * L * L * L * L * L * L / 3628800};
-    const double d = fmax((double)z - (double)top, -900.0 / c), t = fma(d, c, MAGIC), f = fma(d, c, -(t - MAGIC));
+    const double t = fma(d, c, MAGIC), f = fma(d, c, -(t - MAGIC));
     double y = C[10];
 #pragma unroll
     for (int n = 9; n >= 0; --n) y = fma(y, f, C[n]);
     const u64 bits = __builtin_bit_cast(u64, y) + ((u64)(uint32_t)__builtin_bit_cast(u64, t) << 52);       // (the exponent's place: modulo 2^12)
-    return z > -INFINITY ? __builtin_bit_cast(double, bits) : 0.0;
+    return d * c >= -1021.0 ? __builtin_bit_cast(double, bits) : 0.0;             // (0 for -inf too)
 }
+
+// exp((z - top) / tau), c = log2(e) / tau, z <= top.
+__device__ __forceinline__ double exp_64(float z, float top, double c) { return exp2_64((double)z - (double)top, c); }
 
 // Sums over the block, the same in all threads.
 __device__ __forceinline__ double wave_add(double v) {
@@ -182,17 +185,20 @@ __global__ __launch_bounds__(NTV) void verify_drafts_kernel(const VerifyArgs a) 
         whole_row(a, u, a.by_tau, lane, top, sum);
         if (drawn) whole_row(a, a.n_tokens + u, a.by_draft_tau, lane, draft_top, draft_sum);
         if (lane != 0 || t >= hi - 1) continue;
-        double p = 0.0, q = 1.0;
-        float z = -INFINITY;
-        if (known && top > -INFINITY) {
-            z = logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, t), x));
-            p = exp_64(z, top, a.by_tau) / sum;
+        // u < p / q, by the difference of their logarithms: p and q may lie below anything that 64 bits hold.  (Its two products without their roundings: they may be large and near to each other.)
+        const float z = known ? logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, t), x)) : -INFINITY;
+        const float y = known && drawn ? logit(Store<T>::load1(row_of<T>(a.draft_logits, a.draft_stride, t), x)) : -INFINITY;
+        const double dp = (double)z - (double)top;
+        bool stands = z > -INFINITY;             // (then the row's largest is finite too)
+        if (stands && !drawn) stands = (double)as_global(a.u)[t] < exp2_64(fma(dp, a.by_tau, -log2(sum)), 1.0);
+        else if (stands && y > -INFINITY) {      // (q = 0: it stands)
+            const double dq = (double)y - (double)draft_top, lq = dq * a.by_draft_tau, ratio = fma(dp, a.by_tau, -lq) - fma(dq, a.by_draft_tau, -lq) + log2(draft_sum / sum);
+            stands = (double)as_global(a.u)[t] < exp2_64(fmin(ratio, 900.0), 1.0);
         }
-        if (drawn) q = known && draft_top > -INFINITY ? exp_64(logit(Store<T>::load1(row_of<T>(a.draft_logits, a.draft_stride, t), x)), draft_top, a.by_draft_tau) / draft_sum : 0.0;
-        if (!((double)as_global(a.u)[t] * q < p)) atomicMin(&stop, t);
+        if (!stands) atomicMin(&stop, t);
         else if (slice == 0) {
             as_global(a.out_tokens)[t] = x;
-            as_global(a.out_logprobs)[t] = (float)((((double)z - (double)top) * a.by_tau - log2(sum)) * 0.69314718055994530942);
+            as_global(a.out_logprobs)[t] = (float)((dp * a.by_tau - log2(sum)) * 0.69314718055994530942);
         }
     }
     __syncthreads();

@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-import chunk_reference as R
+import verify_reference as V
 from test_gpu_chunk_ops import P, dev, gen, ints, run_verify, say, verify_case, zero  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +52,80 @@ def test_a_draft_is_decided_by_tau_in_64_bits(drawn):
         case = dict(logits=p_row, tokens=ints([0, 0]), first=ints([0, 2]), u=torch.tensor([u, 0.5]), draft_logits=z)
         _, _, out_a, _ = run_verify("fp32", case, tau=1.0, draft_tau=tau)
     assert int(out_a[0]) == int(want)
+
+
+# ------------------------------------------------------------------ decisions and draws against the definition
+def check64(dtype, case, tau=1.0, draft_tau=1.0, sure=2.0 ** -18, got=None):
+    """All outputs are the definition's.  A draft's quotient, of sums of fp32 exponentials, and the random number are further apart than `sure`, relative to the quotient; the draw, in 64 bits whose exponentials are off by 2e-13, is
+    2^-40 of the sum from the nearest border, or u is 0 (which is exact).  A logarithm of a probability is off by 2^-22 and half a step of itself."""
+    out_t, out_l, out_a, err = got or run_verify(dtype, case, tau, draft_tau)
+    first, bad, seen = case["first"].tolist(), False, torch.zeros(len(out_t), dtype=torch.bool)
+    for s, (a, b) in enumerate(zip(first, first[1:])):
+        if a == b:
+            assert out_a[s] == 0
+            continue
+        seen[a:b] = True
+        m, given, logp, wrong, near, far = V.verify(case["logits"][a:b], case["tokens"][a:b], case["u"][a:b], tau, None if case["draft_logits"] is None else case["draft_logits"][a:b], draft_tau)
+        assert near > sure and (far > 2.0 ** -40 or float(case["u"][b - 1]) == 0.0), (s, near, far)
+        bad |= wrong
+        assert int(out_a[s]) == m and out_t[a:a + m + 1].tolist() == given, (s, out_a[s], m, out_t[a:b].tolist(), given)
+        assert (out_t[a + m + 1:b] == -1).all() and (out_l[a + m + 1:b] == 0).all()
+        for i, w in enumerate(logp):
+            assert float(out_l[a + i]) == w or abs(float(out_l[a + i]) - w) <= 2.0 ** -22 + abs(w) * 2.0 ** -24, (s, i, out_l[a + i], w)
+    assert (out_t[~seen] == -5).all() and (out_l[~seen] == 9.0).all() and err == int(bad)
+    return out_t, out_l, out_a
+
+
+def one_draft(target, drafter, u, draft=1, last=0.5):
+    """One sequence per random number: its newest token and one draft, every row `target` and `drafter`."""
+    n = len(u)
+    rows = lambda x: None if x is None else torch.as_tensor(x).expand(2 * n, -1).contiguous()  # noqa: E731
+    return dict(logits=rows(target), draft_logits=rows(drafter), tokens=ints([0, draft] * n), first=ints(range(0, 2 * n + 1, 2)), u=torch.tensor([[x, last] for x in u]).flatten())
+
+
+@pytest.mark.parametrize("tau,z,y,u,stands", [
+    (1.0, -640.0, -630.0, [0.525, 1e-3, 4e-5, 3.5e-5], [0, 0, 0, 1]),        # p / q = e^-10 (1 + e^-2) / (1 + e^-1) = 3.8e-5
+    (1.0, -1072.0, -676.0, [0.525, 1e-30, 0.0], [0, 0, 1]),         # 1e-172
+    (0.05, -40.0, -32.0, [0.525, 1e-30, 0.0], [0, 0, 1]),           # 3e-70
+    (0.01, -12.0, -7.0, [0.525, 1e-30, 0.0], [0, 0, 1]),            # 7e-218
+    (0.01, -12.0, -3.0, [0.525, 0.0], [0, 0]),                      # 1e-391: a quotient that counts as 0
+    (0.01, -7.0, -12.0, [0.525, 1.0 - 2.0 ** -24], [1, 1]),         # more than one
+    (0.01, -12.0, -11.99, [0.3, 0.42], [1, 0]),                     # e^-1 or so (0.37: the logits are rounded)
+    (1.0, -1e9, -1e9, [0.525, 1.0 - 2.0 ** -24], [1, 0]),           # masked alike in both: p / q = (1 + e^-2) / (1 + e^-1) = 0.83
+    (1.0, -1e9, -5.0, [0.525, 0.0], [0, 0]),                        # masked in the target alone
+    (1.0, -5.0, -1e9, [0.525, 0.0], [1, 1]),                        # in the drafter alone
+    (1.0, -math.inf, -math.inf, [0.525, 0.0], [0, 0]),
+    (1.0, -5.0, -math.inf, [0.525, 0.0], [1, 1])])
+def test_drafts_whose_probabilities_64_bits_do_not_hold(tau, z, y, u, stands):
+    say("tiny", tau, z, y)
+    case = one_draft([0.0, z, -1.0], [0.0, y, -2.0], u)
+    _, _, out_a = check64("fp32", case, tau, tau)
+    assert out_a.tolist() == stands
+
+
+@pytest.mark.parametrize("dtype,mask", [("fp32", -1e9), ("fp32", -3.4028234663852886e38), ("bf16", -1e9), ("bf16", -3.3895313892515355e38), ("fp16", -65504.0), ("fp16", -30000.0)])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("u", [0.0, 0.3, 1.0 - 2.0 ** -24])
+def test_finite_masks(dtype, mask, drawn, u):
+    """Every second token is masked with a finite number, in both models, the first among them: none of these stands (but where the drafter drew it) or is drawn, whatever u."""
+    case = verify_case(dtype, [5, 1, 4, 3], 50, seed=31, drawn=drawn)
+    for name in ("logits", "draft_logits"):
+        if case[name] is not None:
+            case[name][:, ::2] = mask
+    case["u"][:] = u
+    odd = torch.randint(0, 25, case["tokens"].shape, generator=gen(32)).int() * 2 + 1
+    case["tokens"] = torch.where(case["tokens"] % 2 == 1, case["tokens"], odd)
+    case["tokens"][8] = 12                       # a masked draft
+    if drawn:
+        case["draft_logits"][7, 12] = 1.0        # that the drafter did not mask
+    out_t, _, _ = check64(dtype, case)
+    given = out_t[out_t >= 0]
+    assert (given % 2 == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("tau,draft_tau", [(0.01, 0.01), (0.003, 0.02), (2.0 ** -100, 2.0 ** -100), (2.0 ** 100, 2.0 ** 100), (1.0, 2.0 ** -100), (40.0, 0.01)])
+def test_temperatures_far_from_one(dtype, drawn, tau, draft_tau):
+    case = verify_case(dtype, [4, 1, 0, 9, 2, 3, 3, 3], 1037, seed=33, drawn=drawn, noise=0.05)
+    check64(dtype, case, tau, draft_tau)
