@@ -442,11 +442,11 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * (DEVICE, `dtype` fp32, fp16 or bf16, rows of row_stride elements) is what the target model expects behind token t, p = softmax(logits / tau); row t of draft_logits (draft_stride) what
  * the drafter drew token t + 1 from, q = softmax(draft_logits / draft_tau), not looked at for a sequence's last token.  draft_logits NULL: drafts that were chosen, not drawn, q
  * is 1 at the draft.  u (DEVICE float [n_tokens], in [0, 1), the caller's draws): draft x behind token t stands if all before it do and u[t] < p(x) / q(x), however small the two are (a
- * quotient below 2^-1021 counts as 0; with p(x) = 0 it does not stand, with q(x) = 0 < p(x) it does); so a text has the target's distribution whatever the drafter's is.  Behind the drafts
+ * quotient below 2^-990 may count as 0; with p(x) = 0 it does not stand, with q(x) = 0 < p(x) it does); so a text has the target's distribution whatever the drafter's is.  Behind the drafts
  * that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0) at the first that does not (from p where that is zero
  * everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  Tokens below 2^-1021 of the likeliest one's probability have none there, so one that is
- * masked with a large negative number is not drawn, with a u of 0 neither.  u and p(x) / q(x) are compared with sums of fp32 exponentials, off by about 1e-8 of themselves; the row that a
- * token is drawn from is summed in 64 bits.  tau and draft_tau, in 64 bits (the draw falls between as many borders as there are tokens, and a temperature rounded to 32 bits moves one in two
+ * masked with a large negative number is not drawn, with a u of 0 neither.  What is drawn, and whether a draft stands, goes by sums of 64
+ * bits (of 32 where those could not turn it); the log p of a draft by sums of 32, off by less than 2^-15 of itself.  tau and draft_tau, in 64 bits (the draw falls between as many borders as there are tokens, and a temperature rounded to 32 bits moves one in two
  * thousand draws over 131072 logits to another token), lie between 2^-100 and 2^100; n_seq is at most 65536.
  * A logit that is no number counts as -inf, +inf as the largest finite number.  A draft outside [0, vocab) does not stand; *err is set.
  * Outputs, DEVICE: out_accepted int32 [n_seq], the number a of drafts that stand; at first[s] .. first[s] + a of out_tokens int32 [n_tokens] those drafts and the token

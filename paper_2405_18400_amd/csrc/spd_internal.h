@@ -337,7 +337,8 @@ struct VerifyArgs {
     float *out_logprobs;
     int32_t *out_accepted, *err;
     int32_t slices;
-    float *top, *sum;                    // scratch: [rows of logits, then of draft_logits; slices] largest logit, sum of exp((logit - that) / tau) in fp32
+    float *top, *sum;                    // scratch: [rows of logits, then of draft_logits; slices] largest logit, sum of exp((logit - that) / tau) of all others in fp32
+    double unsure;                       // how far, relative to itself, p / q of two such sums may be off
     double *exact, *rest;                // scratch: [2, n_seq, pieces] the same sums of a sequence's last row, in 64 bits; [n_seq, pieces] what a draft that does not stand leaves of it
     int32_t pieces;                      // of a row: several to a slice
     struct VerifyPick *pick;             // scratch, [n_seq]

@@ -6,8 +6,8 @@
 //   * a block per slice and sequence puts its sequence's rows together, finds the first draft that does not stand, and sums its slice of that row again, in 64 bits;
 //   * the same blocks sum what that row leaves, max(p - q, 0);
 //   * a block per sequence finds the slice where the draw falls, and the token in it.
-// Whether a draft stands is one comparison, which an error of 1e-8 hardly ever turns.  The draw falls between as many borders as there are tokens: of a hundred thousand, one in a
-// thousand draws meets one that sums of fp32 exponentials have moved.  So that row is in 64 bits; all rows in 64 bits took 61 us where fp32 takes what reading takes.
+// Whether a draft stands is one comparison, which sums of fp32 exponentials hardly ever turn: those that they might (their error is bounded) are made again with sums of 64 bits.  The draw falls between as many
+// borders as there are tokens: of a hundred thousand, one in a thousand draws meets one that such sums have moved.  So that row is in 64 bits always; all rows in 64 bits took 61 us where fp32 takes what reading takes.
 // Measured, the four in turn: 32 sequences with 190 tokens, 131072 logits in bf16, 100 MB in all: 22.4 us (4.1 TB/s), 21.5 and 14.5 (vector unit 50% busy, exponentials in 64 bits), 12.0 (a block's chain of
 // trips and sums); one sequence of five tokens, 32000 logits in fp32: 3.3, 8.8, 5.1 and 8.9, chains all of them.
 #include "spd_attention.h"
@@ -91,7 +91,7 @@ template <typename T, int E>
 __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T), PIECES = E / VEC;
     __shared__ float tops[NWV], red[NWV];
-    const int tid = threadIdx.x, lane = tid & (WAVE - 1), r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
+    const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = tid / WAVE, r = blockIdx.x / a.slices, slice = blockIdx.x - r * a.slices;
     const bool draft = r >= a.n_tokens;
     const int t = draft ? r - a.n_tokens : r;
     // rows that nothing asks about: no sequence's, and the drafter's at a sequence's last token
@@ -112,16 +112,27 @@ __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = fmaxf(top, z[i][e]);
     top = wave_max(top);
-    if (lane == 0) tops[tid / WAVE] = top;
+    if (lane == 0) tops[wv] = top;
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const float from = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
+    float sum = 0.f, all = 0.f;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((z[i][e] - from) * c);
-    sum = wave_sum(sum);
+        for (int e = 0; e < VEC; ++e) {
+            const float x = __builtin_amdgcn_exp2f((z[i][e] - from) * c);
+            all += x;
+            sum += __builtin_amdgcn_fractf(x);
+        }
+    // One of the largest stays out: next to its 1 a likely token's log p, the logarithm of 1 and what the others add up to, would be lost.  So a thread adds up what is less than 1, and counts the ones.
+    float ones = rintf(all - sum);
+    if (const u64 with = __ballot(ones > 0.f)) {
+        bool first = lane == __builtin_ctzll(with) && tops[wv] == top;
+        for (int w = 0; w < wv; ++w) first = first && tops[w] != top;
+        ones -= first ? 1.f : 0.f;
+    }
+    sum = wave_sum(sum + ones);
     if (lane == 0) red[tid / WAVE] = sum;
     __syncthreads();
     if (tid == 0) {
@@ -130,21 +141,25 @@ __global__ __launch_bounds__(NTV) void verify_sums_kernel(const VerifyArgs a) {
     }
 }
 
-// A row's largest logit, and its sum of exponentials to 1e-8, by 16 lanes.
+// A row's largest logit, and its sum of exponentials, by 16 lanes.  How far it may be off, in steps of 2^-24 of itself: an exponent x is off by three steps of itself, and the mean of -x, every term counting as
+// much as it weighs, is at most log2 of their number, so all terms together by 3 ln 2 log2(vocab), and again as much where slices are put together; the exponential by two; the sums of a slice (E terms and nine
+// joins) by one each; and two for every time that a lane's slices so far are brought down.
 constexpr int ROWL = 16;
+double sum_off(int each, int vocab, int slices) { return 0x1p-24 * (4.2 * log2((double)vocab) + (each + 9) + 2.0 * ((slices + ROWL - 1) / ROWL + 3)); }
 __device__ __forceinline__ void whole_row(const VerifyArgs &a, int r, double c, int lane, float &top, double &sum) {
     const size_t at = (size_t)r * a.slices;
-    float m = -INFINITY, s = 0.f;                // the lane's slices so far
+    float m = -INFINITY;                         // the lane's slices so far
+    double s = 0.0;
     for (int i = lane; i < a.slices; i += ROWL) {
         const float x = as_global(a.top)[at + i], y = as_global(a.sum)[at + i], up = fmaxf(m, x);
         if (up == -INFINITY) continue;
-        s = s * __builtin_amdgcn_exp2f((m - up) * (float)c) + y * __builtin_amdgcn_exp2f((x - up) * (float)c);
+        s = s * (double)__builtin_amdgcn_exp2f((m - up) * (float)c) + (1.0 + (double)y) * (double)__builtin_amdgcn_exp2f((x - up) * (float)c);
         m = up;
     }
     top = m;
 #pragma unroll
     for (int o = 1; o < ROWL; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
-    s = m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f((m - top) * (float)c);
+    s = m == -INFINITY ? 0.0 : s * (double)__builtin_amdgcn_exp2f((m - top) * (float)c);
 #pragma unroll
     for (int o = 1; o < ROWL; o <<= 1) s += __shfl_xor(s, o, WAVE);
     sum = s;
@@ -157,14 +172,42 @@ __device__ __forceinline__ bool ascends(const VerifyArgs &a) {
     return !__syncthreads_or(descends);
 }
 
+// p(x) / q(x) for the draft x behind token t, of the rows' largest logits and sums, by the difference of the two logarithms: they may lie below anything that 64 bits hold.  (Its two products without their
+// roundings: they may be large and near to each other.)  0 where p(x) is, some 2^900 where q(x) is 0 or far below p(x).  below_top: how far x's logit lies below the largest, where there is one.
+template <typename T>
+__device__ __forceinline__ double quotient(const VerifyArgs &a, int t, int x, float top, double sum, float draft_top, double draft_sum, double &below_top) {
+    if ((unsigned)x >= (unsigned)a.vocab) return 0.0;
+    const float z = logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, t), x));
+    float y = -INFINITY;
+    if (a.draft_logits) y = logit(Store<T>::load1(row_of<T>(a.draft_logits, a.draft_stride, t), x));
+    if (z == -INFINITY) return 0.0;
+    below_top = (double)z - (double)top;
+    if (!a.draft_logits) return exp2_64(below_top, a.by_tau) / sum;
+    if (y == -INFINITY) return 0x1p900;
+    const double dq = (double)y - (double)draft_top, lq = dq * a.by_draft_tau;
+    return exp2_64(fmin(fma(below_top, a.by_tau, -lq) - fma(dq, a.by_draft_tau, -lq), 900.0), 1.0) * (draft_sum / sum);
+}
+
+// A row's sum of exponentials in 64 bits, by the block.
+template <typename T> __device__ double exact_row(const VerifyArgs &a, const void *row, float top, double c, double *red) {
+    constexpr int VEC = 16 / (int)sizeof(T);
+    double sum = 0.0;
+    for (int v0 = threadIdx.x * VEC; v0 < a.vocab; v0 += NTV * VEC) {
+        float z[VEC];
+        load_logits<T, VEC>(row, v0, a.vocab, z);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum += exp_64(z[e], top, c);
+    }
+    return block_add(sum, red);
+}
+
 template <typename T, int E>
 __global__ __launch_bounds__(NTV) void verify_drafts_kernel(const VerifyArgs a) {
     constexpr int VEC = 16 / (int)sizeof(T), PIECES = E / VEC;
-    __shared__ int stop;
+    __shared__ int stop, unsure;
     __shared__ double red[PIECES][NWV];
     __shared__ float last_top[2];
     const int tid = threadIdx.x, s = blockIdx.x / a.slices, slice = blockIdx.x - s * a.slices, lane = tid % ROWL;
-    if (tid == 0) stop = INT32_MAX;
     const bool sorted = ascends(a);
     const int lo = as_global(a.first)[s], hi = as_global(a.first)[s + 1];
     const bool fits = sorted && lo >= 0 && hi <= a.n_tokens, drawn = a.draft_logits != nullptr;
@@ -176,30 +219,46 @@ __global__ __launch_bounds__(NTV) void verify_drafts_kernel(const VerifyArgs a) 
         }
         return;
     }
-    // 16 lanes per row: does its draft stand?  (Those behind the first that does not are looked at in vain.)
-    for (int t0 = lo; t0 < hi - 1; t0 += NTV / ROWL) {
-        const int t = t0 + tid / ROWL, u = min(t, hi - 2), x = as_global(a.tokens)[u + 1];          // (all lanes take part in the exchange)
-        const bool known = (unsigned)x < (unsigned)a.vocab;
+    // 16 lanes per row: does its draft stand?  (Those behind the first that does not are looked at in vain.)  Where u is nearer to p / q than fp32 sums may be off, which is seldom, the block sums that draft's
+    // rows in 64 bits, and goes on behind it if it stands.
+    for (int from = lo;;) {
+        if (tid == 0) stop = unsure = INT32_MAX;
+        __syncthreads();
+        for (int t0 = from; t0 < hi - 1; t0 += NTV / ROWL) {
+            const int t = t0 + tid / ROWL, row = min(t, hi - 2);           // (all lanes take part in the exchange)
+            float top, draft_top = -INFINITY;
+            double sum, draft_sum = 0.0, below_top = 0.0;
+            whole_row(a, row, a.by_tau, lane, top, sum);
+            if (drawn) whole_row(a, a.n_tokens + row, a.by_draft_tau, lane, draft_top, draft_sum);
+            if (lane != 0 || t >= hi - 1) continue;
+            const int x = as_global(a.tokens)[t + 1];
+            const double r = quotient<T>(a, t, x, top, sum, draft_top, draft_sum, below_top), u = (double)as_global(a.u)[t];
+            const bool near = r > 0.0 && fabs(u - r) <= a.unsure * r;
+            if (near) atomicMin(&unsure, t);
+            else if (!(u < r)) atomicMin(&stop, t);
+            if (slice == 0 && (near || u < r)) {
+                as_global(a.out_tokens)[t] = x;
+                as_global(a.out_logprobs)[t] = (float)((below_top * a.by_tau - log2(sum)) * 0.69314718055994530942);
+            }
+        }
+        __syncthreads();
+        const int t = unsure;
+        if (t >= stop) break;
         float top, draft_top = -INFINITY;
-        double sum, draft_sum = 0.0;
-        whole_row(a, u, a.by_tau, lane, top, sum);
-        if (drawn) whole_row(a, a.n_tokens + u, a.by_draft_tau, lane, draft_top, draft_sum);
-        if (lane != 0 || t >= hi - 1) continue;
-        // u < p / q, by the difference of their logarithms: p and q may lie below anything that 64 bits hold.  (Its two products without their roundings: they may be large and near to each other.)
-        const float z = known ? logit(Store<T>::load1(row_of<T>(a.logits, a.row_stride, t), x)) : -INFINITY;
-        const float y = known && drawn ? logit(Store<T>::load1(row_of<T>(a.draft_logits, a.draft_stride, t), x)) : -INFINITY;
-        const double dp = (double)z - (double)top;
-        bool stands = z > -INFINITY;             // (then the row's largest is finite too)
-        if (stands && !drawn) stands = (double)as_global(a.u)[t] < exp2_64(fma(dp, a.by_tau, -log2(sum)), 1.0);
-        else if (stands && y > -INFINITY) {      // (q = 0: it stands)
-            const double dq = (double)y - (double)draft_top, lq = dq * a.by_draft_tau, ratio = fma(dp, a.by_tau, -lq) - fma(dq, a.by_draft_tau, -lq) + log2(draft_sum / sum);
-            stands = (double)as_global(a.u)[t] < exp2_64(fmin(ratio, 900.0), 1.0);
+        double sum, draft_sum = 0.0, below_top;
+        whole_row(a, t, a.by_tau, lane, top, sum);
+        sum = exact_row<T>(a, row_of<T>(a.logits, a.row_stride, t), top, a.by_tau, red[0]);
+        if (drawn) {
+            whole_row(a, a.n_tokens + t, a.by_draft_tau, lane, draft_top, draft_sum);
+            if (draft_top > -INFINITY) draft_sum = exact_row<T>(a, row_of<T>(a.draft_logits, a.draft_stride, t), draft_top, a.by_draft_tau, red[0]);
         }
-        if (!stands) atomicMin(&stop, t);
-        else if (slice == 0) {
-            as_global(a.out_tokens)[t] = x;
-            as_global(a.out_logprobs)[t] = (float)((dp * a.by_tau - log2(sum)) * 0.69314718055994530942);
+        const bool stands = (double)as_global(a.u)[t] < quotient<T>(a, t, as_global(a.tokens)[t + 1], top, sum, draft_top, draft_sum, below_top);
+        __syncthreads();                         // (everyone has read the marks)
+        if (!stands) {
+            if (tid == 0) stop = t;
+            break;
         }
+        from = t + 1;
     }
     __syncthreads();
     const bool refused = stop < hi - 1;
@@ -432,6 +491,7 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
     a.top = (float *)w; w += up256(row_sums * 4);
     a.sum = (float *)w; w += up256(row_sums * 4);
     a.pieces = slices * (each_for(n_tokens, vocab) / (16 / el));
+    a.unsure = 2.1 * sum_off(each_for(n_tokens, vocab), vocab, slices);          // (two rows)
     a.exact = (double *)w; w += up256(2 * (size_t)n_seq * a.pieces * 8);
     a.rest = (double *)w; w += up256((size_t)n_seq * a.pieces * 8);
     a.pick = (VerifyPick *)w;

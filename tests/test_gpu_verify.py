@@ -6,6 +6,7 @@ import math
 import pytest
 import torch
 
+import chunk_reference as R
 import verify_reference as V
 from test_gpu_chunk_ops import P, dev, gen, ints, run_verify, say, verify_case, zero  # noqa: F401
 
@@ -55,8 +56,8 @@ def test_a_draft_is_decided_by_tau_in_64_bits(drawn):
 
 
 # ------------------------------------------------------------------ decisions and draws against the definition
-def check64(dtype, case, tau=1.0, draft_tau=1.0, sure=2.0 ** -18, got=None):
-    """All outputs are the definition's.  A draft's quotient, of sums of fp32 exponentials, and the random number are further apart than `sure`, relative to the quotient; the draw, in 64 bits whose exponentials are off by 2e-13, is
+def check64(dtype, case, tau=1.0, draft_tau=1.0, sure=2.0 ** -40, got=None):
+    """All outputs are the definition's.  Exponentials of 64 bits are off by 2e-13, a quotient of two sums by 6e-13 < 2^-40 = 9e-13: it and the random number are further apart than `sure`, relative to the quotient; the draw is
     2^-40 of the sum from the nearest border, or u is 0 (which is exact).  A logarithm of a probability is off by 2^-22 and half a step of itself."""
     out_t, out_l, out_a, err = got or run_verify(dtype, case, tau, draft_tau)
     first, bad, seen = case["first"].tolist(), False, torch.zeros(len(out_t), dtype=torch.bool)
@@ -129,3 +130,61 @@ def test_finite_masks(dtype, mask, drawn, u):
 def test_temperatures_far_from_one(dtype, drawn, tau, draft_tau):
     case = verify_case(dtype, [4, 1, 0, 9, 2, 3, 3, 3], 1037, seed=33, drawn=drawn, noise=0.05)
     check64(dtype, case, tau, draft_tau)
+
+
+# ------------------------------------------------------------------ next to the border
+def neighbours(r):
+    """The fp32 numbers on either side of r."""
+    x = torch.tensor(r, dtype=torch.float64).float()
+    other = torch.nextafter(x, torch.tensor(0.0 if float(x) > r else 2.0))
+    return sorted([float(x), float(other)])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("rows,vocab,tau,draft_tau", [(24, 4099, 1.0, 1.0), (140, 4099, 0.7, 1.3), (7, 50258, 0.8, 0.8), (70, 20011, 0.6, 0.7)])
+def test_random_numbers_next_to_a_quotient(dtype, drawn, rows, vocab, tau, draft_tau):
+    """Every row twice, with the fp32 numbers in front of and behind p / q, which sums of fp32 exponentials cannot tell apart: the draft stands with the one and not with the other."""
+    say("border", dtype, drawn, rows, vocab)
+    case = verify_case(dtype, [1] * rows, vocab, seed=rows, drawn=drawn)
+    z, y, tokens, u = case["logits"], case["draft_logits"], [], []
+    for r in range(rows):
+        ratio = V.log2_probabilities(z[r], tau) - (0.0 if y is None else V.log2_probabilities(y[r], draft_tau))
+        x = int(((ratio > -14.0) & (ratio < -0.2)).nonzero()[r % 5])
+        for v in neighbours(2.0 ** float(ratio[x])):
+            tokens += [0, x]
+            u += [v, 0.37]
+    four = lambda t: None if t is None else t.repeat_interleave(4, 0)  # noqa: E731
+    case = dict(logits=four(z), draft_logits=four(y), tokens=ints(tokens), first=ints(range(0, 4 * rows + 1, 2)), u=torch.tensor(u))
+    _, _, out_a = check64(dtype, case, tau, draft_tau)
+    assert out_a.tolist() == [1, 0] * rows
+
+
+def test_many_random_numbers_next_to_quotients_in_one_sequence():
+    """Forty drafts that all stand, but the last, each by the smallest step of its random number."""
+    z, y = (torch.randn(41, 3001, generator=gen(s)) * 2.5 for s in (41, 42))
+    tokens, u = [0], []
+    for r in range(40):
+        ratio = V.log2_probabilities(z[r], 1.0) - V.log2_probabilities(y[r], 1.0)
+        x = int(((ratio > -14.0) & (ratio < -0.2)).nonzero()[r])
+        tokens.append(x)
+        u.append(neighbours(2.0 ** float(ratio[x]))[r == 39])
+    case = dict(logits=z, draft_logits=y, tokens=ints(tokens), first=ints([0, 41]), u=torch.tensor(u + [0.6]))
+    _, _, out_a = check64("fp32", case)
+    assert out_a.tolist() == [39]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab,gap,ties", [(5, 8.0, 1), (5, 8.0, 2)] + [(v, g, n) for v, g in ((300, 12.0), (33000, 20.0), (131, 3.0)) for n in (1, 2, 7)])
+def test_log_probabilities_next_to_nothing(dtype, vocab, gap, ties):
+    """A likely token's log p is the logarithm of 1 and what the other tokens weigh.  Sums of those are off by at most 2^-24 (4.2 log2(vocab) + 41 + 8) < 2^-16 of themselves, and so is the logarithm."""
+    z = torch.randn(3, vocab, generator=gen(vocab)) - gap
+    for i in range(ties):
+        z[:, (vocab // 2 + 3 * i) % vocab] = 4.0     # (in the last row one of as many)
+    z[:2, [(vocab // 2 + 3 * i) % vocab for i in range(1, ties)]] = -gap
+    z = z.to(R.TORCH[dtype])
+    case = dict(logits=z, draft_logits=None, tokens=ints([0, vocab // 2, vocab // 2]), first=ints([0, 3]), u=torch.tensor([0.1, 0.1, 0.0]))
+    out_t, out_l, out_a = check64(dtype, case)
+    want = [float(V.log2_probabilities(z[i], 1.0)[int(out_t[i])]) * math.log(2.0) for i in range(3)]
+    assert out_a.tolist() == [2] and -0.2 < want[0] < 0.0
+    assert all(abs(float(g) - w) <= abs(w) * 2.0 ** -16 for g, w in zip(out_l, want))
