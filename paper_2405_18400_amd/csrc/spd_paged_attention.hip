@@ -159,13 +159,19 @@ template <int BYTES> __device__ __forceinline__ bool not_finite(u32x4 v, bool bf
 // The tile of rows that is the block's: of the launch's x-th, the tiles farthest behind their sequence's beginning first (they see the most keys; a call whose last blocks are its
 // longest ones waits for them: prompts of 2999 tokens in the order of their rows 54 us, so 50 at the time).  Up to 64 sequences are looked at by one wave at once, one trip to memory: sequences with more than T tiles each have one at
 // every height below T, so x is found by going down from the tallest.  More sequences: tiles in the order of rows, sequence s's from over(first[s]) + s on (over: whole tiles in front), which
-// needs no sum over sequences; late ones first.  False: none, or first descends somewhere (then there is no telling whose rows are whose).
+// needs no sum over sequences; late ones first.  False: none, or first descends somewhere (then there is no telling whose rows are whose).  The launch's first block looks for sequences whose numbers do not fit
+// (others see their own only, and a sequence outside of all rows is nobody's).
 struct Whose { int seq, a, b, len, tile; };
+__device__ __forceinline__ bool fits(const PagedAttnArgs &p, int a, int b, int len) {
+    return a >= 0 && b <= p.n_tokens && len >= b - a && len <= p.max_len && (long long)len <= (long long)p.c.table_stride << p.c.page_shift;
+}
 __device__ __forceinline__ bool whose(const PagedAttnArgs &p, int x, int log2_rows, int lane, Whose &w, bool &descends) {
+    const bool look = blockIdx.x == 0 && p.err;
     if (p.c.n_seq <= WAVE) {
         const int i = min(lane, p.c.n_seq - 1), a = as_global(p.first)[i], b = as_global(p.first)[i + 1], len = as_global(p.len)[i];
         descends = __any(b < a);
         if (descends) return false;
+        if (look && !fits(p, a, b, len)) *as_global(p.err) = 1;
         const int tokens = max(min(b, p.n_tokens) - max(a, 0), 0);
         const int tiles = lane < p.c.n_seq ? (tokens * p.group + (1 << log2_rows) - 1) >> log2_rows : 0;
         const auto tallest = [&](int below) { return (int)__int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(tiles < below ? (float)tiles : 0.f)), WAVE - 1)); };
@@ -203,6 +209,7 @@ __device__ __forceinline__ bool whose(const PagedAttnArgs &p, int x, int log2_ro
     for (int i0 = 0; i0 < p.c.n_seq; i0 += WAVE) {
         const int i = min(i0 + lane, p.c.n_seq - 1), a = as_global(p.first)[i], b = as_global(p.first)[i + 1];
         bad = bad || b < a;
+        if (look && !fits(p, a, b, as_global(p.len)[i])) *as_global(p.err) = 1;
         s += __popcll(__ballot(i0 + lane < p.c.n_seq && start(i + 1, b) <= tile));
     }
     descends = __any(bad);
@@ -252,8 +259,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     const int r0 = own.tile * ROWS, n = own.b - own.a, from = max(own.a, 0), n_rows = min(((min(own.b, p.n_tokens) - from) * group) - r0, ROWS);
     if (n_rows <= 0) return;
     const int len = own.len;
-    if (own.a < 0 || own.b > p.n_tokens || len < n || len > p.max_len || (long long)len > (long long)p.c.table_stride << shift) {
-        if (tid == 0 && p.err) *as_global(p.err) = 1;
+    if (!fits(p, own.a, own.b, len)) {
         if (split == 0 && share == 0)
             for (int i = tid; i < n_rows * d / 4; i += NT) {
                 const int r = r0 + i / (d / 4), tok = over(r, p.by_group);
@@ -822,7 +828,7 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(const PagedAttnArgs p) 
     for (int r = 0; r < MR; ++r) {
         if (row0 + r >= rows || s[r] >= p.c.n_seq) continue;
         const int a = as_global(p.first)[s[r]], b = as_global(p.first)[s[r] + 1], len = as_global(p.len)[s[r]], n = b - a;
-        if (t[r] < a || a < 0 || b > p.n_tokens || len < n || len > p.max_len || (long long)len > (long long)p.c.table_stride << p.c.page_shift) continue;    // (not theirs, or zeros already)
+        if (t[r] < a || !fits(p, a, b, len)) continue;           // (not theirs, or zeros already)
         const int chunks = over(len - n + t[r] - a, p.by_chunk) + 1;
         const float m = lane < chunks ? ml[r][0] : -INFINITY;
         const float M = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(m)), WAVE - 1));
