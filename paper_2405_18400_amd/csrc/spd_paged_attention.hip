@@ -76,10 +76,10 @@ template <> __device__ __forceinline__ f32x16 mfma32<bf16_t>(u32x4 a, u32x4 b, f
 }
 
 // 16 bytes per lane straight into LDS, `to` + 16 lane on.  Written out, because the compiler, which knows the instruction, lets every turned read wait for all of them; they are
-// waited for once per stage.  (No vector register is written; M0, which these kernels use for nothing else, is set right before its use.)
+// waited for once per stage.  (No vector register is written; M0 is set right before its use, and named as lost.)
 __device__ __forceinline__ void stage16(const char *from, uint32_t off, const char *to) {     // (from + off, off per lane)
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)to), "v"(off), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)to), "v"(off), "s"(from) : "memory", "m0");
 #endif
 }
 
@@ -89,10 +89,10 @@ template <int N> __device__ __forceinline__ void stage16_each(const char *from, 
     const uint32_t m = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)to;
     if constexpr (N == 1) stage16(from, off[0], to);
     else if constexpr (N == 2)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(m), "v"(off[0]), "v"(off[1]), "s"(from) : "memory");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(m), "v"(off[0]), "v"(off[1]), "s"(from) : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\tglobal_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-                     "global_load_lds_dwordx4 %4, %5 offset:0xc00" ::"s"(m), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory");
+                     "global_load_lds_dwordx4 %4, %5 offset:0xc00" ::"s"(m), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(from) : "memory", "m0");
 #endif
 }
 
