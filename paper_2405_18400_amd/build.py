@@ -14,8 +14,9 @@ LIB = os.path.join(HERE, "libspd.so")
 SOURCES = ["spd_kernels.hip", "spd_attention.hip", "spd_fused.hip", "spd_sampler.hip", "spd_prefill.hip", "spd_noalloc.hip", "spd_paged.hip", "spd_shared_attention.hip", "spd_paged_attention.hip", "spd_verify.hip", "spd_beam.hip", "spd_lib.cpp", "ngram_table.cpp"]
 
 
-# Kernels that must not spill registers: with accumulation registers in use this compiler has left out a word of a spilled
-# tuple on its way back (the products then take what the register held before).
+# Kernels that must not spill vector registers, to accumulation registers or to memory: with accumulation registers in use this
+# compiler has left out a word of a spilled tuple on its way back (the products then take what the register held before).  Scalar
+# registers may go to the lanes of a vector register, one word each: half of the attention kernels put 1 to 60 of them there.
 NO_SPILLS = {"spd_paged_attention.hip"}
 
 
@@ -45,7 +46,7 @@ def build_library(verbose: bool = False, out: str = LIB) -> str:
             for what in ("ScratchSize [bytes/lane]:", "VGPRs Spill:"):
                 spilled = [int(l.split(what)[1].split()[0]) for l in log.splitlines() if what in l]
                 if not spilled or any(spilled):
-                    raise RuntimeError(f"spilled registers ({what} {spilled}, kernel by kernel):\n" + " ".join(cmd))
+                    raise RuntimeError(f"spilled vector registers ({what} {spilled}, kernel by kernel):\n" + " ".join(cmd))
             return
         logs.append(log)
 
