@@ -7,7 +7,8 @@
 //     stand for keys 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3: probabilities never leave their registers;
 //   * V^T's operand for those keys is two reads of four keys each that LDS turns round on the way (16-bit types; fp32 values go in one by one).
 // Keys and values come through LDS in stages of 64 positions, two deep, 16 bytes per lane straight from memory; codes of 8 bits come through registers and
-// lie in LDS as fp16 numbers, which they are exactly: a key's scale multiplies its scores, a value's its probability.  Pieces of a row are permuted by the row's
+// lie in LDS as fp16 numbers, which they are exactly: a key's scale multiplies its scores, a value's its probability
+// (held by the power of two of the largest scale so far, or, where scales lie far apart, row by row by the largest product of both).  Pieces of a row are permuted by the row's
 // number, so that the operand reads meet in no bank.  One barrier per stage.
 // Bound: the matrix cores where there are many rows (and with all 24 bits of them two or three products for each), else the vector unit, which forms some 500 instructions per wave and stage
 // (masks, exponentials, parts of them, codes to numbers) in between: a wave's products and its exponentials follow one another, and two blocks per compute unit are what registers allow.
@@ -26,6 +27,9 @@ namespace {
 
 constexpr int NT = 256, NW = NT / WAVE;
 constexpr int TR = 32;                           // rows (and keys, features) of a matrix product
+// 8 bits: scales of values that lie no further than 2^NARROW apart are held by the largest.  The largest product of a row's is 2^12 2^-13 at least then, and what 16 bits lose, 2^-25, is 2^-24 of it.
+// LIFT_MAX: a row may be up to that power of two larger: its sums, of up to 2^21 keys, stay below 2^(15 + 7 + 21 + 80), inside of fp32's range.
+constexpr int NARROW = 12, LIFT_MAX = 80;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -247,6 +251,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     __shared__ int v_exp[2];
     __shared__ u64 odd_keys[2];
     __shared__ float join_m[RW][WAVE], join_l[RW][WAVE];
+    __shared__ int join_e[Q8 && KW > 1 ? RW : 1][WAVE];
     const int tid = threadIdx.x, lane = tid & (WAVE - 1), wv = __builtin_amdgcn_readfirstlane(tid / WAVE), col = lane & (TR - 1), h = lane / TR, rw = wv % RW, kw = wv / RW;
     const int d = p.c.d_head, shift = p.c.page_shift, in_page = (1 << shift) - 1, group = p.group;
     // which rows, which positions
@@ -305,6 +310,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
     };
     u32x2 kc[LOADS], vc[LOADS];                              // Q8: a stage's codes and scales on their way
     float scale_in = 0.f;
+    float v_low = 200.f;                                     // (of the scales that have been this lane's)
     int drop = 0, drop_next = 0, v_top = -200;               // (drop: bit i: this thread's piece i of the stage is of a key that does not count)
     const auto fetch = [&](int t) {
         char *to = lds + (t % 2) * BYTES + wv * (LOADS * WAVE * 16);
@@ -411,15 +417,17 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
             if (DH > 32 || 8 * v_place<PIECES, F32>(key, slot) < d) *(u32x4 *)(to + HALF + place(i)) = x;
         }
         if (wv == 0 && lane < SK) k_sc[t % 2][lane] = scale_in;
-        if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, which O is held by too
+        if (wv == 1) {                                       // the values' scales by the power of two of the largest so far, and whether some have been far smaller
             const float size = fabsf(scale_in);
             const float ex = size > 0.f && size < INFINITY ? (float)__builtin_amdgcn_frexp_expf(size) : -200.f;
             v_top = max(v_top, (int)__int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_max_last(ex)), WAVE - 1)));
+            v_low = ex > -200.f ? fminf(v_low, ex) : v_low;
             const bool odd = !(size < INFINITY);             // counts as zero; rows that see it get no number
             if (lane < SK) v_sc[t % 2][lane] = odd ? 0.f : ldexpf(scale_in, -v_top);
             const u64 keys = __ballot(odd && lane < SK);
             if (keys && lane == 0) { odd_stage[t % 2] = t + 1; odd_keys[t % 2] = keys; }
-            if (lane == 0) v_exp[t % 2] = v_top;
+            const bool apart = __ballot(v_low < (float)(v_top - NARROW));
+            if (lane == 0) v_exp[t % 2] = 2 * v_top + apart;
         }
     };
 
@@ -484,7 +492,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[f][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-    int o_exp = -200;                                        // Q8: O is held by this power of two
+    int o_exp = -200, scales_now = -400;                     // Q8: the power of two that the row's O is held by; what it went by
     __syncthreads();                                         // (the stages' marks)
     fetch(0);
     drop = drop_next;
@@ -646,12 +654,32 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                         for (int i = 0; i < 16; ++i) st[u][i] = fabsf(m) > FAR && m != -INFINITY ? ((st[u][i] * scale - m) + T::P_BITS) * inv : st[u][i];
                 }
             }
-            const float ref = fabsf(m) > FAR ? 0.f : m - T::P_BITS;      // (-inf, nothing seen yet: no score either)
-            if constexpr (Q8) {
-                const int ex = v_exp[t % 2];
-                if (ex != o_exp) {
-                    const float f0 = ldexpf(1.f, o_exp - ex);
-                    o_exp = ex;
+            float ref = fabsf(m) > FAR ? 0.f : m - T::P_BITS;            // (-inf, nothing seen yet: no score either)
+            const int scales = Q8 ? __builtin_amdgcn_readfirstlane(v_exp[t % 2]) : 0;
+            int lift = 0;                                    // Q8: probabilities are 2^lift times what they are elsewhere
+            if (Q8 && (scales != scales_now || (scales & 1))) {
+                const int ex = scales >> 1;
+                scales_now = scales;
+                if (scales & 1) {
+                    // Next to the largest scale, which the row may not see, or hardly weigh, those that count for it may leave nothing of a probability in 16 bits: rows go by the largest product of both in the stage.
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const float4 s = *(const float4 *)&v_sc[t % 2][key_base + TR * u + 2 * i + 4 * h];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaf(st[u][i + e], scale, -ref) + __builtin_amdgcn_logf(fabsf(e == 0 ? s.x : e == 1 ? s.y : e == 2 ? s.z : s.w)));
+                        }
+                    most = fmaxf(most, __shfl_xor(most, TR, WAVE));
+                    lift = most > -INFINITY ? 14 - (int)ceilf(fminf(fmaxf(most, -100.f), 100.f)) : ex - o_exp;     // (nothing: as it was)
+                    lift = min(max(lift, 0), LIFT_MAX);
+                    ref -= (float)lift;
+                    l = ldexpf(l, lift);
+                }
+                if (__any(ex - lift != o_exp)) {
+                    const float f0 = ldexpf(1.f, o_exp - (ex - lift));
+                    o_exp = ex - lift;
 #pragma unroll
                     for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -740,6 +768,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                     else if (i + VD < VALUES) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                 }
             }
+            if (Q8 && (scales & 1)) l = ldexpf(l, -lift);
         }
         if constexpr (Q8)
             if (t + 1 < stages) put(t + 1);
@@ -756,7 +785,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
                 for (int i = 0; i < 16; ++i) O[(f * 16 + i) * WAVE] = o[f][i];
             join_m[rw][lane] = m;
             join_l[rw][lane] = l;
-            if (Q8 && lane == 0) v_sc[0][rw] = (float)o_exp;
+            if (Q8) join_e[rw][lane] = o_exp;
         }
         __syncthreads();
         if (kw == 1) return;
@@ -764,7 +793,7 @@ __global__ __launch_bounds__(NT, (Shape<KT, IO, DH, RW>::PER_CU)) void paged_att
         float f0 = exp2_below(m, M), f1 = exp2_below(m1, M);
         l = l * f0 + join_l[rw][lane] * f1;
         if constexpr (Q8) {                                  // (a wave with no key to see in the last stages has not followed their scales)
-            const int ex1 = (int)v_sc[0][rw], ex = max(o_exp, ex1);
+            const int ex1 = join_e[rw][lane], ex = max(o_exp, ex1);
             f0 = ldexpf(f0, o_exp - ex);
             f1 = ldexpf(f1, ex1 - ex);
             o_exp = ex;

@@ -47,3 +47,63 @@ def test_sequences_without_a_row_whose_numbers_do_not_fit(dtype, io, n_seq, past
             assert err == 1 and torch.equal(got[keep], want[keep]), (at, bad)
             length[at] = 0
             assert run(first=first, length=length)[1] == 0, at
+
+
+# ------------------------------------------------------------------ 8-bit values of very different scales
+def eight_bits(io, heads, kv, d, page, news, pasts, seed):
+    return attention_case("int8", io, heads, kv, d, page, news, pasts, seed=seed)
+
+
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("heads,kv,d,news,pasts", [(2, 1, 64, [3, 40], [90, 20]), (4, 2, 128, [150, 2], [30, 700]), (2, 2, 256, [70], [0]), (8, 1, 32, [30, 9], [100, 0]), (2, 2, 128, [1, 1, 5], [600, 64, 2000])])
+@pytest.mark.parametrize("grows", [0.6, -0.6])
+def test_attention_over_scales_that_grow_or_fall_along_the_text(io, heads, kv, d, news, pasts, grows):
+    """Values a 64th of 2^40 apart from position to position, so that what lies a stage behind a row, which it does not see, is up to 2^39 larger than all that it sees (and, falling, what it sees last 2^39 smaller): every row is
+    as near as its own largest that counts, see check()."""
+    case = eight_bits(io, heads, kv, d, 16, news, pasts, seed=d)
+    table, length = case["table"], case["length"].tolist()
+    for s, n in enumerate(length):
+        for p in range(n):
+            at = (int(table[s, p // 16]), slice(None), p % 16)
+            case["V_scale"][at] *= 2.0 ** round(grows * ((p - n) % 64 if grows > 0 else -((n - p) % 64)))
+    if io == "fp16":
+        case["V_scale"] *= 2.0 ** -22            # (results from the smallest fp16 numbers to past the largest)
+    check_all_rows("int8", case)
+
+
+def io_of(case):
+    return case["q"].dtype
+
+
+def check_all_rows(dtype, case):
+    """check(), whose bounds hang on the row's own sum of p |v|; results below fp16's normal numbers are off by half of their step, 2^-25, besides."""
+    got, err = attend(dtype, case)
+    assert err == 0
+    want, size = R.attention(**case)
+    half, least = (0.0, 0.0) if got.dtype is torch.float32 else (torch.finfo(got.dtype).eps / 2, 2.0 ** -25 if got.dtype is torch.float16 else 0.0)
+    got = got.double()
+    allowed = 2 * half * size + 1e-5 * size.amax(-1, keepdim=True) + least
+    past = got.isinf()                       # past the largest fp16 number: by what may be off, at least
+    assert io_of(case) is torch.float16 or not past.any()
+    assert (want.abs() + allowed)[past].ge(65520.0).all() and torch.equal(got[past].sign(), want[past].sign())
+    assert float(((got - want).abs() / allowed)[~past].max()) < 1
+
+
+@pytest.mark.parametrize("io", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("heads,d,news,past", [(2, 64, 3, 90), (4, 128, 2, 800), (1, 256, 70, 200), (32, 128, 5, 400), (2, 128, 140, 60)])
+@pytest.mark.parametrize("far", [20, 45, 70])
+def test_attention_over_large_scales_that_hardly_count(io, heads, d, news, past, far):
+    """A few keys with values 2^far times as large as the others' and scores so far below them that their weights are e^-90 = 2^-130: the others' values are what comes out."""
+    case = eight_bits(io, heads, 1, d, 16, [news], [past], seed=far)
+    case["q"][..., 0] = 8.0 * d ** 0.5 / 8.0
+    table, n = case["table"], int(case["length"][0])
+    for p in range(0, n, 37):
+        at = (int(table[0, p // 16]), 0, p % 16)
+        case["K"][at] = 0
+        case["K"][at][0] = -127
+        case["K_scale"][at] = 90.0 / 127.0
+        case["V_scale"][at] *= 2.0 ** far
+    for p in range(n):
+        if p % 37:
+            case["K"][int(table[0, p // 16]), 0, p % 16, 0] = 0
+    check_all_rows("int8", case)
