@@ -107,3 +107,42 @@ def test_attention_over_large_scales_that_hardly_count(io, heads, d, news, past,
         if p % 37:
             case["K"][int(table[0, p // 16]), 0, p % 16, 0] = 0
     check_all_rows("int8", case)
+
+
+# ------------------------------------------------------------------ the forms that large calls take
+@pytest.mark.parametrize("dtype,io", [("fp16", "fp32"), ("fp16", "fp16"), ("bf16", "fp32"), ("bf16", "bf16"), ("int8", "fp32"), ("int8", "fp16"), ("int8", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("heads,kv,d,news,past", [(40, 2, 64, [7, 0, 13, 1, 183, 2, 5], 1500), (33, 3, 32, [3, 250, 1], 700), (43, 1, 128, [1, 1, 200, 1], 900)])
+def test_chunks_of_many_rows_are_put_together_two_at_a_time(dtype, io, heads, kv, d, news, past):
+    """More than 8192 rows with several chunks of positions, odd in number: pairs of rows of one wave that lie in two tokens, in two sequences, and the last one alone."""
+    say("joined", dtype, io, heads, kv, d, news, past)
+    n = sum(news) * heads
+    assert n > 8192
+    check(dtype, attention_case(dtype, io, heads, kv, d, 16, news, [past - 37 * s for s in range(len(news))], seed=d, pad=1))
+
+
+@pytest.mark.parametrize("dtype", ["int8", "fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("out", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("kv,d,lengths", [(8, 128, [4100, 1, 4900]), (3, 64, [20011, 5003]), (5, 256, [3500])])
+def test_many_rows_are_read_four_pieces_at_a_time(dtype, out, kv, d, lengths):
+    """More than 2^20 pieces of eight elements, with a last block that is not full, padding and pages out of range between them."""
+    say("read", dtype, out, kv, d, lengths)
+    pages, table, seq, pos = places(16, lengths, 3, seed=d, pad=(0, 1000, 1001, 3333))
+    bad = table.clone()
+    bad[0, 2:2000:97] = torch.tensor([-1, pages, 2 ** 31 - 1], dtype=torch.int32).repeat(8)[:len(bad[0, 2:2000:97])]
+    n = len(seq)
+    assert n * 2 * kv * d // 8 >= 1 << 20
+    K, V, Ks, Vs = pool(dtype, pages, kv, 16, d, seed=d)
+    for which, expected in ((table, 0), (bad, 1)):
+        k_out, v_out = (torch.full((n, kv, d), 5.0, dtype=R.TORCH[out], device="cuda") for _ in range(2))
+        err = zero()
+        P().spd_op_read_paged(dtype, K.cuda(), V.cuda(), which.cuda(), seq.cuda(), pos.cuda(), k_out, v_out, K_scale=dev(Ks), V_scale=dev(Vs), err=err)
+        at = torch.where(seq >= 0, which[seq.clamp(min=0).long(), (pos // 16).clamp(min=0).long()], -1)
+        ok = (at >= 0) & (at < pages)
+        assert int(err) == expected == int(bool((~ok & (seq >= 0)).any()))
+        for got, x, scale in ((k_out, K, Ks), (v_out, V, Vs)):
+            want = torch.full((n, kv, d), 5.0, dtype=R.TORCH[out])
+            y = x.transpose(1, 2)[at[ok].long(), (pos[ok] % 16).long()].float()
+            if scale is not None:
+                y = y * scale.transpose(1, 2)[at[ok].long(), (pos[ok] % 16).long()][..., None]
+            want[ok] = y.to(R.TORCH[out])
+            assert torch.equal(got.cpu(), want)

@@ -188,3 +188,48 @@ def test_log_probabilities_next_to_nothing(dtype, vocab, gap, ties):
     want = [float(V.log2_probabilities(z[i], 1.0)[int(out_t[i])]) * math.log(2.0) for i in range(3)]
     assert out_a.tolist() == [2] and -0.2 < want[0] < 0.0
     assert all(abs(float(g) - w) <= abs(w) * 2.0 ** -16 for g, w in zip(out_l, want))
+
+
+# ------------------------------------------------------------------ slices of 32 logits per thread
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("counts,vocab,tau,draft_tau,pad", [
+    ([1 + (5 * i) % 9 for i in range(40)], 50258, 0.8, 1.0, 3), ([1 + (3 * i) % 7 for i in range(9)], 131071, 0.9, 0.9, 0), ([2] * 130, 8193, 1.3, 0.7, 1), ([5, 0] * 60, 8192, 1.0, 1.0, 0), ([3] * 90, 40, 1.0, 1.1, 2)])
+def test_verify_calls_of_many_logits(dtype, drawn, counts, vocab, tau, draft_tau, pad):
+    say("verify", dtype, drawn, len(counts), vocab)
+    n = sum(counts) + pad
+    assert n * 2 * -(-vocab // 8192) >= 512
+    case = verify_case(dtype, counts, vocab, seed=vocab, drawn=drawn, pad=pad)
+    _, _, out_a = check64(dtype, case, tau, draft_tau)
+    some = torch.tensor(counts) > 1
+    if drawn:
+        assert 0 < int(out_a.sum()) < int((torch.tensor(counts) - 1).clamp(min=0).sum()) and some.any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_verify_calls_of_many_logits_that_are_no_numbers(dtype):
+    """NaN, infinite and masked logits in every slice, rows of nothing else, rows that start on no grid of 16 bytes."""
+    counts, vocab = [4] * 20, 33333
+    case = verify_case(dtype, counts, vocab, seed=55)
+    z, y = case["logits"], case["draft_logits"]
+    z[:, 5::7] = math.nan
+    y[:, 3::5] = -math.inf
+    z[8, 20000] = y[9, 32000] = math.inf
+    z[12] = -math.inf
+    y[17] = math.nan
+    case["tokens"][case["tokens"] % 7 == 5] += 1
+    check64(dtype, case)
+
+
+@pytest.mark.parametrize("first,lost", [([0, 4, 8, 400], 2), ([-4, 4, 8, 260], 0)])
+def test_verify_calls_of_many_logits_with_firsts_out_of_range(first, lost):
+    case = verify_case("bf16", [4, 4, 252], 8300, seed=56)
+    want = run_verify("bf16", case)
+    out_t, out_l, out_a, err = run_verify("bf16", dict(case, first=ints(first)))
+    assert err == 1 and int(out_a[lost]) == 0
+    for s in range(3):
+        rows = slice(*case["first"][s:s + 2].tolist())
+        if s == lost or (lost == 0 and s == 0):
+            assert (out_t[rows] == -5).all() and (out_l[rows] == 9.0).all()
+        else:
+            assert torch.equal(out_t[rows], want[0][rows]) and torch.equal(out_l[rows], want[1][rows]) and out_a[s] == want[2][s]
