@@ -439,10 +439,14 @@ __global__ __launch_bounds__(NTV) void verify_pick_kernel(const VerifyArgs a) {
 constexpr int SEQS_MAX = 1 << 16;                // (every block looks through the sequences)
 constexpr double TAU_MIN = 0x1p-100;             // (and 1 / tau: what fp32 exponents hold)
 
-// Logits per thread of a slice: 32, or 8 where that leaves too few blocks to fill the GPU.
-int each_for(int n_tokens, int vocab) { return (long long)n_tokens * 2 * ((vocab + 32 * NTV - 1) / (32 * NTV)) < 512 ? 8 : 32; }
-int slices_for(int n_tokens, int vocab) {
-    const int n = NTV * each_for(n_tokens, vocab);
+// Logits per thread of a slice: 32, or 8 where that leaves the GPU with fewer blocks than it is busy with (eight of a kind per compute unit, twice), or where 8 hold a row.  Measured, us with 32 / 8 logits, by blocks of 32:
+//   bf16, 131072 logits:  256: 36.3 / 27.7 | 1024: 45.0 / 34.3 | 3072: 54.1 / 49.6 | 4096: 58.7 / 57.8 | 6080: 68.3 / 83.2        bf16, 32000: 3200: 57.2 / 51.5 | 4800: 62.8 / 60.1 | 7200: 78.7 / 91.3
+//   fp32, 32000 logits:   40: 45.7 / 28.5 | 1520: 56.8 / 39.9 | 4800: 75.4 / 70.6 | 7200: 95.4 / 101.6                            fp32, 1000:  6000: 202 / 173 | 12000: 212 / 173
+int each_for(int n_seq, int n_tokens, int vocab) {
+    return vocab <= 8 * NTV || std::max(2LL * n_tokens, (long long)n_seq) * ((vocab + 32 * NTV - 1) / (32 * NTV)) < 4096 ? 8 : 32;
+}
+int slices_for(int n_seq, int n_tokens, int vocab) {
+    const int n = NTV * each_for(n_seq, n_tokens, vocab);
     return (vocab + n - 1) / n;
 }
 
@@ -453,14 +457,14 @@ template <typename T, int E> hipError_t launch_each(hipStream_t s, const VerifyA
     hipLaunchKernelGGL((verify_pick_kernel<T>), dim3((unsigned)a.n_seq), dim3(NTV), 0, s, a);
     return hipGetLastError();
 }
-template <typename T> hipError_t launch(hipStream_t s, const VerifyArgs &a) { return each_for(a.n_tokens, a.vocab) == 8 ? launch_each<T, 8>(s, a) : launch_each<T, 32>(s, a); }
+template <typename T> hipError_t launch(hipStream_t s, const VerifyArgs &a) { return each_for(a.n_seq, a.n_tokens, a.vocab) == 8 ? launch_each<T, 8>(s, a) : launch_each<T, 32>(s, a); }
 
 }  // namespace
 
 extern "C" size_t spd_op_verify_drafts_scratch_bytes(int32_t n_seq, int32_t n_tokens, int32_t vocab) {
     if (n_seq <= 0 || n_tokens < 0 || vocab <= 0) return 0;
-    const size_t slices = (size_t)slices_for(n_tokens, vocab), rows = 2 * (size_t)n_tokens * slices;
-    const size_t pieces = slices * (each_for(n_tokens, vocab) / 4);            // (of fp32 logits: the most)
+    const size_t slices = (size_t)slices_for(n_seq, n_tokens, vocab), rows = 2 * (size_t)n_tokens * slices;
+    const size_t pieces = slices * (each_for(n_seq, n_tokens, vocab) / 4);            // (of fp32 logits: the most)
     return 2 * up256(rows * 4) + up256(2 * n_seq * pieces * 8) + up256(n_seq * pieces * 8) + up256(n_seq * sizeof(VerifyPick));
 }
 
@@ -482,7 +486,7 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
         oa{out_accepted, (size_t)n_seq * 4}, se{err, 4}, sw{scratch, need};
     if (spdk::over_any(ot, {sz, sd, st, sf, su, ol, oa, se, sw}) || spdk::over_any(ol, {sz, sd, st, sf, su, oa, se, sw}) || spdk::over_any(oa, {sz, sd, st, sf, su, se, sw}) ||
         spdk::over_any(sw, {sz, sd, st, sf, su, se})) return SPD_EINVAL;
-    const int slices = slices_for(n_tokens, vocab);
+    const int slices = slices_for(n_seq, n_tokens, vocab);
     if ((long long)std::max(2 * n_tokens, n_seq) * slices > UINT32_MAX / NTV) return SPD_EINVAL;      // (threads of a grid are counted in 32 bits)
     const double log2e = 1.4426950408889634074;
     char *w = (char *)scratch;
@@ -490,8 +494,8 @@ extern "C" int spd_op_verify_drafts(int32_t dtype, const void *logits, int64_t r
     const size_t row_sums = 2 * (size_t)n_tokens * slices;
     a.top = (float *)w; w += up256(row_sums * 4);
     a.sum = (float *)w; w += up256(row_sums * 4);
-    a.pieces = slices * (each_for(n_tokens, vocab) / (16 / el));
-    a.unsure = 2.1 * sum_off(each_for(n_tokens, vocab), vocab, slices);          // (two rows)
+    a.pieces = slices * (each_for(n_seq, n_tokens, vocab) / (16 / el));
+    a.unsure = 2.1 * sum_off(each_for(n_seq, n_tokens, vocab), vocab, slices);          // (two rows)
     a.exact = (double *)w; w += up256(2 * (size_t)n_seq * a.pieces * 8);
     a.rest = (double *)w; w += up256((size_t)n_seq * a.pieces * 8);
     a.pick = (VerifyPick *)w;

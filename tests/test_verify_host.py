@@ -33,3 +33,18 @@ def test_reference_verification_of_what_64_bits_do_not_hold():
     assert go(mask, mask, [0.5, 0.0]) [0] == 1 and go(mask, z, [0.0, 0.0])[0] == 0 and V.verify(mask, torch.tensor([0, 1]), torch.tensor([0.0, 0.0]), 1.0)[:2] == (0, [0])
     flipped = mask.flip(1)
     assert V.verify(flipped[:1], torch.tensor([0]), torch.tensor([0.0]), 1.0)[1] == [1]             # the masked token comes first, and is not drawn
+
+
+# ------------------------------------------------------------------ how a call is cut
+@pytest.mark.parametrize("n_seq,n_tokens,vocab,each", [
+    (1, 5, 32000, 8), (16, 128, 131072, 32), (16, 127, 131072, 8), (32, 192, 131072, 32), (4, 16, 131072, 8), (64, 600, 32000, 32), (64, 400, 32000, 8), (1000, 6000, 2048, 8), (1000, 6000, 2049, 32),
+    (1 << 16, 15, 1 << 20, 32), (3, 0, 5000, 8)])
+def test_logits_per_thread(pkg, n_seq, n_tokens, vocab, each):  # noqa: F811
+    """The scratch tells: slices of 256 threads of 8 or 32 logits, sums and largest logits of two rows per token and slice, four numbers per piece at most.  Many sequences without tokens count as well: their blocks of
+    small slices would pass a grid's end."""
+    up = lambda x: (x + 255) // 256 * 256  # noqa: E731
+    slices = -(-vocab // (256 * each))
+    pieces = slices * each // 4
+    need = 2 * up(2 * n_tokens * slices * 4) + up(2 * n_seq * pieces * 8) + up(n_seq * pieces * 8) + up(n_seq * 20)
+    assert pkg.lib().spd_op_verify_drafts_scratch_bytes(n_seq, n_tokens, vocab) == need
+    assert max(2 * n_tokens, n_seq) * slices * 256 < 1 << 32
