@@ -869,7 +869,7 @@ __global__ __launch_bounds__(NT) void paged_merge_kernel(const PagedAttnArgs p) 
         for (int c0 = 0; c0 < chunks; c0 += side) {
             const int c = c0 + mine;
             const float f = __shfl(l, min(c, WAVE - 1), WAVE);
-            if (c >= chunks || f == 0.f) continue;
+            if (c >= chunks) continue;           // (one that weighs nothing counts: what is no number in it stays none)
             const float4 z = c0 ? global_load_float4(p.part + (at + c) * d + 4 * (lane % per)) : x[r];
             y.x += f * z.x; y.y += f * z.y; y.z += f * z.z; y.w += f * z.w;
         }

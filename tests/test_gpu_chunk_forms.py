@@ -146,3 +146,37 @@ def test_many_rows_are_read_four_pieces_at_a_time(dtype, out, kv, d, lengths):
                 y = y * scale.transpose(1, 2)[at[ok].long(), (pos[ok] % 16).long()][..., None]
             want[ok] = y.to(R.TORCH[out])
             assert torch.equal(got.cpu(), want)
+
+
+# ------------------------------------------------------------------ what is no number in a chunk that weighs nothing
+@pytest.mark.parametrize("dtype,io", [("fp16", "fp32"), ("fp16", "fp16"), ("bf16", "fp32"), ("bf16", "bf16"), ("int8", "fp32"), ("int8", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("heads,news,past", [(2, 3, 1500), (2, 60, 1500), (40, 230, 900)])
+def test_a_value_that_is_no_number_counts_in_a_chunk_that_weighs_nothing(dtype, io, heads, news, past):
+    """Scores of later chunks are 400 above those of the first, whose weight is 0 in 32 bits: a NaN in it is in the result all the same, as it is where positions are not cut."""
+    case = attention_case(dtype, io, heads, 1, 64, 16, [news], [past], seed=heads)
+    n = past + news
+    case["q"][..., 0] = 80.0
+    table = case["table"][0].long()
+    for p in range(n):
+        at = (table[p // 16], 0, p % 16)
+        if dtype == "int8":
+            case["K"][at][0] = 0 if p < n - 300 else 127
+            case["K_scale"][at] = 40.0 / 127.0 if p >= n - 300 else case["K_scale"][at]
+            case["K"][at][1:] = 0 if p >= n - 300 else case["K"][at][1:]
+        else:
+            case["K"][at][0] = 0.0 if p < n - 300 else 40.0
+    clean, err = attend(dtype, case)
+    assert err == 0 and bool(clean.isfinite().all())
+    at = (table[2], 0, 5)
+    if dtype == "int8":
+        case["V_scale"][at] = float("nan")
+    else:
+        case["V"][at][7] = float("nan")
+    got, err = attend(dtype, case)
+    assert err == 0
+    if dtype == "int8":
+        assert not got.isfinite().any()
+    else:
+        assert not got[..., 7].isfinite().any()
+        rest = [i for i in range(64) if i != 7]
+        assert torch.equal(got[..., rest], clean[..., rest])
