@@ -444,7 +444,7 @@ int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64
  * the drafter drew token t + 1 from, q = softmax(draft_logits / draft_tau), not looked at for a sequence's last token.  draft_logits NULL: drafts that were chosen, not drawn, q
  * is 1 at the draft.  u (DEVICE float [n_tokens], in [0, 1), the caller's draws): draft x behind token t stands if all before it do and u[t] < p(x) / q(x), however small the two are (a
  * quotient below 2^-990 may count as 0; with p(x) = 0 it does not stand, with q(x) = 0 < p(x) it does); so a text has the target's distribution whatever the drafter's is.  Behind the drafts
- * that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0) at the first that does not (from p where that is zero
+ * that stand comes one token more, drawn with u at the sequence's last token: from p where all stand, else from max(p - q, 0), formed in 64 bits, at the first that does not (from p where that is zero
  * everywhere): the first token, in the order of ids, up to which more than u of the sum has gone by.  Tokens below 2^-1021 of the likeliest one's probability have none there, so one that is
  * masked with a large negative number is not drawn, with a u of 0 neither.  What is drawn, and whether a draft stands, goes by sums of 64
  * bits (of 32 where those could not turn it); the log p of a draft by sums of 32, off by less than 2^-15 of itself.  tau and draft_tau, in 64 bits (the draw falls between as many borders as there are tokens, and a temperature rounded to 32 bits moves one in two

@@ -13,7 +13,7 @@
 // Bound: the matrix cores where there are many rows (and with all 24 bits of them two or three products for each), else the vector unit, which forms some 500 instructions per wave and stage
 // (masks, exponentials, parts of them, codes to numbers) in between: a wave's products and its exponentials follow one another, and two blocks per compute unit are what registers allow.
 // Measured (kernel alone; then what the bytes or products alone would take): 512 tokens of 64 heads on 8 behind 32257 positions in fp16, 24 bits, 0.94 ms = 1.16 PFLOP/s in two products each, the rate of a large
-// fp16 product; 2999 tokens of 32 heads in bf16 from their beginnings 51 us (23); 40 tokens of eight sequences over 4001 positions of 8 bits 31 us (9); four tokens behind 73 positions 9 us.
+// fp16 product; 2999 tokens of 32 heads in bf16 from their beginnings 52 us (23); 40 tokens of eight sequences over 4001 positions of 8 bits 31 us (9); four tokens behind 73 positions 9 us.
 // The four waves of a block of 128 rows share out rows; of 64, rows and the stage's halves.  Where there are few tiles the positions are cut into chunks, and a second
 // kernel puts a row's chunks together in order.
 #include "spd_attention.h"

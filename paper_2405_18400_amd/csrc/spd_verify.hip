@@ -3,13 +3,13 @@
 // Bound: every row of logits is read once, whatever stands (which rows count hangs on the rows before them), and the one row that a sequence's last token
 // is drawn from three times more.  Four launches:
 //   * slices of all rows: largest logit and sum of exponentials, in fp32;
-//   * a block per slice and sequence puts its sequence's rows together, finds the first draft that does not stand, and sums its slice of that row again, in 64 bits;
+//   * a block per slice and sequence puts its sequence's rows together, finds the first draft that does not stand (with sums of 64 bits where those of 32 might be wrong), and sums its slice of that row again, in 64 bits;
 //   * the same blocks sum what that row leaves, max(p - q, 0);
 //   * a block per sequence finds the slice where the draw falls, and the token in it.
 // Whether a draft stands is one comparison, which sums of fp32 exponentials hardly ever turn: those that they might (their error is bounded) are made again with sums of 64 bits.  The draw falls between as many
 // borders as there are tokens: of a hundred thousand, one in a thousand draws meets one that such sums have moved.  So that row is in 64 bits always; all rows in 64 bits took 61 us where fp32 takes what reading takes.
-// Measured, the four in turn: 32 sequences with 190 tokens, 131072 logits in bf16, 100 MB in all: 22.4 us (4.1 TB/s), 21.5 and 14.5 (vector unit 50% busy, exponentials in 64 bits), 12.0 (a block's chain of
-// trips and sums); one sequence of five tokens, 32000 logits in fp32: 3.3, 8.8, 5.1 and 8.9, chains all of them.
+// Measured, the four in turn: 32 sequences with 190 tokens, 131072 logits in bf16, 100 MB in all: 24.9 us (3.7 TB/s; vector unit 70% busy), 21.6 and 14.6 (vector unit 50% busy, exponentials in 64 bits), 11.2 (a
+// block's chain of trips and sums); one sequence of five tokens, 32000 logits in fp32: 3.7, 9.9, 5.2 and 8.4, chains all of them.
 #include "spd_attention.h"
 
 #include <algorithm>
