@@ -431,7 +431,7 @@ int spd_op_read_paged(int32_t dtype, const void *K, const void *V, const float *
  * A sequence whose first and len do not fit (first negative or past n_tokens, len below its new tokens or over max_len) gets zeros for the rows that it has; where first descends anywhere no row
  * is written; *err is set, also for a sequence that has no row (no new tokens, or all of them outside of 0 .. n_tokens - 1).  Rows that are no sequence's are left as they were.  (Without tokens, n_tokens 0, nothing is looked at.)  n_seq is at most 65536, n_tokens n_heads at most 2^24.  A position on a page out of range does not count (*err is set).  Keys and values that count have to be finite for a finite result; nothing behind a
  * sequence's last position, or behind a token's own, gets into its result.  (Of an 8-bit cache, values whose
- * scale lies more than 2^80 below the largest one in front of them or at the next 64 positions may count as zero.) */
+ * scale lies more than 2^64 below the largest one in front of them or at the next 64 positions may count as zero.) */
 size_t spd_op_attention_paged_scratch_bytes(int32_t dtype, int32_t io_dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                             int32_t max_new, int32_t max_len);
 int spd_op_attention_paged(int32_t dtype, int32_t io_dtype, const void *q, int64_t q_stride, const void *K, const void *V, const float *K_scale, const float *V_scale,

@@ -28,8 +28,8 @@ namespace {
 constexpr int NT = 256, NW = NT / WAVE;
 constexpr int TR = 32;                           // rows (and keys, features) of a matrix product
 // 8 bits: scales of values that lie no further than 2^NARROW apart are held by the largest.  The largest product of a row's is 2^12 2^-13 at least then, and what 16 bits lose, 2^-25, is 2^-24 of it.
-// LIFT_MAX: a row may be up to that power of two larger: its sums, of up to 2^21 keys, stay below 2^(15 + 7 + 21 + 80), inside of fp32's range.
-constexpr int NARROW = 12, LIFT_MAX = 80;
+// LIFT_MAX: a row may be up to that power of two larger: its sums, of up to 2^30 keys, stay below 2^(15 + 7 + 30 + 64), inside of fp32's range.
+constexpr int NARROW = 12, LIFT_MAX = 64;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
