@@ -440,7 +440,7 @@ constexpr int SEQS_MAX = 1 << 16;                // (every block looks through t
 constexpr double TAU_MIN = 0x1p-100;             // (and 1 / tau: what fp32 exponents hold)
 
 // Logits per thread of a slice: 32, or 8 where that leaves the GPU with fewer blocks than it is busy with (eight of a kind per compute unit, twice), or where 8 hold a row.  Measured, us with 32 / 8 logits, by blocks of 32:
-//   bf16, 131072 logits:  256: 36.3 / 27.7 | 1024: 45.0 / 34.3 | 3072: 54.1 / 49.6 | 4096: 58.7 / 57.8 | 6080: 68.3 / 83.2        bf16, 32000: 3200: 57.2 / 51.5 | 4800: 62.8 / 60.1 | 7200: 78.7 / 91.3
+//   bf16, 131072 logits:  256: 36.3 / 27.7 | 1024: 45.0 / 34.3 | 2048: 50.2 / 41.0 | 4096: 58.7 / 57.8 | 6080: 68.3 / 83.2        bf16, 32000: 3200: 57.2 / 51.5 | 4800: 62.8 / 60.1 | 7200: 78.7 / 91.3
 //   fp32, 32000 logits:   40: 45.7 / 28.5 | 1520: 56.8 / 39.9 | 4800: 75.4 / 70.6 | 7200: 95.4 / 101.6                            fp32, 1000:  6000: 202 / 173 | 12000: 212 / 173
 int each_for(int n_seq, int n_tokens, int vocab) {
     return vocab <= 8 * NTV || std::max(2LL * n_tokens, (long long)n_seq) * ((vocab + 32 * NTV - 1) / (32 * NTV)) < 4096 ? 8 : 32;
